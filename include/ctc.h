@@ -46,7 +46,13 @@ typedef enum {
     CTC_ERR_STATE = -5        /* call out of order (e.g. forward before bind) */
 } ctc_status;
 
-typedef enum { CTC_F32 = 0, CTC_F16 = 1 } ctc_dtype;
+/* CTC_F32 and CTC_F16 are the types of networks and convolutions; the
+ * operators at the end of this file also take bfloat16, and e4m3 (no
+ * infinities, largest value 448) and e5m2 (largest value 57344) for 8-bit
+ * matrices. */
+typedef enum {
+    CTC_F32 = 0, CTC_F16 = 1, CTC_BF16 = 2, CTC_E4M3 = 3, CTC_E5M2 = 4
+} ctc_dtype;
 
 /* Role of a conv layer's last output channel (Sec. II-A):
  *  SUM   carry-through filter: 1 at the kernel centre on every input channel;
@@ -554,6 +560,170 @@ ctc_status ctc_net_profile_read(ctc_net *net, int32_t *launches,
  * rocprofv3), copied into name[cap].  Errors: CTC_ERR_ARG. */
 ctc_status ctc_net_op_kernel(const ctc_net *net, int32_t i, int32_t nimg,
                              char *name, int32_t cap);
+
+/* ---- operators around a protected classifier (device, asynchronous) ----- */
+
+/* What networks without batch normalisation, deployments in 8 bits and the
+ * grading of answers need next to the convolutions: group norm, 8-bit
+ * products with a scale for each block of 128, and the scores of given
+ * classes or tokens, with the gradients a fine-tuning step asks for.  Types
+ * are CTC_F32, CTC_F16 or CTC_BF16 unless said otherwise; sums, statistics
+ * and softmax terms are fp32 and results are rounded once.  Matrices and maps
+ * need only the alignment of their elements unless said otherwise; outputs
+ * must not overlap inputs except where "in place" is allowed.  Workspaces are
+ * caller-owned device scratch of the size the matching _workspace_bytes call
+ * gives (0: NULL will do), 16-byte aligned, not read before the call and free
+ * again once the stream has passed it; overlapping calls must not share one.
+ * Errors: CTC_ERR_ARG, CTC_ERR_UNSUPPORTED (sizes past a limit named below),
+ * CTC_ERR_WORKSPACE, CTC_ERR_DEVICE; a size of 0 is a valid call that does
+ * nothing (gradients over 0 images are zeros). */
+typedef enum { CTC_ACT_NONE = 0, CTC_ACT_RELU = 1, CTC_ACT_SILU = 2 } ctc_act;
+
+/* Group norm of a channels-last map with its activation:
+ *   y = act((x - mean) * rstd * gamma[c] + beta[c] (+ residual))
+ * with mean and rstd = 1 / sqrt(var + eps) over the hw pixels and c / groups
+ * channels of every image and group.
+ *   x, residual, y  [n][hw][c] in dtype; residual may be NULL; y may be x or
+ *                   the residual (in place)
+ *   gamma, beta     [c] fp32 or NULL (1 and 0)
+ *   carry           1: channel c-1 is a carry-through checksum.  Like in
+ *                   Eq. (1) it is not normalised: it takes no part in its
+ *                   group's statistics and passes unchanged, plus the
+ *                   residual's (no activation, gamma and beta not read).  A
+ *                   group of the checksum alone has mean 0 and variance 0.
+ *   mean, rstd      [n][groups] fp32, written (the backward pass reads them)
+ * A NaN or an infinity spoils the group it is in.  hw <= 2^31, c <= 2^20. */
+ctc_status ctc_group_norm_forward(ctc_dtype dtype, int32_t n, int64_t hw,
+                                  int32_t c, int32_t groups, int32_t carry,
+                                  const void *x, const float *gamma,
+                                  const float *beta, const void *residual,
+                                  float eps, int32_t act, void *y, float *mean,
+                                  float *rstd, void *workspace, size_t ws_bytes,
+                                  void *stream);
+
+/* Its gradients: with dz = dy * act'(z), z the activation's argument (its
+ * derivative at 0 is 0 for the ReLU),
+ *   dresidual = dz, dbeta[c] = sum dz, dgamma[c] = sum dz * xhat,
+ *   dx = rstd * (dz gamma - mean(dz gamma) - xhat mean(dz gamma xhat))
+ * (means over image and group).  A checksum channel passes dy; its dgamma
+ * and dbeta are 0.
+ *   dx, dresidual  [n][hw][c] in dtype, each may be NULL; one of them may be
+ *                  dy (in place)
+ *   dgamma, dbeta  [c] fp32, each may be NULL
+ * The same inputs give the same bits every time. */
+ctc_status ctc_group_norm_backward(ctc_dtype dtype, int32_t n, int64_t hw,
+                                   int32_t c, int32_t groups, int32_t carry,
+                                   const void *dy, const void *x,
+                                   const float *mean, const float *rstd,
+                                   const float *gamma, const float *beta,
+                                   const void *residual, int32_t act, void *dx,
+                                   void *dresidual, float *dgamma, float *dbeta,
+                                   void *workspace, size_t ws_bytes,
+                                   void *stream);
+
+/* Workspace of the two (backward: 0 or 1).  Host, synchronous. */
+ctc_status ctc_group_norm_workspace_bytes(ctc_dtype dtype, int32_t n,
+                                          int64_t hw, int32_t c, int32_t groups,
+                                          int32_t backward, size_t *bytes);
+
+/* A matrix in 8 bits with a scale for each block of block_rows (1 or 128)
+ * rows by 128 columns: with amax the block's largest magnitude, at least
+ * 2^-100, and MAX the type's largest value,
+ *   scale = amax / MAX,   q = round(x * (MAX / amax))
+ * (fp32 operations, to nearest, ties to even; x is about q * scale).  A NaN
+ * or an infinity makes its block's scale NaN or infinite, so everything that
+ * is computed from the block shows it.
+ *   x       [rows][cols] in dtype, rows ldx elements apart
+ *   transpose  0: q is the matrix; 1: q is its transpose [cols][rows], blocks
+ *           and scales those of the transpose (what the products of a
+ *           backward pass read)
+ *   q       qtype (CTC_E4M3 or CTC_E5M2), rows ldq bytes apart: 16-byte
+ *           aligned, ldq a multiple of 16.  Up to 15 bytes behind a row's
+ *           columns, to the next multiple of 16, are written too
+ *   scales  [ceil(columns of q / 128)][ld_scales] fp32: scale of rows
+ *           r * block_rows .. at [k block][r] */
+ctc_status ctc_fp8_quantize(ctc_dtype dtype, int64_t rows, int64_t cols,
+                            const void *x, int64_t ldx, ctc_dtype qtype,
+                            int32_t block_rows, int32_t transpose, void *q,
+                            int64_t ldq, float *scales, int64_t ld_scales,
+                            void *stream);
+
+/* Product of such matrices,
+ *   y[m][n] = act(sum_k (a[m][k] sa) (b[n][k] sb) + bias[n])
+ * with every 128-wide block of k summed on its own, scaled and added in fp32.
+ * Results in CTC_F32 have fp32 sums throughout; for 16-bit results the 8-bit
+ * matrix unit sums a block, which drops what lies more than 13 bits below the
+ * largest product in a sum.
+ *   a, b    [m][k] and [n][k] 8-bit (CTC_E4M3 or CTC_E5M2 each), rows lda and
+ *           ldb bytes apart: 16-byte aligned, strides a multiple of 16 up to
+ *           2^22; every row, the last one too, is readable up to k rounded up
+ *           to 16 (what stands there takes no part)
+ *   a_scales, b_scales  as ctc_fp8_quantize writes them, a_block and b_block
+ *           rows (1 or 128) to a scale
+ *   bias    [n] fp32 or NULL
+ *   y       [m][n] in ytype, rows ldy elements apart
+ * A layer's forward product takes activations (a_block 1) and filters
+ * [out][in] (b_block 128); the gradient of its input the output gradients and
+ * the filters' transpose; the gradient of the filters both transposes
+ * (blocks of 1, k the rows of the batch).  k = 0 gives act(bias). */
+ctc_status ctc_fp8_matmul(ctc_dtype atype, ctc_dtype btype, ctc_dtype ytype,
+                          int64_t m, int64_t n, int64_t k, const void *a,
+                          int64_t lda, const float *a_scales, int64_t ld_as,
+                          int32_t a_block, const void *b, int64_t ldb,
+                          const float *b_scales, int64_t ld_bs, int32_t b_block,
+                          const float *bias, int32_t act, void *y, int64_t ldy,
+                          void *workspace, size_t ws_bytes, void *stream);
+
+/* Workspace of ctc_fp8_matmul (partial sums of a split k).  Host,
+ * synchronous. */
+ctc_status ctc_fp8_matmul_workspace_bytes(ctc_dtype ytype, int64_t m, int64_t n,
+                                          int64_t k, size_t *bytes);
+
+/* Scores of rows of logits x: lse = log sum_i exp(x_i), the log probability
+ * of a given class or token x_t - lse, the entropy of the row's distribution
+ * in nats, the target's rank (how many logits stand above it; equal ones are
+ * ordered by index) and the top_k best alternatives.
+ *   logits   [rows][vocab] in dtype, rows ld >= vocab elements apart (a
+ *            protected classifier's row holds the checksum behind its
+ *            classes: vocab = classes, ld = classes + 1)
+ *   targets  [rows] or NULL; outside 0 .. vocab-1: none (log probability 0,
+ *            rank -1)
+ *   top_k    0 .. 32
+ *   lse, logprob, entropy  [rows] fp32, rank [rows]; each may be NULL
+ *   top_ids, top_logprobs  [rows][top_k], best first, equal logits by index
+ * Barred tokens have a logit of -infinity: probability 0, never listed.
+ * Places of top_ids without an alternative hold -1 and -infinity.  A row that
+ * bars everything has lse and logprob -infinity and entropy 0.  A NaN or
+ * +infinity makes a row's fp32 scores NaN; NaN logits are ordered first. */
+ctc_status ctc_token_scores_forward(ctc_dtype dtype, int64_t rows,
+                                    int32_t vocab, const void *logits,
+                                    int64_t ld, const int32_t *targets,
+                                    int32_t top_k, float *lse, float *logprob,
+                                    float *entropy, int32_t *rank,
+                                    int32_t *top_ids, float *top_logprobs,
+                                    void *workspace, size_t ws_bytes,
+                                    void *stream);
+
+/* Gradient of the scores with respect to the logits, with p = exp(x - lse):
+ *   dx_i = p_i (g_lse - g_logprob - g_entropy (log p_i + entropy))
+ *          + (i == target) g_logprob
+ *   lse, entropy  as the forward pass wrote them (entropy only for g_entropy);
+ *           p is off by a factor of as much as lse was rounded (2^-24 of it)
+ *   g_lse, g_logprob, g_entropy  [rows] fp32, each may be NULL (0)
+ *   dlogits  [rows][vocab] in dtype, rows ldd apart; may be logits (in place,
+ *            ldd = ld)
+ * A row that bars everything gets zeros. */
+ctc_status ctc_token_scores_backward(ctc_dtype dtype, int64_t rows,
+                                     int32_t vocab, const void *logits,
+                                     int64_t ld, const int32_t *targets,
+                                     const float *lse, const float *entropy,
+                                     const float *g_lse, const float *g_logprob,
+                                     const float *g_entropy, void *dlogits,
+                                     int64_t ldd, void *stream);
+
+/* Workspace of ctc_token_scores_forward.  Host, synchronous. */
+ctc_status ctc_token_scores_workspace_bytes(int64_t rows, int32_t vocab,
+                                            int32_t top_k, size_t *bytes);
 
 void ctc_net_destroy(ctc_net *net);
 const char *ctc_last_error(void);   /* message of this thread's last error */

@@ -12,6 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libctc.so")
 SOURCES = [os.path.join(HERE, "csrc", "ctc_api.cpp"),
+           os.path.join(HERE, "csrc", "ops_api.cpp"),
            os.path.join(HERE, "csrc", "kernels.hip")]
 ARCH = "gfx950"
 

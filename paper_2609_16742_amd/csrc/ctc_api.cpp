@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/ctc.h"
+#include "errors.h"
 #include "kernels.h"
 
 using namespace ctc;
@@ -1075,6 +1076,8 @@ bool input_faults_armed(const ctc_net *net) {
 // =====================================================================
 // C ABI
 // =====================================================================
+ctc_status ctc::report(ctc_status s, const char *message) { return fail(s, "%s", message); }
+
 extern "C" {
 
 int32_t ctc_abi_version(void) { return CTC_ABI_VERSION; }

@@ -1,0 +1,437 @@
+// Matrix product in 8-bit floating point with a scale for each block of 128:
+//   y[m][n] = act(sum over blocks kb of sa[kb][m'] sb[kb][n'] *
+//                 sum over k in kb of a[m][k] b[n][k]  + bias[n])
+// with m' = m or m / 128, n' = n or n / 128.  A block is summed on the matrix
+// unit, its result scaled and added in fp32, so every scale counts exactly
+// where it belongs.  Two ways to sum a block:
+//  - one 16x16x128 8-bit MFMA.  The unit lines a sum's products up with the
+//    largest exponent among them and drops what lies more than 13 bits below
+//    it (measured: 2^16 + 2^3 arrives, of 2^16 + 2^2 only 2^16), 1.5e-5 of
+//    the result for normal values: a tenth of a 16-bit result's rounding, so
+//    16-bit results are summed like this, at the 8-bit rate;
+//  - four 16x16x32 bf16 MFMAs on the widened values (exact, as are their
+//    products), at half the rate but with fp32 sums: fp32 results, and all
+//    products of few rows, which the bytes of the filters bound.
+//
+// b's rows (filters) are the MFMA's first operand: a lane ends up with four
+// consecutive n of one m.  A lane's 32 values of k are two 16-byte chunks g
+// and g + 4 (g = lane / 16) of the block's 128 bytes, the same in a and b.
+#pragma once
+#include "ops_device.h"
+
+namespace ctc {
+namespace ops {
+
+typedef __amdgpu_buffer_rsrc_t Buf;
+constexpr int PAST = (int)0x80000000u;           // past every buffer: reads 0
+typedef __attribute__((address_space(3))) void *LdsAt;
+
+// One MFMA over a block of 128: rows from b (type FB), columns from a (FA).
+template <int FA, int FB>
+__device__ __forceinline__ f4 mfma_block(i8v b, i8v a) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+        b, a, (f4)(0.f), FB == E5M2 ? 1 : 0, FA == E5M2 ? 1 : 0, 0, 0, 0, 0);
+}
+// Two 16-byte chunks as one operand.
+__device__ __forceinline__ i8v chunks(u4 lo, u4 hi) {
+    i8v r;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        r[e] = (int)lo[e];
+        r[e + 4] = (int)hi[e];
+    }
+    return r;
+}
+// The same sum in fp32: operands widened to bf16.
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+struct Wide { bf8v q[4]; };
+template <int F> __device__ __forceinline__ Wide widen_block(i8v v) {
+    Wide r;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        bf2 lo, hi;
+        if constexpr (F == E4M3) {
+            lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.f, false);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.f, true);
+        } else {
+            lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[i], 1.f, false);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[i], 1.f, true);
+        }
+        const int at = (i & 1) * 4;
+        r.q[i >> 1][at] = lo[0];
+        r.q[i >> 1][at + 1] = lo[1];
+        r.q[i >> 1][at + 2] = hi[0];
+        r.q[i >> 1][at + 3] = hi[1];
+    }
+    return r;
+}
+__device__ __forceinline__ f4 mfma_wide(const Wide &b, const Wide &a) {
+    f4 d = (f4)(0.f);
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.q[i], a.q[i], d, 0, 0, 0);
+    return d;
+}
+// The first `n` bytes of a chunk, the others zero (n may be < 0 or > 16).
+__device__ __forceinline__ u4 first_bytes(u4 v, int n) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const int b = n - 4 * e;
+        if (b <= 0) v[e] = 0;
+        else if (b < 4) v[e] &= (1u << (8 * b)) - 1;
+    }
+    return v;
+}
+
+// Four results of row m from column n on.
+__device__ __forceinline__ void product_out(const ProductArgs &p, int64_t m, int64_t n, f4 v) {
+    if (m >= p.m) return;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (n + e < p.n) v[e] = act_of(p.act, p.bias ? v[e] + p.bias[n + e] : v[e]);
+    float w[4] = {v[0], v[1], v[2], v[3]};
+    const int64_t o = m * p.ldy + n;
+    auto put = [&](auto *y) {
+        typedef typename std::remove_pointer<decltype(y)>::type T;
+        if (n + 4 <= p.n) store<T, 4>(y + o, w);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (n + e < p.n) y[o + e] = narrow<T>(w[e]);
+    };
+    if (p.ytype == F32) put((float *)p.y);
+    else if (p.ytype == F16) put((_Float16 *)p.y);
+    else put((__bf16 *)p.y);
+}
+// ... or as partial sums of range `split`.
+__device__ __forceinline__ void partial_out(const ProductArgs &p, int split, int64_t m,
+                                            int64_t n, f4 v) {
+    if (m >= p.m) return;
+    float *o = p.ws + ((int64_t)split * p.m + m) * p.n + n;
+    if (n + 4 <= p.n) __builtin_memcpy(o, &v, 16);
+    else
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (n + e < p.n) o[e] = v[e];
+}
+
+// ---------------------------------------------------------------------------
+// Few rows of a: the filters are streamed once, straight into registers.  A
+// workgroup of eight waves takes 16 filters and MT tiles of 16 rows; its
+// waves take every eighth block of k and add up in LDS.
+// ---------------------------------------------------------------------------
+template <int MT, int FA, int FB>
+__global__ __launch_bounds__(512) void product_rows(ProductArgs p, int splits, int per) {
+    __shared__ f4 sum[8][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int fr = lane & 15, fg = lane >> 4;
+    const int64_t n0 = (int64_t)(blockIdx.x / splits) * 16;
+    const int split = blockIdx.x % splits;
+    const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int nb = (int)((p.k + 127) / 128);
+    const int kb1 = (split + 1) * per < nb ? (split + 1) * per : nb;
+    // rows past the end: the last one again (they only reach results that
+    // are not stored)
+    const int64_t n = n0 + fr < p.n ? n0 + fr : p.n - 1;
+    const uint8_t *b = p.b + n * p.ldb;
+    const uint8_t *a[MT];
+    const float *sa[MT];
+    f4 acc[MT];
+#pragma unroll
+    for (int j = 0; j < MT; j++) {
+        const int64_t m = m0 + j * 16 + fr < p.m ? m0 + j * 16 + fr : p.m - 1;
+        a[j] = p.a + m * p.lda;
+        sa[j] = p.sa + (p.a_block == 1 ? m : m / 128);
+        acc[j] = (f4)(0.f);
+    }
+    int64_t nq[4];                               // scale of each of four results
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const int64_t q = n0 + fg * 4 + e < p.n ? n0 + fg * 4 + e : p.n - 1;
+        nq[e] = p.b_block == 1 ? q : q / 128;
+    }
+    auto get = [&](const uint8_t *row, int kb, bool whole) {
+        const int64_t k = (int64_t)kb * 128 + fg * 16;
+        if (whole) return chunks(*(const u4 *)(row + k), *(const u4 *)(row + k + 64));
+        // chunks that begin past the end are not read
+        u4 lo = (u4)(0u), hi = (u4)(0u);
+        if (k < p.k) lo = first_bytes(*(const u4 *)(row + k), (int)(p.k - k));
+        if (k + 64 < p.k) hi = first_bytes(*(const u4 *)(row + k + 64), (int)(p.k - k - 64));
+        return chunks(lo, hi);
+    };
+    auto block = [&](int kb, bool whole) {
+        const Wide w = widen_block<FB>(get(b, kb, whole));
+        f4 sb;
+#pragma unroll
+        for (int e = 0; e < 4; e++) sb[e] = p.sb[kb * p.ldsb + nq[e]];
+#pragma unroll
+        for (int j = 0; j < MT; j++) {
+            const Wide x = widen_block<FA>(get(a[j], kb, whole));
+            const float s = sa[j][kb * p.ldsa];
+            acc[j] += mfma_wide(w, x) * (sb * s);
+        }
+    };
+    const int full = (int)(p.k / 128);
+    int kb = split * per + wave;
+    for (; kb < kb1 && kb < full; kb += 8) block(kb, true);
+    if (kb < kb1) block(kb, false);
+#pragma unroll
+    for (int j = 0; j < MT; j++) sum[wave][j][lane] = acc[j];
+    __syncthreads();
+    if (wave < MT) {
+        f4 t = sum[0][wave][lane];
+        for (int i = 1; i < 8; i++) t += sum[i][wave][lane];
+        const int64_t m = m0 + wave * 16 + fr;
+        if (splits > 1) partial_out(p, split, m, n0 + fg * 4, t);
+        else product_out(p, m, n0 + fg * 4, t);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of BM rows of a by BN filters, WM x WN waves.  A step is one block
+// of 128: its rows go from HBM into one of two LDS stages by the buffer
+// unit (16 bytes a lane, 1 KB a wave instruction: eight rows back to back),
+// the next step's while this one's MFMAs run.  Chunk g of row r is kept in
+// slot g ^ (r & 7), which spreads the fragment reads over the banks.
+// ---------------------------------------------------------------------------
+template <int BM, int BN, int WM, int WN, int FA, int FB, bool SB1, bool WIDE>
+__global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int mt, int nt,
+                                                             int splits, int per) {
+    constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN;
+    constexpr int IM = TM / 16, IN = TN / 16;
+    constexpr int AR = BM / 8 / NW, BR = BN / 8 / NW;    // loads of a wave a step
+    constexpr int STAGE = (BM + BN) * 128;
+    static_assert(AR * 8 * NW == BM && BR * 8 * NW == BN && 128 % TN == 0, "tile");
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+    __shared__ __attribute__((aligned(16))) float sbl[2][SB1 ? BN : 4];
+    // each XCD runs a contiguous range of tiles (workgroups go round the
+    // eight XCDs), the filters' tiles of the same rows next to each other
+    const int total = mt * nt * splits, share = (total + 7) / 8;
+    int t = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= share || t >= total) return;
+    const int split = t / (mt * nt);
+    t -= split * (mt * nt);
+    const int64_t m0 = (int64_t)(t / nt) * BM, n0 = (int64_t)(t % nt) * BN;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    const int fr = lane & 15, fg = lane >> 4;
+
+    const int64_t ma = p.m - m0 < BM ? p.m - m0 : BM, nb = p.n - n0 < BN ? p.n - n0 : BN;
+    const Buf ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + m0 * p.lda), 0,
+                                                     (int)(ma * p.lda), 0x00020000);
+    const Buf br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + n0 * p.ldb), 0,
+                                                     (int)(nb * p.ldb), 0x00020000);
+    const int lrow = wave * 8 + (lane >> 3);
+    const int lchunk = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
+    const int kend = (int)p.k;
+    auto issue = [&](int step, int st) {
+        const int k0 = step * 128;
+        const bool ok = k0 + lchunk < kend;
+#pragma unroll
+        for (int i = 0; i < AR; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                ar, (LdsAt)(lds + st * STAGE + (i * NW + wave) * 1024), 16,
+                ok ? ao + i * NW * 8 * (int)p.lda + k0 : PAST, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < BR; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                br, (LdsAt)(lds + st * STAGE + BM * 128 + (i * NW + wave) * 1024), 16,
+                ok ? bo + i * NW * 8 * (int)p.ldb + k0 : PAST, 0, 0, 0);
+    };
+    // scales: a's of a lane's IM columns; b's one of the wave's filters (a
+    // wave's lie in one block of 128), or, SB1, the tile's through LDS
+    int64_t sai[IM], sbi;
+#pragma unroll
+    for (int j = 0; j < IM; j++) {
+        const int64_t m = m0 + wm * TM + j * 16 + fr < p.m ? m0 + wm * TM + j * 16 + fr : p.m - 1;
+        sai[j] = p.a_block == 1 ? m : m / 128;
+    }
+    {
+        const int64_t n = n0 + (SB1 ? (int)threadIdx.x % BN : wn * TN);
+        const int64_t q = n < p.n ? n : p.n - 1;
+        sbi = p.b_block == 1 ? q : q / 128;
+    }
+    const int nblocks = (int)((p.k + 127) / 128);
+    const int first = split * per;
+    const int last = first + per < nblocks ? first + per : nblocks;
+    f4 acc[IN][IM];
+#pragma unroll
+    for (int i = 0; i < IN; i++)
+#pragma unroll
+        for (int j = 0; j < IM; j++) acc[i][j] = (f4)(0.f);
+    float sa[IM], san[IM], sb = 0.f, sbn = 0.f;
+    auto scales = [&](int step) {
+#pragma unroll
+        for (int j = 0; j < IM; j++) san[j] = p.sa[step * p.ldsa + sai[j]];
+        sbn = p.sb[step * p.ldsb + sbi];
+    };
+    if (first < last) {
+        scales(first);
+        issue(first, 0);
+    }
+    const int c0 = (fg ^ (fr & 7)) * 16, c1 = ((fg + 4) ^ (fr & 7)) * 16;
+    for (int step = first; step < last; step++) {
+        const int st = (step - first) & 1;
+#pragma unroll
+        for (int j = 0; j < IM; j++) sa[j] = san[j];
+        sb = sbn;
+        if constexpr (SB1)
+            if (threadIdx.x < BN) sbl[st][threadIdx.x] = sb;
+        __builtin_amdgcn_s_waitcnt(0);           // this wave's rows are in LDS
+        __syncthreads();                         // everyone's; the other stage is read out
+        if (step + 1 < last) {
+            scales(step + 1);
+            issue(step + 1, st ^ 1);
+        }
+        const char *A = lds + st * STAGE + (wm * TM + fr) * 128;
+        const char *B = lds + st * STAGE + BM * 128 + (wn * TN + fr) * 128;
+        const bool ragged = step * 128 + 128 > kend && (kend & 15);
+        const int left = kend - step * 128 - fg * 16;
+        typename std::conditional<WIDE, Wide, i8v>::type x[IM];
+#pragma unroll
+        for (int j = 0; j < IM; j++) {
+            u4 lo = *(const u4 *)(A + j * 2048 + c0), hi = *(const u4 *)(A + j * 2048 + c1);
+            if (ragged) {
+                lo = first_bytes(lo, left);
+                hi = first_bytes(hi, left - 64);
+            }
+            if constexpr (WIDE) x[j] = widen_block<FA>(chunks(lo, hi));
+            else x[j] = chunks(lo, hi);
+        }
+        if constexpr (!SB1)
+#pragma unroll
+            for (int j = 0; j < IM; j++) sa[j] *= sb;
+#pragma unroll
+        for (int i = 0; i < IN; i++) {
+            u4 lo = *(const u4 *)(B + i * 2048 + c0), hi = *(const u4 *)(B + i * 2048 + c1);
+            if (ragged) {
+                lo = first_bytes(lo, left);
+                hi = first_bytes(hi, left - 64);
+            }
+            typename std::conditional<WIDE, Wide, i8v>::type w;
+            if constexpr (WIDE) w = widen_block<FB>(chunks(lo, hi));
+            else w = chunks(lo, hi);
+            f4 s4 = (f4)(1.f);
+            if constexpr (SB1) s4 = *(const f4 *)(sbl[st] + wn * TN + i * 16 + fg * 4);
+#pragma unroll
+            for (int j = 0; j < IM; j++) {
+                f4 d;
+                if constexpr (WIDE) d = mfma_wide(w, x[j]);
+                else d = mfma_block<FA, FB>(w, x[j]);
+                if constexpr (SB1) d *= s4;
+                acc[i][j] += d * sa[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < IM; j++)
+#pragma unroll
+        for (int i = 0; i < IN; i++) {
+            const int64_t m = m0 + wm * TM + j * 16 + fr, n = n0 + wn * TN + i * 16 + fg * 4;
+            if (n >= p.n) continue;
+            if (splits > 1) partial_out(p, split, m, n, acc[i][j]);
+            else product_out(p, m, n, acc[i][j]);
+        }
+}
+
+// Adds the ranges' partial sums, in order: four results a thread.
+static __global__ __launch_bounds__(256) void product_join(ProductArgs p, int splits) {
+    const int64_t nq = (p.n + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.m * nq) return;
+    const int64_t m = i / nq, n = i % nq * 4;
+    f4 t = (f4)(0.f);
+    for (int s = 0; s < splits; s++) {
+        const float *o = p.ws + ((int64_t)s * p.m + m) * p.n + n;
+        f4 v = (f4)(0.f);
+        if (n + 4 <= p.n) __builtin_memcpy(&v, o, 16);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (n + e < p.n) v[e] = o[e];
+        t += v;
+    }
+    product_out(p, m, n, t);
+}
+
+// kind 0: product_rows; product_tile: 1 128 x 128, 2 256 x 256 tiles, 3
+// 128 x 128 with fp32 sums
+struct ProductPlan { int kind, mt, nt, splits, per; };
+static ProductPlan product_plan(const ProductArgs &a) {
+    ProductPlan r{};
+    const int64_t nb = (a.k + 127) / 128;
+    int64_t wgs, want, least;
+    if (a.m <= 64) {
+        r.kind = 0;
+        r.mt = a.m <= 16 ? 1 : a.m <= 32 ? 2 : 4;
+        r.nt = (int)((a.n + 15) / 16);
+        wgs = r.nt;
+        want = 256;
+        least = 16;              // blocks of a range
+    } else {
+        const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
+        r.kind = a.ytype == F32 ? 3 : big >= 192 ? 2 : 1;
+        const int b = r.kind == 2 ? 256 : 128;
+        r.mt = (int)((a.m + b - 1) / b);
+        r.nt = (int)((a.n + b - 1) / b);
+        wgs = (int64_t)r.mt * r.nt;
+        want = r.kind == 2 ? 256 : 512;
+        least = 4;
+    }
+    int64_t s = wgs ? want / wgs : 1;
+    if (s > nb / least) s = nb / least;
+    if (s > 16) s = 16;
+    if (s < 1) s = 1;
+    r.per = (int)((nb + s - 1) / s);
+    r.splits = r.per ? (int)((nb + r.per - 1) / r.per) : 1;
+    return r;
+}
+int product_splits(const ProductArgs &a) { return product_plan(a).splits; }
+size_t product_workspace(const ProductArgs &a) {
+    const ProductPlan r = product_plan(a);
+    return r.splits > 1 ? (size_t)r.splits * a.m * a.n * 4 : 0;
+}
+
+template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hipStream_t st) {
+    const ProductPlan r = product_plan(a);
+    hipError_t e;
+    if (r.kind == 0) {
+        const dim3 grid((unsigned)(r.nt * r.splits), 1);
+        e = r.mt == 1 ? start(product_rows<1, FA, FB>, grid, 512, st, a, r.splits, r.per)
+          : r.mt == 2 ? start(product_rows<2, FA, FB>, grid, 512, st, a, r.splits, r.per)
+                      : start(product_rows<4, FA, FB>, grid, 512, st, a, r.splits, r.per);
+    } else {
+        const unsigned g = ((unsigned)(r.mt * r.nt * r.splits) + 7) / 8 * 8;
+        const bool s1 = a.b_block == 1;
+        auto tile = [&](auto big, auto sb1, auto wide) {
+            constexpr bool B = decltype(big)::value, S = decltype(sb1)::value,
+                           W = decltype(wide)::value;
+            if constexpr (B)
+                return start(product_tile<256, 256, 4, 2, FA, FB, S, W>, dim3(g), 512, st, a,
+                             r.mt, r.nt, r.splits, r.per);
+            else
+                return start(product_tile<128, 128, 2, 2, FA, FB, S, W>, dim3(g), 256, st, a,
+                             r.mt, r.nt, r.splits, r.per);
+        };
+        typedef std::true_type Y;
+        typedef std::false_type N;
+        if (r.kind == 3) e = s1 ? tile(N(), Y(), Y()) : tile(N(), N(), Y());
+        else if (r.kind == 1) e = s1 ? tile(N(), Y(), N()) : tile(N(), N(), N());
+        else e = s1 ? tile(Y(), Y(), N()) : tile(Y(), N(), N());
+    }
+    if (e != hipSuccess || r.splits == 1) return e;
+    const int64_t items = a.m * ((a.n + 3) / 4);
+    return start(product_join, dim3((unsigned)((items + 255) / 256)), 256, st, a, r.splits);
+}
+hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
+    if (a.m == 0 || a.n == 0) return hipSuccess;
+    if (a.atype == E4M3)
+        return a.btype == E4M3 ? product_go<E4M3, E4M3>(a, st) : product_go<E4M3, E5M2>(a, st);
+    return a.btype == E4M3 ? product_go<E5M2, E4M3>(a, st) : product_go<E5M2, E5M2>(a, st);
+}
+
+}  // namespace ops
+}  // namespace ctc

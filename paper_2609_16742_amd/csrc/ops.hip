@@ -1,0 +1,10 @@
+// gfx950 kernels of the operators around a protected classifier.  Part of
+// kernels.hip, so the library holds one code object.
+#include "ops.h"
+
+#include <type_traits>
+
+#include "group_norm.h"
+#include "fp8_quantize.h"
+#include "fp8_product.h"
+#include "token_scores.h"

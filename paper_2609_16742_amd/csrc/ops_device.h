@@ -1,0 +1,100 @@
+// Device helpers of the operators in ops.hip.
+#pragma once
+#include "ops.h"
+
+#include <hip/hip_runtime.h>
+
+namespace ctc {
+namespace ops {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef int i8v __attribute__((ext_vector_type(8)));
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float INF = __builtin_inff();
+
+// One value of a 16-bit type as fp32, and back (to nearest, ties to even).
+// The value is in a register of its own before it is narrowed, so a
+// multiply-add in front is rounded to fp32 first (v_fma_mixlo_f16 would
+// round once, and differently).
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(_Float16 v) { return (float)v; }
+__device__ __forceinline__ float widen(__bf16 v) { return (float)v; }
+template <typename T> __device__ __forceinline__ T narrow(float v) {
+    if constexpr (sizeof(T) == 2) asm("" : "+v"(v));
+    return (T)v;
+}
+
+// V consecutive elements at p, which need only be aligned like one element
+// (global loads and stores of any width take any address of 4 or 2 bytes).
+template <typename T, int V> struct Pack { T e[V]; };
+template <typename T, int V>
+__device__ __forceinline__ void load(const T *p, float (&v)[V]) {
+    Pack<T, V> r;
+    __builtin_memcpy(&r, p, sizeof r);
+#pragma unroll
+    for (int i = 0; i < V; i++) v[i] = widen(r.e[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store(T *p, const float (&v)[V]) {
+    Pack<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V; i++) r.e[i] = narrow<T>(v[i]);
+    __builtin_memcpy(p, &r, sizeof r);
+}
+
+// The larger of values, a NaN lost against a number (as single
+// instructions: fmaxf first quiets its arguments).
+__device__ __forceinline__ float vmax(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float vmax3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float exp_hw(float v) { return exp2_hw(v * LOG2E); }
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// ReLU lets NaN through.
+__device__ __forceinline__ float act_of(int act, float z) {
+    if (act == ACT_RELU) return z < 0.f ? 0.f : z;
+    if (act == ACT_SILU) return z / (1.f + exp_hw(-z));
+    return z;
+}
+// d act(z) / dz
+__device__ __forceinline__ float act_grad(int act, float z) {
+    if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (act == ACT_SILU) {
+        const float s = 1.f / (1.f + exp_hw(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+template <typename K, typename... A>
+static hipError_t start(K kernel, dim3 grid, int block, hipStream_t st, A... args) {
+    hipLaunchKernelGGL(kernel, grid, dim3(block), 0, st, args...);
+    return hipGetLastError();
+}
+
+template <typename T> struct Tag { typedef T type; };
+// f(Tag<T>()) for the element type of `type`.
+template <typename F> static hipError_t by_type(int type, F f) {
+    if (type == F32) return f(Tag<float>());
+    if (type == F16) return f(Tag<_Float16>());
+    return f(Tag<__bf16>());
+}
+
+}  // namespace ops
+}  // namespace ctc

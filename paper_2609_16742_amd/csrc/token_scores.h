@@ -1,0 +1,517 @@
+// Scores of given tokens (or classes) from rows of logits x:
+//   lse = log sum_i exp x_i,   log p_i = x_i - lse,
+//   H = -sum_i p_i log p_i = log s - t / s
+// with the running maximum m, s = sum exp(x_i - m) and
+// t = sum (x_i - m) exp(x_i - m), so one pass over the row gives all three
+// (a new maximum m' scales s by f = exp(m - m') and turns t into
+// f (t + (m - m') s)); in the same pass the rank of the target and every
+// thread's largest value.
+//
+// Top alternatives: with the row dealt out to 64 groups of threads, the k-th
+// largest group maximum is a lower bound T of the k-th largest value (k
+// groups hold one at least), and for values in no order hardly more than k
+// are >= T.  Threads whose maximum reaches T read their part again, the
+// values >= T are collected and ordered by (value, lower index).
+//
+// What bounds it: the bytes of the logits.
+#pragma once
+#include "ops_device.h"
+
+namespace ctc {
+namespace ops {
+
+constexpr int SC_CAP = 512;                      // collected alternatives
+constexpr float SC_LOW = -200.f;                 // exp() of it is 0 in fp32
+
+struct SoftState { float m, s, t; };
+// m = -inf marks an empty state (s = t = 0); s turns NaN with the first NaN
+// or +inf and stays it.
+__device__ __forceinline__ void soft_raise(SoftState &a, float m) {
+    const float d = vmax(a.m - m, SC_LOW);
+    const float f = exp_hw(d);
+    a.t = (a.t + d * a.s) * f;
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ void soft_join(SoftState &a, SoftState b) {
+    const float m = vmax(a.m, b.m);
+    if (m != -INF) {             // (both empty: nothing to scale)
+        if (a.m != m) soft_raise(a, m);
+        if (b.m != m) soft_raise(b, m);
+    }
+    a.s += b.s;
+    a.t += b.t;
+}
+
+// Total order: NaN above +inf, -0 as +0, equal values by the lower index.
+__device__ __forceinline__ uint32_t order_bits(float x) {
+    if (x != x) return 0xfffffffeu;              // (below the key ~0)
+    const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order_key(float x, int i) {
+    return (uint64_t)order_bits(x) << 32 | (uint32_t)~i;
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return (int)~(uint32_t)k; }
+
+// The next value below x; NaN (which !(y <= x) holds for every y) below -inf.
+__device__ __forceinline__ float below(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    if (x == -INF) return __builtin_nanf("");
+    if (x == 0.f) return __builtin_bit_cast(float, 0x80000001u);
+    return __builtin_bit_cast(float, x > 0.f ? b - 1 : b + 1);
+}
+
+__device__ __forceinline__ uint64_t shfl_xor_key(uint64_t k, int o) {
+    const uint32_t lo = __shfl_xor((uint32_t)k, o), hi = __shfl_xor((uint32_t)(k >> 32), o);
+    return (uint64_t)hi << 32 | lo;
+}
+
+// The k-th largest of the 64 lanes' values (k <= 64).
+__device__ __forceinline__ float kth_of_lanes(float v, int k) {
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < 64; j++) {
+        const float o = __builtin_bit_cast(
+            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), j));
+        above += o > v;
+    }
+    // lanes with fewer than k larger values: k of them at least
+    float r = above < k ? v : INF;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) r = fminf(r, __shfl_xor(r, o));
+    return r;
+}
+
+// What a workgroup of NT threads finds in elements [lo, hi) of a row.
+template <typename T, int NT> struct ScorePart {
+    static constexpr int V = 16 / (int)sizeof(T);
+    static constexpr int NW = NT / 64;
+    struct Lds {
+        float gmax[64];
+        SoftState st[NW];
+        int cnt[NW];
+        int found;
+        uint64_t key[SC_CAP];
+        uint64_t best[NW];
+    };
+
+    const T *x;
+    int lo, hi;
+    int target;                  // -1: no rank wanted
+    float xt, thr_before;        // the target's value, and the next below it
+    SoftState st;
+    int cnt;
+
+    // VALS elements from index i on
+    template <int VALS> __device__ __forceinline__ void add(const float (&v)[VALS], int i) {
+        float vm;
+        if constexpr (VALS == 8)
+            vm = vmax3(vmax3(vmax3(v[0], v[1], v[2]), v[3], v[4]), v[5],
+                       vmax(v[6], v[7]));
+        else if constexpr (VALS == 4)
+            vm = vmax3(vmax(v[0], v[1]), v[2], v[3]);
+        else vm = v[0];
+        if (vm > st.m) soft_raise(st, vm);
+        const float mu = st.m == -INF ? 0.f : st.m;
+#pragma unroll
+        for (int e = 0; e < VALS; e++) {
+            const float d = v[e] - mu;
+            const float p = exp_hw(d);
+            st.s += p;
+            st.t = __builtin_fmaf(vmax(d, SC_LOW), p, st.t);
+        }
+        if (target >= 0) {
+            if (i <= target && target < i + VALS) {
+#pragma unroll
+                for (int e = 0; e < VALS; e++)
+                    cnt += !(v[e] <= (i + e < target ? thr_before : xt)) & (i + e != target);
+            } else {
+                const float thr = i < target ? thr_before : xt;
+#pragma unroll
+                for (int e = 0; e < VALS; e++) cnt += !(v[e] <= thr);
+            }
+        }
+    }
+    __device__ void scan() {
+        constexpr int U = 4;
+        const int tid = threadIdx.x;
+        const int nv = (hi - lo) / V;
+        st = SoftState{-INF, 0.f, 0.f};
+        cnt = 0;
+        int i = tid;
+        for (; i + (U - 1) * NT < nv; i += U * NT) {
+            float v[U][V];
+#pragma unroll
+            for (int u = 0; u < U; u++) load<T, V>(x + lo + (i + u * NT) * V, v[u]);
+#pragma unroll
+            for (int u = 0; u < U; u++) add(v[u], lo + (i + u * NT) * V);
+        }
+        for (; i < nv; i += NT) {
+            float v[V];
+            load<T, V>(x + lo + i * V, v);
+            add(v, lo + i * V);
+        }
+        i = lo + nv * V + tid;
+        if (i < hi) {
+            float v[1] = {widen(x[i])};
+            add(v, i);
+        }
+        if (target >= 0 && xt != xt) {           // only NaN stands beside NaN
+            cnt = 0;
+            for (int j = lo + tid; j < hi && j < target; j += NT) {
+                const float v = widen(x[j]);
+                cnt += v != v;
+            }
+        }
+    }
+    // f(value, index) for every element this thread scanned
+    template <typename F> __device__ __forceinline__ void again(F f) {
+        const int nv = (hi - lo) / V;
+        for (int i = threadIdx.x; i < nv; i += NT) {
+            float v[V];
+            load<T, V>(x + lo + i * V, v);
+#pragma unroll
+            for (int e = 0; e < V; e++) f(v[e], lo + i * V + e);
+        }
+        const int i = lo + nv * V + threadIdx.x;
+        if (i < hi) f(widen(x[i]), i);
+    }
+    // Joins the threads' states; every thread returns with the whole.
+    __device__ void join(Lds &l, SoftState &all, int &count) {
+        SoftState a = st;
+        int c = cnt;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) {
+            SoftState b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)};
+            soft_join(a, b);
+            c += __shfl_xor(c, o);
+        }
+        if constexpr (NW > 1) {
+            const int w = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) {
+                l.st[w] = a;
+                l.cnt[w] = c;
+            }
+            __syncthreads();
+            a = l.st[0];
+            c = l.cnt[0];
+#pragma unroll
+            for (int i = 1; i < NW; i++) {
+                soft_join(a, l.st[i]);
+                c += l.cnt[i];
+            }
+        }
+        all = a;
+        count = c;
+    }
+    // The k best entries in descending order to out(rank, key), fewer if the
+    // range holds fewer that are not -inf; returns how many.
+    template <typename F> __device__ int top(Lds &l, int k, F out) {
+        const int tid = threadIdx.x, lane = tid & 63;
+        // (a thread with a NaN or +inf takes part whatever its maximum)
+        const bool odd = st.s != st.s;
+        float g = st.m;
+#pragma unroll
+        for (int o = NW / 2; o; o >>= 1) g = vmax(g, __shfl_xor(g, o));
+        if (tid == 0) l.found = 0;
+        if constexpr (NW > 1) {
+            if (lane % NW == 0) l.gmax[tid / NW] = g;
+            __syncthreads();
+            g = l.gmax[lane];
+        } else {
+            __syncthreads();
+        }
+        const float T0 = kth_of_lanes(g, k);
+        if (st.m >= T0 || odd)
+            again([&](float v, int i) {
+                if (!(v < T0) && v != -INF) {
+                    const int at = atomicAdd(&l.found, 1);
+                    if (at < SC_CAP) l.key[at] = order_key(v, i);
+                }
+            });
+        __syncthreads();
+        const int n = l.found;
+        if (n <= SC_CAP) {
+            for (int i = tid; i < n; i += NT) {
+                const uint64_t mine = l.key[i];
+                int r = 0;
+                for (int j = 0; j < n; j++) r += l.key[j] > mine;
+                if (r < k) out(r, mine);
+            }
+            return n < k ? n : k;
+        }
+        // More values than places at or above T0 (many equal ones): the best
+        // of what is left, one by one.
+        uint64_t last = ~0ull;
+        for (int r = 0; r < k; r++) {
+            uint64_t b = 0;
+            again([&](float v, int i) {
+                if (!(v < T0) && v != -INF) {
+                    const uint64_t q = order_key(v, i);
+                    if (q < last && q > b) b = q;
+                }
+            });
+#pragma unroll
+            for (int o = 32; o; o >>= 1) {
+                const uint64_t q = shfl_xor_key(b, o);
+                b = q > b ? q : b;
+            }
+            if constexpr (NW > 1) {
+                if (lane == 0) l.best[tid >> 6] = b;
+                __syncthreads();
+                b = l.best[0];
+                for (int i = 1; i < NW; i++) b = l.best[i] > b ? l.best[i] : b;
+                __syncthreads();
+            }
+            last = b;
+            if (tid == 0) out(r, b);
+        }
+        return k;
+    }
+};
+
+// What the outputs of a row are, given its joined state.
+__device__ __forceinline__ float soft_lse(SoftState a) {
+    if (a.m == -INF && a.s == 0.f) return -INF;
+    return a.m + LN2 * __builtin_amdgcn_logf(a.s);
+}
+// log p of a logit: about the maximum, so a row far from zero (one of the
+// type's lowest values, say) keeps its digits, which x - lse would lose.
+__device__ __forceinline__ float soft_logprob(SoftState a, float x) {
+    return (x - a.m) - LN2 * __builtin_amdgcn_logf(a.s);
+}
+__device__ __forceinline__ void write_scores(const ScoreArgs &a, int64_t row, SoftState s,
+                                             int count, int target, float xt) {
+    const bool empty = s.m == -INF && s.s == 0.f;
+    const float lse = soft_lse(s);
+    if (a.lse) a.lse[row] = lse;
+    if (a.entropy)
+        a.entropy[row] = empty ? 0.f : LN2 * __builtin_amdgcn_logf(s.s) - s.t / s.s;
+    if (a.logprob) a.logprob[row] = target < 0 ? 0.f : empty ? -INF : soft_logprob(s, xt);
+    if (a.rank) a.rank[row] = target < 0 ? -1 : count;
+}
+
+struct ScorePlan { int splits, chunk; };
+// A split's share in the workspace: m, s, t, rank count, then top_k keys.
+__host__ __device__ inline size_t score_part_bytes(int k) { return 16 + 8 * (size_t)k; }
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void token_scores(ScoreArgs a, ScorePlan p) {
+    typedef ScorePart<T, NT> Part;
+    __shared__ typename Part::Lds l;
+    const int64_t row = blockIdx.x / p.splits;
+    const int split = blockIdx.x % p.splits;
+    const int tid = threadIdx.x;
+    Part w;
+    w.x = (const T *)a.x + row * a.ld;
+    w.lo = split * p.chunk;
+    w.hi = a.vocab - w.lo < p.chunk ? a.vocab : w.lo + p.chunk;
+    int target = a.target ? a.target[row] : -1;
+    if (target >= a.vocab) target = -1;
+    w.xt = target >= 0 ? widen(w.x[target]) : 0.f;
+    w.target = a.rank ? target : -1;
+    w.thr_before = below(w.xt);
+    w.scan();
+    SoftState all;
+    int count;
+    w.join(l, all, count);
+    if (p.splits > 1) {
+        char *part = (char *)a.ws + blockIdx.x * score_part_bytes(a.top_k);
+        if (tid == 0) {
+            float *f = (float *)part;
+            f[0] = all.m;
+            f[1] = all.s;
+            f[2] = all.t;
+            ((int *)part)[3] = count;
+        }
+        if (a.top_k) {
+            uint64_t *keys = (uint64_t *)(part + 16);
+            const int n = w.top(l, a.top_k, [&](int r, uint64_t q) { keys[r] = q; });
+            for (int i = n + tid; i < a.top_k; i += NT) keys[i] = 0;
+        }
+        return;
+    }
+    if (tid == 0) write_scores(a, row, all, count, target, w.xt);
+    if (a.top_k) {
+        int32_t *ids = a.ids + row * a.top_k;
+        float *tops = a.tops + row * a.top_k;
+        const int n = w.top(l, a.top_k, [&](int r, uint64_t q) {
+            const int i = key_index(q);
+            ids[r] = i;
+            tops[r] = soft_logprob(all, widen(w.x[i]));
+        });
+        for (int i = n + tid; i < a.top_k; i += NT) {
+            ids[i] = -1;
+            tops[i] = -INF;
+        }
+    }
+}
+
+// Joins the splits of a row (one workgroup a row).  Every split's list is
+// sorted, so the k best of all hold at most as many of a list as stand
+// before its first miss: a list's entry counts the entries above it by a
+// binary search in every list.
+constexpr int SC_MAX_SPLITS = 64;
+template <typename T>
+__global__ __launch_bounds__(256) void token_scores_join(ScoreArgs a, ScorePlan p) {
+    __shared__ uint64_t keys[SC_MAX_SPLITS * SCORES_MAX_K];
+    __shared__ int found;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, k = a.top_k;
+    const size_t bytes = score_part_bytes(k);
+    const char *part = (const char *)a.ws + row * p.splits * bytes;
+    SoftState all{-INF, 0.f, 0.f};
+    int count = 0;
+    {
+        const int lane = tid & 63;
+        if (lane < p.splits) {
+            const float *f = (const float *)(part + lane * bytes);
+            all = SoftState{f[0], f[1], f[2]};
+            count = ((const int *)f)[3];
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) {
+            SoftState b{__shfl_xor(all.m, o), __shfl_xor(all.s, o), __shfl_xor(all.t, o)};
+            soft_join(all, b);
+            count += __shfl_xor(count, o);
+        }
+    }
+    const T *x = (const T *)a.x + row * a.ld;
+    if (tid == 0) {
+        int target = a.target ? a.target[row] : -1;
+        if (target >= a.vocab) target = -1;
+        write_scores(a, row, all, count, target, target >= 0 ? widen(x[target]) : 0.f);
+    }
+    if (!k) return;
+    if (tid == 0) found = 0;
+    for (int i = tid; i < p.splits * k; i += 256)
+        keys[i] = ((const uint64_t *)(part + i / k * bytes + 16))[i % k];
+    __syncthreads();
+    int32_t *ids = a.ids + row * k;
+    float *tops = a.tops + row * k;
+    for (int i = tid; i < p.splits * k; i += 256) {
+        const uint64_t mine = keys[i];
+        int r = i % k;                           // those above it in its list
+        if (!mine) continue;
+        for (int s = 0; s < p.splits && r < k; s++) {
+            if (s == i / k) continue;
+            const uint64_t *list = keys + s * k;
+            int lo = 0, hi = k;                  // entries > mine: list[0 .. lo)
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (list[mid] > mine) lo = mid + 1;
+                else hi = mid;
+            }
+            r += lo;
+        }
+        if (r < k) {
+            const int at = key_index(mine);
+            ids[r] = at;
+            tops[r] = soft_logprob(all, widen(x[at]));
+            atomicAdd(&found, 1);
+        }
+    }
+    __syncthreads();
+    for (int i = found + tid; i < k; i += 256) {
+        ids[i] = -1;
+        tops[i] = -INF;
+    }
+}
+
+static int score_threads(const ScoreArgs &a) {
+    return a.vocab <= 4096 ? 64 : a.vocab <= 16384 ? 256 : 512;
+}
+static ScorePlan score_plan(const ScoreArgs &a) {
+    ScorePlan p{1, a.vocab};
+    if (score_threads(a) < 512) return p;
+    // one workgroup a row leaves CUs idle below 512 rows: shares of 4096
+    // elements at least
+    const int64_t want = a.rows > 0 ? 512 / a.rows : 1;
+    int64_t s = a.vocab / 4096;
+    if (s > want) s = want;
+    if (s > SC_MAX_SPLITS) s = SC_MAX_SPLITS;
+    if (s < 2) return p;
+    p.chunk = (int)((a.vocab + s - 1) / s + 7) / 8 * 8;
+    p.splits = (a.vocab + p.chunk - 1) / p.chunk;
+    return p;
+}
+size_t scores_workspace(const ScoreArgs &a) {
+    const ScorePlan p = score_plan(a);
+    return p.splits > 1 ? a.rows * p.splits * score_part_bytes(a.top_k) : 0;
+}
+hipError_t launch_scores(const ScoreArgs &a, hipStream_t st) {
+    if (a.rows == 0) return hipSuccess;
+    const ScorePlan p = score_plan(a);
+    const dim3 grid((unsigned)(a.rows * p.splits));
+    return by_type(a.type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        const int nt = score_threads(a);
+        hipError_t e = nt == 64 ? start(token_scores<T, 64>, grid, 64, st, a, p)
+                     : nt == 256 ? start(token_scores<T, 256>, grid, 256, st, a, p)
+                                 : start(token_scores<T, 512>, grid, 512, st, a, p);
+        if (e != hipSuccess || p.splits == 1) return e;
+        return start(token_scores_join<T>, dim3((unsigned)a.rows), 256, st, a, p);
+    });
+}
+
+// Gradient of the scores:
+//   dx_i = p_i (g_lse - g_lp - g_H (log p_i + H)) + [i = target] g_lp
+// one read and one write of the row; dx may be x.
+template <typename T>
+__global__ __launch_bounds__(256) void token_scores_grad(ScoreArgs a, int parts) {
+    constexpr int V = 16 / (int)sizeof(T), U = 4;
+    const int64_t row = blockIdx.x / parts;
+    const int lo = (int)(blockIdx.x % parts) * (256 * V * U);
+    const T *x = (const T *)a.x + row * a.ld;
+    T *dx = (T *)a.dx + row * a.ldd;
+    int target = a.target ? a.target[row] : -1;
+    if (target >= a.vocab) target = -1;
+    const float lse0 = a.lse[row];
+    const bool empty = lse0 == -INF;
+    const float lse = empty ? 0.f : lse0;
+    const float glp = target >= 0 && a.g_logprob && !empty ? a.g_logprob[row] : 0.f;
+    const float gh = a.g_entropy ? a.g_entropy[row] : 0.f;
+    const float c = (a.g_lse ? a.g_lse[row] : 0.f) - glp -
+                    (a.g_entropy ? gh * a.entropy[row] : 0.f);
+    auto one = [&](float v, int i) {
+        const float lp = v - lse;
+        const float g = exp_hw(lp) * __builtin_fmaf(-gh, vmax(lp, SC_LOW), c);
+        return i == target ? g + glp : g;
+    };
+    if (lo + 256 * V * U <= a.vocab) {
+        float v[U][V];
+#pragma unroll
+        for (int u = 0; u < U; u++) load<T, V>(x + lo + (u * 256 + threadIdx.x) * V, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int i = lo + (u * 256 + threadIdx.x) * V;
+#pragma unroll
+            for (int e = 0; e < V; e++) v[u][e] = one(v[u][e], i + e);
+            store<T, V>(dx + i, v[u]);
+        }
+        return;
+    }
+    const int nv = (a.vocab - lo) / V;
+    for (int j = threadIdx.x; j < nv; j += 256) {
+        float v[V];
+        load<T, V>(x + lo + j * V, v);
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] = one(v[e], lo + j * V + e);
+        store<T, V>(dx + lo + j * V, v);
+    }
+    const int i = lo + nv * V + threadIdx.x;
+    if (i < a.vocab) dx[i] = narrow<T>(one(widen(x[i]), i));
+}
+hipError_t launch_scores_backward(const ScoreArgs &a, hipStream_t st) {
+    if (a.rows == 0) return hipSuccess;
+    return by_type(a.type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        constexpr int PER = 256 * 4 * (16 / (int)sizeof(T));
+        const int parts = (a.vocab + PER - 1) / PER;
+        return start(token_scores_grad<T>, dim3((unsigned)(a.rows * parts)), 256, st, a, parts);
+    });
+}
+
+}  // namespace ops
+}  // namespace ctc

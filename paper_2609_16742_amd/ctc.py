@@ -32,12 +32,13 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 CTC_OK, CTC_ERR_ARG, CTC_ERR_UNSUPPORTED, CTC_ERR_DEVICE, \
     CTC_ERR_WORKSPACE, CTC_ERR_STATE = 0, -1, -2, -3, -4, -5
-CTC_F32, CTC_F16 = 0, 1
+CTC_F32, CTC_F16, CTC_BF16, CTC_E4M3, CTC_E5M2 = range(5)
 CTC_ROLE_NONE, CTC_ROLE_SUM, CTC_ROLE_ZERO, CTC_ROLE_PASS = 0, 1, 2, 3
 CTC_OP_CONV, CTC_OP_MAXPOOL, CTC_OP_GAP, CTC_OP_FC = 1, 2, 3, 4
 CTC_REEXEC_NONE, CTC_REEXEC_SYNC, CTC_REEXEC_DEFERRED = 0, 1, 2
 CTC_SITE_WEIGHT, CTC_SITE_BIAS, CTC_SITE_BN_MEAN, CTC_SITE_BN_VAR, \
     CTC_SITE_BN_GAMMA, CTC_SITE_BN_BETA, CTC_SITE_ACT = range(7)
+CTC_ACT_NONE, CTC_ACT_RELU, CTC_ACT_SILU = 0, 1, 2
 DTYPES = {"f32": CTC_F32, "f16": CTC_F16}
 
 CTC_PROTECT_NONE, CTC_PROTECT_REPLACE, CTC_PROTECT_APPEND = 0, 1, 2
@@ -55,6 +56,11 @@ EXPORTS = ["ctc_build_filters", "ctc_build_fc", "ctc_threshold_from_samples",
            "ctc_net_role",
            "ctc_net_profile", "ctc_net_profile_read", "ctc_net_op_kernel",
            "ctc_graph_create", "ctc_graph_launch", "ctc_graph_destroy",
+           "ctc_group_norm_forward", "ctc_group_norm_backward",
+           "ctc_group_norm_workspace_bytes", "ctc_fp8_quantize",
+           "ctc_fp8_matmul", "ctc_fp8_matmul_workspace_bytes",
+           "ctc_token_scores_forward", "ctc_token_scores_backward",
+           "ctc_token_scores_workspace_bytes",
            "ctc_net_destroy", "ctc_last_error", "ctc_abi_version"]
 
 
@@ -146,6 +152,25 @@ _sig("ctc_net_op_kernel", [_P, _I32, _I32, ctypes.c_char_p, _I32])
 _sig("ctc_graph_create", [_P, _I32, _I32, _P, _P, _P, ctypes.POINTER(_P)])
 _sig("ctc_graph_launch", [_P, _I32, ctypes.POINTER(_I32), _P])
 _sig("ctc_graph_destroy", [_P], None)
+_sig("ctc_group_norm_forward", [_I32, _I32, _I64, _I32, _I32, _I32, _P, _P, _P,
+                                _P, _F32, _I32, _P, _P, _P, _P, _SZ, _P])
+_sig("ctc_group_norm_backward", [_I32, _I32, _I64, _I32, _I32, _I32] +
+     [_P] * 7 + [_I32] + [_P] * 5 + [_SZ, _P])
+_sig("ctc_group_norm_workspace_bytes", [_I32, _I32, _I64, _I32, _I32, _I32,
+                                        ctypes.POINTER(_SZ)])
+_sig("ctc_fp8_quantize", [_I32, _I64, _I64, _P, _I64, _I32, _I32, _I32, _P,
+                          _I64, _P, _I64, _P])
+_sig("ctc_fp8_matmul", [_I32, _I32, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64,
+                        _I32, _P, _I64, _P, _I64, _I32, _P, _I32, _P, _I64,
+                        _P, _SZ, _P])
+_sig("ctc_fp8_matmul_workspace_bytes", [_I32, _I64, _I64, _I64,
+                                        ctypes.POINTER(_SZ)])
+_sig("ctc_token_scores_forward", [_I32, _I64, _I32, _P, _I64, _P, _I32] +
+     [_P] * 7 + [_SZ, _P])
+_sig("ctc_token_scores_backward", [_I32, _I64, _I32, _P, _I64] + [_P] * 7 +
+     [_I64, _P])
+_sig("ctc_token_scores_workspace_bytes", [_I64, _I32, _I32,
+                                          ctypes.POINTER(_SZ)])
 _sig("ctc_net_destroy", [_P], None)
 _sig("ctc_last_error", [], ctypes.c_char_p)
 _sig("ctc_abi_version", [], _I32)
@@ -414,6 +439,56 @@ def ctc_net_op_kernel(net, i, nimg):
 
 def ctc_net_destroy(net):
     _lib.ctc_net_destroy(net)
+
+
+# ------------------------------- operators around a protected classifier
+# Pointers (tensors' data_ptr() or None), sizes and the raw stream, in the
+# C order; the ``ops`` module takes tensors.
+
+def ctc_group_norm_forward(*args):
+    _check(_lib.ctc_group_norm_forward(*args))
+
+
+def ctc_group_norm_backward(*args):
+    _check(_lib.ctc_group_norm_backward(*args))
+
+
+def ctc_group_norm_workspace_bytes(dtype, n, hw, c, groups, backward):
+    b = _SZ()
+    _check(_lib.ctc_group_norm_workspace_bytes(dtype, n, hw, c, groups,
+                                               int(backward),
+                                               ctypes.byref(b)))
+    return b.value
+
+
+def ctc_fp8_quantize(*args):
+    _check(_lib.ctc_fp8_quantize(*args))
+
+
+def ctc_fp8_matmul(*args):
+    _check(_lib.ctc_fp8_matmul(*args))
+
+
+def ctc_fp8_matmul_workspace_bytes(ytype, m, n, k):
+    b = _SZ()
+    _check(_lib.ctc_fp8_matmul_workspace_bytes(ytype, m, n, k,
+                                               ctypes.byref(b)))
+    return b.value
+
+
+def ctc_token_scores_forward(*args):
+    _check(_lib.ctc_token_scores_forward(*args))
+
+
+def ctc_token_scores_backward(*args):
+    _check(_lib.ctc_token_scores_backward(*args))
+
+
+def ctc_token_scores_workspace_bytes(rows, vocab, top_k):
+    b = _SZ()
+    _check(_lib.ctc_token_scores_workspace_bytes(rows, vocab, top_k,
+                                                 ctypes.byref(b)))
+    return b.value
 
 
 # -------------------------------------------------- network description

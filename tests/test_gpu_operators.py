@@ -1,0 +1,798 @@
+"""The operators around a protected classifier against plain 64-bit forms:
+group norm, 8-bit quantiser and product, token scores, with their gradients.
+
+Tolerances follow from the arithmetic: fp32 sums of n terms in sequence are
+off by n * 2^-24 of the sum of magnitudes at most, a result is rounded once
+to its type (2^-24, 2^-11 or 2^-8 of it), the hardware's exp and log by a few
+2^-23.
+"""
+
+import itertools
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 0.0, "f16": 2.0 ** -25, "bf16": 0.0}     # half a subnormal step
+F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_16742_amd import ops
+    return ops
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, device="cuda", generator=g)
+
+
+def _within(got, want, bound, what):
+    """|got - want| <= bound elementwise; NaN and infinities agree."""
+    got, want = got.double(), want.double()
+    bound = torch.as_tensor(bound, dtype=torch.float64, device=got.device)
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    assert torch.equal(got[~fine].nan_to_num(0), want[~fine].nan_to_num(0)), what
+    off = (got - want).abs()
+    over = fine & ~(off <= bound)
+    if bool(over.any()):
+        b = bound.expand_as(off)
+        i = int((off / b.clamp(min=1e-300)).masked_fill(~over, 0).argmax())
+        raise AssertionError("%s: %d of %d off, worst at %d: %.9g for %.9g, bound %.3g" % (
+            what, int(over.sum()), over.numel(), i, got.flatten()[i],
+            want.flatten()[i], b.flatten()[i]))
+
+
+# -------------------------------------------------------------- group norm
+
+# n, pixels, channels, groups: one value, one pixel, vectors of every width,
+# groups narrower than a vector and not a multiple of one, one channel a
+# group, more channel vectors than a workgroup has threads, long maps
+MAPS = [(1, 1, 1, 1), (1, 1, 8, 8), (1, 1, 64, 4), (2, 49, 512, 32),
+        (3, 35, 12, 4), (2, 31, 30, 5), (2, 17, 33, 11), (5, 9, 24, 8),
+        (1, 5000, 24, 3), (2, 6, 2064, 8), (1, 3, 4112, 16), (3, 196, 40, 40),
+        (2, 3137, 64, 16), (1, 12545, 8, 1), (130, 4, 16, 4)]
+
+
+def _norm_case(shape, dtype, seed, offset=0):
+    n, hw, c, groups = shape
+    g = _gen(seed)
+
+    def make(scale=1.0):
+        v = (_randn(g, n, hw, c) * scale).to(DT[dtype])
+        if not offset:
+            return v
+        store = torch.empty(v.numel() + offset, dtype=v.dtype, device="cuda")
+        store[offset:].copy_(v.flatten())
+        return store[offset:].view(n, hw, c)
+    x = make(1.5)
+    return (x, make(), make(), 0.5 + torch.rand(c, device="cuda", generator=g),
+            0.3 * _randn(g, c))
+
+
+def _norm_ref(x, groups, gamma, beta, residual, act, carry, eps):
+    """(z, y, mean, rstd, xhat, count) in 64 bits."""
+    n, hw, c = x.shape
+    x = x.double()
+    v = x.view(n, hw, groups, c // groups)
+    use = torch.ones(groups, c // groups, dtype=torch.float64, device=x.device)
+    if carry:
+        use[-1, -1] = 0
+    count = (use.sum(1) * hw)
+    den = count.clamp(min=1)
+    mean = (v * use).sum((1, 3)) / den
+    d = (v - mean[:, None, :, None])
+    var = (d * d * use).sum((1, 3)) / den
+    rstd = 1 / torch.sqrt(var + eps)
+    xhat = (d * rstd[:, None, :, None]).view(n, hw, c)
+    z = xhat
+    if gamma is not None:
+        z = z * gamma.double()
+    if beta is not None:
+        z = z + beta.double()
+    if carry:
+        z = torch.cat([z[..., :-1], x[..., -1:]], -1)
+    if residual is not None:
+        z = z + residual.double()
+    y = z
+    if act == "relu":
+        y = torch.where(z < 0, torch.zeros_like(z), z)
+    elif act == "silu":
+        y = z * torch.sigmoid(z)
+    if carry:
+        y = torch.cat([y[..., :-1], z[..., -1:]], -1)
+    return z, y, mean, rstd, xhat, den
+
+
+def _norm_grad_ref(dy, x, groups, gamma, beta, residual, act, carry, eps):
+    z, _, _, rstd, xhat, den = _norm_ref(x, groups, gamma, beta, residual, act,
+                                         carry, eps)
+    n, hw, c = x.shape
+    dz = dy.double()
+    if act == "relu":
+        d = (z > 0).double()
+    elif act == "silu":
+        s = torch.sigmoid(z)
+        d = s + z * s * (1 - s)
+    else:
+        d = torch.ones_like(z)
+    if carry:
+        d[..., -1] = 1
+    dz = dz * d
+    use = dz.clone()
+    if carry:
+        use[..., -1] = 0
+    dn = use * gamma.double() if gamma is not None else use
+    sh = (n, hw, groups, c // groups)
+    m1 = (dn.view(sh).sum((1, 3)) / den)[:, None, :, None]
+    m2 = ((dn * xhat).view(sh).sum((1, 3)) / den)[:, None, :, None]
+    dx = ((dn.view(sh) - m1 - xhat.view(sh) * m2) * rstd[:, None, :, None]).view(n, hw, c)
+    size = ((dn.abs().view(sh) + (dn.abs().view(sh).sum((1, 3)) / den)[:, None, :, None] +
+             xhat.abs().view(sh) * ((dn * xhat).abs().view(sh).sum((1, 3)) / den)
+             [:, None, :, None]) * rstd[:, None, :, None]).view(n, hw, c)
+    if carry:
+        dx = torch.cat([dx[..., :-1], dz[..., -1:]], -1)
+    return dx, dz, (use * xhat).sum((0, 1)), use.sum((0, 1)), size, use, xhat
+
+
+# longest fp32 sum in sequence: pixels of a thread, pixel lanes, entries of a
+# wave when chunks and channels are joined
+SEQ = 1024
+
+
+@pytest.mark.parametrize("shape", MAPS, ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_group_norm(ops, shape, dtype):
+    """Every activation, residual, checksum and affine form; the statistics,
+    the map, in place, and from an address of one element past alignment."""
+    n, hw, c, groups = shape
+    for i, (act, res, carry, affine) in enumerate(
+            [("none", 0, 0, 0), ("relu", 1, 0, 1), ("silu", 0, 0, 1), ("relu", 1, 1, 1),
+             ("silu", 1, 1, 0)]):
+        x, r, _, gamma, beta = _norm_case(shape, dtype, 10 * i + c, offset=i % 2)
+        gamma, beta = (gamma, beta) if affine else (None, None)
+        r = r if res else None
+        y, mean, rstd = ops.group_norm(x, groups, gamma, beta, r, act, bool(carry))
+        _, wy, wm, wr, xhat, _ = _norm_ref(x, groups, gamma, beta, r, act, carry, 1e-5)
+        what = (shape, dtype, act, res, carry)
+        spread = 1 / wr                                      # >= deviation
+        u = 2.0 ** -24
+        _within(mean, wm, SEQ * u * (wm.abs() + spread), what)
+        _within(rstd, wr, wr * SEQ * u, what)
+        size = 1 + xhat.abs()
+        if affine:
+            size = size * gamma.double().abs() + beta.double().abs()
+        if res:
+            size = size + r.double().abs()
+        if carry:
+            size = size.clone()
+            size[..., -1] = wy[..., -1].abs()
+        _within(y, wy, 2 * SEQ * u * size + HALF_ULP[dtype] * wy.abs() + TINY[dtype], what)
+        if carry and not res:
+            assert torch.equal(y[..., -1], x[..., -1])
+        # in place on x (and the residual): the same bits
+        xc = x.clone()
+        y2, _, _ = ops.group_norm(xc, groups, gamma, beta, r, act, bool(carry),
+                                  out=(xc, mean.clone(), rstd.clone()))
+        assert y2.data_ptr() == xc.data_ptr()
+        y3 = ops.group_norm(x.clone(), groups, gamma, beta, r, act, bool(carry))[0]
+        assert torch.equal(y2.nan_to_num(7), y3.nan_to_num(7)), what
+
+
+@pytest.mark.parametrize("shape", MAPS, ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_group_norm_backward(ops, shape, dtype):
+    n, hw, c, groups = shape
+    u = 2.0 ** -24
+    for i, (act, res, carry, affine) in enumerate(
+            [("none", 0, 0, 0), ("silu", 0, 0, 1), ("silu", 1, 1, 1), ("relu", 1, 1, 1)]):
+        x, r, dy, gamma, beta = _norm_case(shape, dtype, 10 * i + c + 1, offset=i % 2)
+        gamma, beta = (gamma, beta) if affine else (None, None)
+        r = r if res else None
+        z, _, mean, rstd, _, _ = _norm_ref(x, groups, gamma, beta, r, act, carry, 1e-5)
+        if act == "relu":
+            # away from the kink, which side a rounded z is on is certain
+            dy = torch.where(z.abs() < 1e-3, torch.zeros_like(dy), dy)
+        mean, rstd = mean.float(), rstd.float()
+        dx, dr, dgamma, dbeta = ops.group_norm_backward(
+            dy, x, mean, rstd, groups, gamma, beta, r, act, bool(carry))
+        wx, wr, wg, wb, size, use, xhat = _norm_grad_ref(dy, x, groups, gamma, beta, r, act,
+                                                         carry, 1e-5)
+        what = (shape, dtype, act, res, carry)
+        # (silu' is at most 1.1 and moves by at most 0.5 a unit of z)
+        size = 2 * size * (1 + z.abs()) + wx.abs()
+        _within(dx, wx, 2 * SEQ * u * size + HALF_ULP[dtype] * wx.abs() + TINY[dtype], what)
+        if res:
+            _within(dr, wr, 16 * u * (1 + z.abs()) * (1 + dy.double().abs()) +
+                    HALF_ULP[dtype] * wr.abs() + TINY[dtype], what)
+        else:
+            assert dr is None
+        zz = 1 + z.abs()
+        _within(dgamma, wg, 4 * SEQ * u * (use.abs() * (1 + xhat.abs()) * zz).sum((0, 1)), what)
+        _within(dbeta, wb, 4 * SEQ * u * (use.abs() * zz).sum((0, 1)), what)
+        if carry:
+            assert float(dgamma[-1]) == 0 and float(dbeta[-1]) == 0
+            assert torch.equal(dx[..., -1], dy[..., -1])
+        # the same bits again, and in place on dy
+        again = ops.group_norm_backward(dy, x, mean, rstd, groups, gamma, beta, r, act,
+                                        bool(carry))
+        for a, b in zip(again, (dx, dr, dgamma, dbeta)):
+            assert a is None and b is None or torch.equal(a, b), what
+        d2 = dy.clone()
+        ops.group_norm_backward(d2, x, mean, rstd, groups, gamma, beta, r, act, bool(carry),
+                                out=(d2, None, None, None))
+        assert torch.equal(d2, dx), what
+
+
+@pytest.mark.parametrize("carry", [False, True])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_group_norm_gradient_against_differences(ops, act, carry):
+    """sum w y along a direction: central differences of the 64-bit form."""
+    shape = (2, 23, 24, 4)
+    x, r, w, gamma, beta = _norm_case(shape, "f32", 5)
+    z, _, mean, rstd, _, _ = _norm_ref(x, 4, gamma, beta, r, act, carry, 1e-5)
+    dx, dr, dgamma, dbeta = ops.group_norm_backward(
+        w, x, mean.float(), rstd.float(), 4, gamma, beta, r, act, carry)
+    g = _gen(6)
+    for k, (p, d) in enumerate([(x, dx), (r, dr), (gamma, dgamma), (beta, dbeta)]):
+        v = torch.randn(p.shape, device="cuda", generator=g, dtype=torch.float64)
+        h = 1e-5
+
+        def at(s):
+            q = [t.double() for t in (x, r, gamma, beta)]
+            q[k] = q[k] + s * v
+            return float((_norm_ref(q[0], 4, q[2], q[3], q[1], act, carry, 1e-5)[1]
+                          * w.double()).sum())
+        want = (at(h) - at(-h)) / (2 * h)
+        got = float((d.double() * v).sum())
+        size = float((d.double() * v).abs().sum())
+        assert abs(got - want) <= 1e-5 * size + 1e-6, (k, got, want)
+
+
+@pytest.mark.parametrize("shape", [(2, 49, 64, 8), (1, 5000, 24, 3)], ids=str)
+def test_group_norm_far_from_zero(ops, shape):
+    """A mean 10^4 deviations away: values are multiples of 2^-10 about 1000,
+    so the deviations are exact and only their sums are rounded."""
+    n, hw, c, groups = shape
+    g = _gen(9)
+    x = 1000 + torch.round(_randn(g, n, hw, c) * 100) / 1024
+    y, mean, rstd = ops.group_norm(x, groups)
+    _, wy, wm, wr, xhat, _ = _norm_ref(x, groups, None, None, None, "none", False, 1e-5)
+    # the mean is rounded to fp32 (2^-24 of 1000): 6e-4 of a deviation
+    off = 2 * 2.0 ** -24 * 1000 * wr
+    _within(mean, wm, 2 * 2.0 ** -24 * 1000, "mean")
+    _within(rstd, wr, wr * (1e-4 + off * off), "rstd")
+    _within(y.view(n, -1, groups, c // groups), wy.view(n, -1, groups, c // groups),
+            (off[:, None, :, None] + 2e-4) * (1 + xhat.view(n, -1, groups, c // groups).abs()),
+            "y")
+
+
+def test_group_norm_spoiled_group_stays_alone(ops):
+    for shape in [(2, 49, 64, 8), (1, 5000, 24, 3)]:
+        n, hw, c, groups = shape
+        x = _randn(_gen(3), n, hw, c)
+        x[0, 7, 0] = float("nan")
+        x[0, 9, c - 1] = float("inf")
+        y, mean, rstd = ops.group_norm(x, groups, act="relu")
+        bad = torch.isnan(y).view(n, hw, groups, c // groups).all(3).all(1)
+        want = torch.zeros_like(bad)
+        want[0, 0] = want[0, groups - 1] = True
+        assert torch.equal(bad, want)
+        assert int(torch.isnan(y).sum()) == 2 * hw * (c // groups)
+
+
+# --------------------------------------------------------------- quantiser
+
+def _quantize_ref(x, qtype, block_rows):
+    """On the CPU, in the fp32 operations the header states."""
+    most = {"e4m3": 448.0, "e5m2": 57344.0}[qtype]
+    x = x.float().cpu()
+    rows, cols = x.shape
+    kb, rb = -(-cols // 128), -(-rows // block_rows)
+    q = torch.empty((rows, cols), dtype=F8[qtype])
+    scales = torch.empty((kb, rb))
+    for i, j in itertools.product(range(kb), range(rb)):
+        rs, cs = slice(j * block_rows, (j + 1) * block_rows), slice(i * 128, (i + 1) * 128)
+        amax = x[rs, cs].abs().max().clamp(min=2.0 ** -100)
+        scales[i, j] = amax / most
+        q[rs, cs] = (x[rs, cs] * (torch.tensor(most) / amax)).to(F8[qtype])
+    return q, scales
+
+
+def _same_bytes(a, b):
+    """Equal 8-bit patterns, NaN patterns of either sign alike."""
+    x, y = a.float().cpu(), b.float().cpu()
+    same = (a.cpu().contiguous().view(torch.uint8) ==
+            b.cpu().contiguous().view(torch.uint8)) | (torch.isnan(x) & torch.isnan(y))
+    return bool(same.all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (17, 127), (130, 40),
+                                       (129, 257), (64, 320), (5, 1000), (260, 16)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_quantize(ops, rows, cols, dtype):
+    """Bits of values and scales, every form, contiguous and strided."""
+    for qtype, block, tr in itertools.product(["e4m3", "e5m2"], [1, 128], [False, True]):
+        g = _gen(rows * cols + block)
+        wide = _randn(g, rows, cols + 3) * torch.exp(2 * _randn(g, rows, 1))
+        x = wide.to(DT[dtype])[:, 1:1 + cols]
+        if block == 1:
+            x = x.contiguous()
+        q, s = ops.fp8_quantize(x, qtype, block, transpose=tr)
+        wq, ws = _quantize_ref(x.t() if tr else x, qtype, block)
+        what = (rows, cols, dtype, qtype, block, tr)
+        assert torch.equal(s.cpu(), ws), what
+        assert _same_bytes(q, wq), what
+
+
+@pytest.mark.parametrize("block,tr", [(1, False), (128, False), (1, True), (128, True)])
+def test_quantize_special_blocks(ops, block, tr):
+    """Zeros, magnitudes below 2^-100, the largest numbers, NaN, infinity:
+    each in a block of its own."""
+    x = _randn(_gen(1), 128 * 6, 128)
+    x[:128] = 0
+    x[128:256] *= 1e-38
+    x[256:384] *= 1e37
+    x[384 + 5, 3] = float("nan")
+    x[512 + 5, 3] = float("-inf")
+    x[640:768] = 2.0 ** -110
+    if tr:
+        x = x.t().contiguous()
+    q, s = ops.fp8_quantize(x, "e4m3", block, transpose=tr)
+    t = x.t() if tr else x
+    r = torch.arange(768, device="cuda") // block
+    s0 = s[0][r]
+    bad = ~torch.isfinite(t).all(1) if block == 1 else \
+        (r == 3) | (r == 4)
+    assert bool((~torch.isfinite(s0))[bad].all()) and bool(torch.isfinite(s0)[~bad].all())
+    v = q.float() * s0[:, None]
+    assert bool(torch.isnan(v)[bad].all())
+    assert not bool(torch.isnan(v)[~bad].any())
+    assert bool((v[:256] == 0).all())
+    # 2^-110 against 2^-100: 448 * 2^-10 is an e4m3 value, so it comes back
+    assert bool((v[640:] == 2.0 ** -110).all())
+    big = v[256:384]
+    # half a step of e4m3: 2^-4 of a value, 2^-10 steps below the least normal
+    amax = t[256:384].abs().amax(1 if block == 1 else None, keepdim=True)
+    assert bool(((big - t[256:384]).abs() <= t[256:384].abs() / 16 + amax * 2.0 ** -18).all())
+
+
+# ----------------------------------------------------------------- product
+
+def _bytes(g, rows, cols, qtype, pad=0, special=False):
+    """Random finite 8-bit values; what stands behind the columns is NaN."""
+    ld = -(-cols // 16) * 16 + pad
+    v = torch.randn((rows, ld), device="cuda", generator=g) * 30
+    q = v.to(F8[qtype])
+    raw = q.view(torch.uint8)
+    raw[:, cols:] = 0x7f                         # NaN in both types
+    return q[:, :cols]
+
+
+def _largest_products(a, sa, b, sb, ab, bb, k):
+    """Sum over the blocks of the largest product a block can hold, scaled."""
+    tot = 0.0
+    for i in range(-(-k // 128)):
+        ks = slice(i * 128, min(k, (i + 1) * 128))
+        ta = a[:, ks].double().abs().amax(1) * sa[i].double().repeat_interleave(ab)[:a.shape[0]]
+        tb = b[:, ks].double().abs().amax(1) * sb[i].double().repeat_interleave(bb)[:b.shape[0]]
+        tot = tot + ta[:, None] * tb
+    return tot
+
+
+def _product_ref(a, sa, b, sb, ab, bb, k):
+    ea = sa.double().t().repeat_interleave(128, 1)[:, :k]
+    eb = sb.double().t().repeat_interleave(128, 1)[:, :k]
+    if ab == 128:
+        ea = ea.repeat_interleave(128, 0)[:a.shape[0]]
+    if bb == 128:
+        eb = eb.repeat_interleave(128, 0)[:b.shape[0]]
+    A, B = a.double() * ea, b.double() * eb
+    return A @ B.t().contiguous(), A.abs() @ B.abs().t().contiguous()
+
+
+def _check_product(ops, m, n, k, at="e4m3", bt="e4m3", ab=1, bb=128, ydt="f32", bias=False,
+                   act="none", pad=0, seed=0, ypad=0):
+    g = _gen(1000 * m + 10 * n + k + seed)
+    a, b = _bytes(g, m, k, at, pad), _bytes(g, n, k, bt, 2 * pad)
+    kb = -(-k // 128)
+    sa = torch.exp(_randn(g, kb, -(-m // ab))) / 30
+    sb = torch.exp(_randn(g, kb, -(-n // bb))) / 30 / math.sqrt(max(k, 1))
+    bv = _randn(g, n) if bias else None
+    out = torch.full((m, n + ypad), 7.0, dtype=DT[ydt], device="cuda")
+    y = ops.fp8_matmul(a, sa, b, sb, bias=bv, act=act, out=out[:, :n])
+    want, size = _product_ref(a, sa, b, sb, ab, bb, k)
+    if bias:
+        want, size = want + bv.double(), size + bv.double().abs()
+    if act == "relu":
+        want = want.clamp(min=0)
+    elif act == "silu":
+        want = want * torch.sigmoid(want)
+    # a block's 128 products in the matrix unit (each addition within 2^-23),
+    # then the blocks' scaled sums
+    bound = (128 + 2 * kb + 16) * 2.0 ** -23 * size
+    if ydt != "f32":
+        # 16-bit results: the matrix unit drops what lies more than 13 bits
+        # below a block's largest product
+        bound = bound + 128 * 2.0 ** -13 * _largest_products(a, sa, b, sb, ab, bb, k)
+        # (one by one that is wide; as a whole the drops average out)
+        off = float((y.double() - want).norm())
+        assert off <= (2.0 ** -12 * float(size.norm()) +
+                       (HALF_ULP[ydt] + 2.0 ** -20) * float(want.norm()) +
+                       TINY[ydt] * y.numel()), (m, n, k, off)
+    if act == "silu":
+        bound = bound * 1.1 + 2.0 ** -20 * want.abs()
+    _within(y, want, bound + HALF_ULP[ydt] * want.abs() + TINY[ydt] + 1e-30,
+            (m, n, k, at, bt, ab, bb, ydt, act, pad))
+    assert bool((out[:, n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("m", [1, 5, 16, 17, 33, 64, 65, 130, 300])
+@pytest.mark.parametrize("k", [1, 15, 16, 17, 127, 128, 129, 320, 1000])
+def test_product_sizes(ops, m, k):
+    for n, ydt in [(1, "f32"), (10, "f16"), (130, "bf16"), (257, "f32")]:
+        _check_product(ops, m, n, k, ydt=ydt, bias=n > 1, ypad=n % 3)
+
+
+@pytest.mark.parametrize("at", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("bt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("ab", [1, 128])
+@pytest.mark.parametrize("bb", [1, 128])
+def test_product_types_and_scales(ops, at, bt, ab, bb):
+    for m, n, k in [(3, 40, 260), (40, 200, 500), (200, 136, 400), (260, 520, 144)]:
+        for act in ("none", "relu", "silu"):
+            _check_product(ops, m, n, k, at, bt, ab, bb, "f16", True, act, pad=16)
+
+
+@pytest.mark.parametrize("bb", [1, 128])
+@pytest.mark.parametrize("m,n,k", [(3601, 3540, 200), (1, 1001, 4096), (32, 512, 25088),
+                                   (1280, 320, 6272), (65, 64, 12000), (300, 129, 5000),
+                                   (20000, 70, 130), (70, 20000, 130), (1025, 2049, 257)])
+def test_product_large(ops, m, n, k, bb):
+    """Every tile, and sums of k that are split over workgroups."""
+    _check_product(ops, m, n, k, bb=bb, ydt="f32", bias=True, act="relu")
+
+
+def test_product_without_a_sum(ops):
+    _check_product(ops, 5, 7, 0, bias=True)
+    _check_product(ops, 300, 7, 0, bias=True, ydt="f16")
+    e = torch.empty
+    z = ops.fp8_matmul(e((0, 128), dtype=F8["e4m3"], device="cuda"), e((1, 0), device="cuda"),
+                       e((4, 128), dtype=F8["e4m3"], device="cuda"), e((1, 4), device="cuda"))
+    assert z.shape == (0, 4)
+
+
+@pytest.mark.parametrize("m", [3, 100, 400])
+def test_product_shows_spoiled_blocks(ops, m):
+    """A NaN value spoils its row of y, an infinite scale its row too, and
+    nothing else."""
+    n, k = 300, 700
+    g = _gen(m)
+    a, b = _bytes(g, m, k, "e4m3"), _bytes(g, n, k, "e4m3")
+    sa, sb = torch.rand((6, m), device="cuda") + 0.1, torch.rand((6, 3), device="cuda") + 0.1
+    a.view(torch.uint8)[1, 650] = 0x7f
+    sa[2, 2] = float("nan")
+    y = ops.fp8_matmul(a, sa, b, sb, dtype=torch.float32)
+    bad = torch.isnan(y)
+    want = torch.zeros_like(bad)
+    want[1:3] = True
+    assert torch.equal(bad, want)
+
+
+# ------------------------------------------------------------------ scores
+
+def _scores_ref(x, targets, k):
+    """In 64 bits on the CPU; order by value (NaN first), then index."""
+    x = x.double().cpu().numpy()
+    rows, vocab = x.shape
+    out = {"lse": np.empty(rows), "entropy": np.empty(rows), "logprob": np.zeros(rows),
+           "rank": np.full(rows, -1, np.int32), "top_ids": np.full((rows, k), -1, np.int32),
+           "top_logprobs": np.full((rows, k), -np.inf)}
+    for r in range(rows):
+        v = x[r]
+        t = -1 if targets is None else int(targets[r])
+        if np.isnan(v).any() or (v == np.inf).any():
+            lse = ent = np.nan
+            lp = v * np.nan
+        elif (v == -np.inf).all():
+            lse, ent = -np.inf, 0.0
+            lp = v
+        else:
+            m = v.max()
+            with np.errstate(over="ignore"):
+                e = np.exp(v - m)
+            lse = m + np.log(e.sum())
+            with np.errstate(invalid="ignore", over="ignore"):
+                lp = (v - m) - np.log(e.sum())
+                ent = -np.where(e > 0, e / e.sum() * lp, 0.0).sum()
+        out["lse"][r], out["entropy"][r] = lse, ent
+        key = np.where(np.isnan(v), np.inf, v)
+        nan = np.isnan(v)
+        order = np.lexsort((np.arange(vocab), -key, ~nan))
+        if 0 <= t < vocab:
+            out["logprob"][r] = np.nan if np.isnan(lse) else \
+                -np.inf if lse == -np.inf else lp[t]
+            out["rank"][r] = int(np.nonzero(order == t)[0][0])
+        if k:
+            top = [i for i in order[:k] if v[i] != -np.inf]
+            out["top_ids"][r, :len(top)] = top
+            out["top_logprobs"][r, :len(top)] = np.nan if np.isnan(lse) else lp[top]
+    return {n: torch.from_numpy(a) for n, a in out.items()}
+
+
+def _check_scores(ops, x, targets, k, what):
+    got = ops.token_scores(x, targets, k)
+    want = _scores_ref(x, targets, k)
+    vocab = x.shape[1]
+    # terms a thread adds in sequence, the joins, exp and log of the hardware
+    n = vocab / 64 if vocab <= 4096 else vocab / 256 if vocab <= 16384 else vocab / 512
+    rel = (n + 64) * 2.0 ** -24 + 2.0 ** -20
+    tol = rel + 4 * 2.0 ** -23 * want["lse"].abs().nan_to_num(0, 0, 0)
+    _within(got.lse.cpu(), want["lse"], tol, what)
+    _within(got.entropy.cpu(), want["entropy"],
+            2 * rel * (2 + want["entropy"].abs().nan_to_num(0)), what)
+    if targets is not None:
+        lp = want["logprob"].abs().nan_to_num(0, 0, 0)
+        _within(got.logprob.cpu(), want["logprob"], tol + 2.0 ** -23 * lp, what)
+        assert torch.equal(got.rank.cpu(), want["rank"]), what
+    else:
+        assert got.logprob is None and got.rank is None
+    if k:
+        assert torch.equal(got.top_ids.cpu(), want["top_ids"]), what
+        lp = want["top_logprobs"].abs().nan_to_num(0, 0, 0)
+        _within(got.top_logprobs.cpu(), want["top_logprobs"],
+                tol[:, None] + 2.0 ** -23 * lp, what)
+    return got
+
+
+VOCABS = [1, 2, 7, 10, 63, 64, 65, 513, 1000, 4096, 4097, 16385, 100003]
+
+
+@pytest.mark.parametrize("vocab", VOCABS)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_token_scores(ops, vocab, dtype):
+    """Random logits, strided rows, with and without targets, every k."""
+    for rows, pad, k in [(1, 0, 1), (5, 1, 5), (7, 3, 32), (3, 0, 0)]:
+        g = _gen(vocab + rows)
+        x = (3 * _randn(g, rows, vocab + pad)).to(DT[dtype])[:, :vocab]
+        t = torch.randint(0, vocab, (rows,), device="cuda", generator=g, dtype=torch.int32)
+        t[rows // 2] = [-1, vocab, -7][rows % 3] if rows > 1 else 0
+        _check_scores(ops, x, t, k, (vocab, dtype, rows, k))
+        if rows == 3:
+            _check_scores(ops, x, None, 20, (vocab, dtype))
+
+
+@pytest.mark.parametrize("vocab", [5, 100, 1000, 5000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_token_scores_masks_and_ties(ops, vocab, dtype):
+    """Barred tokens, rows that bar everything, rows of the type's lowest
+    value, rows of equal values (more of them than are collected), rising and
+    falling rows, few values, NaN and infinities of both signs."""
+    g = _gen(vocab)
+    dt = DT[dtype]
+    low = torch.finfo(dt).min
+    x = (3 * _randn(g, 16, vocab)).to(dt)
+    x[0, torch.rand(vocab, device="cuda", generator=g) < 0.5] = -math.inf
+    x[1] = -math.inf
+    x[2] = low
+    x[3] = 0.25
+    x[4] = -math.inf
+    x[4, vocab // 2] = 1.0
+    x[5] = low
+    x[5, vocab - 1] = 0.0
+    x[6] = torch.arange(vocab, device="cuda").to(dt)
+    x[7] = torch.arange(vocab, 0, -1, device="cuda").to(dt)
+    x[8] = torch.randint(-1, 2, (vocab,), device="cuda", generator=g).to(dt)
+    x[9] = torch.where(torch.rand(vocab, device="cuda", generator=g) < 0.5, 0.0, -0.0).to(dt)
+    x[10, vocab // 3] = math.nan
+    x[11, vocab // 3] = math.inf
+    x[12, vocab // 3] = -math.nan
+    x[12, vocab - 1] = math.inf
+    x[13] = math.nan
+    x[14, :vocab // 2] = math.inf
+    x[15] = x[15] * 0 - 60.0
+    x[15, 0] = 60.0
+    for at in (0, vocab // 3, vocab // 2, vocab - 1):
+        t = torch.full((16,), at, device="cuda", dtype=torch.int32)
+        _check_scores(ops, x, t, 5 if at else 32, (vocab, dtype, at))
+    # one row at a time: rows that are shared out over workgroups
+    for r in range(16):
+        t = torch.full((1,), vocab // 3, device="cuda", dtype=torch.int32)
+        _check_scores(ops, x[r:r + 1], t, 20, (vocab, dtype, "row", r))
+
+
+def test_token_scores_long_rows(ops):
+    """131072 tokens: one row over many workgroups, and a row each."""
+    g = _gen(77)
+    for rows in (1, 3, 600):
+        x = (2.5 * _randn(g, rows, 131072)).to(torch.bfloat16)
+        t = torch.randint(0, 131072, (rows,), device="cuda", generator=g, dtype=torch.int32)
+        got = ops.token_scores(x, t, 20)
+        pick = [0, rows // 2, rows - 1]
+        want = _scores_ref(x[pick], t[pick], 20)
+        assert torch.equal(got.rank[pick].cpu(), want["rank"])
+        assert torch.equal(got.top_ids[pick].cpu(), want["top_ids"])
+        _within(got.lse[pick].cpu(), want["lse"], 4e-5, rows)
+
+
+def _scores_grad_ref(x, t, g_lse, g_lp, g_h):
+    x = x.double()
+    lse = torch.logsumexp(x, 1, keepdim=True)
+    empty = lse == -math.inf
+    lp = torch.where(empty, torch.full_like(x, -math.inf), x - lse)
+    p = torch.exp(lp)
+    h = -torch.where(p > 0, p * lp, torch.zeros_like(p)).sum(1, keepdim=True)
+    ok = (t >= 0) & (t < x.shape[1])
+    zero = torch.zeros_like(lse[:, 0])
+    glp = zero if g_lp is None else torch.where(ok & ~empty[:, 0], g_lp.double(), zero)
+    gl = zero if g_lse is None else g_lse.double()
+    gh = zero if g_h is None else g_h.double()
+    inner = torch.where(p > 0, lp, torch.zeros_like(lp)) + h
+    dx = p * (gl[:, None] - glp[:, None] - gh[:, None] * inner)
+    size = p * (gl.abs()[:, None] + glp.abs()[:, None] +
+                gh.abs()[:, None] * (inner.abs() + h.abs() + 1))
+    one = torch.zeros_like(p)
+    one.scatter_(1, t.clamp(0, x.shape[1] - 1).long()[:, None], 1.0)
+    dx = dx + one * glp[:, None]
+    return dx, (size + one * glp.abs()[:, None]) * (1 + lp.abs().nan_to_num(0, 0, 0)), lse, h
+
+
+@pytest.mark.parametrize("vocab", [1, 10, 1000, 4097, 8200, 32001])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_token_scores_backward(ops, vocab, dtype):
+    for form in range(4):
+        g = _gen(vocab + form)
+        rows, pad = 5, form
+        full = (2 * _randn(g, rows, vocab + pad)).to(DT[dtype])
+        x = full[:, :vocab]
+        if vocab > 4:
+            x[1, ::3] = -math.inf
+            x[2] = -math.inf
+            x[3] = torch.finfo(DT[dtype]).min
+        t = torch.randint(0, vocab, (rows,), device="cuda", generator=g, dtype=torch.int32)
+        t[4] = -1
+        gs = [_randn(g, rows) if form in on else None for on in ((0, 1), (0, 2, 3), (0, 3))]
+        want, size, lse, h = _scores_grad_ref(x, t, *gs)
+        lse32, h32 = lse[:, 0].float(), h[:, 0].float()
+        got = ops.token_scores_backward(x, t, lse32, h32, *gs)
+        # p is off by the rounding of lse and of the exponent's argument
+        rel = 2.0 ** -21 + 2.0 ** -23 * lse.abs().nan_to_num(0, 0, 0)
+        _within(got, want, rel * size + HALF_ULP[dtype] * want.abs() + TINY[dtype],
+                (vocab, dtype, form))
+        inplace = ops.token_scores_backward(x, t, lse32, h32, *gs, out=x)
+        assert torch.equal(inplace, got)
+
+
+def test_token_scores_gradient_against_differences(ops):
+    g = _gen(4)
+    x = 2 * _randn(g, 4, 300)
+    t = torch.tensor([3, 0, -1, 299], device="cuda", dtype=torch.int32)
+    gs = [_randn(g, 4) for _ in range(3)]
+    r = ops.token_scores(x, t)
+    d = ops.token_scores_backward(x, t, r.lse, r.entropy, *gs)
+    v = torch.randn(x.shape, device="cuda", generator=g, dtype=torch.float64)
+
+    def at(s):
+        w = _scores_ref(x.double() + s * v, t, 0)
+        return float(sum((w[n].cuda() * c.double()).sum() for n, c in
+                         zip(("lse", "logprob", "entropy"), gs)))
+    want = (at(1e-5) - at(-1e-5)) / 2e-5
+    got = float((d.double() * v).sum())
+    assert abs(got - want) <= 1e-5 * float((d.double() * v).abs().sum()) + 1e-6
+
+
+# ----------------------------------------------------- streams and refusals
+
+def test_operators_on_another_stream(ops):
+    """Work queued on a side stream behind the inputs' own: the results of
+    the current stream, with workspaces allocated per call."""
+    g = _gen(8)
+    side = torch.cuda.Stream()
+    x = _randn(g, 4, 900, 64)
+    logits = _randn(g, 2, 100000)
+    t = torch.tensor([5, 99999], device="cuda", dtype=torch.int32)
+    qa, sa = ops.fp8_quantize(_randn(g, 8, 9000))
+    qb, sb = ops.fp8_quantize(_randn(g, 64, 9000), block_rows=128)
+    want = [ops.group_norm(x, 8)[0], ops.token_scores(logits, t, 4).top_ids,
+            ops.fp8_matmul(qa, sa, qb, sb)]
+    torch.cuda.synchronize()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [ops.group_norm(x, 8, stream=side)[0],
+           ops.token_scores(logits, t, 4, stream=side).top_ids,
+           ops.fp8_matmul(qa, sa, qb, sb, stream=side)]
+    junk = [torch.full((1 << 20,), 9.0, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    assert len(junk) == 4
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_operators_in_a_graph(ops):
+    """Captured once with caller-owned outputs, replayed on new inputs with
+    eager work in between."""
+    g = _gen(12)
+    x = _randn(g, 2, 196, 256)
+    w = _randn(g, 100, 256) / 16
+    t = torch.tensor([1, 50], device="cuda", dtype=torch.int32)
+    qw, sw = ops.fp8_quantize(w, block_rows=128)
+
+    def chain():
+        y, _, _ = ops.group_norm(x, 32, act="silu")
+        qa, sa = ops.fp8_quantize(y.view(-1, 256))
+        z = ops.fp8_matmul(qa, sa, qw, sw, dtype=torch.float32)
+        r = ops.token_scores(z[:2], t, 3)
+        return z, r.logprob, r.top_ids
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = chain()
+    for i in range(4):
+        x.copy_(_randn(g, 2, 196, 256) + i)
+        want = [v.clone() for v in chain()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured, want):
+            assert torch.equal(a, b), i
+
+
+def test_operators_refuse(ops):
+    x = torch.zeros((2, 4, 8), device="cuda")
+    f8 = torch.zeros((4, 32), device="cuda").to(F8["e4m3"])
+    s1 = torch.ones((1, 4), device="cuda")
+    refused = [
+        lambda: ops.group_norm(x, 3),
+        lambda: ops.group_norm(x.double(), 2),
+        lambda: ops.group_norm(x.cpu(), 2),
+        lambda: ops.group_norm(x[:, ::2], 2),
+        lambda: ops.group_norm(x, 2, gamma=torch.ones(7, device="cuda")),
+        lambda: ops.group_norm(x, 2, residual=x.half()),
+        lambda: ops.group_norm(x, 2, act="tanh"),
+        lambda: ops.group_norm_backward(x, x, s1, s1, 2),
+        lambda: ops.fp8_quantize(x),
+        lambda: ops.fp8_quantize(x[0], qtype="e3m4"),
+        lambda: ops.fp8_quantize(x[0], block_rows=64),
+        lambda: ops.fp8_quantize(x[0].t()),
+        lambda: ops.fp8_matmul(f8, s1, f8[:, :16].contiguous(), s1),
+        lambda: ops.fp8_matmul(f8[:, 1:], s1, f8[:, 1:], s1),
+        lambda: ops.fp8_matmul(f8, s1[:, :3], f8, s1),
+        lambda: ops.fp8_matmul(f8, s1, f8, s1, bias=torch.ones(3, device="cuda")),
+        lambda: ops.fp8_matmul(f8, s1, f8, s1, dtype=torch.int32),
+        # a last row that ends before a multiple of 16 bytes
+        lambda: ops.fp8_matmul(torch.zeros(3 * 32 + 17, device="cuda").to(F8["e4m3"])
+                               .as_strided((4, 17), (32, 1)), s1, f8[:, :17], s1),
+        lambda: ops.token_scores(x),
+        lambda: ops.token_scores(x[0], torch.zeros(4, device="cuda", dtype=torch.int64)),
+        lambda: ops.token_scores(x[0].t()),
+        lambda: ops.token_scores_backward(x[0], None, None),
+        lambda: ops.token_scores_backward(x[0], None, s1[0], out=x[0].half()),
+    ]
+    for i, f in enumerate(refused):
+        with pytest.raises(ValueError):
+            f()
+            raise AssertionError("accepted: %d" % i)
+    from paper_2609_16742_amd import ctc
+    for f in (lambda: ops.token_scores(x[0], top_k=33),
+              lambda: ops.group_norm(x, 2, eps=-1.0),
+              lambda: ops.token_scores_backward(x[0], None, s1[0], g_logprob=s1[0])):
+        with pytest.raises(ctc.CtcError) as e:
+            f()
+        assert e.value.status == ctc.CTC_ERR_ARG
