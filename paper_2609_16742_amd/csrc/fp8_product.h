@@ -78,8 +78,7 @@ __device__ __forceinline__ u4 first_bytes(u4 v, int n) {
 #pragma unroll
     for (int e = 0; e < 4; e++) {
         const int b = n - 4 * e;
-        if (b <= 0) v[e] = 0;
-        else if (b < 4) v[e] &= (1u << (8 * b)) - 1;
+        v[e] = b >= 4 ? v[e] : b <= 0 ? 0 : v[e] & ((1u << (8 * (b & 3))) - 1);
     }
     return v;
 }
@@ -227,32 +226,37 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int 
     const int lchunk = ((lane & 7) ^ (lane >> 3)) * 16;
     const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
     const int kend = (int)p.k;
+    // (a tile's rows span less than 2^31 bytes: PAST stays past the end with
+    // a row offset added)
     auto issue = [&](int step, int st) {
         const int k0 = step * 128;
         const bool ok = k0 + lchunk < kend;
+        const int av = ok ? ao + k0 : PAST, bv = ok ? bo + k0 : PAST;
+        const int arow = NW * 8 * (int)p.lda, brow = NW * 8 * (int)p.ldb;
 #pragma unroll
         for (int i = 0; i < AR; i++)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                ar, (LdsAt)(lds + st * STAGE + (i * NW + wave) * 1024), 16,
-                ok ? ao + i * NW * 8 * (int)p.lda + k0 : PAST, 0, 0, 0);
+                ar, (LdsAt)(lds + st * STAGE + (i * NW + wave) * 1024), 16, av + i * arow, 0, 0,
+                0);
 #pragma unroll
         for (int i = 0; i < BR; i++)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 br, (LdsAt)(lds + st * STAGE + BM * 128 + (i * NW + wave) * 1024), 16,
-                ok ? bo + i * NW * 8 * (int)p.ldb + k0 : PAST, 0, 0, 0);
+                bv + i * brow, 0, 0, 0);
     };
     // scales: a's of a lane's IM columns; b's one of the wave's filters (a
     // wave's lie in one block of 128), or, SB1, the tile's through LDS
-    int64_t sai[IM], sbi;
+    const int ash = p.a_block == 1 ? 0 : 7, bsh = p.b_block == 1 ? 0 : 7;
+    const float *sab = p.sa + (m0 >> ash), *sbb = p.sb + (n0 >> bsh);
+    uint32_t sai[IM], sbi;
 #pragma unroll
     for (int j = 0; j < IM; j++) {
-        const int64_t m = m0 + wm * TM + j * 16 + fr < p.m ? m0 + wm * TM + j * 16 + fr : p.m - 1;
-        sai[j] = p.a_block == 1 ? m : m / 128;
+        const int r = wm * TM + j * 16 + fr;
+        sai[j] = (uint32_t)(((int64_t)(r < ma ? r : ma - 1) + m0 >> ash) - (m0 >> ash));
     }
     {
-        const int64_t n = n0 + (SB1 ? (int)threadIdx.x % BN : wn * TN);
-        const int64_t q = n < p.n ? n : p.n - 1;
-        sbi = p.b_block == 1 ? q : q / 128;
+        const int r = SB1 ? (int)threadIdx.x % BN : wn * TN;
+        sbi = (uint32_t)(((int64_t)(r < nb ? r : nb - 1) + n0 >> bsh) - (n0 >> bsh));
     }
     const int nblocks = (int)((p.k + 127) / 128);
     const int first = split * per;
@@ -262,70 +266,94 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int 
     for (int i = 0; i < IN; i++)
 #pragma unroll
         for (int j = 0; j < IM; j++) acc[i][j] = (f4)(0.f);
-    float sa[IM], san[IM], sb = 0.f, sbn = 0.f;
+    float sa[IM], san[IM], sbn = 0.f;
     auto scales = [&](int step) {
 #pragma unroll
-        for (int j = 0; j < IM; j++) san[j] = p.sa[step * p.ldsa + sai[j]];
-        sbn = p.sb[step * p.ldsb + sbi];
+        for (int j = 0; j < IM; j++) san[j] = (sab + step * p.ldsa)[sai[j]];
+        sbn = (sbb + step * p.ldsb)[sbi];
     };
     if (first < last) {
         scales(first);
         issue(first, 0);
     }
     const int c0 = (fg ^ (fr & 7)) * 16, c1 = ((fg + 4) ^ (fr & 7)) * 16;
-    for (int step = first; step < last; step++) {
+    const int abase = (wm * TM + fr) * 128, bbase = BM * 128 + (wn * TN + fr) * 128;
+    typedef typename std::conditional<WIDE, Wide, i8v>::type Frag;
+    // RAG: the last block of a k that is no multiple of 16
+    auto compute = [&](auto ragc, int step, int st) {
+        constexpr bool RAG = decltype(ragc)::value;
+        const int left = kend - step * 128 - fg * 16;
+        auto frag = [&](int at) {
+            u4 lo = *(const u4 *)(lds + st * STAGE + at + c0);
+            u4 hi = *(const u4 *)(lds + st * STAGE + at + c1);
+            if constexpr (RAG) {
+                lo = first_bytes(lo, left);
+                hi = first_bytes(hi, left - 64);
+            }
+            return chunks(lo, hi);
+        };
+        auto wide = [&](auto fc, i8v v) {
+            if constexpr (WIDE) return widen_block<decltype(fc)::value>(v);
+            else return v;
+        };
+        typedef std::integral_constant<int, FA> TA;
+        typedef std::integral_constant<int, FB> TB;
+        Frag x[IM];
+#pragma unroll
+        for (int j = 0; j < IM; j++) x[j] = wide(TA(), frag(abase + j * 2048));
+        i8v w = frag(bbase);
+        // The results of filter tile i are scaled and added while the MFMAs
+        // of tile i + 1 run.
+        f4 d[2][IM];
+#pragma unroll
+        for (int i = 0; i <= IN; i++) {
+            if (i < IN) {
+                const Frag wf = wide(TB(), w);
+                if (i + 1 < IN) w = frag(bbase + (i + 1) * 2048);
+#pragma unroll
+                for (int j = 0; j < IM; j++) {
+                    if constexpr (WIDE) d[i & 1][j] = mfma_wide(wf, x[j]);
+                    else d[i & 1][j] = mfma_block<FA, FB>(wf, x[j]);
+                }
+            }
+            if (i > 0) {
+                f4 s4 = (f4)(1.f);
+                if constexpr (SB1)
+                    s4 = *(const f4 *)(sbl[st] + wn * TN + (i - 1) * 16 + fg * 4);
+#pragma unroll
+                for (int j = 0; j < IM; j++) {
+                    if constexpr (SB1) d[(i - 1) & 1][j] *= s4;
+                    acc[i - 1][j] += d[(i - 1) & 1][j] * sa[j];
+                }
+            }
+            if constexpr (!WIDE) {
+#pragma unroll
+                for (int j = 0; j < IM; j++) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // MFMA
+                    __builtin_amdgcn_sched_group_barrier(0x002, SB1 ? 8 : 4, 0);   // VALU
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    auto block = [&](auto ragc, int step) {
         const int st = (step - first) & 1;
 #pragma unroll
-        for (int j = 0; j < IM; j++) sa[j] = san[j];
-        sb = sbn;
+        for (int j = 0; j < IM; j++) sa[j] = SB1 ? san[j] : san[j] * sbn;
         if constexpr (SB1)
-            if (threadIdx.x < BN) sbl[st][threadIdx.x] = sb;
+            if (threadIdx.x < BN) sbl[st][threadIdx.x] = sbn;
         __builtin_amdgcn_s_waitcnt(0);           // this wave's rows are in LDS
         __syncthreads();                         // everyone's; the other stage is read out
         if (step + 1 < last) {
             scales(step + 1);
             issue(step + 1, st ^ 1);
         }
-        const char *A = lds + st * STAGE + (wm * TM + fr) * 128;
-        const char *B = lds + st * STAGE + BM * 128 + (wn * TN + fr) * 128;
-        const bool ragged = step * 128 + 128 > kend && (kend & 15);
-        const int left = kend - step * 128 - fg * 16;
-        typename std::conditional<WIDE, Wide, i8v>::type x[IM];
-#pragma unroll
-        for (int j = 0; j < IM; j++) {
-            u4 lo = *(const u4 *)(A + j * 2048 + c0), hi = *(const u4 *)(A + j * 2048 + c1);
-            if (ragged) {
-                lo = first_bytes(lo, left);
-                hi = first_bytes(hi, left - 64);
-            }
-            if constexpr (WIDE) x[j] = widen_block<FA>(chunks(lo, hi));
-            else x[j] = chunks(lo, hi);
-        }
-        if constexpr (!SB1)
-#pragma unroll
-            for (int j = 0; j < IM; j++) sa[j] *= sb;
-#pragma unroll
-        for (int i = 0; i < IN; i++) {
-            u4 lo = *(const u4 *)(B + i * 2048 + c0), hi = *(const u4 *)(B + i * 2048 + c1);
-            if (ragged) {
-                lo = first_bytes(lo, left);
-                hi = first_bytes(hi, left - 64);
-            }
-            typename std::conditional<WIDE, Wide, i8v>::type w;
-            if constexpr (WIDE) w = widen_block<FB>(chunks(lo, hi));
-            else w = chunks(lo, hi);
-            f4 s4 = (f4)(1.f);
-            if constexpr (SB1) s4 = *(const f4 *)(sbl[st] + wn * TN + i * 16 + fg * 4);
-#pragma unroll
-            for (int j = 0; j < IM; j++) {
-                f4 d;
-                if constexpr (WIDE) d = mfma_wide(w, x[j]);
-                else d = mfma_block<FA, FB>(w, x[j]);
-                if constexpr (SB1) d *= s4;
-                acc[i][j] += d * sa[j];
-            }
-        }
-    }
+        compute(ragc, step, st);
+    };
+    const int whole = (kend & 15) && last == nblocks ? last - 1 : last;
+    int step = first;
+    for (; step < whole; step++) block(std::false_type(), step);
+    if (step < last) block(std::true_type(), step);
 #pragma unroll
     for (int j = 0; j < IM; j++)
 #pragma unroll
