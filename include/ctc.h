@@ -677,7 +677,8 @@ ctc_status ctc_fp8_matmul(ctc_dtype atype, ctc_dtype btype, ctc_dtype ytype,
 /* Workspace of ctc_fp8_matmul (partial sums of a split k).  Host,
  * synchronous. */
 ctc_status ctc_fp8_matmul_workspace_bytes(ctc_dtype ytype, int64_t m, int64_t n,
-                                          int64_t k, size_t *bytes);
+                                          int64_t k, int32_t b_block,
+                                          size_t *bytes);
 
 /* Scores of rows of logits x: lse = log sum_i exp(x_i), the log probability
  * of a given class or token x_t - lse, the entropy of the row's distribution

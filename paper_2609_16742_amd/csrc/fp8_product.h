@@ -195,23 +195,28 @@ __global__ __launch_bounds__(512) void product_rows(ProductArgs p, int splits, i
 // slot g ^ (r & 7), which spreads the fragment reads over the banks.
 // ---------------------------------------------------------------------------
 template <int BM, int BN, int WM, int WN, int FA, int FB, bool SB1, bool WIDE>
-__global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int mt, int nt,
+__global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, int mt, int nt,
                                                              int splits, int per) {
     constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN;
     constexpr int IM = TM / 16, IN = TN / 16;
     constexpr int AR = BM / 8 / NW, BR = BN / 8 / NW;    // loads of a wave a step
     constexpr int STAGE = (BM + BN) * 128;
-    static_assert(AR * 8 * NW == BM && BR * 8 * NW == BN && 128 % TN == 0, "tile");
+    constexpr int DQ = IN >= 8 ? 2 : 4;          // loads sent between two groups
+    static_assert((AR + BR) % DQ == 0 && (AR + BR) / DQ <= IN, "loads");
+    static_assert(AR * 8 * NW == BM && BR * 8 * NW == BN && 128 % TN == 0 && IN % 2 == 0, "tile");
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
-    __shared__ __attribute__((aligned(16))) float sbl[2][SB1 ? BN : 4];
+    __shared__ __attribute__((aligned(16))) float sbl[3][SB1 ? BN : 4];
     // each XCD runs a contiguous range of tiles (workgroups go round the
-    // eight XCDs), the filters' tiles of the same rows next to each other
+    // eight XCDs), which goes down four tiles of rows, then along the filters:
+    // 32 tiles at a time share 4 and 8 panels
     const int total = mt * nt * splits, share = (total + 7) / 8;
     int t = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= share || t >= total) return;
     const int split = t / (mt * nt);
     t -= split * (mt * nt);
-    const int64_t m0 = (int64_t)(t / nt) * BM, n0 = (int64_t)(t % nt) * BN;
+    const int group = t / (4 * nt), rows = mt - 4 * group < 4 ? mt - 4 * group : 4;
+    t -= group * 4 * nt;
+    const int64_t m0 = (int64_t)(4 * group + t % rows) * BM, n0 = (int64_t)(t / rows) * BN;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM;
@@ -222,27 +227,30 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int 
                                                      (int)(ma * p.lda), 0x00020000);
     const Buf br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + n0 * p.ldb), 0,
                                                      (int)(nb * p.ldb), 0x00020000);
+    const int nblocks = (int)((p.k + 127) / 128);
+    const int first = split * per;
+    const int last = first + per < nblocks ? first + per : nblocks;
     const int lrow = wave * 8 + (lane >> 3);
     const int lchunk = ((lane & 7) ^ (lane >> 3)) * 16;
     const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
     const int kend = (int)p.k;
-    // (a tile's rows span less than 2^31 bytes: PAST stays past the end with
-    // a row offset added)
-    auto issue = [&](int step, int st) {
+    // Loads q0 .. q1 - 1 of a wave's AR + BR for a step (a tile's rows span
+    // less than 2^31 bytes: PAST stays past the end with a row offset added)
+    auto issue = [&](int step, int st, int q0, int q1) {
         const int k0 = step * 128;
-        const bool ok = k0 + lchunk < kend;
+        const bool ok = step < last && k0 + lchunk < kend;
         const int av = ok ? ao + k0 : PAST, bv = ok ? bo + k0 : PAST;
         const int arow = NW * 8 * (int)p.lda, brow = NW * 8 * (int)p.ldb;
 #pragma unroll
-        for (int i = 0; i < AR; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                ar, (LdsAt)(lds + st * STAGE + (i * NW + wave) * 1024), 16, av + i * arow, 0, 0,
-                0);
-#pragma unroll
-        for (int i = 0; i < BR; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                br, (LdsAt)(lds + st * STAGE + BM * 128 + (i * NW + wave) * 1024), 16,
-                bv + i * brow, 0, 0, 0);
+        for (int q = q0; q < q1; q++) {
+            char *to = lds + st * STAGE + (q * NW + wave) * 1024;
+            if (q < AR)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (LdsAt)to, 16, av + q * arow, 0, 0,
+                                                         0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(br, (LdsAt)to, 16,
+                                                         bv + (q - AR) * brow, 0, 0, 0);
+        }
     };
     // scales: a's of a lane's IM columns; b's one of the wave's filters (a
     // wave's lie in one block of 128), or, SB1, the tile's through LDS
@@ -258,102 +266,145 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tile(ProductArgs p, int 
         const int r = SB1 ? (int)threadIdx.x % BN : wn * TN;
         sbi = (uint32_t)(((int64_t)(r < nb ? r : nb - 1) + n0 >> bsh) - (n0 >> bsh));
     }
-    const int nblocks = (int)((p.k + 127) / 128);
-    const int first = split * per;
-    const int last = first + per < nblocks ? first + per : nblocks;
-    f4 acc[IN][IM];
+    f4 acc[IN][IM], d[2][IM];
 #pragma unroll
-    for (int i = 0; i < IN; i++)
+    for (int j = 0; j < IM; j++) {
 #pragma unroll
-        for (int j = 0; j < IM; j++) acc[i][j] = (f4)(0.f);
-    float sa[IM], san[IM], sbn = 0.f;
+        for (int i = 0; i < IN; i++) acc[i][j] = (f4)(0.f);
+        d[1][j] = (f4)(0.f);
+    }
+    float sa[IM] = {}, san[IM] = {}, sbn = 0.f;
     auto scales = [&](int step) {
 #pragma unroll
         for (int j = 0; j < IM; j++) san[j] = (sab + step * p.ldsa)[sai[j]];
         sbn = (sbb + step * p.ldsb)[sbi];
     };
-    if (first < last) {
-        scales(first);
-        issue(first, 0);
-    }
+    // The last block of a k that is no multiple of 16: zeros behind the end
+    // in the 16 bytes it lies in (a and b: what stands there may be NaN).
+    auto blank = [&](int st) {
+        const int c = (kend & 127) >> 4;
+        for (int r = threadIdx.x; r < BM + BN; r += 64 * NW) {
+            u4 *v = (u4 *)(lds + st * STAGE + r * 128 + ((c ^ (r & 7)) << 4));
+            *v = first_bytes(*v, kend & 15);
+        }
+        __syncthreads();
+    };
+    auto arrived = [&]() {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+    };
     const int c0 = (fg ^ (fr & 7)) * 16, c1 = ((fg + 4) ^ (fr & 7)) * 16;
     const int abase = (wm * TM + fr) * 128, bbase = BM * 128 + (wn * TN + fr) * 128;
+    auto frag = [&](int at) {
+        return chunks(*(const u4 *)(lds + at + c0), *(const u4 *)(lds + at + c1));
+    };
     typedef typename std::conditional<WIDE, Wide, i8v>::type Frag;
-    // RAG: the last block of a k that is no multiple of 16
-    auto compute = [&](auto ragc, int step, int st) {
-        constexpr bool RAG = decltype(ragc)::value;
-        const int left = kend - step * 128 - fg * 16;
-        auto frag = [&](int at) {
-            u4 lo = *(const u4 *)(lds + st * STAGE + at + c0);
-            u4 hi = *(const u4 *)(lds + st * STAGE + at + c1);
-            if constexpr (RAG) {
-                lo = first_bytes(lo, left);
-                hi = first_bytes(hi, left - 64);
-            }
-            return chunks(lo, hi);
-        };
-        auto wide = [&](auto fc, i8v v) {
-            if constexpr (WIDE) return widen_block<decltype(fc)::value>(v);
-            else return v;
-        };
-        typedef std::integral_constant<int, FA> TA;
-        typedef std::integral_constant<int, FB> TB;
-        Frag x[IM];
+    auto afrag = [&](int at) -> Frag {
+        if constexpr (WIDE) return widen_block<FA>(frag(at));
+        else return frag(at);
+    };
+    auto bfrag = [&](i8v v) -> Frag {
+        if constexpr (WIDE) return widen_block<FB>(v);
+        else return v;
+    };
+    Frag x[IM];
+    i8v w;
+    // A step: IN groups of IM MFMAs.  The results of a group are scaled and
+    // added while the next group's MFMAs run, and the next filter fragment
+    // is read.  The one barrier stands before the last group: by then every
+    // wave has read this stage out, so the step after next goes into it, and
+    // the next step's rows have arrived; the last group's MFMAs hide the
+    // reads of the next step's first fragments.  Loads go out a few at a time
+    // between the groups: a wave's MFMAs wait behind a load that finds the
+    // address unit busy (16 clocks for each load of eight waves).
+    if (first < last) {
+        issue(first, 0, 0, AR + BR);
+        scales(first);
+        if constexpr (SB1)
+            if (threadIdx.x < BN) sbl[0][threadIdx.x] = sbn;
+        arrived();
+        issue(first + 1, 1, 0, DQ);
+    }
+    auto begin = [&](int cur) {
 #pragma unroll
-        for (int j = 0; j < IM; j++) x[j] = wide(TA(), frag(abase + j * 2048));
-        i8v w = frag(bbase);
-        // The results of filter tile i are scaled and added while the MFMAs
-        // of tile i + 1 run.
-        f4 d[2][IM];
+        for (int j = 0; j < IM; j++) x[j] = afrag(cur + abase + j * 2048);
+        w = frag(cur + bbase);
+    };
+    begin(0);
+    int slot = 0;                                // of sbl: step modulo 3
+    const bool ragged = (kend & 15) && last == nblocks && first < last;
+    int step = first, stop = ragged ? last - 1 : last;
+    for (;;) {
+    for (; step < stop; step++) {
+        const int cur = ((step - first) & 1) * STAGE, nxt = STAGE - cur;
+        const int before = slot == 0 ? 2 : slot - 1, after = slot == 2 ? 0 : slot + 1;
+        float sp[IM];                            // the scales of the step before
 #pragma unroll
-        for (int i = 0; i <= IN; i++) {
-            if (i < IN) {
-                const Frag wf = wide(TB(), w);
-                if (i + 1 < IN) w = frag(bbase + (i + 1) * 2048);
+        for (int j = 0; j < IM; j++) {
+            sp[j] = sa[j];
+            sa[j] = SB1 ? san[j] : san[j] * sbn;
+        }
+        scales(step + 1 < last ? step + 1 : step);
 #pragma unroll
-                for (int j = 0; j < IM; j++) {
-                    if constexpr (WIDE) d[i & 1][j] = mfma_wide(wf, x[j]);
-                    else d[i & 1][j] = mfma_block<FA, FB>(wf, x[j]);
-                }
-            }
-            if (i > 0) {
-                f4 s4 = (f4)(1.f);
+        for (int i = 0; i < IN; i++) {
+            const bool end = i == IN - 1;
+            if (end) {
                 if constexpr (SB1)
-                    s4 = *(const f4 *)(sbl[st] + wn * TN + (i - 1) * 16 + fg * 4);
-#pragma unroll
-                for (int j = 0; j < IM; j++) {
-                    if constexpr (SB1) d[(i - 1) & 1][j] *= s4;
-                    acc[i - 1][j] += d[(i - 1) & 1][j] * sa[j];
-                }
+                    if (threadIdx.x < BN) sbl[after][threadIdx.x] = sbn;
+                arrived();
             }
-            if constexpr (!WIDE) {
+            // the stage that the barrier freed: DQ loads a group
+            const int q = end ? 0 : (i + 1) * DQ;
+            if (q < AR + BR) issue(step + (end ? 2 : 1), end == (cur != 0), q, q + DQ);
+            const Frag wf = bfrag(w);
+            if (!end) w = frag(cur + bbase + (i + 1) * 2048);
+            f4 s4 = (f4)(1.f);
+            if constexpr (SB1)
+                s4 = *(const f4 *)(sbl[i ? slot : before] + wn * TN + (i ? i - 1 : IN - 1) * 16 +
+                                   fg * 4);
+#pragma unroll
+            for (int j = 0; j < IM; j++) {
+                if constexpr (WIDE) d[i & 1][j] = mfma_wide(wf, x[j]);
+                else d[i & 1][j] = mfma_block<FA, FB>(wf, x[j]);
+                if (end) x[j] = afrag(nxt + abase + j * 2048);
+            }
+            if (end) w = frag(nxt + bbase);
+#pragma unroll
+            for (int j = 0; j < IM; j++) {
+                f4 &r = d[(i & 1) ^ 1][j];
+                if constexpr (SB1) r *= s4;
+                acc[i ? i - 1 : IN - 1][j] += r * (i ? sa[j] : sp[j]);
+            }
+            if constexpr (WIDE) {
+                __builtin_amdgcn_sched_barrier(0);
+            } else {
 #pragma unroll
                 for (int j = 0; j < IM; j++) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // MFMA
+                    if (end) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // LDS reads
                     __builtin_amdgcn_sched_group_barrier(0x002, SB1 ? 8 : 4, 0);   // VALU
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-    };
-    auto block = [&](auto ragc, int step) {
-        const int st = (step - first) & 1;
+        slot = after;
+    }
+    if (stop == last) break;
+    // (its stage has arrived; its first fragments are read again)
+    blank((step - first) & 1);
+    begin(((step - first) & 1) * STAGE);
+    stop = last;
+    }
+    {
+        const int before = slot == 0 ? 2 : slot - 1;
+        f4 s4 = (f4)(1.f);
+        if constexpr (SB1) s4 = *(const f4 *)(sbl[before] + wn * TN + (IN - 1) * 16 + fg * 4);
 #pragma unroll
-        for (int j = 0; j < IM; j++) sa[j] = SB1 ? san[j] : san[j] * sbn;
-        if constexpr (SB1)
-            if (threadIdx.x < BN) sbl[st][threadIdx.x] = sbn;
-        __builtin_amdgcn_s_waitcnt(0);           // this wave's rows are in LDS
-        __syncthreads();                         // everyone's; the other stage is read out
-        if (step + 1 < last) {
-            scales(step + 1);
-            issue(step + 1, st ^ 1);
+        for (int j = 0; j < IM; j++) {
+            if constexpr (SB1) d[1][j] *= s4;
+            if (first < last) acc[IN - 1][j] += d[1][j] * sa[j];
         }
-        compute(ragc, step, st);
-    };
-    const int whole = (kend & 15) && last == nblocks ? last - 1 : last;
-    int step = first;
-    for (; step < whole; step++) block(std::false_type(), step);
-    if (step < last) block(std::true_type(), step);
+    }
 #pragma unroll
     for (int j = 0; j < IM; j++)
 #pragma unroll
@@ -401,7 +452,7 @@ static ProductPlan product_plan(const ProductArgs &a) {
         least = 16;              // blocks of a range
     } else {
         const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-        r.kind = a.ytype == F32 ? 3 : big >= 192 ? 2 : 1;
+        r.kind = a.ytype == F32 ? 3 : big >= 192 && a.b_block > 1 ? 2 : 1;
         const int b = r.kind == 2 ? 256 : 128;
         r.mt = (int)((a.m + b - 1) / b);
         r.nt = (int)((a.n + b - 1) / b);
@@ -448,7 +499,7 @@ template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hip
         typedef std::false_type N;
         if (r.kind == 3) e = s1 ? tile(N(), Y(), Y()) : tile(N(), N(), Y());
         else if (r.kind == 1) e = s1 ? tile(N(), Y(), N()) : tile(N(), N(), N());
-        else e = s1 ? tile(Y(), Y(), N()) : tile(Y(), N(), N());
+        else e = tile(Y(), N(), N());
     }
     if (e != hipSuccess || r.splits == 1) return e;
     const int64_t items = a.m * ((a.n + 3) / 4);

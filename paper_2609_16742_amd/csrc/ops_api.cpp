@@ -180,10 +180,10 @@ ctc_status ctc_fp8_quantize(ctc_dtype dtype, int64_t rows, int64_t cols, const v
 }
 
 ctc_status ctc_fp8_matmul_workspace_bytes(ctc_dtype ytype, int64_t m, int64_t n, int64_t k,
-                                          size_t *bytes) {
+                                          int32_t b_block, size_t *bytes) {
     if (!bytes) return fail(CTC_ERR_ARG, "NULL bytes");
     ProductArgs p;
-    ctc_status s = product_args(CTC_E4M3, CTC_E4M3, ytype, m, n, k, 1, 1, p);
+    ctc_status s = product_args(CTC_E4M3, CTC_E4M3, ytype, m, n, k, 1, b_block, p);
     if (s != CTC_OK) return s;
     *bytes = m && n ? product_workspace(p) : 0;
     return CTC_OK;

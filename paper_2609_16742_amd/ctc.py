@@ -163,7 +163,7 @@ _sig("ctc_fp8_quantize", [_I32, _I64, _I64, _P, _I64, _I32, _I32, _I32, _P,
 _sig("ctc_fp8_matmul", [_I32, _I32, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64,
                         _I32, _P, _I64, _P, _I64, _I32, _P, _I32, _P, _I64,
                         _P, _SZ, _P])
-_sig("ctc_fp8_matmul_workspace_bytes", [_I32, _I64, _I64, _I64,
+_sig("ctc_fp8_matmul_workspace_bytes", [_I32, _I64, _I64, _I64, _I32,
                                         ctypes.POINTER(_SZ)])
 _sig("ctc_token_scores_forward", [_I32, _I64, _I32, _P, _I64, _P, _I32] +
      [_P] * 7 + [_SZ, _P])
@@ -469,9 +469,9 @@ def ctc_fp8_matmul(*args):
     _check(_lib.ctc_fp8_matmul(*args))
 
 
-def ctc_fp8_matmul_workspace_bytes(ytype, m, n, k):
+def ctc_fp8_matmul_workspace_bytes(ytype, m, n, k, b_block):
     b = _SZ()
-    _check(_lib.ctc_fp8_matmul_workspace_bytes(ytype, m, n, k,
+    _check(_lib.ctc_fp8_matmul_workspace_bytes(ytype, m, n, k, b_block,
                                                ctypes.byref(b)))
     return b.value
 

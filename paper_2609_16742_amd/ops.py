@@ -270,8 +270,8 @@ def _rows_8bit(q, name, dev):
 
 
 @lru_cache(maxsize=512)
-def _matmul_bytes(ytype, m, n, k):
-    return ctc.ctc_fp8_matmul_workspace_bytes(ytype, m, n, k)
+def _matmul_bytes(ytype, m, n, k, b_block):
+    return ctc.ctc_fp8_matmul_workspace_bytes(ytype, m, n, k, b_block)
 
 
 def _scale_rows(scales, name, rows, kb, dev):
@@ -307,7 +307,7 @@ def fp8_matmul(a, a_scales, b, b_scales, bias=None, act="none",
           "out must be a real matrix of shape %s", (m, n))
     ldy = _rows(out, "out", dev)
     raw, current = _on(dev, stream)
-    nb = _matmul_bytes(_REAL[out.dtype], m, n, k)
+    nb = _matmul_bytes(_REAL[out.dtype], m, n, k, bb)
     ws, wsp = _workspace(nb, dev, stream, current)
     with _Device(dev):
         ctc.ctc_fp8_matmul(

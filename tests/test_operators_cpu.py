@@ -88,7 +88,7 @@ def test_matmul_refusals(status, change):
 
 
 def test_matmul_needs_the_workspace_it_names():
-    need = ctc.ctc_fp8_matmul_workspace_bytes(F16, 4, 64, 25088)
+    need = ctc.ctc_fp8_matmul_workspace_bytes(F16, 4, 64, 25088, 128)
     assert need > 0
     base = dict(MATMUL, m=4, n=64, k=25088, lda=25088, ldb=25088)
     _call(ctc.ctc_fp8_matmul, base, WORKSPACE, ws=None)
