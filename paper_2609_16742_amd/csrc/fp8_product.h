@@ -88,8 +88,9 @@ __device__ __forceinline__ void product_out(const ProductArgs &p, int64_t m, int
     if (m >= p.m) return;
 #pragma unroll
     for (int e = 0; e < 4; e++)
-        if (n + e < p.n) v[e] = act_of(p.act, p.bias ? v[e] + p.bias[n + e] : v[e]);
+        if (p.bias && n + e < p.n) v[e] += p.bias[n + e];
     float w[4] = {v[0], v[1], v[2], v[3]};
+    act_of<4>(p.act, w);
     const int64_t o = m * p.ldy + n;
     auto put = [&](auto *y) {
         typedef typename std::remove_pointer<decltype(y)>::type T;

@@ -45,6 +45,21 @@ __device__ __forceinline__ void store(T *p, const float (&v)[V]) {
     __builtin_memcpy(p, &r, sizeof r);
 }
 
+// 16 bytes kept in four registers, and their values.  held() hides where
+// they came from: the compiler would keep the widened values instead, twice
+// the registers for 16-bit types.
+template <typename T, int V = 16 / (int)sizeof(T)>
+__device__ __forceinline__ void values_of(u4 r, float (&v)[V]) {
+    const Pack<T, V> q = __builtin_bit_cast(Pack<T, V>, r);
+#pragma unroll
+    for (int i = 0; i < V; i++) v[i] = widen(q.e[i]);
+}
+__device__ __forceinline__ void held(u4 &r) {
+    uint32_t a = r[0], b = r[1], c = r[2], d = r[3];
+    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+    r = u4{a, b, c, d};
+}
+
 // The larger of values, a NaN lost against a number (as single
 // instructions: fmaxf first quiets its arguments).
 __device__ __forceinline__ float vmax(float a, float b) {
@@ -66,20 +81,37 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// ReLU lets NaN through.
-__device__ __forceinline__ float act_of(int act, float z) {
-    if (act == ACT_RELU) return z < 0.f ? 0.f : z;
-    if (act == ACT_SILU) return z / (1.f + exp_hw(-z));
-    return z;
+// ReLU lets NaN through.  (The hardware's reciprocal is good to one ulp.)
+__device__ __forceinline__ float relu(float z) { return z < 0.f ? 0.f : z; }
+__device__ __forceinline__ float sigmoid(float z) {
+    return __builtin_amdgcn_rcpf(1.f + exp_hw(-z));
 }
-// d act(z) / dz
-__device__ __forceinline__ float act_grad(int act, float z) {
-    if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (act == ACT_SILU) {
-        const float s = 1.f / (1.f + exp_hw(-z));
-        return s * (1.f + z * (1.f - s));
+// act(z) of V values; `act` is the same for the whole launch, so the choice
+// is one branch.
+template <int V> __device__ __forceinline__ void act_of(int act, float (&z)[V]) {
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < V; e++) z[e] = relu(z[e]);
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < V; e++) z[e] *= sigmoid(z[e]);
     }
-    return 1.f;
+}
+// d act(z) / dz in place of z
+template <int V> __device__ __forceinline__ void act_grad(int act, float (&z)[V]) {
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < V; e++) z[e] = z[e] > 0.f ? 1.f : 0.f;
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            const float s = sigmoid(z[e]);
+            z[e] = s * (1.f + z[e] * (1.f - s));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) z[e] = 1.f;
+    }
 }
 
 template <typename K, typename... A>
