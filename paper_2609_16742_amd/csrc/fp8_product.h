@@ -10,8 +10,7 @@
 //    the result for normal values: a tenth of a 16-bit result's rounding, so
 //    16-bit results are summed like this, at the 8-bit rate;
 //  - four 16x16x32 bf16 MFMAs on the widened values (exact, as are their
-//    products), at half the rate but with fp32 sums: fp32 results, and all
-//    products of few rows, which the bytes of the filters bound.
+//    products), at half the rate but with fp32 sums: fp32 results.
 //
 // b's rows (filters) are the MFMA's first operand: a lane ends up with four
 // consecutive n of one m.  A lane's 32 values of k are two 16-byte chunks g
@@ -117,72 +116,125 @@ __device__ __forceinline__ void partial_out(const ProductArgs &p, int split, int
 }
 
 // ---------------------------------------------------------------------------
-// Few rows of a: the filters are streamed once, straight into registers.  A
-// workgroup of eight waves takes 16 filters and MT tiles of 16 rows; its
-// waves take every eighth block of k and add up in LDS.
+// Few rows of a: the filters are streamed once.  A workgroup of NW waves
+// takes 16 filters and MT tiles of 16 rows; its waves take every NW-th block
+// of k, each through a ring of R stages in LDS of its own (no barrier: a
+// wave waits for its own loads), and add up at the end.  A stage holds the
+// block's rows as product_tile's do, filters first, then their scales.
+// What bounds it: the bytes of the filters, and how many are under way (R - 1
+// stages of each wave).  Loading fragments straight into registers took as
+// long for one row, but 41 us instead of N for 32 (k = 25088, 4096 filters):
+// a load whose neighbouring lanes are in different rows keeps the address
+// unit four times as long.
 // ---------------------------------------------------------------------------
-template <int MT, int FA, int FB>
-__global__ __launch_bounds__(512) void product_rows(ProductArgs p, int splits, int per) {
-    __shared__ f4 sum[8][MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <int MT, int FA, int FB, bool WIDE>
+__global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p, int splits,
+                                                                   int per) {
+    constexpr int NW = MT < 4 ? 8 : 4, R = MT == 1 ? 4 : 3;
+    constexpr int ROWS = 16 * (1 + MT), STAGE = ROWS * 128 + 512;
+    constexpr int LOADS = ROWS / 8 + 2;          // of a stage
+    static_assert(NW * R * STAGE <= 160 * 1024 && NW * MT * 1024 <= NW * R * STAGE, "LDS");
+    __shared__ __attribute__((aligned(16))) char lds[NW * R * STAGE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int fr = lane & 15, fg = lane >> 4;
     const int64_t n0 = (int64_t)(blockIdx.x / splits) * 16;
     const int split = blockIdx.x % splits;
-    const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int nb = (int)((p.k + 127) / 128);
-    const int kb1 = (split + 1) * per < nb ? (split + 1) * per : nb;
-    // rows past the end: the last one again (they only reach results that
-    // are not stored)
-    const int64_t n = n0 + fr < p.n ? n0 + fr : p.n - 1;
-    const uint8_t *b = p.b + n * p.ldb;
-    const uint8_t *a[MT];
-    const float *sa[MT];
+    const int nblocks = (int)((p.k + 127) / 128);
+    const int kb0 = split * per, kb1 = kb0 + per < nblocks ? kb0 + per : nblocks;
+    const int kend = (int)p.k;
+    const int ma = (int)p.m, nb = p.n - n0 < 16 ? (int)(p.n - n0) : 16;
+    const Buf ar = __builtin_amdgcn_make_buffer_rsrc((void *)p.a, 0, (int)(ma * p.lda),
+                                                     0x00020000);
+    const Buf br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + n0 * p.ldb), 0,
+                                                     (int)(nb * p.ldb), 0x00020000);
+    const int ash = p.a_block == 1 ? 0 : 7, bsh = p.b_block == 1 ? 0 : 7;
+    const float *sab = p.sa, *sbb = p.sb + (n0 >> bsh);
+    // the scales' places: lane l for row l of a and filter l
+    const int sai = (lane < ma ? lane >> ash : 0) * 4;
+    const int sbi = lane < nb ? (int)((n0 + lane >> bsh) - (n0 >> bsh)) * 4 : 0;
+    const int lrow = lane >> 3, lchunk = ((lane & 7) ^ lrow) * 16;
+    const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
+    char *ring = lds + wave * R * STAGE;
+    auto issue = [&](int kb, int slot) {
+        const bool on = kb < kb1;                // past the range: zeros
+        const int k0 = kb * 128;
+        const bool ok = on && k0 + lchunk < kend;
+        const int av = ok ? ao + k0 : PAST, bv = ok ? bo + k0 : PAST;
+        char *to = ring + slot * STAGE;
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(br, (LdsAt)(to + i * 1024), 16,
+                                                     bv + i * 8 * (int)p.ldb, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * MT; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (LdsAt)(to + (i + 2) * 1024), 16,
+                                                     av + i * 8 * (int)p.lda, 0, 0, 0);
+        const int64_t q = on ? kb : 0;
+        const Buf sar = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(sab + q * p.ldsa), 0, on ? (((ma - 1) >> ash) + 1) * 4 : 0, 0x00020000);
+        const Buf sbr = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(sbb + q * p.ldsb), 0,
+            on ? (int)((n0 + nb - 1 >> bsh) - (n0 >> bsh) + 1) * 4 : 0, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sar, (LdsAt)(to + ROWS * 128), 4, sai, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sbr, (LdsAt)(to + ROWS * 128 + 256), 4, sbi, 0,
+                                                 0, 0);
+    };
     f4 acc[MT];
 #pragma unroll
-    for (int j = 0; j < MT; j++) {
-        const int64_t m = m0 + j * 16 + fr < p.m ? m0 + j * 16 + fr : p.m - 1;
-        a[j] = p.a + m * p.lda;
-        sa[j] = p.sa + (p.a_block == 1 ? m : m / 128);
-        acc[j] = (f4)(0.f);
-    }
-    int64_t nq[4];                               // scale of each of four results
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-        const int64_t q = n0 + fg * 4 + e < p.n ? n0 + fg * 4 + e : p.n - 1;
-        nq[e] = p.b_block == 1 ? q : q / 128;
-    }
-    auto get = [&](const uint8_t *row, int kb, bool whole) {
-        const int64_t k = (int64_t)kb * 128 + fg * 16;
-        if (whole) return chunks(*(const u4 *)(row + k), *(const u4 *)(row + k + 64));
-        // chunks that begin past the end are not read
-        u4 lo = (u4)(0u), hi = (u4)(0u);
-        if (k < p.k) lo = first_bytes(*(const u4 *)(row + k), (int)(p.k - k));
-        if (k + 64 < p.k) hi = first_bytes(*(const u4 *)(row + k + 64), (int)(p.k - k - 64));
-        return chunks(lo, hi);
-    };
-    auto block = [&](int kb, bool whole) {
-        const Wide w = widen_block<FB>(get(b, kb, whole));
-        f4 sb;
-#pragma unroll
-        for (int e = 0; e < 4; e++) sb[e] = p.sb[kb * p.ldsb + nq[e]];
+    for (int j = 0; j < MT; j++) acc[j] = (f4)(0.f);
+    const int c0 = (fg ^ (fr & 7)) * 16, c1 = ((fg + 4) ^ (fr & 7)) * 16;
+    auto block = [&](int kb, int slot) {
+        const char *at = ring + slot * STAGE + fr * 128;
+        // the block k ends in, in the middle of 16 bytes
+        const bool ragged = (kb + 1) * 128 > kend && (kend & 15);
+        const int left = kend - kb * 128 - fg * 16;
+        auto frag = [&](int tile) {
+            u4 lo = *(const u4 *)(at + tile * 2048 + c0), hi = *(const u4 *)(at + tile * 2048 + c1);
+            if (ragged) {
+                lo = first_bytes(lo, left);
+                hi = first_bytes(hi, left - 64);
+            }
+            return chunks(lo, hi);
+        };
+        const float *sc = (const float *)(ring + slot * STAGE + ROWS * 128);
+        const f4 sb = *(const f4 *)(sc + 64 + fg * 4);
+        const i8v w = frag(0);
 #pragma unroll
         for (int j = 0; j < MT; j++) {
-            const Wide x = widen_block<FA>(get(a[j], kb, whole));
-            const float s = sa[j][kb * p.ldsa];
-            acc[j] += mfma_wide(w, x) * (sb * s);
+            const i8v x = frag(1 + j);
+            const float s = sc[j * 16 + fr];
+            if constexpr (WIDE)
+                acc[j] += mfma_wide(widen_block<FB>(w), widen_block<FA>(x)) * (sb * s);
+            else
+                acc[j] += mfma_block<FA, FB>(w, x) * (sb * s);
         }
     };
-    const int full = (int)(p.k / 128);
-    int kb = split * per + wave;
-    for (; kb < kb1 && kb < full; kb += 8) block(kb, true);
-    if (kb < kb1) block(kb, false);
+    int kb = kb0 + wave;
 #pragma unroll
-    for (int j = 0; j < MT; j++) sum[wave][j][lane] = acc[j];
+    for (int r = 0; r < R - 1; r++) issue(kb + r * NW, r);
+    int slot = 0;
+    for (; kb < kb1; kb += NW) {
+        const int fill = slot == 0 ? R - 1 : slot - 1;   // the one read last
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        issue(kb + (R - 1) * NW, fill);
+        // all but the loads of the R - 1 later stages
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 1) * LOADS) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        block(kb, slot);
+        slot = slot == R - 1 ? 0 : slot + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    if (wave < MT) {
-        f4 t = sum[0][wave][lane];
-        for (int i = 1; i < 8; i++) t += sum[i][wave][lane];
-        const int64_t m = m0 + wave * 16 + fr;
+    f4 *sum = (f4 *)lds;                         // [NW][MT][64]
+#pragma unroll
+    for (int j = 0; j < MT; j++) sum[(wave * MT + j) * 64 + lane] = acc[j];
+    __syncthreads();
+    for (int j = wave; j < MT; j += NW) {
+        f4 t = sum[j * 64 + lane];
+        for (int i = 1; i < NW; i++) t += sum[(i * MT + j) * 64 + lane];
+        const int64_t m = j * 16 + fr;
         if (splits > 1) partial_out(p, split, m, n0 + fg * 4, t);
         else product_out(p, m, n0 + fg * 4, t);
     }
@@ -450,7 +502,9 @@ static ProductPlan product_plan(const ProductArgs &a) {
         r.nt = (int)((a.n + 15) / 16);
         wgs = r.nt;
         want = 256;
-        least = 16;              // blocks of a range
+        // blocks of a range: eight a wave, joining costs as much as reading
+        // them
+        least = 64;
     } else {
         const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
         r.kind = a.ytype == F32 ? 3 : big >= 192 && a.b_block > 1 ? 2 : 1;
@@ -480,9 +534,13 @@ template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hip
     hipError_t e;
     if (r.kind == 0) {
         const dim3 grid((unsigned)(r.nt * r.splits), 1);
-        e = r.mt == 1 ? start(product_rows<1, FA, FB>, grid, 512, st, a, r.splits, r.per)
-          : r.mt == 2 ? start(product_rows<2, FA, FB>, grid, 512, st, a, r.splits, r.per)
-                      : start(product_rows<4, FA, FB>, grid, 512, st, a, r.splits, r.per);
+        auto rows = [&](auto wide) {
+            constexpr bool W = decltype(wide)::value;
+            return r.mt == 1 ? start(product_rows<1, FA, FB, W>, grid, 512, st, a, r.splits, r.per)
+                 : r.mt == 2 ? start(product_rows<2, FA, FB, W>, grid, 512, st, a, r.splits, r.per)
+                             : start(product_rows<4, FA, FB, W>, grid, 256, st, a, r.splits, r.per);
+        };
+        e = a.ytype == F32 ? rows(std::true_type()) : rows(std::false_type());
     } else {
         const unsigned g = ((unsigned)(r.mt * r.nt * r.splits) + 7) / 8 * 8;
         const bool s1 = a.b_block == 1;
