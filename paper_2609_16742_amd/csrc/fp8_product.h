@@ -123,7 +123,7 @@ __device__ __forceinline__ void partial_out(const ProductArgs &p, int split, int
 // block's rows as product_tile's do, filters first, then their scales.
 // What bounds it: the bytes of the filters, and how many are under way (R - 1
 // stages of each wave).  Loading fragments straight into registers took as
-// long for one row, but 41 us instead of N for 32 (k = 25088, 4096 filters):
+// long for one row, but 41 us instead of 23 for 32 (k = 25088, 4096 filters):
 // a load whose neighbouring lanes are in different rows keeps the address
 // unit four times as long.
 // ---------------------------------------------------------------------------

@@ -21,10 +21,10 @@ def _call(f, defaults, status, **change):
     assert e.value.status == status, (change, str(e.value))
 
 
-NORM = dict(dtype=F16, n=2, hw=4096, c=64, groups=8, carry=0, x=P, gamma=P,
+NORM = dict(dtype=F16, n=2, hw=1 << 20, c=64, groups=8, carry=0, x=P, gamma=P,
             beta=P, residual=None, eps=1e-5, act=0, y=P, mean=P, rstd=P,
             ws=P, ws_bytes=1 << 30, stream=None)
-NORM_BACK = dict(dtype=F16, n=2, hw=4096, c=64, groups=8, carry=0, dy=P, x=P,
+NORM_BACK = dict(dtype=F16, n=2, hw=1 << 20, c=64, groups=8, carry=0, dy=P, x=P,
                  mean=P, rstd=P, gamma=P, beta=P, residual=None, act=0, dx=P,
                  dr=None, dgamma=P, dbeta=P, ws=P, ws_bytes=1 << 30,
                  stream=None)
