@@ -7,11 +7,18 @@
 // f (t + (m - m') s)); in the same pass the rank of the target and every
 // thread's largest value.
 //
+// Exponents are in powers of two, about m2 = m log2(e) rounded: a value
+// costs one multiply-add x log2(e) - m2, one exp2, and two more for s and t.
+// s belongs to m2 exactly, so what m2 was rounded by comes back at the end
+// (soft_shift).  Maxima of magnitude above 1e38 (rows of the type's lowest
+// value; none yet, -inf), whose m2 would overflow, take x - m first.
+//
 // Top alternatives: with the row dealt out to 64 groups of threads, the k-th
 // largest group maximum is a lower bound T of the k-th largest value (k
 // groups hold one at least), and for values in no order hardly more than k
 // are >= T.  Threads whose maximum reaches T read their part again, the
-// values >= T are collected and ordered by (value, lower index).
+// values >= T are collected and ordered by (value, lower index).  The order
+// they are found in does not matter.
 //
 // What bounds it: the bytes of the logits.
 #pragma once
@@ -21,14 +28,24 @@ namespace ctc {
 namespace ops {
 
 constexpr int SC_CAP = 512;                      // collected alternatives
-constexpr float SC_LOW = -200.f;                 // exp() of it is 0 in fp32
+constexpr float SC_LOW = -200.f;                 // 2^ of it is 0 in fp32
 
+// t in powers of two as well
 struct SoftState { float m, s, t; };
+// m2: the product in a register of its own, so that it is rounded the same
+// wherever it is used (not contracted into a multiply-add)
+__device__ __forceinline__ float soft_m2(float m) {
+    float r = m * LOG2E;
+    asm("" : "+v"(r));
+    return r;
+}
+__device__ __forceinline__ bool soft_wide(float m) { return !(__builtin_fabsf(m) <= 1e38f); }
 // m = -inf marks an empty state (s = t = 0); s turns NaN with the first NaN
-// or +inf and stays it.
+// or +inf and stays it.  (vmax drops the NaN of two overflown maxima, whose
+// distance is as good as infinite.)
 __device__ __forceinline__ void soft_raise(SoftState &a, float m) {
-    const float d = vmax(a.m - m, SC_LOW);
-    const float f = exp_hw(d);
+    const float d = vmax(soft_m2(a.m) - soft_m2(m), SC_LOW);
+    const float f = exp2_hw(d);
     a.t = (a.t + d * a.s) * f;
     a.s *= f;
     a.m = m;
@@ -41,6 +58,13 @@ __device__ __forceinline__ void soft_join(SoftState &a, SoftState b) {
     }
     a.s += b.s;
     a.t += b.t;
+}
+// m - m2 ln 2: what x - m is off by as the exponent of s
+__device__ __forceinline__ float soft_shift(float m) {
+    if (soft_wide(m)) return 0.f;
+    const float m2 = soft_m2(m);
+    constexpr float LN2_LO = -1.9046542e-9f;     // ln 2 - LN2
+    return __builtin_fmaf(-m2, LN2_LO, __builtin_fmaf(-m2, LN2, m));
 }
 
 // Total order: NaN above +inf, -0 as +0, equal values by the lower index.
@@ -91,7 +115,8 @@ template <typename T, int NT> struct ScorePart {
         float gmax[64];
         SoftState st[NW];
         int cnt[NW];
-        int found;
+        int found, threads;
+        uint16_t thread[NT];
         uint64_t key[SC_CAP];
         uint64_t best[NW];
     };
@@ -101,9 +126,11 @@ template <typename T, int NT> struct ScorePart {
     int target;                  // -1: no rank wanted
     float xt, thr_before;        // the target's value, and the next below it
     SoftState st;
+    float m2;                    // st.m in powers of two
     int cnt;
 
-    // VALS elements from index i on
+    // VALS elements from index i on.  The rank counts a wave at a time: `cnt`
+    // is right in the lane that takes part longest, the first.
     template <int VALS> __device__ __forceinline__ void add(const float (&v)[VALS], int i) {
         float vm;
         if constexpr (VALS == 8)
@@ -112,25 +139,34 @@ template <typename T, int NT> struct ScorePart {
         else if constexpr (VALS == 4)
             vm = vmax3(vmax(v[0], v[1]), v[2], v[3]);
         else vm = v[0];
-        if (vm > st.m) soft_raise(st, vm);
-        const float mu = st.m == -INF ? 0.f : st.m;
+        if (vm > st.m) {
+            soft_raise(st, vm);
+            m2 = soft_m2(vm);
+        }
+        if (!soft_wide(st.m)) {
 #pragma unroll
-        for (int e = 0; e < VALS; e++) {
-            const float d = v[e] - mu;
-            const float p = exp_hw(d);
-            st.s += p;
-            st.t = __builtin_fmaf(vmax(d, SC_LOW), p, st.t);
+            for (int e = 0; e < VALS; e++) {
+                const float d = __builtin_fmaf(v[e], LOG2E, -m2);
+                const float p = exp2_hw(d);
+                st.s += p;
+                st.t = __builtin_fmaf(vmax(d, SC_LOW), p, st.t);
+            }
+        } else {
+            const float mu = st.m == -INF ? 0.f : st.m;
+#pragma unroll
+            for (int e = 0; e < VALS; e++) {
+                const float d = (v[e] - mu) * LOG2E;
+                const float p = exp2_hw(d);
+                st.s += p;
+                st.t = __builtin_fmaf(vmax(d, SC_LOW), p, st.t);
+            }
         }
         if (target >= 0) {
-            if (i <= target && target < i + VALS) {
+            // (the target's own vector: scan() adds what stands before it)
+            const float thr = i + VALS <= target ? thr_before : xt;
 #pragma unroll
-                for (int e = 0; e < VALS; e++)
-                    cnt += !(v[e] <= (i + e < target ? thr_before : xt)) & (i + e != target);
-            } else {
-                const float thr = i < target ? thr_before : xt;
-#pragma unroll
-                for (int e = 0; e < VALS; e++) cnt += !(v[e] <= thr);
-            }
+            for (int e = 0; e < VALS; e++)
+                cnt += __builtin_popcountll(__ballot(!(v[e] <= thr)));
         }
     }
     __device__ void scan() {
@@ -138,31 +174,42 @@ template <typename T, int NT> struct ScorePart {
         const int tid = threadIdx.x;
         const int nv = (hi - lo) / V;
         st = SoftState{-INF, 0.f, 0.f};
+        m2 = 0.f;
         cnt = 0;
         int i = tid;
-        for (; i + (U - 1) * NT < nv; i += U * NT) {
+        if (U * NT <= nv) thr_before = below(xt);
+        // (all threads together: lane 0 stays to the end, see add)
+        for (; i - tid + U * NT <= nv; i += U * NT) {
             float v[U][V];
 #pragma unroll
             for (int u = 0; u < U; u++) load<T, V>(x + lo + (i + u * NT) * V, v[u]);
 #pragma unroll
             for (int u = 0; u < U; u++) add(v[u], lo + (i + u * NT) * V);
         }
-        for (; i < nv; i += NT) {
-            float v[V];
-            load<T, V>(x + lo + i * V, v);
-            add(v, lo + i * V);
-        }
-        i = lo + nv * V + tid;
-        if (i < hi) {
-            float v[1] = {widen(x[i])};
-            add(v, i);
+        // what is left: U vectors a thread at most and one value, sent for
+        // together (and ahead of the wait for the target's value)
+        {
+            float v[U][V], w[1];
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * NT < nv) load<T, V>(x + lo + (i + u * NT) * V, v[u]);
+            const int j = lo + nv * V + tid;
+            if (j < hi) w[0] = widen(x[j]);
+            thr_before = below(xt);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (i + u * NT < nv) add(v[u], lo + (i + u * NT) * V);
+            if (j < hi) add(w, j);
         }
         if (target >= 0 && xt != xt) {           // only NaN stands beside NaN
             cnt = 0;
             for (int j = lo + tid; j < hi && j < target; j += NT) {
                 const float v = widen(x[j]);
-                cnt += v != v;
+                cnt += __builtin_popcountll(__ballot(v != v));
             }
+        } else if (target >= lo && target < lo + nv * V && tid == 0) {
+            // equal values before the target in its vector
+            for (int j = target - (target - lo) % V; j < target; j++) cnt += widen(x[j]) == xt;
         }
     }
     // f(value, index) for every element this thread scanned
@@ -180,12 +227,11 @@ template <typename T, int NT> struct ScorePart {
     // Joins the threads' states; every thread returns with the whole.
     __device__ void join(Lds &l, SoftState &all, int &count) {
         SoftState a = st;
-        int c = cnt;
+        int c = __builtin_amdgcn_readfirstlane(cnt);
 #pragma unroll
         for (int o = 32; o; o >>= 1) {
             SoftState b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)};
             soft_join(a, b);
-            c += __shfl_xor(c, o);
         }
         if constexpr (NW > 1) {
             const int w = threadIdx.x >> 6;
@@ -214,7 +260,7 @@ template <typename T, int NT> struct ScorePart {
         float g = st.m;
 #pragma unroll
         for (int o = NW / 2; o; o >>= 1) g = vmax(g, __shfl_xor(g, o));
-        if (tid == 0) l.found = 0;
+        if (tid == 0) l.found = l.threads = 0;
         if constexpr (NW > 1) {
             if (lane % NW == 0) l.gmax[tid / NW] = g;
             __syncthreads();
@@ -223,13 +269,31 @@ template <typename T, int NT> struct ScorePart {
             __syncthreads();
         }
         const float T0 = kth_of_lanes(g, k);
-        if (st.m >= T0 || odd)
-            again([&](float v, int i) {
-                if (!(v < T0) && v != -INF) {
-                    const int at = atomicAdd(&l.found, 1);
-                    if (at < SC_CAP) l.key[at] = order_key(v, i);
-                }
-            });
+        auto take = [&](float v, int i) {
+            if (!(v < T0) && v != -INF) {
+                const int at = atomicAdd(&l.found, 1);
+                if (at < SC_CAP) l.key[at] = order_key(v, i);
+            }
+        };
+        // The vectors of the threads that hold such values are dealt out to
+        // all (each reading its own again, one after the other, was a fifth
+        // of the kernel at 131072 tokens).
+        const int nv = (hi - lo) / V, own = (nv + NT - 1) / NT;
+        if (st.m >= T0 || odd) {
+            l.thread[atomicAdd(&l.threads, 1)] = (uint16_t)tid;
+            const int i = lo + nv * V + tid;
+            if (i < hi) take(widen(x[i]), i);
+        }
+        __syncthreads();
+        for (int q = tid; q < l.threads * own; q += NT) {
+            const int i = l.thread[q / own] + q % own * NT;
+            if (i < nv) {
+                float v[V];
+                load<T, V>(x + lo + i * V, v);
+#pragma unroll
+                for (int e = 0; e < V; e++) take(v[e], lo + i * V + e);
+            }
+        }
         __syncthreads();
         const int n = l.found;
         if (n <= SC_CAP) {
@@ -272,14 +336,16 @@ template <typename T, int NT> struct ScorePart {
 };
 
 // What the outputs of a row are, given its joined state.
+__device__ __forceinline__ float soft_log(SoftState a) {
+    return LN2 * __builtin_amdgcn_logf(a.s) - soft_shift(a.m);
+}
 __device__ __forceinline__ float soft_lse(SoftState a) {
-    if (a.m == -INF && a.s == 0.f) return -INF;
-    return a.m + LN2 * __builtin_amdgcn_logf(a.s);
+    return a.m == -INF && a.s == 0.f ? -INF : a.m + soft_log(a);
 }
 // log p of a logit: about the maximum, so a row far from zero (one of the
 // type's lowest values, say) keeps its digits, which x - lse would lose.
 __device__ __forceinline__ float soft_logprob(SoftState a, float x) {
-    return (x - a.m) - LN2 * __builtin_amdgcn_logf(a.s);
+    return (x - a.m) - soft_log(a);
 }
 __device__ __forceinline__ void write_scores(const ScoreArgs &a, int64_t row, SoftState s,
                                              int count, int target, float xt) {
@@ -287,7 +353,7 @@ __device__ __forceinline__ void write_scores(const ScoreArgs &a, int64_t row, So
     const float lse = soft_lse(s);
     if (a.lse) a.lse[row] = lse;
     if (a.entropy)
-        a.entropy[row] = empty ? 0.f : LN2 * __builtin_amdgcn_logf(s.s) - s.t / s.s;
+        a.entropy[row] = empty ? 0.f : LN2 * (__builtin_amdgcn_logf(s.s) - s.t / s.s);
     if (a.logprob) a.logprob[row] = target < 0 ? 0.f : empty ? -INF : soft_logprob(s, xt);
     if (a.rank) a.rank[row] = target < 0 ? -1 : count;
 }
@@ -311,7 +377,6 @@ __global__ __launch_bounds__(NT) void token_scores(ScoreArgs a, ScorePlan p) {
     if (target >= a.vocab) target = -1;
     w.xt = target >= 0 ? widen(w.x[target]) : 0.f;
     w.target = a.rank ? target : -1;
-    w.thr_before = below(w.xt);
     w.scan();
     SoftState all;
     int count;
@@ -348,34 +413,35 @@ __global__ __launch_bounds__(NT) void token_scores(ScoreArgs a, ScorePlan p) {
     }
 }
 
-// Joins the splits of a row (one workgroup a row).  Every split's list is
-// sorted, so the k best of all hold at most as many of a list as stand
-// before its first miss: a list's entry counts the entries above it by a
-// binary search in every list.
+// Joins the splits of a row (one workgroup a row).  Their lists are sorted,
+// so with n lists the smallest of their ceil(k / n)-th entries, and for
+// n >= k the k-th largest first entry, is a lower bound of the k-th best:
+// hardly more than k entries are left to be ordered.
 constexpr int SC_MAX_SPLITS = 64;
 template <typename T>
 __global__ __launch_bounds__(256) void token_scores_join(ScoreArgs a, ScorePlan p) {
     __shared__ uint64_t keys[SC_MAX_SPLITS * SCORES_MAX_K];
+    __shared__ uint64_t bound;
     __shared__ int found;
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x, k = a.top_k;
+    const int tid = threadIdx.x, k = a.top_k, lane = tid & 63;
     const size_t bytes = score_part_bytes(k);
     const char *part = (const char *)a.ws + row * p.splits * bytes;
+    auto entry = [&](int list, int i) {
+        return ((const uint64_t *)(part + list * bytes + 16))[i];
+    };
     SoftState all{-INF, 0.f, 0.f};
     int count = 0;
-    {
-        const int lane = tid & 63;
-        if (lane < p.splits) {
-            const float *f = (const float *)(part + lane * bytes);
-            all = SoftState{f[0], f[1], f[2]};
-            count = ((const int *)f)[3];
-        }
+    if (lane < p.splits) {
+        const float *f = (const float *)(part + lane * bytes);
+        all = SoftState{f[0], f[1], f[2]};
+        count = ((const int *)f)[3];
+    }
 #pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            SoftState b{__shfl_xor(all.m, o), __shfl_xor(all.s, o), __shfl_xor(all.t, o)};
-            soft_join(all, b);
-            count += __shfl_xor(count, o);
-        }
+    for (int o = 32; o; o >>= 1) {
+        SoftState b{__shfl_xor(all.m, o), __shfl_xor(all.s, o), __shfl_xor(all.t, o)};
+        soft_join(all, b);
+        count += __shfl_xor(count, o);
     }
     const T *x = (const T *)a.x + row * a.ld;
     if (tid == 0) {
@@ -384,36 +450,40 @@ __global__ __launch_bounds__(256) void token_scores_join(ScoreArgs a, ScorePlan 
         write_scores(a, row, all, count, target, target >= 0 ? widen(x[target]) : 0.f);
     }
     if (!k) return;
-    if (tid == 0) found = 0;
-    for (int i = tid; i < p.splits * k; i += 256)
-        keys[i] = ((const uint64_t *)(part + i / k * bytes + 16))[i % k];
+    if (tid < 64) {
+        const int at = (k + p.splits - 1) / p.splits - 1;
+        const uint64_t mine = lane < p.splits ? entry(lane, at) : 0;
+        int above = 0;
+        for (int j = 0; j < p.splits; j++) {
+            const uint64_t o = (uint64_t)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32 |
+                               (uint32_t)__builtin_amdgcn_readlane((int)mine, j);
+            above += o > mine;
+        }
+        if (tid == 0) bound = found = 0;
+        // (equal entries are empty ones, 0: any of them will do)
+        if (lane < p.splits && above == (p.splits >= k ? k : p.splits) - 1) bound = mine;
+    }
     __syncthreads();
+    const uint64_t least = bound > 1 ? bound : 1;
+    for (int i = tid; i < p.splits * k; i += 256) {
+        const uint64_t q = entry(i / k, i % k);
+        if (q >= least) keys[atomicAdd(&found, 1)] = q;
+    }
+    __syncthreads();
+    const int n = found;
     int32_t *ids = a.ids + row * k;
     float *tops = a.tops + row * k;
-    for (int i = tid; i < p.splits * k; i += 256) {
+    for (int i = tid; i < n; i += 256) {
         const uint64_t mine = keys[i];
-        int r = i % k;                           // those above it in its list
-        if (!mine) continue;
-        for (int s = 0; s < p.splits && r < k; s++) {
-            if (s == i / k) continue;
-            const uint64_t *list = keys + s * k;
-            int lo = 0, hi = k;                  // entries > mine: list[0 .. lo)
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (list[mid] > mine) lo = mid + 1;
-                else hi = mid;
-            }
-            r += lo;
-        }
+        int r = 0;
+        for (int j = 0; j < n; j++) r += keys[j] > mine;
         if (r < k) {
             const int at = key_index(mine);
             ids[r] = at;
             tops[r] = soft_logprob(all, widen(x[at]));
-            atomicAdd(&found, 1);
         }
     }
-    __syncthreads();
-    for (int i = found + tid; i < k; i += 256) {
+    for (int i = n + tid; i < k; i += 256) {
         ids[i] = -1;
         tops[i] = -INF;
     }
