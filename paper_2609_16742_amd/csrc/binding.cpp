@@ -103,11 +103,10 @@ int64_t rows_8bit(const Tensor &t, const char *name, const Tensor &ref) {
 Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor &ref) {
     return at::empty(shape, at::TensorOptions().dtype(type).device(ref.device()));
 }
-// Device scratch of a call: `given` (made by the caller where the stream is
-// not the current one) or a new block of the current stream's.
-void *scratch(size_t bytes, const Maybe &given, Tensor &keep, const Tensor &ref) {
+// Device scratch of a call on the current stream.
+void *scratch(size_t bytes, Tensor &keep, const Tensor &ref) {
     if (!bytes) return nullptr;
-    keep = given ? *given : empty({(int64_t)bytes}, at::kByte, ref);
+    keep = empty({(int64_t)bytes}, at::kByte, ref);
     return keep.data_ptr();
 }
 
@@ -135,7 +134,7 @@ size_t norm_bytes(const Tensor &x, const Map &m, int64_t groups, bool backward) 
 std::tuple<Tensor, Tensor, Tensor> group_norm(const Tensor &x, int64_t groups, const Maybe &gamma,
                                               const Maybe &beta, const Maybe &residual, int act,
                                               bool carry, double eps, Maybe y, Maybe mean,
-                                              Maybe rstd, const Maybe &ws, int64_t stream) {
+                                              Maybe rstd, int64_t stream) {
     const Map m = map_of(x, groups);
     c10::DeviceGuard guard(x.device());
     if (!y) {
@@ -154,7 +153,7 @@ std::tuple<Tensor, Tensor, Tensor> group_norm(const Tensor &x, int64_t groups, c
     const size_t bytes = norm_bytes(x, m, groups, false);
     done(ctc_group_norm_forward(code(x), m.n, m.hw, m.c, (int32_t)groups, carry, x.data_ptr(),
                                 (float *)g, (float *)b, r, (float)eps, act, yp, (float *)mp,
-                                (float *)rp, scratch(bytes, ws, keep, x), bytes, (void *)stream));
+                                (float *)rp, scratch(bytes, keep, x), bytes, (void *)stream));
     return {*y, *mean, *rstd};
 }
 
@@ -162,7 +161,7 @@ std::tuple<Maybe, Maybe, Maybe, Maybe>
 group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean, const Tensor &rstd,
                     int64_t groups, const Maybe &gamma, const Maybe &beta, const Maybe &residual,
                     int act, bool carry, bool make, Maybe dx, Maybe dr, Maybe dgamma, Maybe dbeta,
-                    const Maybe &ws, int64_t stream) {
+                    int64_t stream) {
     const Map m = map_of(x, groups);
     c10::DeviceGuard guard(x.device());
     if (make) {
@@ -188,7 +187,7 @@ group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean, const
     done(ctc_group_norm_backward(code(x), m.n, m.hw, m.c, (int32_t)groups, carry, dyp,
                                  x.data_ptr(), (float *)mp, (float *)rp, (float *)g, (float *)b, r,
                                  act, dxp, drp, (float *)dg, (float *)db,
-                                 scratch(bytes, ws, keep, x), bytes, (void *)stream));
+                                 scratch(bytes, keep, x), bytes, (void *)stream));
     return {dx, dr, dgamma, dbeta};
 }
 
@@ -236,7 +235,7 @@ int32_t scale_rows(const Tensor &s, const char *name, int64_t rows, int64_t kb, 
 
 Tensor fp8_matmul(const Tensor &a, const Tensor &a_scales, const Tensor &b,
                   const Tensor &b_scales, const Maybe &bias, int act, at::ScalarType dtype,
-                  const Maybe &out, const Maybe &ws, int64_t stream) {
+                  const Maybe &out, int64_t stream) {
     on_gpu(a, "a");
     need(byte_type(a) && byte_type(b), "a and b must be float8 tensors");
     const int64_t lda = rows_8bit(a, "a", a), ldb = rows_8bit(b, "b", a);
@@ -259,7 +258,7 @@ Tensor fp8_matmul(const Tensor &a, const Tensor &a_scales, const Tensor &b,
     done(ctc_fp8_matmul(code(a), code(b), code(y), m, n, k, a.data_ptr(), lda,
                         a_scales.data_ptr<float>(), a_scales.size(1), ab, b.data_ptr(), ldb,
                         b_scales.data_ptr<float>(), b_scales.size(1), bb, (float *)bp, act,
-                        y.data_ptr(), ldy, scratch(bytes, ws, keep, a), bytes, (void *)stream));
+                        y.data_ptr(), ldy, scratch(bytes, keep, a), bytes, (void *)stream));
     return y;
 }
 
@@ -277,7 +276,7 @@ int64_t logits_of(const Tensor &x) {
 // lse, entropy, logprob, rank, top_ids, top_logprobs
 typedef std::tuple<Maybe, Maybe, Maybe, Maybe, Maybe, Maybe> Scores;
 Scores token_scores(const Tensor &x, const Maybe &targets, int64_t top_k, bool make, Scores out,
-                    const Maybe &ws, int64_t stream) {
+                    int64_t stream) {
     const int64_t ld = logits_of(x), rows = x.size(0);
     const int32_t vocab = (int32_t)x.size(1);
     c10::DeviceGuard guard(x.device());
@@ -308,7 +307,7 @@ Scores token_scores(const Tensor &x, const Maybe &targets, int64_t top_k, bool m
     done(ctc_token_scores_forward(code(x), rows, vocab, x.data_ptr(), ld, (int32_t *)tp,
                                   (int32_t)top_k, (float *)lp, (float *)pp, (float *)ep,
                                   (int32_t *)rp, (int32_t *)ip, (float *)vp,
-                                  scratch(bytes, ws, keep, x), bytes, (void *)stream));
+                                  scratch(bytes, keep, x), bytes, (void *)stream));
     return out;
 }
 

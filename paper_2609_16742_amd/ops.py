@@ -9,8 +9,9 @@ in libctc.so's HIP kernels (include/ctc.h states what each computes).
 
 Every call takes tensors of one GPU, enqueues on ``stream`` (default: the
 current stream of that GPU) and returns without waiting.  Outputs are
-allocated unless given.  Tensors used on a stream that is not current have to
-outlive their use there, as with any torch operator.  Wrong shapes, types or
+allocated unless given, as that stream's tensors (as under
+``torch.cuda.stream``): work on another stream that reads them has to wait for
+it and call ``record_stream``.  Inputs have to outlive their use there.  Wrong shapes, types or
 devices raise ValueError before anything is enqueued; the library's own
 refusals raise :class:`ctc.CtcError`.
 """
@@ -46,41 +47,24 @@ def _act(act):
         raise ValueError("act must be one of %s" % sorted(_ACT)) from None
 
 
-def _stream(t, stream):
-    """Raw handle of ``stream`` (None: the current one) for work on t."""
+def _run(f, t, stream, *args):
+    """f(*args, raw stream) on ``stream`` (None: the current one) of t's GPU.
+    Outputs and workspaces are allocated with that stream current: a block
+    of another stream's could still be in use there."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise ValueError("GPU tensors are needed")
+    current = _current_raw(t.get_device())
     if stream is None:
-        return _current_raw(t.get_device())
-    return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _scratch(t, stream, nbytes):
-    """Workspace of a call on a stream that is not current (None: the call
-    allocates its own).  It is allocated on the current stream, so the
-    allocator has to know where it is used."""
-    if stream is None:
-        return None
-    raw = _stream(t, stream)
-    if raw == _current_raw(t.get_device()):
-        return None
-    n = nbytes()
-    if not n:
-        return None
-    ws = torch.empty(n, dtype=torch.uint8, device=t.device)
-    ws.record_stream(torch.cuda.ExternalStream(raw, device=t.device)
-                     if isinstance(stream, int) else stream)
-    return ws
-
-
-def _norm_bytes(x, groups, backward):
-    hw = x[0, ..., 0].numel() if x.shape[0] else 1
-    return ctc.ctc_group_norm_workspace_bytes(
-        _TYPE[x.dtype], x.shape[0], hw, x.shape[-1], groups, backward)
-
-
-_TYPE = {torch.float32: ctc.CTC_F32, torch.float16: ctc.CTC_F16,
-         torch.bfloat16: ctc.CTC_BF16}
+        return f(*args, current)
+    raw = stream if isinstance(stream, int) else stream.cuda_stream
+    if raw == current:
+        return f(*args, raw)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(raw, device=t.device)
+    if stream.device != t.device:
+        raise ValueError("the stream is another GPU's")
+    with torch.cuda.stream(stream):
+        return f(*args, raw)
 
 
 def group_norm(x, groups, gamma=None, beta=None, residual=None, act="none",
@@ -92,11 +76,9 @@ def group_norm(x, groups, gamma=None, beta=None, residual=None, act="none",
     With ``carry`` the last channel is a carry-through checksum, which takes
     no part and passes (plus the residual's).  ``out``: a (y, mean, rstd) of
     an earlier call to write into; its y may be x or residual."""
-    raw = _stream(x, stream)
     y, mean, rstd = out or (None, None, None)
-    ws = stream and _scratch(x, stream, lambda: _norm_bytes(x, groups, 0))
-    return _binding.group_norm(x, groups, gamma, beta, residual, _act(act),
-                               carry, eps, y, mean, rstd, ws, raw)
+    return _run(_binding.group_norm, x, stream, x, groups, gamma, beta,
+                residual, _act(act), carry, eps, y, mean, rstd)
 
 
 def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None,
@@ -107,12 +89,10 @@ def group_norm_backward(dy, x, mean, rstd, groups, gamma=None, beta=None,
     residual, dgamma and dbeta are always given (fp32).  ``out``: a tuple of
     an earlier call to write into, or of tensors and None (not wanted); its
     dx or its dresidual may be dy."""
-    raw = _stream(x, stream)
     dx, dr, dgamma, dbeta = out or (None, None, None, None)
-    ws = stream and _scratch(x, stream, lambda: _norm_bytes(x, groups, 1))
-    return _binding.group_norm_backward(
-        dy, x, mean, rstd, groups, gamma, beta, residual, _act(act), carry,
-        out is None, dx, dr, dgamma, dbeta, ws, raw)
+    return _run(_binding.group_norm_backward, x, stream, dy, x, mean, rstd,
+                groups, gamma, beta, residual, _act(act), carry, out is None,
+                dx, dr, dgamma, dbeta)
 
 
 def fp8_quantize(x, qtype="e4m3", block_rows=1, transpose=False, out=None,
@@ -123,10 +103,9 @@ def fp8_quantize(x, qtype="e4m3", block_rows=1, transpose=False, out=None,
     scales [column blocks, row blocks] fp32; x is about q * scale."""
     if qtype not in _QTYPE:
         raise ValueError("qtype must be one of %s" % sorted(_QTYPE))
-    raw = _stream(x, stream)
     q, scales = out or (None, None)
-    return _binding.fp8_quantize(x, _QTYPE[qtype], block_rows, transpose, q,
-                                 scales, raw)
+    return _run(_binding.fp8_quantize, x, stream, x, _QTYPE[qtype],
+                block_rows, transpose, q, scales)
 
 
 def fp8_matmul(a, a_scales, b, b_scales, bias=None, act="none",
@@ -134,14 +113,8 @@ def fp8_matmul(a, a_scales, b, b_scales, bias=None, act="none",
     """act(A @ B.T + bias) in ``dtype`` for 8-bit matrices a [m, k] and
     b [n, k] with the scales of :func:`fp8_quantize` (A and B are the values
     they stand for)."""
-    raw = _stream(a, stream)
-    ws = stream and _scratch(
-        a, stream, lambda: ctc.ctc_fp8_matmul_workspace_bytes(
-            _TYPE[dtype if out is None else out.dtype], a.shape[0],
-            b.shape[0], a.shape[1],
-            1 if b_scales.shape[1] == b.shape[0] else 128))
-    return _binding.fp8_matmul(a, a_scales, b, b_scales, bias, _act(act),
-                               dtype, out, ws, raw)
+    return _run(_binding.fp8_matmul, a, stream, a, a_scales, b, b_scales,
+                bias, _act(act), dtype, out)
 
 
 class TokenScores(NamedTuple):
@@ -164,12 +137,9 @@ def token_scores(logits, targets=None, top_k=0, out=None, stream=None):
     rank, and the ``top_k`` best alternatives with their log probabilities
     (ties to the lower index; -1 and -inf where there is none).  ``out``: a
     TokenScores of an earlier call to write into."""
-    raw = _stream(logits, stream)
-    ws = stream and _scratch(
-        logits, stream, lambda: ctc.ctc_token_scores_workspace_bytes(
-            logits.shape[0], logits.shape[1], top_k))
-    return TokenScores._make(_binding.token_scores(
-        logits, targets, top_k, out is None, out or _NO_SCORES, ws, raw))
+    return TokenScores._make(_run(
+        _binding.token_scores, logits, stream, logits, targets, top_k,
+        out is None, out or _NO_SCORES))
 
 
 def token_scores_backward(logits, targets, lse, entropy=None, g_lse=None,
@@ -180,6 +150,5 @@ def token_scores_backward(logits, targets, lse, entropy=None, g_lse=None,
     None).  ``out`` may be logits itself."""
     if lse is None:
         raise ValueError("lse is needed")
-    return _binding.token_scores_backward(logits, targets, lse, entropy,
-                                          g_lse, g_logprob, g_entropy, out,
-                                          _stream(logits, stream))
+    return _run(_binding.token_scores_backward, logits, stream, logits,
+                targets, lse, entropy, g_lse, g_logprob, g_entropy, out)

@@ -721,6 +721,26 @@ def test_operators_on_another_stream(ops):
         assert torch.equal(a, b)
 
 
+def test_another_stream_takes_no_block_of_the_current_one(ops):
+    """A block that was freed on the current stream may be in use there
+    until its queued work is done: outputs and workspaces of a call on
+    another stream come from that one's blocks."""
+    side = torch.cuda.Stream()
+    x = _randn(_gen(4), 3, 64, 250)
+    logits = _randn(_gen(5), 1, 100000)
+    torch.cuda.synchronize()
+    for call, size in [(lambda: ops.group_norm(x, 5, stream=side)[0], x.numel() * 4),
+                       (lambda: ops.fp8_quantize(x[0], stream=side)[0], 64 * 256),
+                       (lambda: ops.token_scores(logits, None, 8, stream=side.cuda_stream)[0],
+                        8)]:
+        freed = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        there = {t.data_ptr() for t in freed}
+        del freed
+        out = call()
+        assert out.data_ptr() not in there
+        torch.cuda.synchronize()
+
+
 def test_operators_in_a_graph(ops):
     """Captured once with caller-owned outputs, replayed on new inputs with
     eager work in between."""
