@@ -27,10 +27,15 @@ struct NormPlan {
     int ctiles, chunks;          // of a pixel row, of an image
     int64_t chunk;               // pixels
 };
+// Channels of a vector: 16 bytes, or what divides the channels.
+static int norm_width(const NormArgs &a) {
+    int v = 16 / type_bytes(a.type);
+    while (a.c % v) v /= 2;
+    return v;
+}
 static NormPlan norm_plan(const NormArgs &a) {
     NormPlan p{};
-    p.v = 16 / type_bytes(a.type);
-    while (a.c % p.v) p.v /= 2;
+    p.v = norm_width(a);
     const int cv = a.c / p.v;
     p.tx = cv < 256 ? cv : 256;
     p.pl = 256 / p.tx;
@@ -124,35 +129,89 @@ __device__ __forceinline__ int norm_count(const NormArgs &a, int g) {
     return a.c / a.groups - (a.carry && g == a.groups - 1);
 }
 
-// Joins the chunks and channels of an (image, group): one wave each.
-static __global__ __launch_bounds__(256) void norm_stats_join(NormArgs a, NormPlan p) {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+// Joining an (image, group): W waves over its chunks and channels.
+constexpr int JOIN_WAVES = 16;
+template <int W> struct NormJoin {
+    int64_t img, t;
+    int g, per, nc, entries, at; // at: the thread's place among the W waves
+    const float *part;
+    // `t`th (image, group); part: [n][chunks][c][2]
+    __device__ NormJoin(const NormArgs &a, const NormPlan &p, int64_t t_) : t(t_) {
+        img = t / a.groups;
+        g = (int)(t % a.groups);
+        per = a.c / a.groups;
+        nc = norm_count(a, g);
+        entries = p.chunks * nc;
+        part = a.ws + img * p.chunks * a.c * 2 + g * per * 2;
+        at = threadIdx.x % (64 * W);
+    }
+    // f(entry, chunk, channel of the group), eight loads under way
+    template <typename F> __device__ __forceinline__ void each(const NormArgs &a, F f) {
+        if (nc == 0) return;
+        const int step = 64 * W, dch = step / nc, dc = step % nc;
+        int ch = at / nc, c = at % nc;
+#pragma unroll 8
+        for (int i = at; i < entries; i += step) {
+            f(*(const float2 *)(part + ((int64_t)ch * a.c + c) * 2), ch, c);
+            ch += dch;
+            c += dc;
+            if (c >= nc) {
+                c -= nc;
+                ch++;
+            }
+        }
+    }
+    // Sum over the W waves, for all of them.
+    __device__ __forceinline__ float sum(float v, float *lds) {
+        v = wave_sum(v);
+        if constexpr (W > 1) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; i++) v += lds[i];
+        }
+        return v;
+    }
+};
+// A wave takes an (image, group) of up to 1024 entries, a workgroup of 16 a
+// longer one (30690 entries: 247 us by one wave, 12 by 16).
+static bool norm_join_wide(const NormArgs &a, const NormPlan &p) {
+    return (int64_t)p.chunks * (a.c / a.groups) > 1024;
+}
+template <int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_stats_join(NormArgs a, NormPlan p) {
+    __shared__ float lds[W];
+    const int64_t t = W == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (t >= a.n * a.groups) return;
-    const int64_t img = t / a.groups;
-    const int g = (int)(t % a.groups), per = a.c / a.groups, nc = norm_count(a, g);
-    const int lane = threadIdx.x & 63;
-    const float *part = a.ws + img * p.chunks * a.c * 2;
-    const int entries = p.chunks * nc;
-    float mean = 0.f, m2 = 0.f;
-    const float total = (float)a.hw * nc;
-    for (int i = lane; i < entries; i += 64) {
-        const int ch = i / nc;
-        const float *e = part + ((int64_t)ch * a.c + g * per + i % nc) * 2;
+    NormJoin<W> j(a, p, t);
+    const float total = (float)a.hw * j.nc;
+    auto pixels = [&](int ch) {
         const int64_t left = a.hw - ch * p.chunk;
-        mean += e[0] * (float)(left < p.chunk ? left : p.chunk);
-    }
-    mean = nc ? wave_sum(mean) / total : 0.f;
-    for (int i = lane; i < entries; i += 64) {
-        const int ch = i / nc;
-        const float *e = part + ((int64_t)ch * a.c + g * per + i % nc) * 2;
-        const int64_t left = a.hw - ch * p.chunk;
-        const float d = e[0] - mean;
-        m2 += e[1] + d * d * (float)(left < p.chunk ? left : p.chunk);
-    }
-    m2 = nc ? wave_sum(m2) / total : 0.f;
-    if (lane == 0) {
-        a.mean[t] = mean;
-        a.rstd[t] = 1.f / __builtin_sqrtf(m2 + a.eps);
+        return (float)(left < p.chunk ? left : p.chunk);
+    };
+    // about the mean of the first entries (of up to 64 W channels), which lies
+    // within the group's spread: one loop, and no digits lost
+    const int some = j.entries < 64 * W ? j.entries : 64 * W;
+    float at = 0.f;
+    if (j.at < some) at = j.part[((int64_t)(j.at / j.nc) * a.c + j.at % j.nc) * 2];
+    at = j.sum(at, lds);
+    at = some ? at / (float)some : 0.f;
+    float s1 = 0.f, s2 = 0.f;
+    j.each(a, [&](float2 e, int ch, int) {
+        const float d = e.x - at, w = d * pixels(ch);
+        s1 += w;
+        s2 += __builtin_fmaf(d, w, e.y);
+    });
+    s1 = j.sum(s1, lds);
+    s2 = j.sum(s2, lds);
+    if (j.at == 0) {
+        const float d = j.nc ? s1 / total : 0.f;
+        float var = j.nc ? s2 / total - d * d : 0.f;
+        var = var < 0.f ? 0.f : var;             // (a NaN stays)
+        a.mean[t] = at + d;
+        a.rstd[t] = 1.f / __builtin_sqrtf(var + a.eps);
     }
 }
 
@@ -305,33 +364,30 @@ __device__ __forceinline__ void norm_dx(const NormChannels<V> &k, const float (&
 __host__ __device__ inline int64_t norm_sums_at(const NormArgs &a, const NormPlan &p) {
     return a.n * p.chunks * a.c * 2;
 }
-// Joins them: the first workgroups take 16 (image, group)s each, a wave each;
+// Joins them: the first workgroups take the (image, group)s, W waves each;
 // the others 16 channels each (dgamma, dbeta over all images), by 64 rows of
 // threads with eight loads in flight (16 rows took 17 us for 2048 chunks of
 // 128 channels, these 6).
 constexpr int JOIN_ROWS = 64;
-static __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
-                                                              int64_t group_blocks) {
-    const int lane = threadIdx.x & 63;
+template <int W>
+__global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
+                                                       int64_t group_blocks) {
     if (blockIdx.x < group_blocks) {
-        const int64_t t = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 6);
+        __shared__ float lds[W];
+        const int64_t t = W == 1 ? (int64_t)blockIdx.x * 16 + (threadIdx.x >> 6) : blockIdx.x;
         if (t >= a.n * a.groups) return;
-        const int64_t img = t / a.groups;
-        const int g = (int)(t % a.groups), per = a.c / a.groups, nc = norm_count(a, g);
-        const float *part = a.ws + img * p.chunks * a.c * 2;
+        NormJoin<W> j(a, p, t);
         float s1 = 0.f, s2 = 0.f;
-        for (int i = lane; i < p.chunks * nc; i += 64) {
-            const int c = g * per + i % nc;
-            const float *e = part + ((int64_t)(i / nc) * a.c + c) * 2;
-            const float w = a.gamma ? a.gamma[c] : 1.f;
-            s1 += e[0] * w;
-            s2 += e[1] * w;
-        }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
-        if (lane == 0) {
+        j.each(a, [&](float2 e, int, int c) {
+            const float w = a.gamma ? a.gamma[j.g * j.per + c] : 1.f;
+            s1 = __builtin_fmaf(e.x, w, s1);
+            s2 = __builtin_fmaf(e.y, w, s2);
+        });
+        s1 = j.sum(s1, lds);
+        s2 = j.sum(s2, lds);
+        if (j.at == 0) {
             float *out = a.ws + norm_sums_at(a, p) + t * 2;
-            const float inv = nc ? 1.f / ((float)a.hw * nc) : 0.f;
+            const float inv = j.nc ? 1.f / ((float)a.hw * j.nc) : 0.f;
             out[0] = s1 * inv;
             out[1] = s2 * inv;
         }
@@ -396,10 +452,11 @@ __global__ __launch_bounds__(256) void norm_grad_apply(NormArgs a, NormPlan p) {
 // vectors a thread holds, of x (and of dy)
 template <int NT> constexpr int slab_r() { return 4; }
 template <int NT> constexpr int slab_r_forward() { return NT == 256 ? 4 : 8; }
-struct SlabPlan { int w, tx, pl, slabs, nt; bool ok, by_xcd; };
+// lanes: pixel lanes that hold pixels; slices: threads that add up a channel's
+struct SlabPlan { int v, w, tx, pl, slabs, nt, lanes, slices; bool ok, by_xcd; };
 
-template <typename T, int NT, int N> struct Slab {
-    static constexpr int V = 16 / (int)sizeof(T), NW = NT / 64;
+template <typename T, int V, int NT, int N> struct Slab {
+    static constexpr int NW = NT / 64;
     struct Lds {
         float v[N][NT * V];
         float chan[N][NT];                       // per channel, of w <= NT
@@ -433,11 +490,13 @@ template <typename T, int NT, int N> struct Slab {
 #pragma unroll
                 for (int e = 0; e < V; e++) l.v[n][(px * p.tx + cx) * V + e] = s[n][e];
         __syncthreads();
-        // a channel's lanes in slices, then the slices
-        const int slices = NT / p.w, i = threadIdx.x, c = i % p.w, q = i / p.w;
+        // a channel's lanes in slices, then the slices: about as many slices
+        // as lanes of one (as many as there are threads took 15 us, these 9,
+        // for 12 images of 2 x 2 x 4)
+        const int slices = p.slices, i = threadIdx.x, c = i % p.w, q = i / p.w;
         float t[N] = {};
         if (q < slices)
-            for (int x = q; x < p.pl; x += slices)
+            for (int x = q; x < p.lanes; x += slices)
 #pragma unroll
                 for (int n = 0; n < N; n++) t[n] += l.v[n][x * p.w + c];
         __syncthreads();
@@ -469,21 +528,21 @@ template <typename T, int NT, int N> struct Slab {
     }
 };
 
-template <typename T, int NT>
+template <typename T, int V, int NT>
 __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
-    typedef Slab<T, NT, 1> S;
-    constexpr int V = S::V, R = slab_r_forward<NT>();
+    typedef Slab<T, V, NT, 1> S;
+    constexpr int R = slab_r_forward<NT>();
     __shared__ typename S::Lds l;
     S s;
     if (!s.place(a, p)) return;
     const int per = a.c / a.groups, gs = p.w / per, g0 = s.slab * gs;
     const int64_t base = s.img * a.hw * a.c + s.c0;
     const T *x = (const T *)a.x + base;
-    u4 raw[R];
+    Raw<T, V> raw[R];
 #pragma unroll
     for (int r = 0; r < R; r++) {
         const int64_t q = s.px + (int64_t)r * p.pl;
-        if (s.on && q < a.hw) __builtin_memcpy(&raw[r], x + q * a.c, 16);
+        if (s.on && q < a.hw) raw[r].load(x + q * a.c);
     }
     const int ck = a.carry ? a.c - 1 - s.slab * p.w : -1;   // its channel here
     auto count = [&](int g) { return (float)a.hw * (per - (ck >= 0 && ck / per == g)); };
@@ -493,10 +552,10 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
     for (int r = 0; r < R; r++)
         if (s.on && s.px + (int64_t)r * p.pl < a.hw) {
             float v[V];
-            values_of<T>(raw[r], v);
+            raw[r].values(v);
 #pragma unroll
             for (int e = 0; e < V; e++) sum[0][e] += v[e];
-            held(raw[r]);
+            raw[r].hold();
         }
     s.channels(l, p, sum);
     s.groups(gs, per,
@@ -513,13 +572,13 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
     for (int r = 0; r < R; r++)
         if (s.on && s.px + (int64_t)r * p.pl < a.hw) {
             float v[V];
-            values_of<T>(raw[r], v);
+            raw[r].values(v);
 #pragma unroll
             for (int e = 0; e < V; e++) {
                 const float d = v[e] - mean[e];
                 sq[0][e] = __builtin_fmaf(d, d, sq[0][e]);
             }
-            held(raw[r]);
+            raw[r].hold();
         }
     s.channels(l, p, sq);
     s.groups(gs, per,
@@ -543,7 +602,7 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
         if (q < a.hw) {
             float v[V], rv[V] = {};
             if (a.residual) load<T, V>(res + q * a.c, rv);
-            values_of<T>(raw[r], v);
+            raw[r].values(v);
             norm_values<V>(a, k, v, rv);
             store<T, V>(y + q * a.c, v);
         }
@@ -551,11 +610,12 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
 }
 
 // The same for the gradients: x and dy in registers; the channels' sums over
-// the image go to ws [n][c][2] for norm_grad_join (a plan of one chunk).
-template <typename T, int NT>
+// the image go to ws [n][c][2] for norm_grad_join (a plan of one chunk), or,
+// of a single image, where they belong.
+template <typename T, int V, int NT>
 __global__ __launch_bounds__(NT) void norm_grad_slab(NormArgs a, SlabPlan p) {
-    typedef Slab<T, NT, 2> S;
-    constexpr int V = S::V, R = slab_r<NT>();
+    typedef Slab<T, V, NT, 2> S;
+    constexpr int R = slab_r<NT>();
     __shared__ typename S::Lds l;
     S s;
     if (!s.place(a, p)) return;
@@ -563,21 +623,21 @@ __global__ __launch_bounds__(NT) void norm_grad_slab(NormArgs a, SlabPlan p) {
     const int64_t base = s.img * a.hw * a.c + s.c0;
     const T *x = (const T *)a.x + base, *dy = (const T *)a.dy + base;
     const T *res = (const T *)a.residual + base;
-    u4 xr[R], dr[R];
+    Raw<T, V> xr[R], dr[R];
 #pragma unroll
     for (int r = 0; r < R; r++) {
         const int64_t q = s.px + (int64_t)r * p.pl;
         if (s.on && q < a.hw) {
-            __builtin_memcpy(&xr[r], x + q * a.c, 16);
-            __builtin_memcpy(&dr[r], dy + q * a.c, 16);
+            xr[r].load(x + q * a.c);
+            dr[r].load(dy + q * a.c);
         }
     }
     const NormChannels<V> k = norm_channels<V>(a, s.img, s.on ? s.c0 : 0);
     auto values = [&](int r, int64_t q, float (&dz)[V], float (&xh)[V]) {
         float v[V], g[V], rv[V] = {};
         if (a.residual) load<T, V>(res + q * a.c, rv);
-        values_of<T>(xr[r], v);
-        values_of<T>(dr[r], g);
+        xr[r].values(v);
+        dr[r].values(g);
         norm_dz<V>(a, k, v, g, rv, dz, xh);
     };
     float sum[2][V] = {};
@@ -592,17 +652,22 @@ __global__ __launch_bounds__(NT) void norm_grad_slab(NormArgs a, SlabPlan p) {
                 sum[0][e] += dz[e];
                 sum[1][e] = __builtin_fmaf(dz[e], xh[e], sum[1][e]);
             }
-            held(xr[r]);
-            held(dr[r]);
+            xr[r].hold();
+            dr[r].hold();
         }
     }
     s.channels(l, p, sum);
-    for (int c = threadIdx.x; c < p.w; c += NT) {
-        float *out = a.ws + (s.img * a.c + s.slab * p.w + c) * 2;
-        out[0] = l.chan[0][c];
-        out[1] = l.chan[1][c];
-    }
     const int ck = a.carry ? a.c - 1 - s.slab * p.w : -1;
+    for (int c = threadIdx.x; c < p.w; c += NT) {
+        if (a.n == 1) {
+            if (a.dbeta) a.dbeta[s.slab * p.w + c] = c == ck ? 0.f : l.chan[0][c];
+            if (a.dgamma) a.dgamma[s.slab * p.w + c] = c == ck ? 0.f : l.chan[1][c];
+        } else {
+            float *out = a.ws + (s.img * a.c + s.slab * p.w + c) * 2;
+            out[0] = l.chan[0][c];
+            out[1] = l.chan[1][c];
+        }
+    }
     s.groups(gs, per,
              [&](int c, float (&t)[2]) {
                  const float w = a.gamma ? a.gamma[s.slab * p.w + c] : 1.f;
@@ -636,11 +701,11 @@ __global__ __launch_bounds__(NT) void norm_grad_slab(NormArgs a, SlabPlan p) {
     }
 }
 
-// Whether and how a map is taken in slabs.  Vectors of 16 bytes only.
+// Whether and how a map is taken in slabs.
 static SlabPlan slab_plan(const NormArgs &a, bool backward) {
     SlabPlan p{};
-    const int v = 16 / type_bytes(a.type), per = a.c / a.groups;
-    if (a.c % v || a.n < 1) return p;
+    const int v = norm_width(a), full = 16 / type_bytes(a.type), per = a.c / a.groups;
+    if (a.n < 1) return p;
     int g = per, b = v;                          // least common multiple
     while (b) {
         const int t = g % b;
@@ -658,7 +723,7 @@ static SlabPlan slab_plan(const NormArgs &a, bool backward) {
             const int pl = nt / (int)(w / v);
             return (a.hw + pl - 1) / pl <= r;
         };
-        const int nt = fits(256, 4) ? 256 : fits(1024, backward ? 4 : 8) ? 1024 : 0;
+        const int nt = v == full && fits(256, 4) ? 256 : fits(1024, backward ? 4 : 8) ? 1024 : 0;
         if (!nt) break;
         // pieces of 16 bytes only where latency is all
         if (w * type_bytes(a.type) < 32 && a.c * type_bytes(a.type) >= 32 &&
@@ -667,11 +732,16 @@ static SlabPlan slab_plan(const NormArgs &a, bool backward) {
         // wider slabs read longer pieces of a row, down to one workgroup a CU
         if (p.ok && (w * type_bytes(a.type) > 128 || a.n * (k / m) < 256)) break;
         p.ok = true;
+        p.v = v;
         p.w = (int)w;
         p.nt = nt;
         p.tx = (int)(w / v);
         p.pl = nt / p.tx;
         p.slabs = k / m;
+    }
+    if (p.ok) {
+        p.lanes = a.hw < p.pl ? (int)a.hw : p.pl;
+        while (p.slices * p.slices < p.lanes && (p.slices + 1) * p.w <= p.nt) p.slices++;
     }
     p.by_xcd = a.n >= 8;
     return p;
@@ -682,7 +752,7 @@ static dim3 slab_grid(const NormArgs &a, const SlabPlan &p) {
 
 size_t norm_workspace(const NormArgs &a, bool backward) {
     const SlabPlan sp = slab_plan(a, backward);
-    if (sp.ok) return backward ? (size_t)a.n * a.c * 2 * 4 : 0;
+    if (sp.ok) return backward && a.n > 1 ? (size_t)a.n * a.c * 2 * 4 : 0;
     const NormPlan p = norm_plan(a);
     return 4 * (size_t)(norm_sums_at(a, p) + (backward ? a.n * a.groups * 2 : 0));
 }
@@ -704,10 +774,13 @@ hipError_t launch_norm_forward(const NormArgs &a, hipStream_t st) {
     if (a.n == 0) return hipSuccess;
     const SlabPlan sp = slab_plan(a, false);
     if (sp.ok)
-        return by_type(a.type, [&](auto tag) {
+        return by_width(a.type, sp.v, [&](auto tag, auto vc) {
             typedef typename decltype(tag)::type T;
-            return sp.nt == 256 ? start(norm_slab<T, 256>, slab_grid(a, sp), 256, st, a, sp)
-                                : start(norm_slab<T, 1024>, slab_grid(a, sp), 1024, st, a, sp);
+            constexpr int V = decltype(vc)::value;
+            if constexpr (V * sizeof(T) == 16)
+                if (sp.nt == 256)
+                    return start(norm_slab<T, V, 256>, slab_grid(a, sp), 256, st, a, sp);
+            return start(norm_slab<T, V, 1024>, slab_grid(a, sp), 1024, st, a, sp);
         });
     const NormPlan p = norm_plan(a);
     const dim3 grid((unsigned)(a.n * p.chunks * p.ctiles));
@@ -716,7 +789,11 @@ hipError_t launch_norm_forward(const NormArgs &a, hipStream_t st) {
         constexpr int V = decltype(vc)::value;
         hipError_t e = start(norm_stats<T, V>, grid, 256, st, a, p);
         if (e != hipSuccess) return e;
-        e = start(norm_stats_join, dim3((unsigned)((a.n * a.groups + 3) / 4)), 256, st, a, p);
+        e = norm_join_wide(a, p)
+                ? start(norm_stats_join<JOIN_WAVES>, dim3((unsigned)(a.n * a.groups)),
+                        64 * JOIN_WAVES, st, a, p)
+                : start(norm_stats_join<1>, dim3((unsigned)((a.n * a.groups + 3) / 4)), 256, st,
+                        a, p);
         if (e != hipSuccess) return e;
         return start(norm_apply<T, V>, grid, 256, st, a, p);
     });
@@ -726,17 +803,19 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t st) {
     if (a.n == 0 && !a.dgamma && !a.dbeta) return hipSuccess;
     const SlabPlan sp = slab_plan(a, true);
     if (sp.ok) {
-        hipError_t e = by_type(a.type, [&](auto tag) {
+        hipError_t e = by_width(a.type, sp.v, [&](auto tag, auto vc) {
             typedef typename decltype(tag)::type T;
-            return sp.nt == 256
-                       ? start(norm_grad_slab<T, 256>, slab_grid(a, sp), 256, st, a, sp)
-                       : start(norm_grad_slab<T, 1024>, slab_grid(a, sp), 1024, st, a, sp);
+            constexpr int V = decltype(vc)::value;
+            if constexpr (V * sizeof(T) == 16)
+                if (sp.nt == 256)
+                    return start(norm_grad_slab<T, V, 256>, slab_grid(a, sp), 256, st, a, sp);
+            return start(norm_grad_slab<T, V, 1024>, slab_grid(a, sp), 1024, st, a, sp);
         });
-        if (e != hipSuccess || (!a.dgamma && !a.dbeta)) return e;
+        if (e != hipSuccess || a.n == 1 || (!a.dgamma && !a.dbeta)) return e;
         NormPlan one{};
         one.chunks = 1;
         one.chunk = a.hw;
-        return start(norm_grad_join, dim3((unsigned)((a.c + 15) / 16)), 1024, st, a, one,
+        return start(norm_grad_join<1>, dim3((unsigned)((a.c + 15) / 16)), 1024, st, a, one,
                      (int64_t)0);
     }
     const NormPlan p = norm_plan(a);
@@ -749,8 +828,11 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t st) {
             e = start(norm_grad_sums<T, V>, grid, 256, st, a, p);
             if (e != hipSuccess) return e;
         }
-        const int64_t gb = (a.n * a.groups + 15) / 16;
-        e = start(norm_grad_join, dim3((unsigned)(gb + (a.c + 15) / 16)), 1024, st, a, p, gb);
+        const bool wide = norm_join_wide(a, p);
+        const int64_t gb = wide ? a.n * a.groups : (a.n * a.groups + 15) / 16;
+        const dim3 jg((unsigned)(gb + (a.c + 15) / 16));
+        e = wide ? start(norm_grad_join<JOIN_WAVES>, jg, 1024, st, a, p, gb)
+                 : start(norm_grad_join<1>, jg, 1024, st, a, p, gb);
         if (e != hipSuccess || !a.n || (!a.dx && !a.dresidual)) return e;
         return start(norm_grad_apply<T, V>, grid, 256, st, a, p);
     });

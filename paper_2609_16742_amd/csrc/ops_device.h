@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 namespace ctc {
 namespace ops {
 
@@ -45,20 +47,31 @@ __device__ __forceinline__ void store(T *p, const float (&v)[V]) {
     __builtin_memcpy(p, &r, sizeof r);
 }
 
-// 16 bytes kept in four registers, and their values.  held() hides where
-// they came from: the compiler would keep the widened values instead, twice
-// the registers for 16-bit types.
-template <typename T, int V = 16 / (int)sizeof(T)>
-__device__ __forceinline__ void values_of(u4 r, float (&v)[V]) {
-    const Pack<T, V> q = __builtin_bit_cast(Pack<T, V>, r);
+// V elements kept as they stand in memory.  hold() hides where they came
+// from: the compiler would keep the widened values instead, twice the
+// registers for 16-bit types.
+template <typename T, int V> struct Raw {
+    typedef typename std::conditional<
+        V * sizeof(T) == 16, u4,
+        typename std::conditional<
+            V * sizeof(T) == 8, u2,
+            typename std::conditional<V * sizeof(T) == 4, uint32_t, uint16_t>::type>::type>::type
+        Bits;
+    Bits bits;
+    __device__ __forceinline__ void load(const T *p) { __builtin_memcpy(&bits, p, sizeof bits); }
+    __device__ __forceinline__ void values(float (&v)[V]) const {
+        const Pack<T, V> q = __builtin_bit_cast(Pack<T, V>, bits);
 #pragma unroll
-    for (int i = 0; i < V; i++) v[i] = widen(q.e[i]);
-}
-__device__ __forceinline__ void held(u4 &r) {
-    uint32_t a = r[0], b = r[1], c = r[2], d = r[3];
-    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
-    r = u4{a, b, c, d};
-}
+        for (int i = 0; i < V; i++) v[i] = widen(q.e[i]);
+    }
+    __device__ __forceinline__ void hold() {
+        if constexpr (V * sizeof(T) == 16) {
+            uint32_t a = bits[0], b = bits[1], c = bits[2], d = bits[3];
+            asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+            bits = u4{a, b, c, d};
+        }
+    }
+};
 
 // The larger of values, a NaN lost against a number (as single
 // instructions: fmaxf first quiets its arguments).
