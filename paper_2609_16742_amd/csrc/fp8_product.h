@@ -82,12 +82,19 @@ __device__ __forceinline__ u4 first_bytes(u4 v, int n) {
     return v;
 }
 
-// Four results of row m from column n on.
-__device__ __forceinline__ void product_out(const ProductArgs &p, int64_t m, int64_t n, f4 v) {
-    if (m >= p.m) return;
+// The bias of four columns.
+__device__ __forceinline__ f4 bias_of(const ProductArgs &p, int64_t n) {
+    f4 b = (f4)(0.f);
 #pragma unroll
     for (int e = 0; e < 4; e++)
-        if (p.bias && n + e < p.n) v[e] += p.bias[n + e];
+        if (p.bias && n + e < p.n) b[e] = p.bias[n + e];
+    return b;
+}
+// Four results of row m from column n on.
+__device__ __forceinline__ void product_out(const ProductArgs &p, int64_t m, int64_t n, f4 v,
+                                            f4 bias) {
+    if (m >= p.m) return;
+    v += bias;
     float w[4] = {v[0], v[1], v[2], v[3]};
     act_of<4>(p.act, w);
     const int64_t o = m * p.ldy + n;
@@ -116,11 +123,12 @@ __device__ __forceinline__ void partial_out(const ProductArgs &p, int split, int
 }
 
 // ---------------------------------------------------------------------------
-// Few rows of a: the filters are streamed once.  A workgroup of NW waves
-// takes 16 filters and MT tiles of 16 rows; its waves take every NW-th block
-// of k, each through a ring of R stages in LDS of its own (no barrier: a
-// wave waits for its own loads), and add up at the end.  A stage holds the
-// block's rows as product_tile's do, filters first, then their scales.
+// Few rows of a: the filters are streamed once (for each 64 rows).  A
+// workgroup of NW waves takes 16 filters and MT tiles of 16 rows; its waves
+// take every NW-th block of k, each through a ring of R stages in LDS of its
+// own (no barrier: a wave waits for its own loads), and add up at the end.  A
+// stage holds the block's rows as product_tile's do, filters first, then
+// their scales.
 // What bounds it: the bytes of the filters, and how many are under way (R - 1
 // stages of each wave).  Loading fragments straight into registers took as
 // long for one row, but 41 us instead of 23 for 32 (k = 25088, 4096 filters):
@@ -128,8 +136,8 @@ __device__ __forceinline__ void partial_out(const ProductArgs &p, int split, int
 // unit four times as long.
 // ---------------------------------------------------------------------------
 template <int MT, int FA, int FB, bool WIDE>
-__global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p, int splits,
-                                                                   int per) {
+__global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p, int nt,
+                                                                   int splits, int per) {
     constexpr int NW = MT < 4 ? 8 : 4, R = MT == 1 ? 4 : 3;
     constexpr int ROWS = 16 * (1 + MT), STAGE = ROWS * 128 + 512;
     constexpr int LOADS = ROWS / 8 + 2;          // of a stage
@@ -138,21 +146,22 @@ __global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int fr = lane & 15, fg = lane >> 4;
-    const int64_t n0 = (int64_t)(blockIdx.x / splits) * 16;
-    const int split = blockIdx.x % splits;
+    const int split = blockIdx.x % splits, tile = blockIdx.x / splits;
+    const int64_t n0 = (int64_t)(tile % nt) * 16, m0 = (int64_t)(tile / nt) * (16 * MT);
     const int nblocks = (int)((p.k + 127) / 128);
     const int kb0 = split * per, kb1 = kb0 + per < nblocks ? kb0 + per : nblocks;
     const int kend = (int)p.k;
-    const int ma = (int)p.m, nb = p.n - n0 < 16 ? (int)(p.n - n0) : 16;
-    const Buf ar = __builtin_amdgcn_make_buffer_rsrc((void *)p.a, 0, (int)(ma * p.lda),
-                                                     0x00020000);
+    const int ma = p.m - m0 < 16 * MT ? (int)(p.m - m0) : 16 * MT;
+    const int nb = p.n - n0 < 16 ? (int)(p.n - n0) : 16;
+    const Buf ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + m0 * p.lda), 0,
+                                                     (int)(ma * p.lda), 0x00020000);
     const Buf br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + n0 * p.ldb), 0,
                                                      (int)(nb * p.ldb), 0x00020000);
     const int ash = p.a_block == 1 ? 0 : 7, bsh = p.b_block == 1 ? 0 : 7;
-    const float *sab = p.sa, *sbb = p.sb + (n0 >> bsh);
+    const float *sab = p.sa + (m0 >> ash), *sbb = p.sb + (n0 >> bsh);
     // the scales' places: lane l for row l of a and filter l
-    const int sai = (lane < ma ? lane >> ash : 0) * 4;
-    const int sbi = lane < nb ? (int)((n0 + lane >> bsh) - (n0 >> bsh)) * 4 : 0;
+    const int sai = lane < ma ? (int)(((m0 + lane) >> ash) - (m0 >> ash)) * 4 : 0;
+    const int sbi = lane < nb ? (int)(((n0 + lane) >> bsh) - (n0 >> bsh)) * 4 : 0;
     const int lrow = lane >> 3, lchunk = ((lane & 7) ^ lrow) * 16;
     const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
     char *ring = lds + wave * R * STAGE;
@@ -172,10 +181,10 @@ __global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p
                                                      av + i * 8 * (int)p.lda, 0, 0, 0);
         const int64_t q = on ? kb : 0;
         const Buf sar = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)(sab + q * p.ldsa), 0, on ? (((ma - 1) >> ash) + 1) * 4 : 0, 0x00020000);
+            (void *)(sab + q * p.ldsa), 0, on ? (int)(((m0 + ma - 1) >> ash) - (m0 >> ash) + 1) * 4 : 0, 0x00020000);
         const Buf sbr = __builtin_amdgcn_make_buffer_rsrc(
             (void *)(sbb + q * p.ldsb), 0,
-            on ? (int)((n0 + nb - 1 >> bsh) - (n0 >> bsh) + 1) * 4 : 0, 0x00020000);
+            on ? (int)(((n0 + nb - 1) >> bsh) - (n0 >> bsh) + 1) * 4 : 0, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(sar, (LdsAt)(to + ROWS * 128), 4, sai, 0, 0, 0);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(sbr, (LdsAt)(to + ROWS * 128 + 256), 4, sbi, 0,
                                                  0, 0);
@@ -234,9 +243,9 @@ __global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p
     for (int j = wave; j < MT; j += NW) {
         f4 t = sum[j * 64 + lane];
         for (int i = 1; i < NW; i++) t += sum[(i * MT + j) * 64 + lane];
-        const int64_t m = j * 16 + fr;
+        const int64_t m = m0 + j * 16 + fr;
         if (splits > 1) partial_out(p, split, m, n0 + fg * 4, t);
-        else product_out(p, m, n0 + fg * 4, t);
+        else product_out(p, m, n0 + fg * 4, t, bias_of(p, n0 + fg * 4));
     }
 }
 
@@ -313,11 +322,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, i
 #pragma unroll
     for (int j = 0; j < IM; j++) {
         const int r = wm * TM + j * 16 + fr;
-        sai[j] = (uint32_t)(((int64_t)(r < ma ? r : ma - 1) + m0 >> ash) - (m0 >> ash));
+        sai[j] = (uint32_t)((((int64_t)(r < ma ? r : ma - 1) + m0) >> ash) - (m0 >> ash));
     }
     {
         const int r = SB1 ? (int)threadIdx.x % BN : wn * TN;
-        sbi = (uint32_t)(((int64_t)(r < nb ? r : nb - 1) + n0 >> bsh) - (n0 >> bsh));
+        sbi = (uint32_t)((((int64_t)(r < nb ? r : nb - 1) + n0) >> bsh) - (n0 >> bsh));
     }
     f4 acc[IN][IM], d[2][IM];
 #pragma unroll
@@ -458,15 +467,38 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, i
             if (first < last) acc[IN - 1][j] += d[1][j] * sa[j];
         }
     }
+    // The results go through LDS, each wave's through its own part of the
+    // stages, piece g of row r in place g ^ (r & 15): a lane holds four
+    // columns of one of 16 rows, from where a store would write 16 pieces of
+    // a line, and the code that writes would stand here IN x IM times.
+    constexpr int PART = 2 * STAGE / NW, LINE = TN / 4;   // bytes; pieces of a row
+    constexpr int HELD = PART / (TN * 4) < TM ? PART / (TN * 4) : TM;
+    static_assert(HELD % 16 == 0 && TM % HELD == 0 && LINE <= 64, "rows held");
+    arrived();                                   // (loads past the range wrote zeros)
+    f4 *held = (f4 *)(lds + wave * PART);
+    const int64_t n = n0 + wn * TN + lane % LINE * 4;
+    const f4 bias = splits > 1 ? (f4)(0.f) : bias_of(p, n);
 #pragma unroll
-    for (int j = 0; j < IM; j++)
+    for (int h = 0; h < TM / HELD; h++) {
 #pragma unroll
-        for (int i = 0; i < IN; i++) {
-            const int64_t m = m0 + wm * TM + j * 16 + fr, n = n0 + wn * TN + i * 16 + fg * 4;
+        for (int j = 0; j < HELD / 16; j++)
+#pragma unroll
+            for (int i = 0; i < IN; i++)
+                held[(j * 16 + fr) * LINE + ((i * 4 + fg) ^ fr)] = acc[i][h * (HELD / 16) + j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+        for (int t = 0; t < HELD * LINE / 64; t++) {
+            const int q = t * (64 / LINE) + lane / LINE;
+            const f4 v = held[q * LINE + (lane % LINE ^ (q & 15))];
+            const int64_t m = m0 + wm * TM + h * HELD + q;
             if (n >= p.n) continue;
-            if (splits > 1) partial_out(p, split, m, n, acc[i][j]);
-            else product_out(p, m, n, acc[i][j]);
+            if (splits > 1) partial_out(p, split, m, n, v);
+            else product_out(p, m, n, v, bias);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // Adds the ranges' partial sums, in order: four results a thread.
@@ -486,7 +518,7 @@ static __global__ __launch_bounds__(256) void product_join(ProductArgs p, int sp
                 if (n + e < p.n) v[e] = o[e];
         t += v;
     }
-    product_out(p, m, n, t);
+    product_out(p, m, n, t, bias_of(p, n));
 }
 
 // kind 0: product_rows; product_tile: 1 128 x 128, 2 256 x 256 tiles, 3
@@ -496,15 +528,19 @@ static ProductPlan product_plan(const ProductArgs &a) {
     ProductPlan r{};
     const int64_t nb = (a.k + 127) / 128;
     int64_t wgs, want, least;
-    if (a.m <= 64) {
+    // Short products too go to product_rows, whose waves have several blocks
+    // under way: 214 x 102 x 2912 in 8 us instead of 14, 10807 x 10 x 5933 in
+    // 15 instead of 22; at 3467 x 120 x 4227 (14520 below) it takes 26, tiles 18.
+    const int64_t few = ((a.m + 63) / 64) * ((a.n + 15) / 16);
+    if (a.m <= 64 || (few <= 512 && few * nb <= 8192)) {
         r.kind = 0;
         r.mt = a.m <= 16 ? 1 : a.m <= 32 ? 2 : 4;
         r.nt = (int)((a.n + 15) / 16);
-        wgs = r.nt;
+        wgs = few;
         want = 256;
         // blocks of a range: eight a wave, joining costs as much as reading
         // them
-        least = 64;
+        least = r.mt < 4 ? 64 : 32;
     } else {
         const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
         r.kind = a.ytype == F32 ? 3 : big >= 192 && a.b_block > 1 ? 2 : 1;
@@ -533,12 +569,15 @@ template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hip
     const ProductPlan r = product_plan(a);
     hipError_t e;
     if (r.kind == 0) {
-        const dim3 grid((unsigned)(r.nt * r.splits), 1);
+        const dim3 grid((unsigned)((a.m + 16 * r.mt - 1) / (16 * r.mt) * r.nt * r.splits));
         auto rows = [&](auto wide) {
             constexpr bool W = decltype(wide)::value;
-            return r.mt == 1 ? start(product_rows<1, FA, FB, W>, grid, 512, st, a, r.splits, r.per)
-                 : r.mt == 2 ? start(product_rows<2, FA, FB, W>, grid, 512, st, a, r.splits, r.per)
-                             : start(product_rows<4, FA, FB, W>, grid, 256, st, a, r.splits, r.per);
+            auto go = [&](auto kernel, int threads) {
+                return start(kernel, grid, threads, st, a, r.nt, r.splits, r.per);
+            };
+            return r.mt == 1   ? go(product_rows<1, FA, FB, W>, 512)
+                   : r.mt == 2 ? go(product_rows<2, FA, FB, W>, 512)
+                               : go(product_rows<4, FA, FB, W>, 256);
         };
         e = a.ytype == F32 ? rows(std::true_type()) : rows(std::false_type());
     } else {
