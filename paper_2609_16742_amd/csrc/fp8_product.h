@@ -501,6 +501,153 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, i
     }
 }
 
+// ---------------------------------------------------------------------------
+// 128 x 128 tiles with three steps of loads under way: a ring of four LDS
+// stages (rows as in product_tile, then the scales of the 128 rows and the
+// 128 filters), one workgroup of 2 x 4 waves a CU.  Every wave sends as many
+// loads a step, so a wait for all but the last two steps' is a count.
+// What bounds it: the latency of a step's loads, where there are few steps.
+// ---------------------------------------------------------------------------
+template <int FA, int FB, bool WIDE>
+__global__ __launch_bounds__(512) void product_ring(ProductArgs p, int mt, int nt, int splits,
+                                                    int per) {
+    constexpr int B = 128, S = 4, IM = 4, IN = 2, TM = 64, TN = 32;
+    constexpr int STAGE = 2 * B * 128 + 2 * B * 4, LOADS = 5;
+    __shared__ __attribute__((aligned(16))) char lds[S * STAGE];
+    static_assert(B * B * 4 <= S * STAGE, "results");
+    // each XCD runs a contiguous range of tiles (workgroups go round them)
+    const int total = mt * nt * splits, share = (total + 7) / 8;
+    int t = (blockIdx.x & 7) * share + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= share || t >= total) return;
+    const int split = t / (mt * nt);
+    t -= split * (mt * nt);
+    const int64_t m0 = (int64_t)(t % mt) * B, n0 = (int64_t)(t / mt) * B;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const int fr = lane & 15, fg = lane >> 4;
+    const int ma = p.m - m0 < B ? (int)(p.m - m0) : B, nb = p.n - n0 < B ? (int)(p.n - n0) : B;
+    const Buf ar = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + m0 * p.lda), 0,
+                                                     (int)(ma * p.lda), 0x00020000);
+    const Buf br = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + n0 * p.ldb), 0,
+                                                     (int)(nb * p.ldb), 0x00020000);
+    const int nblocks = (int)((p.k + 127) / 128), kend = (int)p.k;
+    const int first = split * per, last = first + per < nblocks ? first + per : nblocks;
+    const int lrow = wave * 8 + (lane >> 3), lchunk = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int ao = lrow * (int)p.lda + lchunk, bo = lrow * (int)p.ldb + lchunk;
+    // the scales' quarter of this wave (waves 4 .. 7 send the same again):
+    // rows 0 .. 63, 64 .. 127, filters 0 .. 63, 64 .. 127
+    const int part = wave & 3, srow = (part & 1) * 64 + lane;
+    const int sh = (part < 2 ? p.a_block : p.b_block) == 1 ? 0 : 7;
+    const int64_t s0 = part < 2 ? m0 : n0;
+    const int rows = part < 2 ? ma : nb;
+    const float *sbase = (part < 2 ? p.sa : p.sb) + (s0 >> sh);
+    const int64_t sld = part < 2 ? p.ldsa : p.ldsb;
+    const int sbytes = (int)(((s0 + rows - 1) >> sh) - (s0 >> sh) + 1) * 4;
+    const int si = srow < rows ? (int)(((s0 + srow) >> sh) - (s0 >> sh)) * 4 : 0;
+    auto issue = [&](int step, int slot) {
+        const bool on = step < last;             // past the range: zeros
+        const int k0 = step * 128;
+        const bool ok = on && k0 + lchunk < kend;
+        const int av = ok ? ao + k0 : PAST, bv = ok ? bo + k0 : PAST;
+        char *to = lds + slot * STAGE;
+#pragma unroll
+        for (int q = 0; q < 2; q++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (LdsAt)(to + (q * 8 + wave) * 1024), 16,
+                                                     av + q * 64 * (int)p.lda, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < 2; q++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                br, (LdsAt)(to + B * 128 + (q * 8 + wave) * 1024), 16,
+                bv + q * 64 * (int)p.ldb, 0, 0, 0);
+        const Buf sr = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(sbase + (on ? step : 0) * sld), 0, on ? sbytes : 0, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, (LdsAt)(to + 2 * B * 128 + part * 256), 4,
+                                                 si, 0, 0, 0);
+    };
+    f4 acc[IN][IM];
+#pragma unroll
+    for (int i = 0; i < IN; i++)
+#pragma unroll
+        for (int j = 0; j < IM; j++) acc[i][j] = (f4)(0.f);
+    const int c0 = (fg ^ (fr & 7)) * 16, c1 = ((fg + 4) ^ (fr & 7)) * 16;
+    typedef typename std::conditional<WIDE, Wide, i8v>::type Frag;
+#pragma unroll
+    for (int q = 0; q < S - 1; q++) issue(first + q, q);
+    int slot = 0;
+    for (int step = first; step < last; step++) {
+        __builtin_amdgcn_sched_barrier(0);
+        // this step's loads of the wave have arrived, and its reads of the
+        // step before, whose stage is filled next
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        issue(step + S - 1, (slot + S - 1) % S);
+        char *at = lds + slot * STAGE;
+        if ((step + 1) * 128 > kend && (kend & 15)) {
+            // k ends in the middle of 16 bytes: zeros behind it
+            if (threadIdx.x < 2 * B) {
+                const int row = threadIdx.x, c = (kend & 127) >> 4;
+                u4 *v = (u4 *)(at + row * 128 + ((c ^ (row & 7)) << 4));
+                *v = first_bytes(*v, kend & 15);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        auto frag = [&](int row) {
+            return chunks(*(const u4 *)(at + row * 128 + c0), *(const u4 *)(at + row * 128 + c1));
+        };
+        const float *sc = (const float *)(at + 2 * B * 128);
+        Frag x[IM];
+        float sa[IM];
+#pragma unroll
+        for (int j = 0; j < IM; j++) {
+            const i8v v = frag(wm * TM + j * 16 + fr);
+            if constexpr (WIDE) x[j] = widen_block<FA>(v);
+            else x[j] = v;
+            sa[j] = sc[wm * TM + j * 16 + fr];
+        }
+#pragma unroll
+        for (int i = 0; i < IN; i++) {
+            const i8v w = frag(B + wn * TN + i * 16 + fr);
+            const f4 sb = *(const f4 *)(sc + B + wn * TN + i * 16 + fg * 4);
+            if constexpr (WIDE) {
+                const Wide ww = widen_block<FB>(w);
+#pragma unroll
+                for (int j = 0; j < IM; j++) acc[i][j] += mfma_wide(ww, x[j]) * (sb * sa[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < IM; j++)
+                    acc[i][j] += mfma_block<FA, FB>(w, x[j]) * (sb * sa[j]);
+            }
+        }
+        slot = (slot + 1) % S;
+    }
+    // The results through LDS, for whole lines (see product_tile)
+    constexpr int LINE = B / 4;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    f4 *held = (f4 *)lds;
+#pragma unroll
+    for (int j = 0; j < IM; j++)
+#pragma unroll
+        for (int i = 0; i < IN; i++)
+            held[(wm * TM + j * 16 + fr) * LINE + ((wn * (TN / 4) + i * 4 + fg) ^ fr)] =
+                acc[i][j];
+    __syncthreads();
+    const int64_t n = n0 + threadIdx.x % LINE * 4;
+    if (n >= p.n) return;
+    const f4 bias = splits > 1 ? (f4)(0.f) : bias_of(p, n);
+#pragma unroll 2
+    for (int h = 0; h < B * LINE / 512; h++) {
+        const int q = h * (512 / LINE) + (int)threadIdx.x / LINE;
+        const f4 v = held[q * LINE + ((int)threadIdx.x % LINE ^ (q & 15))];
+        if (splits > 1) partial_out(p, split, m0 + q, n, v);
+        else product_out(p, m0 + q, n, v, bias);
+    }
+}
+
 // Adds the ranges' partial sums, in order: four results a thread.
 static __global__ __launch_bounds__(256) void product_join(ProductArgs p, int splits) {
     const int64_t nq = (p.n + 3) / 4;
@@ -521,43 +668,68 @@ static __global__ __launch_bounds__(256) void product_join(ProductArgs p, int sp
     product_out(p, m, n, t, bias_of(p, n));
 }
 
-// kind 0: product_rows; product_tile: 1 128 x 128, 2 256 x 256 tiles, 3
-// 128 x 128 with fp32 sums
+// How a product runs.  Kinds: product_rows; product_tile of 128 x 128 or of
+// 256 x 256; product_ring.
+enum { ROWS, TILE, BIG_TILE, RING };
 struct ProductPlan { int kind, mt, nt, splits, per; };
 static ProductPlan product_plan(const ProductArgs &a) {
     ProductPlan r{};
     const int64_t nb = (a.k + 127) / 128;
-    int64_t wgs, want, least;
+    auto done = [&](int64_t s) {
+        s = s < 1 ? 1 : s > 16 ? 16 : s;
+        r.per = (int)((nb + s - 1) / s);
+        r.splits = r.per ? (int)((nb + r.per - 1) / r.per) : 1;
+        return r;
+    };
     // Short products too go to product_rows, whose waves have several blocks
     // under way: 214 x 102 x 2912 in 8 us instead of 14, 10807 x 10 x 5933 in
     // 15 instead of 22; at 3467 x 120 x 4227 (14520 below) it takes 26, tiles 18.
     const int64_t few = ((a.m + 63) / 64) * ((a.n + 15) / 16);
     if (a.m <= 64 || (few <= 512 && few * nb <= 8192)) {
-        r.kind = 0;
+        r.kind = ROWS;
         r.mt = a.m <= 16 ? 1 : a.m <= 32 ? 2 : 4;
         r.nt = (int)((a.n + 15) / 16);
-        wgs = few;
-        want = 256;
         // blocks of a range: eight a wave, joining costs as much as reading
         // them
-        least = r.mt < 4 ? 64 : 32;
-    } else {
-        const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-        r.kind = a.ytype == F32 ? 3 : big >= 192 && a.b_block > 1 ? 2 : 1;
-        const int b = r.kind == 2 ? 256 : 128;
-        r.mt = (int)((a.m + b - 1) / b);
-        r.nt = (int)((a.n + b - 1) / b);
-        wgs = (int64_t)r.mt * r.nt;
-        want = r.kind == 2 ? 256 : 512;
-        least = 4;
+        const int64_t s = few ? 256 / few : 1, most = nb / (r.mt < 4 ? 64 : 32);
+        return done(s < most ? s : most);
     }
-    int64_t s = wgs ? want / wgs : 1;
-    if (s > nb / least) s = nb / least;
-    if (s > 16) s = 16;
-    if (s < 1) s = 1;
-    r.per = (int)((nb + s - 1) / s);
-    r.splits = r.per ? (int)((nb + r.per - 1) / r.per) : 1;
-    return r;
+    const bool wide = a.ytype == F32;
+    const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
+    if (!wide && a.b_block > 1 && big >= 192) {
+        r.kind = BIG_TILE;
+        r.mt = (int)((a.m + 255) / 256);
+        r.nt = (int)((a.n + 255) / 256);
+        return done(1);
+    }
+    r.mt = (int)((a.m + 127) / 128);
+    r.nt = (int)((a.n + 127) / 128);
+    const int64_t tiles = (int64_t)r.mt * r.nt;
+    // Ranges of k: a step takes `one` us where a CU has one workgroup, `two`
+    // where it has two; adding the ranges up takes 4 us and the time of
+    // writing and reading them at 4 TB/s.  (Within 10% of the times of 1 to
+    // 16 ranges at sizes from 1024 x 1024 x 1024 to 256 x 4096 x 25088.)
+    const double one = wide ? 1.15 : a.b_block > 1 ? 0.75 : 1.25;
+    const double two = wide ? 1.9 : a.b_block > 1 ? 0.75 : 1.3;
+    double best = 0;
+    int64_t s = 1;
+    for (int64_t t = 1; t <= 16 && t * 2 <= nb + 1; t++) {
+        const int64_t wgs = tiles * t;
+        const double us =
+            (double)((nb + t - 1) / t) *
+                (wgs <= 256 ? one : two * (double)((wgs + 511) / 512)) +
+            (t > 1 ? 4 + (double)t * (double)a.m * (double)a.n * 8 / 4e6 : 0);
+        if (t == 1 || us < best) {
+            best = us;
+            s = t;
+        }
+    }
+    // product_ring where a CU has one workgroup (fp32: 1280 x 320 x 6272 in
+    // 23 us, tiles 25; 2048 x 2048 x 2048 in 29, tiles 32), for 16-bit results
+    // only of the whole k (16384 x 64 x 576 in 9.4 us, tiles 10.5; 3467 x 120 x
+    // 4227 in four ranges 18.0, tiles 17.2)
+    r.kind = tiles * s <= 256 && (wide || s == 1) ? RING : TILE;
+    return done(s);
 }
 int product_splits(const ProductArgs &a) { return product_plan(a).splits; }
 size_t product_workspace(const ProductArgs &a) {
@@ -568,7 +740,7 @@ size_t product_workspace(const ProductArgs &a) {
 template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hipStream_t st) {
     const ProductPlan r = product_plan(a);
     hipError_t e;
-    if (r.kind == 0) {
+    if (r.kind == ROWS) {
         const dim3 grid((unsigned)((a.m + 16 * r.mt - 1) / (16 * r.mt) * r.nt * r.splits));
         auto rows = [&](auto wide) {
             constexpr bool W = decltype(wide)::value;
@@ -595,9 +767,19 @@ template <int FA, int FB> static hipError_t product_go(const ProductArgs &a, hip
         };
         typedef std::true_type Y;
         typedef std::false_type N;
-        if (r.kind == 3) e = s1 ? tile(N(), Y(), Y()) : tile(N(), N(), Y());
-        else if (r.kind == 1) e = s1 ? tile(N(), Y(), N()) : tile(N(), N(), N());
-        else e = tile(Y(), N(), N());
+        if (r.kind == RING) {
+            auto ring = [&](auto wide) {
+                return start(product_ring<FA, FB, decltype(wide)::value>, dim3(g), 512, st, a,
+                             r.mt, r.nt, r.splits, r.per);
+            };
+            e = a.ytype == F32 ? ring(Y()) : ring(N());
+        } else if (r.kind == BIG_TILE) {
+            e = tile(Y(), N(), N());
+        } else if (a.ytype == F32) {
+            e = s1 ? tile(N(), Y(), Y()) : tile(N(), N(), Y());
+        } else {
+            e = s1 ? tile(N(), Y(), N()) : tile(N(), N(), N());
+        }
     }
     if (e != hipSuccess || r.splits == 1) return e;
     const int64_t items = a.m * ((a.n + 3) / 4);

@@ -467,6 +467,18 @@ def test_product_large(ops, m, n, k, bb):
     _check_product(ops, m, n, k, bb=bb, ydt="f32", bias=True, act="relu")
 
 
+@pytest.mark.parametrize("ydt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("ab,bb", [(1, 128), (1, 1), (128, 128), (128, 1)])
+@pytest.mark.parametrize("m,n,k", [(2000, 300, 700), (300, 1500, 9001), (2070, 2130, 140),
+                                   (3601, 3540, 200), (700, 1300, 1)])
+def test_product_tiles(ops, m, n, k, ab, bb, ydt):
+    """Sizes past the short products: few and many tiles, whole and split k,
+    k that ends inside 16 bytes, inside a block and after one value."""
+    _check_product(ops, m, n, k, "e4m3" if n % 4 else "e5m2", "e4m3", ab, bb, ydt,
+                   bias=n % 4 == 0, act="silu" if k < 200 else "none", pad=16 * (m % 2),
+                   ypad=n % 7)
+
+
 def test_product_without_a_sum(ops):
     _check_product(ops, 5, 7, 0, bias=True)
     _check_product(ops, 300, 7, 0, bias=True, ydt="f16")
