@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libctc.so")
 SOURCES = [os.path.join(HERE, "csrc", "ctc_api.cpp"),
            os.path.join(HERE, "csrc", "ops_api.cpp"),
-           os.path.join(HERE, "csrc", "kernels.hip")]
+           os.path.join(HERE, "csrc", "library.hip")]
 BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(HERE, "csrc", "binding.cpp")
 ARCH = "gfx950"

@@ -8,7 +8,8 @@
 //   dx = rstd (dz gamma - (s1 + xhat s2) / count),
 //   s1 = sum dz gamma,  s2 = sum dz gamma xhat  over (image, group).
 //
-// Sums are fp32.  A channel's sum and sum of squares are taken about the
+// Sums over pixels are fp32, the joins over chunks and channels fp64 (a group
+// whose channels' means cancel keeps the digits of its mean).  A channel's sum and sum of squares are taken about the
 // chunk's first pixel, which lies within a few deviations of the mean, and
 // channels and chunks are joined as (count, mean, squared deviations), so a
 // mean far from zero costs no digits.
@@ -162,13 +163,13 @@ template <int W> struct NormJoin {
         }
     }
     // Sum over the W waves, for all of them.
-    __device__ __forceinline__ float sum(float v, float *lds) {
+    __device__ __forceinline__ double sum(double v, double *lds) {
         v = wave_sum(v);
         if constexpr (W > 1) {
             __syncthreads();
             if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
             __syncthreads();
-            v = 0.f;
+            v = 0;
 #pragma unroll
             for (int i = 0; i < W; i++) v += lds[i];
         }
@@ -182,36 +183,32 @@ static bool norm_join_wide(const NormArgs &a, const NormPlan &p) {
 }
 template <int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_stats_join(NormArgs a, NormPlan p) {
-    __shared__ float lds[W];
+    __shared__ double lds[W];
     const int64_t t = W == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (t >= a.n * a.groups) return;
     NormJoin<W> j(a, p, t);
-    const float total = (float)a.hw * j.nc;
-    auto pixels = [&](int ch) {
-        const int64_t left = a.hw - ch * p.chunk;
-        return (float)(left < p.chunk ? left : p.chunk);
-    };
+    const double total = (double)a.hw * j.nc;
     // about the mean of the first entries (of up to 64 W channels), which lies
     // within the group's spread: one loop, and no digits lost
     const int some = j.entries < 64 * W ? j.entries : 64 * W;
     float at = 0.f;
     if (j.at < some) at = j.part[((int64_t)(j.at / j.nc) * a.c + j.at % j.nc) * 2];
-    at = j.sum(at, lds);
-    at = some ? at / (float)some : 0.f;
-    float s1 = 0.f, s2 = 0.f;
+    at = (float)(j.sum(at, lds) / (some ? some : 1));
+    double s1 = 0, s2 = 0;
     j.each(a, [&](float2 e, int ch, int) {
-        const float d = e.x - at, w = d * pixels(ch);
+        const int64_t left = a.hw - ch * p.chunk;
+        const double d = (double)e.x - at, w = d * (double)(left < p.chunk ? left : p.chunk);
         s1 += w;
-        s2 += __builtin_fmaf(d, w, e.y);
+        s2 += d * w + e.y;
     });
     s1 = j.sum(s1, lds);
     s2 = j.sum(s2, lds);
     if (j.at == 0) {
-        const float d = j.nc ? s1 / total : 0.f;
-        float var = j.nc ? s2 / total - d * d : 0.f;
-        var = var < 0.f ? 0.f : var;             // (a NaN stays)
-        a.mean[t] = at + d;
-        a.rstd[t] = 1.f / __builtin_sqrtf(var + a.eps);
+        const double d = j.nc ? s1 / total : 0;
+        double var = j.nc ? s2 / total - d * d : 0;
+        var = var < 0 ? 0 : var;                 // (a NaN stays)
+        a.mean[t] = (float)(at + d);
+        a.rstd[t] = 1.f / __builtin_sqrtf((float)(var + a.eps));
     }
 }
 
@@ -373,30 +370,30 @@ template <int W>
 __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
                                                        int64_t group_blocks) {
     if (blockIdx.x < group_blocks) {
-        __shared__ float lds[W];
+        __shared__ double lds[W];
         const int64_t t = W == 1 ? (int64_t)blockIdx.x * 16 + (threadIdx.x >> 6) : blockIdx.x;
         if (t >= a.n * a.groups) return;
         NormJoin<W> j(a, p, t);
-        float s1 = 0.f, s2 = 0.f;
+        double s1 = 0, s2 = 0;
         j.each(a, [&](float2 e, int, int c) {
-            const float w = a.gamma ? a.gamma[j.g * j.per + c] : 1.f;
-            s1 = __builtin_fmaf(e.x, w, s1);
-            s2 = __builtin_fmaf(e.y, w, s2);
+            const double w = a.gamma ? a.gamma[j.g * j.per + c] : 1;
+            s1 += e.x * w;
+            s2 += e.y * w;
         });
         s1 = j.sum(s1, lds);
         s2 = j.sum(s2, lds);
         if (j.at == 0) {
             float *out = a.ws + norm_sums_at(a, p) + t * 2;
-            const float inv = j.nc ? 1.f / ((float)a.hw * j.nc) : 0.f;
-            out[0] = s1 * inv;
-            out[1] = s2 * inv;
+            const double total = j.nc ? (double)a.hw * j.nc : 1;
+            out[0] = (float)(s1 / total);
+            out[1] = (float)(s2 / total);
         }
         return;
     }
-    __shared__ float sum[2][JOIN_ROWS][17];
+    __shared__ double sum[2][JOIN_ROWS][17];
     const int cl = threadIdx.x & 15, row = threadIdx.x >> 4;
     const int c = (int)(blockIdx.x - group_blocks) * 16 + cl;
-    float s1 = 0.f, s2 = 0.f;
+    double s1 = 0, s2 = 0;
     if (c < a.c && !(a.carry && c == a.c - 1))
 #pragma unroll 8
         for (int64_t i = row; i < a.n * p.chunks; i += JOIN_ROWS) {
@@ -412,8 +409,8 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
             s1 += sum[0][i][cl];
             s2 += sum[1][i][cl];
         }
-        if (a.dbeta) a.dbeta[c] = s1;
-        if (a.dgamma) a.dgamma[c] = s2;
+        if (a.dbeta) a.dbeta[c] = (float)s1;
+        if (a.dgamma) a.dgamma[c] = (float)s2;
     }
 }
 
@@ -518,7 +515,7 @@ template <typename T, int V, int NT, int N> struct Slab {
     __device__ void groups(int gs, int per, G value, F f) {
         const int lane = threadIdx.x & 63;
         for (int g = threadIdx.x >> 6; g < gs; g += NW) {
-            float t[2] = {};
+            double t[2] = {};
             for (int c = lane; c < per; c += 64) value(g * per + c, t);
             t[0] = wave_sum(t[0]);
             t[1] = wave_sum(t[1]);
@@ -545,7 +542,7 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
         if (s.on && q < a.hw) raw[r].load(x + q * a.c);
     }
     const int ck = a.carry ? a.c - 1 - s.slab * p.w : -1;   // its channel here
-    auto count = [&](int g) { return (float)a.hw * (per - (ck >= 0 && ck / per == g)); };
+    auto count = [&](int g) { return (double)a.hw * (per - (ck >= 0 && ck / per == g)); };
     // the mean, then the squared deviations from it
     float sum[1][V] = {};
 #pragma unroll
@@ -559,12 +556,12 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
         }
     s.channels(l, p, sum);
     s.groups(gs, per,
-             [&](int c, float (&t)[2]) {
+             [&](int c, double (&t)[2]) {
                  if (c != ck) t[0] += l.chan[0][c];
              },
-             [&](int g, float (&t)[2]) {
-                 const float n = count(g);
-                 l.a[g] = n > 0.f ? t[0] / n : 0.f;
+             [&](int g, double (&t)[2]) {
+                 const double n = count(g);
+                 l.a[g] = n > 0 ? (float)(t[0] / n) : 0.f;
              });
     float mean[V], sq[1][V] = {};
     per_group<V>(a, s.cx * V, mean, [&](int g) { return l.a[g]; });
@@ -582,12 +579,13 @@ __global__ __launch_bounds__(NT) void norm_slab(NormArgs a, SlabPlan p) {
         }
     s.channels(l, p, sq);
     s.groups(gs, per,
-             [&](int c, float (&t)[2]) {
+             [&](int c, double (&t)[2]) {
                  if (c != ck) t[0] += l.chan[0][c];
              },
-             [&](int g, float (&t)[2]) {
-                 const float n = count(g);
-                 const float rs = 1.f / __builtin_sqrtf((n > 0.f ? t[0] / n : 0.f) + a.eps);
+             [&](int g, double (&t)[2]) {
+                 const double n = count(g);
+                 const float rs =
+                     1.f / __builtin_sqrtf((float)((n > 0 ? t[0] / n : 0) + a.eps));
                  l.b[g] = rs;
                  a.mean[s.img * a.groups + g0 + g] = l.a[g];
                  a.rstd[s.img * a.groups + g0 + g] = rs;
@@ -669,17 +667,17 @@ __global__ __launch_bounds__(NT) void norm_grad_slab(NormArgs a, SlabPlan p) {
         }
     }
     s.groups(gs, per,
-             [&](int c, float (&t)[2]) {
-                 const float w = a.gamma ? a.gamma[s.slab * p.w + c] : 1.f;
+             [&](int c, double (&t)[2]) {
+                 const double w = a.gamma ? a.gamma[s.slab * p.w + c] : 1;
                  if (c != ck) {
                      t[0] += l.chan[0][c] * w;
                      t[1] += l.chan[1][c] * w;
                  }
              },
-             [&](int g, float (&t)[2]) {
-                 const float n = (float)a.hw * (per - (ck >= 0 && ck / per == g));
-                 l.a[g] = n > 0.f ? t[0] / n : 0.f;
-                 l.b[g] = n > 0.f ? t[1] / n : 0.f;
+             [&](int g, double (&t)[2]) {
+                 const double n = (double)a.hw * (per - (ck >= 0 && ck / per == g));
+                 l.a[g] = n > 0 ? (float)(t[0] / n) : 0.f;
+                 l.b[g] = n > 0 ? (float)(t[1] / n) : 0.f;
              });
     if (!s.on) return;
     float m1[V], m2[V];

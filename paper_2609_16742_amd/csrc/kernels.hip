@@ -6437,6 +6437,3 @@ hipError_t conv_scratch(void **ptr) {
 }
 
 }  // namespace ctc
-
-// One source, so the library holds one code object.
-#include "ops.hip"

@@ -1,5 +1,5 @@
-// gfx950 kernels of the operators around a protected classifier.  Part of
-// kernels.hip, so the library holds one code object.
+// gfx950 kernels of the operators around a protected classifier (compiled
+// with kernels.hip, see library.hip).
 #include "ops.h"
 
 #include <type_traits>

@@ -88,7 +88,7 @@ __device__ __forceinline__ float vmax3(float a, float b, float c) {
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float exp_hw(float v) { return exp2_hw(v * LOG2E); }
 
-__device__ __forceinline__ float wave_sum(float v) {
+template <typename F> __device__ __forceinline__ F wave_sum(F v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     return v;
