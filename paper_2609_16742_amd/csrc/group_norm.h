@@ -8,8 +8,9 @@
 //   dx = rstd (dz gamma - (s1 + xhat s2) / count),
 //   s1 = sum dz gamma,  s2 = sum dz gamma xhat  over (image, group).
 //
-// Sums over pixels are fp32, the joins over chunks and channels fp64 (a group
-// whose channels' means cancel keeps the digits of its mean).  A channel's sum and sum of squares are taken about the
+// Sums over pixels and images are fp32, those over a group's chunks and
+// channels fp64 (a group whose channels' means cancel keeps the digits of its
+// mean).  A channel's sum and sum of squares are taken about the
 // chunk's first pixel, which lies within a few deviations of the mean, and
 // channels and chunks are joined as (count, mean, squared deviations), so a
 // mean far from zero costs no digits.
@@ -177,7 +178,7 @@ template <int W> struct NormJoin {
     }
 };
 // A wave takes an (image, group) of up to 1024 entries, a workgroup of 16 a
-// longer one (30690 entries: 247 us by one wave, 12 by 16).
+// longer one (30690 entries: 247 us by one wave, 13 by 16).
 static bool norm_join_wide(const NormArgs &a, const NormPlan &p) {
     return (int64_t)p.chunks * (a.c / a.groups) > 1024;
 }
@@ -269,7 +270,7 @@ __device__ __forceinline__ void norm_values(const NormArgs &a, const NormChannel
                                             float (&v)[V], const float (&r)[V]) {
 #pragma unroll
     for (int e = 0; e < V; e++)
-        v[e] = __builtin_fmaf((v[e] - k.mean[e]) * k.rstd[e], k.gamma[e], k.beta[e]) + r[e];
+        v[e] = __builtin_fmaf(v[e] - k.mean[e], k.rstd[e] * k.gamma[e], k.beta[e]) + r[e];
     if (k.ck < 0) {
         act_of<V>(a.act, v);
     } else {
@@ -390,10 +391,10 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
         }
         return;
     }
-    __shared__ double sum[2][JOIN_ROWS][17];
+    __shared__ float sum[2][JOIN_ROWS][17];
     const int cl = threadIdx.x & 15, row = threadIdx.x >> 4;
     const int c = (int)(blockIdx.x - group_blocks) * 16 + cl;
-    double s1 = 0, s2 = 0;
+    float s1 = 0.f, s2 = 0.f;
     if (c < a.c && !(a.carry && c == a.c - 1))
 #pragma unroll 8
         for (int64_t i = row; i < a.n * p.chunks; i += JOIN_ROWS) {
@@ -409,8 +410,8 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
             s1 += sum[0][i][cl];
             s2 += sum[1][i][cl];
         }
-        if (a.dbeta) a.dbeta[c] = (float)s1;
-        if (a.dgamma) a.dgamma[c] = (float)s2;
+        if (a.dbeta) a.dbeta[c] = s1;
+        if (a.dgamma) a.dgamma[c] = s2;
     }
 }
 
