@@ -182,7 +182,8 @@ __global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p
                                                      av + i * 8 * (int)p.lda, 0, 0, 0);
         const int64_t q = on ? kb : 0;
         const Buf sar = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)(sab + q * p.ldsa), 0, on ? (int)(((m0 + ma - 1) >> ash) - (m0 >> ash) + 1) * 4 : 0, 0x00020000);
+            (void *)(sab + q * p.ldsa), 0,
+            on ? (int)(((m0 + ma - 1) >> ash) - (m0 >> ash) + 1) * 4 : 0, 0x00020000);
         const Buf sbr = __builtin_amdgcn_make_buffer_rsrc(
             (void *)(sbb + q * p.ldsb), 0,
             on ? (int)(((n0 + nb - 1) >> bsh) - (n0 >> bsh) + 1) * 4 : 0, 0x00020000);
