@@ -387,7 +387,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, i
         issue(first, 0, 0, AR + BR);
         scales(first);
         if constexpr (SB1)
-            if (threadIdx.x < BN) sbl[0][threadIdx.x] = sbn;
+            if (threadIdx.x < BN) {
+                sbl[0][threadIdx.x] = sbn;
+                // (the scales of no step, which the first step multiplies its
+                // zeros by: what LDS held may be NaN)
+                sbl[2][threadIdx.x] = 0.f;
+            }
         arrived();
         issue(first + 1, 1, 0, DQ);
     }

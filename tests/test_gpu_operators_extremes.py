@@ -1,0 +1,93 @@
+"""The operators around a protected classifier on inputs at the ends of their
+ranges: spoiled blocks and scales, values far from zero, outliers, many
+images.  References are 64-bit forms; tolerances follow from the arithmetic
+(fp32 sums of n terms are off by n * 2^-24 of their magnitudes at most)."""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_16742_amd import ops
+    return ops
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(shape, device="cuda", generator=g)
+
+
+# ----------------------------------------------------------------- product
+
+def _bytes(g, rows, cols, qtype):
+    ld = -(-cols // 16) * 16
+    return (30 * _randn(g, rows, ld)).to(F8[qtype])[:, :cols]
+
+
+# short products, 128 x 128 tiles in one and in several ranges of k, one tile
+# a compute unit, tiles that fill the card
+@pytest.mark.parametrize("m,n,k,dtype", [(3, 300, 700, "f16"), (50, 300, 700, "f32"),
+                                         (1280, 320, 6272, "f32"),
+                                         (300, 1500, 4100, "f16"),
+                                         (3601, 3540, 200, "f32"),
+                                         (3601, 3540, 200, "f16"),
+                                         (3601, 3540, 300, "bf16")])
+@pytest.mark.parametrize("bb", [1, 128])
+def test_product_spoiled_and_clean(ops, m, n, k, dtype, bb):
+    """A NaN value or a NaN or infinite scale spoils its rows and columns of
+    y; nothing else, not the next product's results either."""
+    g = _gen(m + n + k)
+    kb, nb = -(-k // 128), -(-n // bb)
+    a, b = _bytes(g, m, k, "e4m3"), _bytes(g, n, k, "e4m3")
+    sa = torch.rand((kb, m), device="cuda", generator=g) + 0.5
+    sb = torch.rand((kb, nb), device="cuda", generator=g) + 0.5
+    # (16-bit results stay finite)
+    sa /= 100 * math.sqrt(k)
+    sb /= 100
+
+    def product(a, sa, b, sb):
+        return ops.fp8_matmul(a, sa, b, sb, dtype=DT[dtype])
+    first = product(a, sa, b, sb)
+    assert bool(torch.isfinite(first).all())
+    for where in ("a", "b", "sa", "sb", "sb inf"):
+        args = dict(a=a, sa=sa, b=b, sb=sb)
+        bad = torch.zeros((m, n), dtype=torch.bool, device="cuda")
+        if where in ("a", "b"):
+            v = args[where].view(torch.uint8).clone()
+            v[1::37, k // 2] = 0x7f
+            full = _bytes(g, *args[where].shape, "e4m3")
+            full.view(torch.uint8).copy_(v)
+            args[where] = full
+            if where == "a":
+                bad[1::37] = True
+            else:
+                bad[:, 1::37] = True
+        elif where == "sa":
+            args["sa"] = sa.clone()
+            args["sa"][kb // 2, 2::37] = math.nan
+            bad[2::37] = True
+        else:
+            v = sb.clone()
+            v[:, 1::5] = math.inf if where == "sb inf" else math.nan
+            args["sb"] = v
+            cols = (torch.arange(n, device="cuda") // bb) % 5 == 1
+            bad[:, cols] = True
+        y = product(**args)
+        assert torch.equal(~torch.isfinite(y), bad), where
+        assert torch.equal(y[~bad], first[~bad]), where
+        assert torch.equal(product(a, sa, b, sb), first), where
