@@ -65,12 +65,10 @@ __device__ __forceinline__ void soft_join(SoftState &a, SoftState b) {
     a.s = a.s * fa + b.s * fb;
     a.m = m;
 }
-// m - m2 ln 2: what x - m is off by as the exponent of s
+// What the exponents x LOG2E - m2 are off by, as natural ones: they are
+// (x - m) LOG2E + (m LOG2E - m2), with the same LOG2E in both.
 __device__ __forceinline__ float soft_shift(float m) {
-    if (soft_wide(m)) return 0.f;
-    const float m2 = soft_m2(m);
-    constexpr float LN2_LO = -1.9046542e-9f;     // ln 2 - LN2
-    return __builtin_fmaf(-m2, LN2_LO, __builtin_fmaf(-m2, LN2, m));
+    return soft_wide(m) ? 0.f : LN2 * __builtin_fmaf(m, LOG2E, -soft_m2(m));
 }
 
 // Total order: NaN above +inf, -0 as +0, equal values by the lower index.

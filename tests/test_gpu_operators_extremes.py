@@ -91,3 +91,53 @@ def test_product_spoiled_and_clean(ops, m, n, k, dtype, bb):
         assert torch.equal(~torch.isfinite(y), bad), where
         assert torch.equal(y[~bad], first[~bad]), where
         assert torch.equal(product(a, sa, b, sb), first), where
+
+
+# ------------------------------------------------------------------ scores
+
+def _check_far(ops, x, t, k, what):
+    """Scores in 64 bits.  Log probabilities and entropies do not depend on
+    how far from zero a row lies, so their bounds know nothing of lse: fp32
+    sums of a thread's terms and the joins, exp and log of the hardware, and
+    the rounding of x - max."""
+    got = ops.token_scores(x, t, k)
+    vocab = x.shape[1]
+    v = x.double()
+    m = v.amax(1, keepdim=True)
+    e = torch.exp(v - m)
+    s = e.sum(1, keepdim=True)
+    lp = (v - m) - torch.log(s)
+    h = -torch.where(e > 0, e / s * lp, 0.0).sum(1)
+    lse = (m + torch.log(s))[:, 0]
+    threads = 64 if vocab <= 4096 else 256 if vocab <= 16384 else 512
+    rel = (vocab / threads + 64) * 2.0 ** -24 + 2.0 ** -20
+
+    def near(a, b, bound, name):
+        off = (a.double() - b).abs()
+        assert bool((off <= bound).all()), (what, name, float(off.max()), a, b)
+    near(got.lse, lse, rel + 2.0 ** -23 * lse.abs(), "lse")
+    near(got.entropy, h, 2 * rel * (2 + h), "entropy")
+    want = lp.gather(1, t.long()[:, None])[:, 0]
+    near(got.logprob, want, rel + 2.0 ** -22 * want.abs(), "logprob")
+    order = torch.sort(v, dim=1, descending=True, stable=True)
+    k = min(k, vocab)
+    assert torch.equal(got.top_ids[:, :k].long(), order[1][:, :k]), what
+    want = lp.gather(1, order[1][:, :k])
+    near(got.top_logprobs[:, :k], want, rel + 2.0 ** -22 * want.abs(), "top")
+
+
+@pytest.mark.parametrize("vocab", [5, 100, 1000, 5000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_token_scores_far_from_zero(ops, vocab, dtype):
+    """Maxima up to fp16's largest and lowest numbers."""
+    g = _gen(vocab)
+    at = [-65504.0, -60000.0, -1000.0, 1000.0, 30000.0, 65504.0]
+    x = torch.tensor(at, device="cuda")[:, None].repeat(2, vocab)
+    x[6:] -= 4 * torch.rand((6, vocab), device="cuda", generator=g)
+    x = x.to(DT[dtype])
+    x = torch.cat([x.clamp(-65504, 65504), x[:2]]) if dtype != "bf16" else x
+    t = torch.randint(0, vocab, (x.shape[0],), device="cuda", generator=g,
+                      dtype=torch.int32)
+    _check_far(ops, x, t, 5, (vocab, dtype))
+    for r in range(x.shape[0]):
+        _check_far(ops, x[r:r + 1], t[r:r + 1], 20, (vocab, dtype, "row", r))
