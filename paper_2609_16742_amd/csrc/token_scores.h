@@ -7,11 +7,13 @@
 // f (t + (m - m') s)); in the same pass the rank of the target and every
 // thread's largest value.
 //
-// Exponents are in powers of two, about m2 = m log2(e) rounded: a value
-// costs one multiply-add x log2(e) - m2, one exp2, and two more for s and t.
-// s belongs to m2 exactly, so what m2 was rounded by comes back at the end
-// (soft_shift).  Maxima of magnitude above 1e38 (rows of the type's lowest
-// value; none yet, -inf), whose m2 would overflow, take x - m first.
+// Exponents are in powers of two, in a thread's pass about m2 = m log2(e)
+// rounded: a value costs one multiply-add x log2(e) - m2, one exp2, and two
+// more for s and t.  s belongs to m2 exactly, so what m2 was rounded by
+// (soft_shift, up to 2^-8) comes off when the pass ends, and the joins are
+// about m.  Maxima past fp16's range (rows of a type's lowest value or of a
+// constant like -1e30; none yet, -inf), whose m2 would be rounded by more
+// than exp2 can hold or overflow, take x - m first.
 //
 // Top alternatives: with the row dealt out to 64 groups of threads, the k-th
 // largest group maximum is a lower bound T of the k-th largest value (k
@@ -34,7 +36,9 @@ namespace ops {
 constexpr int SC_CAP = 512;                      // collected alternatives
 constexpr float SC_LOW = -200.f;                 // 2^ of it is 0 in fp32
 
-// t in powers of two as well
+// About m: s = sum p, t = sum d p with p = 2^d, d = (x - m) log2(e).  m = -inf
+// marks an empty state (s = t = 0); s turns NaN with the first NaN or +inf and
+// stays it.
 struct SoftState { float m, s, t; };
 // m2: the product in a register of its own, so that it is rounded the same
 // wherever it is used (not contracted into a multiply-add)
@@ -43,32 +47,27 @@ __device__ __forceinline__ float soft_m2(float m) {
     asm("" : "+v"(r));
     return r;
 }
-__device__ __forceinline__ bool soft_wide(float m) { return !(__builtin_fabsf(m) <= 1e38f); }
-// m = -inf marks an empty state (s = t = 0); s turns NaN with the first NaN
-// or +inf and stays it.  (vmax drops the NaN of two overflown maxima, whose
-// distance is as good as infinite.)
-__device__ __forceinline__ void soft_raise(SoftState &a, float m) {
-    const float d = vmax(soft_m2(a.m) - soft_m2(m), SC_LOW);
+__device__ __forceinline__ bool soft_wide(float m) { return !(__builtin_fabsf(m) <= 65536.f); }
+// What the pass adds to the exponents d: x LOG2E - m2 = (x - m) LOG2E +
+// (m LOG2E - m2), with the same LOG2E in both.
+__device__ __forceinline__ float soft_shift(float m) {
+    return soft_wide(m) ? 0.f : __builtin_fmaf(m, LOG2E, -soft_m2(m));
+}
+// The state with every exponent larger by d.
+__device__ __forceinline__ void soft_scale(SoftState &a, float d) {
     const float f = exp2_hw(d);
     a.t = (a.t + d * a.s) * f;
     a.s *= f;
-    a.m = m;
 }
 // (No branches: the joins of a wave are a chain.  An empty state has the
 // distance SC_LOW, or none from another empty one.)
 __device__ __forceinline__ void soft_join(SoftState &a, SoftState b) {
-    const float m = vmax(a.m, b.m), m2 = soft_m2(m);
-    const float da = a.m == m ? 0.f : vmax(soft_m2(a.m) - m2, SC_LOW);
-    const float db = b.m == m ? 0.f : vmax(soft_m2(b.m) - m2, SC_LOW);
-    const float fa = exp2_hw(da), fb = exp2_hw(db);
-    a.t = (a.t + da * a.s) * fa + (b.t + db * b.s) * fb;
-    a.s = a.s * fa + b.s * fb;
+    const float m = vmax(a.m, b.m);
+    soft_scale(a, a.m == m ? 0.f : vmax((a.m - m) * LOG2E, SC_LOW));
+    soft_scale(b, b.m == m ? 0.f : vmax((b.m - m) * LOG2E, SC_LOW));
+    a.s += b.s;
+    a.t += b.t;
     a.m = m;
-}
-// What the exponents x LOG2E - m2 are off by, as natural ones: they are
-// (x - m) LOG2E + (m LOG2E - m2), with the same LOG2E in both.
-__device__ __forceinline__ float soft_shift(float m) {
-    return soft_wide(m) ? 0.f : LN2 * __builtin_fmaf(m, LOG2E, -soft_m2(m));
 }
 
 // Total order: NaN above +inf, -0 as +0, equal values by the lower index.
@@ -141,8 +140,8 @@ template <typename T, int NT> struct ScorePart {
     int lo, hi;
     int target;                  // -1: no rank wanted
     float xt, thr_before;        // the target's value, and the next below it
-    SoftState st;
-    float m2;                    // st.m in powers of two
+    SoftState st;                // in scan(): exponents larger by `shift`
+    float m2, shift;             // of st.m
     int cnt;
 
     // VALS elements from index i on.  The rank counts a wave at a time: `cnt`
@@ -156,8 +155,12 @@ template <typename T, int NT> struct ScorePart {
             vm = vmax3(vmax(v[0], v[1]), v[2], v[3]);
         else vm = v[0];
         if (vm > st.m) {
-            soft_raise(st, vm);
+            const float sh = soft_shift(vm);
+            // (vmax drops the NaN of infinity from infinity)
+            soft_scale(st, vmax(__builtin_fmaf(st.m - vm, LOG2E, sh - shift), SC_LOW));
+            st.m = vm;
             m2 = soft_m2(vm);
+            shift = sh;
         }
         if (!soft_wide(st.m)) {
 #pragma unroll
@@ -190,7 +193,7 @@ template <typename T, int NT> struct ScorePart {
         const int tid = threadIdx.x;
         const int nv = (hi - lo) / V;
         st = SoftState{-INF, 0.f, 0.f};
-        m2 = 0.f;
+        m2 = shift = 0.f;
         cnt = 0;
         int i = tid;
         if (U * NT <= nv) thr_before = below(xt);
@@ -217,6 +220,7 @@ template <typename T, int NT> struct ScorePart {
                 if (i + u * NT < nv) add(v[u], lo + (i + u * NT) * V);
             if (j < hi) add(w, j);
         }
+        soft_scale(st, -shift);
         if (target >= 0 && xt != xt) {           // only NaN stands beside NaN
             cnt = 0;
             for (int j = lo + tid; j < hi && j < target; j += NT) {
@@ -354,7 +358,7 @@ template <typename T, int NT> struct ScorePart {
 
 // What the outputs of a row are, given its joined state.
 __device__ __forceinline__ float soft_log(SoftState a) {
-    return LN2 * __builtin_amdgcn_logf(a.s) - soft_shift(a.m);
+    return LN2 * __builtin_amdgcn_logf(a.s);
 }
 __device__ __forceinline__ float soft_lse(SoftState a) {
     return a.m == -INF && a.s == 0.f ? -INF : a.m + soft_log(a);

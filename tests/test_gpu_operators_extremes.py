@@ -141,3 +141,39 @@ def test_token_scores_far_from_zero(ops, vocab, dtype):
     _check_far(ops, x, t, 5, (vocab, dtype))
     for r in range(x.shape[0]):
         _check_far(ops, x[r:r + 1], t[r:r + 1], 20, (vocab, dtype, "row", r))
+
+
+# magnitudes that a type holds, up to where sums of two overflow
+MAGNITUDES = [7e4, 1e6, 3e7, 1e8, 3e9, 5e9, 1e10, 1e12, 1e20, 1e30, 1e37, 3e38]
+
+
+@pytest.mark.parametrize("vocab", [5, 100, 1000, 5000, 40000, 131072])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_token_scores_of_any_magnitude(ops, vocab, dtype):
+    """Rows of one value, rows that spread about it by a few units of its last
+    place, and ordinary rows of which a part, whole threads and workgroups
+    among them, is barred by it: one wave, one workgroup, rows split over
+    workgroups."""
+    g = _gen(vocab)
+    dt = DT[dtype]
+    step = {"f32": 2.0 ** -23, "bf16": 2.0 ** -7}[dtype]
+    rows = []
+    for mag in MAGNITUDES:
+        for v in (mag, -mag):
+            rows.append(torch.full((vocab,), v, device="cuda"))
+            rows.append(v * (1 + step * torch.randint(0, 4, (vocab,), device="cuda",
+                                                      generator=g)))
+        for part in range(3):
+            x = 3 * _randn(g, vocab)
+            if part == 0:
+                x[torch.rand(vocab, device="cuda", generator=g) < 0.5] = -mag
+            elif part == 1:
+                x[vocab // 2:] = -mag
+            else:
+                x[:vocab - 3] = -mag
+            rows.append(x)
+    x = torch.stack(rows).to(dt).clamp(-3.3e38, 3.3e38)
+    t = torch.randint(0, vocab, (len(rows),), device="cuda", generator=g, dtype=torch.int32)
+    _check_far(ops, x, t, 5, (vocab, dtype))
+    for r in range(0, len(rows), 5):
+        _check_far(ops, x[r:r + 1], t[r:r + 1], 20, (vocab, dtype, "row", r))
