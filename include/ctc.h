@@ -709,7 +709,8 @@ ctc_status ctc_token_scores_forward(ctc_dtype dtype, int64_t rows,
  *   dx_i = p_i (g_lse - g_logprob - g_entropy (log p_i + entropy))
  *          + (i == target) g_logprob
  *   lse, entropy  as the forward pass wrote them (entropy only for g_entropy);
- *           p is off by a factor of as much as lse was rounded (2^-24 of it)
+ *           up to |lse| = 256 p is off by a factor of as much as lse was
+ *           rounded (2^-17 at most); past it the row's sum is taken again
  *   g_lse, g_logprob, g_entropy  [rows] fp32, each may be NULL (0)
  *   dlogits  [rows][vocab] in dtype, rows ldd apart; may be logits (in place,
  *            ldd = ld)

@@ -549,8 +549,14 @@ hipError_t launch_scores(const ScoreArgs &a, hipStream_t st) {
 //   dx_i = p_i (g_lse - g_lp - g_H (log p_i + H)) + [i = target] g_lp
 // one read and one write of the row; dx may be x.  Bound by the bytes: 4096 x
 // 32001 fp16 in 102 us, 5.1 TB/s.
+//
+// p = exp(x - lse) is off by what lse was rounded by, 2^-17 up to |lse| = 256.
+// Past it (a row of fp32's lowest value has lse = max for every length) one
+// workgroup takes the row, its maximum and its sum first; the row may be
+// written in place, so no other can.
+constexpr float SC_FAR = 256.f;
 template <typename T>
-__global__ __launch_bounds__(256) void token_scores_grad(ScoreArgs a, int parts) {
+__global__ __launch_bounds__(256, 8) void token_scores_grad(ScoreArgs a, int parts) {
     constexpr int V = 16 / (int)sizeof(T), U = 4;
     const int64_t row = blockIdx.x / parts;
     const int lo = (int)(blockIdx.x % parts) * (256 * V * U);
@@ -565,11 +571,31 @@ __global__ __launch_bounds__(256) void token_scores_grad(ScoreArgs a, int parts)
     const float gh = a.g_entropy ? a.g_entropy[row] : 0.f;
     const float c = (a.g_lse ? a.g_lse[row] : 0.f) - glp -
                     (a.g_entropy ? gh * a.entropy[row] : 0.f);
-    auto one = [&](float v, int i) {
-        const float lp = v - lse;
+    auto grad = [&](float lp, int i) {
         const float g = exp_hw(lp) * __builtin_fmaf(-gh, vmax(lp, SC_LOW), c);
         return i == target ? g + glp : g;
     };
+    if (__builtin_fabsf(lse) > SC_FAR) {
+        if (lo) return;
+        __shared__ float of[2][4];
+        const int wave = threadIdx.x >> 6;
+        float m = -INF, s = 0.f;
+        for (int i = threadIdx.x; i < a.vocab; i += 256) m = vmax(m, widen(x[i]));
+#pragma unroll
+        for (int o = 32; o; o >>= 1) m = vmax(m, __shfl_xor(m, o));
+        of[0][wave] = m;
+        __syncthreads();
+        for (int i = 0; i < 4; i++) m = vmax(m, of[0][i]);
+        for (int i = threadIdx.x; i < a.vocab; i += 256) s += exp_hw(widen(x[i]) - m);
+        of[1][wave] = wave_sum(s);
+        __syncthreads();                         // (the row is read)
+        s = of[1][0] + of[1][1] + of[1][2] + of[1][3];
+        const float log_s = LN2 * __builtin_amdgcn_logf(s);
+        for (int i = threadIdx.x; i < a.vocab; i += 256)
+            dx[i] = narrow<T>(grad((widen(x[i]) - m) - log_s, i));
+        return;
+    }
+    auto one = [&](float v, int i) { return grad(v - lse, i); };
     if (lo + 256 * V * U <= a.vocab) {
         float v[U][V];
 #pragma unroll

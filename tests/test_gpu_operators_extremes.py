@@ -177,3 +177,60 @@ def test_token_scores_of_any_magnitude(ops, vocab, dtype):
     _check_far(ops, x, t, 5, (vocab, dtype))
     for r in range(0, len(rows), 5):
         _check_far(ops, x[r:r + 1], t[r:r + 1], 20, (vocab, dtype, "row", r))
+
+
+@pytest.mark.parametrize("vocab", [1, 5, 1000, 8200, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_token_scores_backward_of_any_magnitude(ops, vocab, dtype):
+    """Rows as above; probabilities follow from distances within the row, so
+    their bound knows of lse only where the gradient reads it (up to 256:
+    2^-17), and a row of the type's lowest value has probabilities of
+    1 / vocab."""
+    g = _gen(vocab)
+    dt = DT[dtype]
+    step = {"f32": 2.0 ** -23, "f16": 2.0 ** -10, "bf16": 2.0 ** -7}[dtype]
+    mags = [0.5, 60.0, 250.0, 300.0, 5000.0, 3e4] + (
+        [65504.0] if dtype == "f16" else MAGNITUDES + [torch.finfo(dt).max])
+    rows = []
+    for mag in mags:
+        for v in (mag, -mag):
+            rows.append(torch.full((vocab,), v, device="cuda", dtype=torch.float64))
+            rows.append(v * (1 - step * torch.randint(0, 4, (vocab,), device="cuda",
+                                                      generator=g).double()))
+            rows.append(torch.where(torch.rand(vocab, device="cuda", generator=g) < 0.3,
+                                    -math.inf, v))
+        x = 3 * _randn(g, vocab).double()
+        x[vocab // 2:] = -mag
+        rows.append(x)
+    x = torch.stack(rows).to(dt)
+    n = len(rows)
+    t = torch.randint(0, vocab, (n,), device="cuda", generator=g, dtype=torch.int32)
+    t[::5] = -1
+    gl, glp, gh = (_randn(g, n) for _ in range(3))
+    r = ops.token_scores(x, t)
+    got = ops.token_scores_backward(x, t, r.lse, r.entropy, gl, glp, gh)
+    v = x.double()
+    m = v.amax(1, keepdim=True)
+    empty = m == -math.inf
+    m = torch.where(empty, 0.0, m)
+    e = torch.exp(v - m)
+    s = torch.where(empty, 1.0, e.sum(1, keepdim=True))
+    lp = (v - m) - torch.log(s)
+    p = e / s
+    inner = torch.where(p > 0, lp, 0.0)
+    h = -(p * inner).sum(1, keepdim=True)
+    gl, gh = gl.double()[:, None], gh.double()[:, None]
+    glp = torch.where((t >= 0)[:, None] & ~empty, glp.double()[:, None], 0.0)
+    one = torch.zeros_like(p).scatter_(1, t.clamp(min=0).long()[:, None], 1.0)
+    want = p * (gl - glp - gh * (inner + h)) + one * glp
+    size = (p * (gl.abs() + glp.abs() + gh.abs() * ((inner + h).abs() + h + 1)) *
+            (1 + inner.abs()) + one * glp.abs())
+    rel = (vocab / 256 + 64) * 2.0 ** -24 + 2.0 ** -19
+    rel = torch.where((m + torch.log(s)).abs() <= 257, rel + 2.0 ** -17, rel)
+    half = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+    off = (got.double() - want).abs()
+    bound = rel * size + half * want.abs() + 2.0 ** -25
+    assert bool((off <= bound).all()), float((off / bound).max())
+    assert torch.equal(ops.token_scores_backward(x, t, r.lse, r.entropy, gl[:, 0].float(),
+                                                 torch.where(t >= 0, glp[:, 0], 0.0).float(),
+                                                 gh[:, 0].float(), out=x), got)
