@@ -592,7 +592,8 @@ typedef enum { CTC_ACT_NONE = 0, CTC_ACT_RELU = 1, CTC_ACT_SILU = 2 } ctc_act;
  *                   residual's (no activation, gamma and beta not read).  A
  *                   group of the checksum alone has mean 0 and variance 0.
  *   mean, rstd      [n][groups] fp32, written (the backward pass reads them)
- * A NaN or an infinity spoils the group it is in.  hw <= 2^31, c <= 2^20. */
+ * A NaN or an infinity spoils the group it is in.  hw <= 2^31, c <= 2^20,
+ * n * c < 2^32. */
 ctc_status ctc_group_norm_forward(ctc_dtype dtype, int32_t n, int64_t hw,
                                   int32_t c, int32_t groups, int32_t carry,
                                   const void *x, const float *gamma,
@@ -641,7 +642,8 @@ ctc_status ctc_group_norm_workspace_bytes(ctc_dtype dtype, int32_t n,
  *           aligned, ldq a multiple of 16.  Up to 15 bytes behind a row's
  *           columns, to the next multiple of 16, are written too
  *   scales  [ceil(columns of q / 128)][ld_scales] fp32: scale of rows
- *           r * block_rows .. at [k block][r] */
+ *           r * block_rows .. at [k block][r]
+ * (rows / 16 + 1) * (cols / 128 + 1) < 2^23. */
 ctc_status ctc_fp8_quantize(ctc_dtype dtype, int64_t rows, int64_t cols,
                             const void *x, int64_t ldx, ctc_dtype qtype,
                             int32_t block_rows, int32_t transpose, void *q,
@@ -665,7 +667,8 @@ ctc_status ctc_fp8_quantize(ctc_dtype dtype, int64_t rows, int64_t cols,
  * A layer's forward product takes activations (a_block 1) and filters
  * [out][in] (b_block 128); the gradient of its input the output gradients and
  * the filters' transpose; the gradient of the filters both transposes
- * (blocks of 1, k the rows of the batch).  k = 0 gives act(bias). */
+ * (blocks of 1, k the rows of the batch).  k = 0 gives act(bias).
+ * m, k <= 2^30, n < 2^23 - 1, m * (n + 4) < 2^33 - 256. */
 ctc_status ctc_fp8_matmul(ctc_dtype atype, ctc_dtype btype, ctc_dtype ytype,
                           int64_t m, int64_t n, int64_t k, const void *a,
                           int64_t lda, const float *a_scales, int64_t ld_as,
@@ -695,7 +698,8 @@ ctc_status ctc_fp8_matmul_workspace_bytes(ctc_dtype ytype, int64_t m, int64_t n,
  * Barred tokens have a logit of -infinity: probability 0, never listed.
  * Places of top_ids without an alternative hold -1 and -infinity.  A row that
  * bars everything has lse and logprob -infinity and entropy 0.  A NaN or
- * +infinity makes a row's fp32 scores NaN; NaN logits are ordered first. */
+ * +infinity makes a row's fp32 scores NaN; NaN logits are ordered first.
+ * vocab <= 2^30, rows * (vocab / 4096 + 1) < 2^23. */
 ctc_status ctc_token_scores_forward(ctc_dtype dtype, int64_t rows,
                                     int32_t vocab, const void *logits,
                                     int64_t ld, const int32_t *targets,

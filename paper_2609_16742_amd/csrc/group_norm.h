@@ -59,17 +59,19 @@ static NormPlan norm_plan(const NormArgs &a) {
 // Position of a workgroup's threads in the map.
 struct NormPos {
     int64_t img, p0, p1;         // image, pixels [p0, p1)
-    int c0, pix;                 // first channel, first pixel's offset
-    bool on;
+    int ct, c0, pix;             // channel tile, first channel, first pixel's offset
+    bool in, on;                 // the workgroup is one of the map's, the thread works
     __device__ NormPos(const NormArgs &a, const NormPlan &p) {
-        const int64_t t = blockIdx.x / p.ctiles;
-        const int ct = blockIdx.x % p.ctiles;
+        const uint32_t wg = workgroup();
+        const int64_t t = wg / p.ctiles;
+        ct = wg % p.ctiles;
         img = t / p.chunks;
+        in = img < a.n;
         p0 = t % p.chunks * p.chunk;
         p1 = p0 + p.chunk < a.hw ? p0 + p.chunk : a.hw;
         c0 = (ct * p.tx + (int)threadIdx.x % p.tx) * p.v;
         pix = threadIdx.x / p.tx;
-        on = pix < p.pl && c0 < a.c;
+        on = in && pix < p.pl && c0 < a.c;
     }
 };
 
@@ -88,7 +90,7 @@ __device__ __forceinline__ void norm_lanes(const NormArgs &a, const NormPlan &p,
             sum[1][i] = s2[e];
         }
     __syncthreads();
-    const int first = (int)(blockIdx.x % p.ctiles) * w;
+    const int first = at.ct * w;
     for (int i = threadIdx.x; i < w && first + i < a.c; i += 256) {
         float t1 = 0.f, t2 = 0.f;
         for (int l = 0; l < p.pl; l++) {
@@ -104,6 +106,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_stats(NormArgs a, NormPlan p) {
     __shared__ float sum[2][256 * V];
     const NormPos at(a, p);
+    if (!at.in) return;
     float s1[V] = {}, s2[V] = {}, k[V];
     const T *x = (const T *)a.x + at.img * a.hw * a.c;
     if (at.on) {
@@ -189,7 +192,7 @@ static bool norm_join_wide(const NormArgs &a, const NormPlan &p) {
 template <int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void norm_stats_join(NormArgs a, NormPlan p) {
     __shared__ double lds[W];
-    const int64_t t = W == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int64_t t = W == 1 ? (int64_t)workgroup() * 4 + (threadIdx.x >> 6) : workgroup();
     if (t >= a.n * a.groups) return;
     NormJoin<W> j(a, p, t);
     const double total = (double)a.hw * j.nc;
@@ -325,6 +328,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_grad_sums(NormArgs a, NormPlan p) {
     __shared__ float sum[2][256 * V];
     const NormPos at(a, p);
+    if (!at.in) return;
     float s1[V] = {}, s2[V] = {};
     if (at.on) {
         const NormChannels<V> k = norm_channels<V>(a, at.img, at.c0);
@@ -374,9 +378,10 @@ constexpr int JOIN_ROWS = 64;
 template <int W>
 __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
                                                        int64_t group_blocks) {
-    if (blockIdx.x < group_blocks) {
+    const uint32_t wg = workgroup();
+    if (wg < group_blocks) {
         __shared__ double lds[W];
-        const int64_t t = W == 1 ? (int64_t)blockIdx.x * 16 + (threadIdx.x >> 6) : blockIdx.x;
+        const int64_t t = W == 1 ? (int64_t)wg * 16 + (threadIdx.x >> 6) : wg;
         if (t >= a.n * a.groups) return;
         NormJoin<W> j(a, p, t);
         double s1 = 0, s2 = 0;
@@ -397,7 +402,7 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
     }
     __shared__ float sum[2][JOIN_ROWS][17];
     const int cl = threadIdx.x & 15, row = threadIdx.x >> 4;
-    const int c = (int)(blockIdx.x - group_blocks) * 16 + cl;
+    const int64_t c = (wg - group_blocks) * 16 + cl;
     float s1 = 0.f, s2 = 0.f;
     if (c < a.c && !(a.carry && c == a.c - 1))
 #pragma unroll 8
@@ -468,16 +473,12 @@ template <typename T, int V, int NT, int N> struct Slab {
     int slab, px, cx, c0;        // c0: the thread's first channel
     bool on;
     __device__ bool place(const NormArgs &a, const SlabPlan &p) {
-        if (p.by_xcd) {
-            // workgroups go round the eight XCDs: an image's slabs share the
-            // lines that one XCD's L2 holds
-            const int64_t u = blockIdx.x >> 3;
-            img = u / p.slabs * 8 + (blockIdx.x & 7);
-            slab = (int)(u % p.slabs);
-        } else {
-            img = blockIdx.x / p.slabs;
-            slab = (int)(blockIdx.x % p.slabs);
-        }
+        const uint32_t wg = workgroup(), u = p.by_xcd ? wg >> 3 : wg;
+        img = u / p.slabs;
+        slab = (int)(u % p.slabs);
+        // workgroups go round the eight XCDs: an image's slabs share the
+        // lines that one XCD's L2 holds
+        if (p.by_xcd) img = img * 8 + (wg & 7);
         cx = (int)threadIdx.x % p.tx;
         px = (int)threadIdx.x / p.tx;
         on = px < p.pl;
@@ -750,7 +751,7 @@ static SlabPlan slab_plan(const NormArgs &a, bool backward) {
     return p;
 }
 static dim3 slab_grid(const NormArgs &a, const SlabPlan &p) {
-    return dim3((unsigned)((p.by_xcd ? (a.n + 7) / 8 * 8 : a.n) * p.slabs));
+    return grid_of((p.by_xcd ? (a.n + 7) / 8 * 8 : a.n) * p.slabs);
 }
 
 size_t norm_workspace(const NormArgs &a, bool backward) {
@@ -786,17 +787,16 @@ hipError_t launch_norm_forward(const NormArgs &a, hipStream_t st) {
             return start(norm_slab<T, V, 1024>, slab_grid(a, sp), 1024, st, a, sp);
         });
     const NormPlan p = norm_plan(a);
-    const dim3 grid((unsigned)(a.n * p.chunks * p.ctiles));
+    const dim3 grid = grid_of(a.n * p.chunks * p.ctiles);
     return by_width(a.type, p.v, [&](auto tag, auto vc) {
         typedef typename decltype(tag)::type T;
         constexpr int V = decltype(vc)::value;
         hipError_t e = start(norm_stats<T, V>, grid, 256, st, a, p);
         if (e != hipSuccess) return e;
         e = norm_join_wide(a, p)
-                ? start(norm_stats_join<JOIN_WAVES>, dim3((unsigned)(a.n * a.groups)),
-                        64 * JOIN_WAVES, st, a, p)
-                : start(norm_stats_join<1>, dim3((unsigned)((a.n * a.groups + 3) / 4)), 256, st,
-                        a, p);
+                ? start(norm_stats_join<JOIN_WAVES>, grid_of(a.n * a.groups), 64 * JOIN_WAVES, st,
+                        a, p)
+                : start(norm_stats_join<1>, grid_of((a.n * a.groups + 3) / 4), 256, st, a, p);
         if (e != hipSuccess) return e;
         return start(norm_apply<T, V>, grid, 256, st, a, p);
     });
@@ -818,11 +818,11 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t st) {
         NormPlan one{};
         one.chunks = 1;
         one.chunk = a.hw;
-        return start(norm_grad_join<1>, dim3((unsigned)((a.c + 15) / 16)), 1024, st, a, one,
+        return start(norm_grad_join<1>, grid_of((a.c + 15) / 16), 1024, st, a, one,
                      (int64_t)0);
     }
     const NormPlan p = norm_plan(a);
-    const dim3 grid((unsigned)(a.n * p.chunks * p.ctiles));
+    const dim3 grid = grid_of(a.n * p.chunks * p.ctiles);
     return by_width(a.type, p.v, [&](auto tag, auto vc) {
         typedef typename decltype(tag)::type T;
         constexpr int V = decltype(vc)::value;
@@ -833,7 +833,7 @@ hipError_t launch_norm_backward(const NormArgs &a, hipStream_t st) {
         }
         const bool wide = norm_join_wide(a, p);
         const int64_t gb = wide ? a.n * a.groups : (a.n * a.groups + 15) / 16;
-        const dim3 jg((unsigned)(gb + (a.c + 15) / 16));
+        const dim3 jg = grid_of(gb + (a.c + 15) / 16);
         e = wide ? start(norm_grad_join<JOIN_WAVES>, jg, 1024, st, a, p, gb)
                  : start(norm_grad_join<1>, jg, 1024, st, a, p, gb);
         if (e != hipSuccess || !a.n || (!a.dx && !a.dresidual)) return e;

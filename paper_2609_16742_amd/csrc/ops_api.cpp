@@ -30,7 +30,9 @@ hipStream_t S(void *s) { return (hipStream_t)s; }
 bool real_type(int t) { return t == CTC_F32 || t == CTC_F16 || t == CTC_BF16; }
 bool byte_type(int t) { return t == CTC_E4M3 || t == CTC_E5M2; }
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-// A launch takes fewer than 2^32 threads; the largest workgroups have 512.
+// A launch along one dimension takes fewer than 2^32 threads, and the largest
+// workgroups of the quantiser, the product and the scores have 512.  (Those of
+// the group norm have 1024, in grids of two dimensions.)
 bool grid_ok(double workgroups) { return workgroups < 8388608.0; }
 
 ctc_status need_workspace(size_t need, const void *ws, size_t bytes) {
@@ -52,12 +54,12 @@ ctc_status norm_args(ctc_dtype dtype, int32_t n, int64_t hw, int32_t c, int32_t 
     if (act < CTC_ACT_NONE || act > CTC_ACT_SILU) return fail(CTC_ERR_ARG, "bad activation");
     if (hw > ((int64_t)1 << 31) || c > (1 << 20))
         return fail(CTC_ERR_UNSUPPORTED, "maps of up to 2^31 pixels and 2^20 channels");
+    // (workgroups have numbers of 32 bits; there are at most n * c of them, or
+    // 2048)
+    if ((int64_t)n * c >> 32) return fail(CTC_ERR_UNSUPPORTED, "too many images");
     a = NormArgs{};
     a.type = dtype; a.n = n; a.hw = hw; a.c = c; a.groups = groups;
     a.carry = carry != 0; a.act = act;
-    if (!grid_ok((double)n * 2048 + (double)n * ((double)c / 256 + 1)) ||
-        !grid_ok((double)n * groups / 4 + c))
-        return fail(CTC_ERR_UNSUPPORTED, "too many images");
     return CTC_OK;
 }
 

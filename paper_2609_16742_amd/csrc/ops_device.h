@@ -127,6 +127,17 @@ template <int V> __device__ __forceinline__ void act_grad(int act, float (&z)[V]
     }
 }
 
+// Workgroups numbered over two dimensions of a grid: along one a launch takes
+// fewer than 2^32 threads.  (Those past the last have to leave.)
+constexpr int64_t GRID_ROW = 1 << 20;
+static dim3 grid_of(int64_t workgroups) {
+    if (workgroups <= GRID_ROW) return dim3((unsigned)workgroups);
+    return dim3((unsigned)GRID_ROW, (unsigned)((workgroups + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ __forceinline__ uint32_t workgroup() {
+    return blockIdx.y * (uint32_t)GRID_ROW + blockIdx.x;
+}
+
 template <typename K, typename... A>
 static hipError_t start(K kernel, dim3 grid, int block, hipStream_t st, A... args) {
     hipLaunchKernelGGL(kernel, grid, dim3(block), 0, st, args...);

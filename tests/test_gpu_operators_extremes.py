@@ -234,3 +234,63 @@ def test_token_scores_backward_of_any_magnitude(ops, vocab, dtype):
     assert torch.equal(ops.token_scores_backward(x, t, r.lse, r.entropy, gl[:, 0].float(),
                                                  torch.where(t >= 0, glp[:, 0], 0.0).float(),
                                                  gh[:, 0].float(), out=x), got)
+
+
+# -------------------------------------------------------------- group norm
+
+def _norm_ref(x, dy, groups, gamma, beta):
+    """y, mean, rstd, dx, dgamma, dbeta in 64 bits, with the magnitudes that
+    their sums are of; act is the SiLU."""
+    n, hw, c = x.shape
+    sh = (n, hw, groups, c // groups)
+    v = x.double().view(sh)
+    var, mean = torch.var_mean(v, (1, 3), correction=0, keepdim=True)
+    rstd = 1 / torch.sqrt(var + 1e-5)
+    xhat = ((v - mean) * rstd).view(n, hw, c)
+    z = xhat * gamma.double() + beta.double()
+    s = torch.sigmoid(z)
+    dz = dy.double() * (s + z * s * (1 - s))
+    dn = (dz * gamma.double()).view(sh)
+    xg = xhat.view(sh)
+    m1, m2 = dn.mean((1, 3), keepdim=True), (dn * xg).mean((1, 3), keepdim=True)
+    dx = ((dn - m1 - xg * m2) * rstd).view(n, hw, c)
+    size = ((dn.abs() + dn.abs().mean((1, 3), keepdim=True) + xg.abs() *
+             (dn * xg).abs().mean((1, 3), keepdim=True)) * rstd).view(n, hw, c)
+    return dict(y=z * s, mean=mean[:, 0, :, 0], rstd=rstd[:, 0, :, 0], dx=dx,
+                dgamma=(dz * xhat).sum((0, 1)), dbeta=dz.sum((0, 1)), size=size,
+                z=z, xhat=xhat, sg=(dz * xhat).abs().sum((0, 1)),
+                sb=dz.abs().sum((0, 1)))
+
+
+# workgroups of one image's slabs and of chunks, of more than 2^20 in all
+@pytest.mark.parametrize("n,hw,c,groups", [(4093, 1, 512, 32), (4094, 1, 16, 4),
+                                           (4100, 4, 24, 3), (10000, 9, 64, 8),
+                                           (4097, 2, 1028, 1), (1100000, 1, 8, 2),
+                                           (530000, 1, 1028, 1)], ids=str)
+def test_group_norm_of_many_images(ops, n, hw, c, groups):
+    g = _gen(n)
+    x, dy = _randn(g, n, hw, c), _randn(g, n, hw, c)
+    gamma, beta = 0.5 + torch.rand(c, device="cuda", generator=g), 0.3 * _randn(g, c)
+    y, mean, rstd = ops.group_norm(x, groups, gamma, beta, act="silu")
+    dx, _, dgamma, dbeta = ops.group_norm_backward(dy, x, mean, rstd, groups, gamma, beta,
+                                                   act="silu")
+    # an image's sums are of hw * c / groups terms (and 24 more operations);
+    # silu' is at most 1.1 and moves by at most 0.5 a unit of z
+    u = (hw * c / groups + 24) * 2.0 ** -24
+    totals = {k: 0 for k in ("dgamma", "dbeta", "sg", "sb")}
+    for i in range(0, n, 100000):
+        part = slice(i, i + 100000)
+        w = _norm_ref(x[part], dy[part], groups, gamma, beta)
+        for k in totals:
+            totals[k] = totals[k] + w[k]
+        spread = 1 / w["rstd"]
+        for got, k, bound in [
+                (mean, "mean", u * (w["mean"].abs() + spread)), (rstd, "rstd", u * w["rstd"]),
+                (y, "y", 2 * u * (1 + w["xhat"].abs() + w["z"].abs())),
+                (dx, "dx", 4 * u * w["size"] * (1 + w["z"].abs()) ** 2)]:
+            off = (got[part].double() - w[k]).abs()
+            assert bool((off <= bound).all()), (k, i, float((off / bound).max()))
+    u = (n * hw / 64 + 64) * 2.0 ** -24
+    for got, k, s in ((dgamma, "dgamma", "sg"), (dbeta, "dbeta", "sb")):
+        off = (got.double() - totals[k]).abs()
+        assert bool((off <= 4 * u * totals[s]).all()), (k, float((off / totals[s]).max()))

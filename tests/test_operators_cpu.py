@@ -135,3 +135,16 @@ def test_the_networks_refuse_the_operators_types():
         with pytest.raises(ctc.CtcError) as e:
             ctc.ctc_conv2d_workspace_bytes(d, dt, 1, 8, 8)
         assert e.value.status == ARG
+
+
+def test_group_norm_takes_many_images():
+    """n * c below 2^32 (and no less) is taken, whatever the map's size."""
+    for n, hw, c in [(4093, 1, 512), (4094, 1, 16), (10000, 4, 64), (1 << 20, 1, 2048),
+                     ((1 << 31) - 1, 1, 2), (1 << 24, 1 << 20, 255), (5, 1 << 31, 24)]:
+        for backward in (0, 1):
+            for dtype in (F32, F16, BF16):
+                ctc.ctc_group_norm_workspace_bytes(dtype, n, hw, c, 1, backward)
+    for n, c in [(1 << 16, 1 << 16), (1 << 30, 4)]:
+        for f, base in ((ctc.ctc_group_norm_forward, NORM),
+                        (ctc.ctc_group_norm_backward, NORM_BACK)):
+            _call(f, base, UNSUPPORTED, n=n, c=c, groups=4)
