@@ -8,12 +8,15 @@
 //   dx = rstd (dz gamma - (s1 + xhat s2) / count),
 //   s1 = sum dz gamma,  s2 = sum dz gamma xhat  over (image, group).
 //
-// Sums over pixels and images are fp32, those over a group's chunks and
-// channels fp64 (a group whose channels' means cancel keeps the digits of its
-// mean).  A channel's sum and sum of squares are taken about the
-// chunk's first pixel, which lies within a few deviations of the mean, and
-// channels and chunks are joined as (count, mean, squared deviations), so a
-// mean far from zero costs no digits.
+// Statistics of maps beyond a workgroup (norm_stats): a channel's sum and sum
+// of squares over a chunk's pixels are fp64, about the chunk's first pixel, so
+// neither a mean far from zero nor an outlier there costs digits; chunks and
+// channels are joined as (count, mean, squared deviations), kept in fp32 and
+// added in fp64.  Of maps held by a workgroup (norm_slab): the mean, then the
+// squared deviations from it, summed in fp32 over up to 8 pixels of a thread
+// and the pixel lanes, in fp64 over a group's channels; a mean far from zero
+// is off by a few 2^-24 of itself, and the statistics with it.  Gradients' sums
+// over pixels and images are fp32, those over a group's channels fp64.
 //
 // What bounds it: the bytes of the maps.  Maps held by a workgroup are read
 // once (norm_slab: 64 x 56 x 56 x 64 fp16 with a residual in 22.6 us, 3.4
@@ -76,38 +79,61 @@ struct NormPos {
 };
 
 // Sums two numbers per channel over a workgroup's pixel lanes; f(channel,
-// sum1, sum2) for each.
-template <int V, typename F>
-__device__ __forceinline__ void norm_lanes(const NormArgs &a, const NormPlan &p,
-                                           float (*sum)[256 * V], const NormPos &at,
-                                           const float (&s1)[V], const float (&s2)[V], F f) {
+// sum1, sum2) for each.  fp64 takes LDS for one number after the other (for
+// both, 32 KB, a CU holds five workgroups instead of eight).
+template <int V, typename N> constexpr int lanes_lds() { return 256 * V * (8 / sizeof(N)); }
+template <int V, typename N, typename F>
+__device__ __forceinline__ void norm_lanes(const NormArgs &a, const NormPlan &p, N *lds,
+                                           const NormPos &at, const N (&s1)[V],
+                                           const N (&s2)[V], F f) {
     const int w = p.tx * V;
-    if (at.pix < p.pl)
+    N t1[V] = {}, t2[V] = {};
+    auto put = [&](N *to, const N (&s)[V]) {
+        if (at.pix < p.pl)
+#pragma unroll
+            for (int e = 0; e < V; e++) to[at.pix * w + (int)threadIdx.x % p.tx * V + e] = s[e];
+    };
+    auto add = [&](const N *from, N (&t)[V]) {
 #pragma unroll
         for (int e = 0; e < V; e++) {
-            const int i = at.pix * w + (int)threadIdx.x % p.tx * V + e;
-            sum[0][i] = s1[e];
-            sum[1][i] = s2[e];
+            const int i = threadIdx.x + e * 256;
+            if (i < w)
+                for (int l = 0; l < p.pl; l++) t[e] += from[l * w + i];
         }
-    __syncthreads();
+    };
+    if constexpr (sizeof(N) == 4) {
+        put(lds, s1);
+        put(lds + 256 * V, s2);
+        __syncthreads();
+        add(lds, t1);
+        add(lds + 256 * V, t2);
+    } else {
+        put(lds, s1);
+        __syncthreads();
+        add(lds, t1);
+        __syncthreads();
+        put(lds, s2);
+        __syncthreads();
+        add(lds, t2);
+    }
     const int first = at.ct * w;
-    for (int i = threadIdx.x; i < w && first + i < a.c; i += 256) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int l = 0; l < p.pl; l++) {
-            t1 += sum[0][l * w + i];
-            t2 += sum[1][l * w + i];
-        }
-        f(first + i, t1, t2);
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+        const int i = threadIdx.x + e * 256;
+        if (i < w && first + i < a.c) f(first + i, t1[e], t2[e]);
     }
 }
 
-// Per chunk and channel: mean and squared deviations -> ws [n][chunks][c][2]
+// Per chunk and channel: mean and squared deviations -> ws [n][chunks][c][2].
+// In fp64, about the chunk's first pixel: fp32 sums lose a chunk's length in
+// digits where that pixel is an outlier (rstd of 12544 x 8 off by 7e-5).
 template <typename T, int V>
-__global__ __launch_bounds__(256) void norm_stats(NormArgs a, NormPlan p) {
-    __shared__ float sum[2][256 * V];
+__global__ __launch_bounds__(256, 8) void norm_stats(NormArgs a, NormPlan p) {
+    __shared__ double sum[lanes_lds<V, double>()];
     const NormPos at(a, p);
     if (!at.in) return;
-    float s1[V] = {}, s2[V] = {}, k[V];
+    double s1[V] = {}, s2[V] = {};
+    float k[V];
     const T *x = (const T *)a.x + at.img * a.hw * a.c;
     if (at.on) {
         load<T, V>(x + at.p0 * a.c + at.c0, k);
@@ -116,20 +142,19 @@ __global__ __launch_bounds__(256) void norm_stats(NormArgs a, NormPlan p) {
             load<T, V>(x + q * a.c + at.c0, v);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float d = v[e] - k[e];
+                const double d = (double)v[e] - k[e];
                 s1[e] += d;
-                s2[e] = __builtin_fmaf(d, d, s2[e]);
+                s2[e] = __builtin_fma(d, d, s2[e]);
             }
         }
     }
-    const float count = (float)(at.p1 - at.p0), inv = 1.f / count;
+    const double inv = 1. / (double)(at.p1 - at.p0);
     float *out = a.ws + (at.img * p.chunks + at.p0 / p.chunk) * a.c * 2;
-    norm_lanes<V>(a, p, sum, at, s1, s2, [&](int c, float t1, float t2) {
-        const float k0 = widen(x[at.p0 * a.c + c]), d = t1 * inv;
-        const float m2 = t2 - t1 * d;
-        out[c * 2] = k0 + d;
-        // (not fmaxf, which would drop a NaN)
-        out[c * 2 + 1] = m2 < 0.f ? 0.f : m2;
+    norm_lanes<V>(a, p, sum, at, s1, s2, [&](int c, double t1, double t2) {
+        const double d = t1 * inv, m2 = t2 - t1 * d;
+        out[c * 2] = (float)(widen(x[at.p0 * a.c + c]) + d);
+        // (not fmax, which would drop a NaN)
+        out[c * 2 + 1] = m2 < 0 ? 0.f : (float)m2;
     });
 }
 
@@ -326,7 +351,7 @@ __device__ __forceinline__ void norm_dz(const NormArgs &a, const NormChannels<V>
 // Per chunk and channel: sum dz, sum dz xhat -> ws [n][chunks][c][2]
 template <typename T, int V>
 __global__ __launch_bounds__(256) void norm_grad_sums(NormArgs a, NormPlan p) {
-    __shared__ float sum[2][256 * V];
+    __shared__ float sum[lanes_lds<V, float>()];
     const NormPos at(a, p);
     if (!at.in) return;
     float s1[V] = {}, s2[V] = {};

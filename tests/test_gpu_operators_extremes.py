@@ -294,3 +294,26 @@ def test_group_norm_of_many_images(ops, n, hw, c, groups):
     for got, k, s in ((dgamma, "dgamma", "sg"), (dbeta, "dbeta", "sb")):
         off = (got.double() - totals[k]).abs()
         assert bool((off <= 4 * u * totals[s]).all()), (k, float((off / totals[s]).max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("n,hw,c,groups", [(4, 12544, 8, 1), (1, 50176, 8, 1), (1, 50176, 24, 3),
+                                           (3, 9000, 32, 4)], ids=str)
+def test_group_norm_outliers(ops, n, hw, c, groups, dtype):
+    """Pixels up to 1000 deviations out, the first one of the map among them:
+    chunks are summed in 64 bits and joined so, and rounded a few times."""
+    for far in (0.0, 10.0, 100.0, 1000.0, -30000.0):
+        x = _randn(_gen(hw), n, hw, c)
+        if far:
+            x[:, 0] = far
+            x[:, hw // 3, 1] = -far
+            x[:, -1] = far
+        x = x.to(DT[dtype])
+        _, mean, rstd = ops.group_norm(x, groups)
+        v = x.double().view(n, hw, groups, c // groups)
+        var, want = torch.var_mean(v, (1, 3), correction=0)
+        wr = 1 / torch.sqrt(var + 1e-5)
+        off = (rstd.double() / wr - 1).abs().max()
+        assert float(off) <= 16 * 2.0 ** -24, (far, float(off))
+        off = ((mean.double() - want).abs() * wr).max()
+        assert float(off) <= 4 * 2.0 ** -24, (far, float(off))
