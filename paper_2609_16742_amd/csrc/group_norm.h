@@ -16,7 +16,8 @@
 // squared deviations from it, summed in fp32 over up to 8 pixels of a thread
 // and the pixel lanes, in fp64 over a group's channels; a mean far from zero
 // is off by a few 2^-24 of itself, and the statistics with it.  Gradients' sums
-// over pixels and images are fp32, those over a group's channels fp64.
+// over a chunk's pixels are fp32, those over chunks, images and a group's
+// channels fp64.
 //
 // What bounds it: the bytes of the maps.  Maps held by a workgroup are read
 // once (norm_slab: 64 x 56 x 56 x 64 fp16 with a residual in 22.6 us, 3.4
@@ -425,10 +426,10 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
         }
         return;
     }
-    __shared__ float sum[2][JOIN_ROWS][17];
+    __shared__ double sum[2][JOIN_ROWS / 4][16];
     const int cl = threadIdx.x & 15, row = threadIdx.x >> 4;
     const int64_t c = (wg - group_blocks) * 16 + cl;
-    float s1 = 0.f, s2 = 0.f;
+    double s1 = 0, s2 = 0;
     if (c < a.c && !(a.carry && c == a.c - 1))
 #pragma unroll 8
         for (int64_t i = row; i < a.n * p.chunks; i += JOIN_ROWS) {
@@ -436,16 +437,25 @@ __global__ __launch_bounds__(1024) void norm_grad_join(NormArgs a, NormPlan p,
             s1 += e.x;
             s2 += e.y;
         }
-    sum[0][row][cl] = s1;
-    sum[1][row][cl] = s2;
+    // the four rows of a wave, then the waves
+#pragma unroll
+    for (int o = 16; o < 64; o *= 2) {
+        s1 += __shfl_xor(s1, o);
+        s2 += __shfl_xor(s2, o);
+    }
+    if ((row & 3) == 0) {
+        sum[0][row >> 2][cl] = s1;
+        sum[1][row >> 2][cl] = s2;
+    }
     __syncthreads();
     if (row == 0 && c < a.c) {
-        for (int i = 1; i < JOIN_ROWS; i++) {
+#pragma unroll
+        for (int i = 1; i < JOIN_ROWS / 4; i++) {
             s1 += sum[0][i][cl];
             s2 += sum[1][i][cl];
         }
-        if (a.dbeta) a.dbeta[c] = s1;
-        if (a.dgamma) a.dgamma[c] = s2;
+        if (a.dbeta) a.dbeta[c] = (float)s1;
+        if (a.dgamma) a.dgamma[c] = (float)s2;
     }
 }
 

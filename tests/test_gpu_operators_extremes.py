@@ -317,3 +317,22 @@ def test_group_norm_outliers(ops, n, hw, c, groups, dtype):
         assert float(off) <= 16 * 2.0 ** -24, (far, float(off))
         off = ((mean.double() - want).abs() * wr).max()
         assert float(off) <= 4 * 2.0 ** -24, (far, float(off))
+
+
+# held by a workgroup, and beyond one: a group of its own, several chunks
+@pytest.mark.parametrize("n,hw,c,groups", [(3, 1, 64, 4), (130, 1, 16, 2), (3, 1, 1028, 1),
+                                           (3, 9000, 32, 8)], ids=str)
+def test_group_norm_gradient_sums_that_cancel(ops, n, hw, c, groups):
+    """dbeta and dgamma over images whose parts cancel: 2^24, 1 and -2^24 of
+    one pixel, all of them exact, of which fp32 sums leave 0."""
+    x = _randn(_gen(c), 1, hw, c).repeat(n, 1, 1)
+    dy = torch.zeros_like(x)
+    dy[0, 0], dy[1, 0], dy[-1, 0] = 2.0 ** 24, 1.0, -2.0 ** 24
+    _, mean, rstd = ops.group_norm(x, groups)
+    _, _, dgamma, dbeta = ops.group_norm_backward(dy, x, mean, rstd, groups)
+    assert bool((dbeta == 1).all())
+    per = c // groups
+    want = (x[0, 0].double() - mean[0].double().repeat_interleave(per)) * \
+        rstd[0].double().repeat_interleave(per)
+    # (the difference and the product are rounded once each)
+    assert bool(((dgamma.double() - want).abs() <= 2.0 ** -22 * (1 + want.abs())).all())
