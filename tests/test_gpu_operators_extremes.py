@@ -336,3 +336,16 @@ def test_group_norm_gradient_sums_that_cancel(ops, n, hw, c, groups):
         rstd[0].double().repeat_interleave(per)
     # (the difference and the product are rounded once each)
     assert bool(((dgamma.double() - want).abs() <= 2.0 ** -22 * (1 + want.abs())).all())
+
+
+@pytest.mark.parametrize("hw,c", [(16, 64), (16, 12), (30000, 24), (1, 1028)])
+def test_group_norm_of_channels_whose_means_cancel(ops, hw, c):
+    """Channels of 2^20, 1, -2^20 and 0: their sums are exact, and the group's
+    mean is a quarter."""
+    x = torch.tensor([2.0 ** 20, 1.0, -2.0 ** 20, 0.0], device="cuda").repeat(c // 4)
+    x = x.expand(2, hw, c).contiguous()
+    for groups in {1, c // 4}:
+        y, mean, rstd = ops.group_norm(x, groups)
+        assert bool(((mean - 0.25).abs() <= 2.0 ** -24).all()), mean
+        want = 1 / math.sqrt((2.0 ** 41 + 1) / 4 - 1 / 16 + 1e-5)
+        assert bool(((rstd.double() / want - 1).abs() <= 2.0 ** -21).all())
