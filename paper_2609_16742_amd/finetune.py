@@ -105,12 +105,17 @@ class Head:
 def features(net, x):
     """The protected network's last feature map [n, h, w, c] for images x
     (what its global pool or its first FC layer reads); valid until the
-    network's next pass."""
+    network's next pass.  This pass fuses no residual blocks; the kinds of
+    :meth:`CtcNet.set_fusion` stay in effect for others."""
     if net.mode != 1:
         raise ValueError("a network protected in replace mode is needed")
     # (a block fused with the classifier would not store the map)
-    net.set_fusion(ctc.CTC_FUSE_IR | ctc.CTC_FUSE_STEM | ctc.CTC_FUSE_POOL)
-    net.forward(x)
+    chosen = net.fusion
+    net.set_fusion(chosen & ~ctc.CTC_FUSE_BLOCK)
+    try:
+        net.forward(x)
+    finally:
+        net.set_fusion(chosen)
     i = next(i for i, l in enumerate(net.layers) if l["op"] in ("gap", "fc"))
     at = net.layers[i]["inp"]
     t = at

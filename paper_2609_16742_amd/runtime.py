@@ -8,6 +8,9 @@ import torch
 
 from . import ctc
 
+_FUSE_ALL = (ctc.CTC_FUSE_IR | ctc.CTC_FUSE_BLOCK | ctc.CTC_FUSE_STEM
+             | ctc.CTC_FUSE_POOL)
+
 
 class CtcNet:
     def __init__(self, layers, in_shape, classes, dtype, params, protect=True,
@@ -21,6 +24,7 @@ class CtcNet:
         self.protect = mode > 0
         self.mode = mode
         self.max_batch = max_batch
+        self.fusion = _FUSE_ALL      # as the last set_fusion left it
         self.out_cols = classes + (1 if mode else 0)
         self.h = ctc.ctc_net_create(ctc.ops_from_layers(layers), in_shape[0],
                                     in_shape[1], in_shape[2], classes,
@@ -49,9 +53,9 @@ class CtcNet:
         """Fusion kinds in effect: a CTC_FUSE_* bit mask; True selects every
         kind, False none (default: every kind)."""
         if kinds is True:
-            kinds = (ctc.CTC_FUSE_IR | ctc.CTC_FUSE_BLOCK | ctc.CTC_FUSE_STEM
-                     | ctc.CTC_FUSE_POOL)
+            kinds = _FUSE_ALL
         ctc.ctc_net_set_fusion(self.h, int(kinds))
+        self.fusion = int(kinds)
 
     def set_threshold(self, ref, tau):
         ctc.ctc_net_set_threshold(self.h, ref, tau)
