@@ -6,6 +6,7 @@
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 
 #include <optional>
 #include <stdexcept>
@@ -103,6 +104,15 @@ int64_t rows_8bit(const Tensor &t, const char *name, const Tensor &ref) {
 Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor &ref) {
     return at::empty(shape, at::TensorOptions().dtype(type).device(ref.device()));
 }
+// Nothing is recorded for autograd, so a gradient that someone waits for would
+// be lost without a word.
+bool wants_grad(const Tensor &t) { return t.defined() && t.requires_grad(); }
+bool wants_grad(const Maybe &t) { return t && wants_grad(*t); }
+template <typename... Ts> void no_grad(const Ts &...t) {
+    need(!at::GradMode::is_enabled() || !(wants_grad(t) || ...),
+         "a tensor requires grad, and the operators record nothing for autograd: detach it or "
+         "call under torch.no_grad()");
+}
 // Device scratch of a call on the current stream.
 void *scratch(size_t bytes, Tensor &keep, const Tensor &ref) {
     if (!bytes) return nullptr;
@@ -136,6 +146,7 @@ std::tuple<Tensor, Tensor, Tensor> group_norm(const Tensor &x, int64_t groups, c
                                               bool carry, double eps, Maybe y, Maybe mean,
                                               Maybe rstd, int64_t stream) {
     const Map m = map_of(x, groups);
+    no_grad(x, gamma, beta, residual, y, mean, rstd);
     c10::DeviceGuard guard(x.device());
     if (!y) {
         y = at::empty_like(x);
@@ -163,6 +174,7 @@ group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean, const
                     int act, bool carry, bool make, Maybe dx, Maybe dr, Maybe dgamma, Maybe dbeta,
                     int64_t stream) {
     const Map m = map_of(x, groups);
+    no_grad(dy, x, mean, rstd, gamma, beta, residual, dx, dr, dgamma, dbeta);
     c10::DeviceGuard guard(x.device());
     if (make) {
         dx = at::empty_like(x);
@@ -198,6 +210,7 @@ std::tuple<Tensor, Tensor> fp8_quantize(const Tensor &x, bool e5m2, int64_t bloc
     on_gpu(x, "x");
     need(real_type(x), "x must be float32, float16 or bfloat16");
     need(block == 1 || block == 128, "block_rows must be 1 or 128");
+    no_grad(x, q, scales);
     const int64_t ldx = rows_of(x, "x", x);
     const int64_t rows = x.size(0), cols = x.size(1);
     const int64_t qr = transpose ? cols : rows, qc = transpose ? rows : cols;
@@ -238,6 +251,7 @@ Tensor fp8_matmul(const Tensor &a, const Tensor &a_scales, const Tensor &b,
                   const Maybe &out, int64_t stream) {
     on_gpu(a, "a");
     need(byte_type(a) && byte_type(b), "a and b must be float8 tensors");
+    no_grad(a, a_scales, b, b_scales, bias, out);
     const int64_t lda = rows_8bit(a, "a", a), ldb = rows_8bit(b, "b", a);
     const int64_t m = a.size(0), k = a.size(1), n = b.size(0), kb = (k + 127) / 128;
     need(b.size(1) == k, "a and b must have the same number of columns");
@@ -281,6 +295,7 @@ Scores token_scores(const Tensor &x, const Maybe &targets, int64_t top_k, bool m
     const int32_t vocab = (int32_t)x.size(1);
     c10::DeviceGuard guard(x.device());
     auto &[lse, entropy, logprob, rank, ids, tops] = out;
+    no_grad(x, lse, entropy, logprob, tops);
     if (make) {
         const Tensor f = empty({targets ? 3 : 2, rows}, at::kFloat, x);
         lse = f[0];
@@ -315,6 +330,7 @@ Tensor token_scores_backward(const Tensor &x, const Maybe &targets, const Tensor
                              const Maybe &entropy, const Maybe &g_lse, const Maybe &g_logprob,
                              const Maybe &g_entropy, const Maybe &out, int64_t stream) {
     const int64_t ld = logits_of(x), rows = x.size(0);
+    no_grad(x, lse, entropy, g_lse, g_logprob, g_entropy, out);
     c10::DeviceGuard guard(x.device());
     const Tensor dx = out ? *out : empty({rows, x.size(1)}, x.scalar_type(), x);
     need(dx.scalar_type() == x.scalar_type() && dx.sizes() == x.sizes(), "out must be like logits");

@@ -11,9 +11,11 @@ Every call takes tensors of one GPU, enqueues on ``stream`` (default: the
 current stream of that GPU) and returns without waiting.  Outputs are
 allocated unless given, as that stream's tensors (as under
 ``torch.cuda.stream``): work on another stream that reads them has to wait for
-it and call ``record_stream``.  Inputs have to outlive their use there.  Wrong shapes, types or
-devices raise ValueError before anything is enqueued; the library's own
-refusals raise :class:`ctc.CtcError`.
+it and call ``record_stream``.  Inputs have to outlive their use there.  Nothing
+is recorded for autograd: the backward passes are calls of their own, and
+tensors that require grad are refused unless under ``torch.no_grad()``.  Wrong
+shapes, types or devices raise ValueError before anything is enqueued; the
+library's own refusals raise :class:`ctc.CtcError`.
 """
 
 from __future__ import annotations

@@ -349,3 +349,60 @@ def test_group_norm_of_channels_whose_means_cancel(ops, hw, c):
         assert bool(((mean - 0.25).abs() <= 2.0 ** -24).all()), mean
         want = 1 / math.sqrt((2.0 ** 41 + 1) / 4 - 1 / 16 + 1e-5)
         assert bool(((rstd.double() / want - 1).abs() <= 2.0 ** -21).all())
+
+
+# ------------------------------------------------------ torch's own accounts
+
+def _calls(ops):
+    """(call, tensors it takes by name, names of its outputs) of each entry
+    point; outputs are given."""
+    e = torch.empty
+    x = torch.randn((2, 4, 8), device="cuda")
+    m = torch.randn((4, 32), device="cuda")
+    q, s = ops.fp8_quantize(m)
+    t = torch.tensor([1, 2, 3, 4], device="cuda", dtype=torch.int32)
+    _, mean, rstd = ops.group_norm(x, 2)
+    r = ops.token_scores(m, t, 2)
+    g = torch.ones(4, device="cuda")
+    f = dict(device="cuda")
+    return [
+        (lambda x, gamma, beta, residual, y, mean, rstd: ops.group_norm(
+            x, 2, gamma, beta, residual, out=(y, mean, rstd)),
+         dict(x=x, gamma=e(8, **f), beta=e(8, **f), residual=x.clone(), y=x.clone(),
+              mean=mean.clone(), rstd=rstd.clone()), ("y", "mean", "rstd")),
+        (lambda dy, x, mean, rstd, gamma, beta, residual, dx, dr, dg, db:
+         ops.group_norm_backward(dy, x, mean, rstd, 2, gamma, beta, residual,
+                                 out=(dx, dr, dg, db)),
+         dict(dy=x.clone(), x=x, mean=mean, rstd=rstd, gamma=e(8, **f), beta=e(8, **f),
+              residual=x.clone(), dx=x.clone(), dr=x.clone(), dg=e(8, **f),
+              db=e(8, **f)), ("dx", "dr", "dg", "db")),
+        (lambda x, q, s: ops.fp8_quantize(x, out=(q, s)),
+         dict(x=m, q=q.clone(), s=s.clone()), ("q", "s")),
+        (lambda sa, sb, bias, out: ops.fp8_matmul(q, sa, q, sb, bias, out=out),
+         dict(sa=s, sb=s.clone(), bias=g, out=e((4, 4), **f)), ("out",)),
+        (lambda x, lse, entropy, logprob, rank, ids, tops: ops.token_scores(
+            x, t, 2, out=ops.TokenScores(lse, entropy, logprob, rank, ids, tops)),
+         dict(x=m, lse=r.lse.clone(), entropy=r.entropy.clone(), logprob=r.logprob.clone(),
+              rank=r.rank.clone(), ids=r.top_ids.clone(), tops=r.top_logprobs.clone()),
+         ("lse", "entropy", "logprob", "rank", "ids", "tops")),
+        (lambda x, lse, entropy, g1, g2, g3, out: ops.token_scores_backward(
+            x, t, lse, entropy, g1, g2, g3, out=out),
+         dict(x=m, lse=r.lse, entropy=r.entropy, g1=g, g2=g.clone(), g3=g.clone(),
+              out=m.clone()), ("out",)),
+    ]
+
+
+def test_tensors_that_require_grad_are_refused(ops):
+    """Results carry no graph, so a gradient would be lost silently."""
+    for i, (call, args, _) in enumerate(_calls(ops)):
+        call(**args)
+        for name, v in args.items():
+            if v.dtype != torch.float32:
+                continue
+            with_grad = dict(args, **{name: v.clone().requires_grad_()})
+            with pytest.raises(ValueError, match="grad"):
+                call(**with_grad)
+                raise AssertionError((i, name))
+            with torch.no_grad():
+                call(**with_grad)
+            call(**dict(with_grad, **{name: with_grad[name].detach()}))
