@@ -113,6 +113,10 @@ template <typename... Ts> void no_grad(const Ts &...t) {
          "a tensor requires grad, and the operators record nothing for autograd: detach it or "
          "call under torch.no_grad()");
 }
+// Given outputs have changed: what autograd saved of them is stale.
+void wrote(const Maybe &t) {
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 // Device scratch of a call on the current stream.
 void *scratch(size_t bytes, Tensor &keep, const Tensor &ref) {
     if (!bytes) return nullptr;
@@ -165,6 +169,7 @@ std::tuple<Tensor, Tensor, Tensor> group_norm(const Tensor &x, int64_t groups, c
     done(ctc_group_norm_forward(code(x), m.n, m.hw, m.c, (int32_t)groups, carry, x.data_ptr(),
                                 (float *)g, (float *)b, r, (float)eps, act, yp, (float *)mp,
                                 (float *)rp, scratch(bytes, keep, x), bytes, (void *)stream));
+    for (const Maybe *t : {&y, &mean, &rstd}) wrote(*t);
     return {*y, *mean, *rstd};
 }
 
@@ -200,6 +205,7 @@ group_norm_backward(const Tensor &dy, const Tensor &x, const Tensor &mean, const
                                  x.data_ptr(), (float *)mp, (float *)rp, (float *)g, (float *)b, r,
                                  act, dxp, drp, (float *)dg, (float *)db,
                                  scratch(bytes, keep, x), bytes, (void *)stream));
+    for (const Maybe *t : {&dx, &dr, &dgamma, &dbeta}) wrote(*t);
     return {dx, dr, dgamma, dbeta};
 }
 
@@ -231,6 +237,8 @@ std::tuple<Tensor, Tensor> fp8_quantize(const Tensor &x, bool e5m2, int64_t bloc
     void *sp = like(scales, "scales", at::kFloat, shape, x);
     done(ctc_fp8_quantize(code(x), rows, cols, x.data_ptr(), ldx, code(*q), (int32_t)block,
                           transpose, q->data_ptr(), ldq, (float *)sp, shape[1], (void *)stream));
+    wrote(q);
+    wrote(scales);
     return {*q, *scales};
 }
 
@@ -273,6 +281,7 @@ Tensor fp8_matmul(const Tensor &a, const Tensor &a_scales, const Tensor &b,
                         a_scales.data_ptr<float>(), a_scales.size(1), ab, b.data_ptr(), ldb,
                         b_scales.data_ptr<float>(), b_scales.size(1), bb, (float *)bp, act,
                         y.data_ptr(), ldy, scratch(bytes, keep, a), bytes, (void *)stream));
+    wrote(out);
     return y;
 }
 
@@ -323,6 +332,7 @@ Scores token_scores(const Tensor &x, const Maybe &targets, int64_t top_k, bool m
                                   (int32_t)top_k, (float *)lp, (float *)pp, (float *)ep,
                                   (int32_t *)rp, (int32_t *)ip, (float *)vp,
                                   scratch(bytes, keep, x), bytes, (void *)stream));
+    for (const Maybe *t : {&lse, &entropy, &logprob, &rank, &ids, &tops}) wrote(*t);
     return out;
 }
 
@@ -344,6 +354,7 @@ Tensor token_scores_backward(const Tensor &x, const Maybe &targets, const Tensor
     done(ctc_token_scores_backward(code(x), rows, (int32_t)x.size(1), x.data_ptr(), ld,
                                    (int32_t *)tp, (float *)lp, (float *)ep, (float *)gl,
                                    (float *)gp, (float *)ge, dx.data_ptr(), ldd, (void *)stream));
+    wrote(out);
     return dx;
 }
 

@@ -406,3 +406,25 @@ def test_tensors_that_require_grad_are_refused(ops):
             with torch.no_grad():
                 call(**with_grad)
             call(**dict(with_grad, **{name: with_grad[name].detach()}))
+
+
+def test_given_outputs_count_as_changed(ops):
+    """torch's version of a tensor rises when it is written, so a backward
+    pass that saved its values refuses them; other tensors' do not."""
+    for i, (call, args, outs) in enumerate(_calls(ops)):
+        before = {name: v._version for name, v in args.items()}
+        call(**args)
+        for name, v in args.items():
+            assert (v._version > before[name]) == (name in outs), (i, name)
+    # in place, where a saved value is lost
+    w = torch.ones((2, 4, 8), device="cuda", requires_grad=True)
+    z = torch.randn((2, 4, 8), device="cuda")
+    loss = (w * z).sum()
+    ops.group_norm(z, 2, out=(z, torch.empty((2, 2), device="cuda"),
+                              torch.empty((2, 2), device="cuda")))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():
+        m = torch.randn((4, 32), device="cuda")
+        r = ops.token_scores(m)
+        ops.token_scores(m, out=r)
