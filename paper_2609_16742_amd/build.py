@@ -1,5 +1,6 @@
 """Builds libctc.so (the C ABI of include/ctc.h) for gfx950 with hipcc, and
-_binding.so (the operators' Python binding, host code) with g++.
+_binding.so (the operators' Python binding, host code) with g++ and torch's
+headers.  Networks need libctc.so alone (``--library``).
 
 Every HIP source is compiled with packed-FP32 instruction selection turned
 off; the host runtime and the kernels link into one shared library that
@@ -26,7 +27,8 @@ def hipcc():
     return p if os.path.exists(p) else "hipcc"
 
 
-def build(verbose=False):
+def build(verbose=False, binding=True):
+    """libctc.so and, unless not wanted, _binding.so; returns libctc.so."""
     tmp = "%s.tmp%d" % (SO, os.getpid())
     cmd = [hipcc(), "--offload-arch=" + ARCH, "-mcode-object-version=5",
            "-O3", "-std=c++17", "-fPIC",
@@ -35,7 +37,8 @@ def build(verbose=False):
            "-I", os.path.join(ROOT, "include"), "-o", tmp] + SOURCES
     _run(cmd, verbose)
     os.replace(tmp, SO)
-    build_binding(verbose)
+    if binding:
+        build_binding(verbose)
     return SO
 
 
@@ -71,5 +74,5 @@ def _run(cmd, verbose):
 
 
 if __name__ == "__main__":
-    build(verbose="-v" in sys.argv)
+    build(verbose="-v" in sys.argv, binding="--library" not in sys.argv)
     print(SO)
