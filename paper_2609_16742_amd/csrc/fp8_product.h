@@ -742,7 +742,6 @@ static ProductPlan product_plan(const ProductArgs &a) {
     r.kind = tiles * s <= 256 && (wide || s == 1) ? RING : TILE;
     return done(s);
 }
-int product_splits(const ProductArgs &a) { return product_plan(a).splits; }
 size_t product_workspace(const ProductArgs &a) {
     const ProductPlan r = product_plan(a);
     return r.splits > 1 ? (size_t)r.splits * a.m * a.n * 4 : 0;

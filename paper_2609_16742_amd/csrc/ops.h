@@ -56,8 +56,7 @@ struct ProductArgs {
     void *y;
     float *ws;                   // partial sums [splits][m][n]
 };
-// Ranges a product's k is split into over a.ws (1: none), and their bytes.
-int product_splits(const ProductArgs &a);
+// Bytes of a.ws a product needs (partial sums of a split k).
 size_t product_workspace(const ProductArgs &a);
 hipError_t launch_product(const ProductArgs &a, hipStream_t st);
 
