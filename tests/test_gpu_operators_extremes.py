@@ -93,6 +93,42 @@ def test_product_spoiled_and_clean(ops, m, n, k, dtype, bb):
         assert torch.equal(product(a, sa, b, sb), first), where
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 200, 700), (60, 200, 4096), (400, 700, 1000),
+                                   (3601, 3540, 256)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_product_of_blocks_with_outliers(ops, m, n, k, dtype):
+    """Activations with a few channels hundreds of deviations out.  fp32
+    results have fp32 sums; for 16-bit ones the matrix unit drops less than
+    7 * 2^-13 of the largest product of every eight in a row."""
+    g = _gen(m + k)
+    kb = -(-k // 128)
+    for far in (30.0, 300.0, 3000.0):
+        x = _randn(g, m, k)
+        x[:, 5::131] = far * (1 + 0.1 * _randn(g, m, len(range(5, k, 131))))
+        w = _randn(g, n, k) / math.sqrt(k)
+        qa, sa = ops.fp8_quantize(x)
+        qb, sb = ops.fp8_quantize(w, block_rows=128)
+        y = ops.fp8_matmul(qa, sa, qb, sb, dtype=DT[dtype]).double()
+        want = size = drop = 0
+        for i in range(kb):
+            ks = slice(i * 128, min(k, i * 128 + 128))
+            a, b = qa[:, ks].double(), qb[:, ks].double()
+            s = sa[i].double()[:, None] * sb[i].double().repeat_interleave(128)[:n]
+            want = want + (a @ b.t().contiguous()) * s
+            size = size + (a.abs() @ b.abs().t().contiguous()) * s
+            for j in range(0, a.shape[1], 8):
+                # (the largest product is no larger than the largest of each)
+                e = slice(j, j + 8)
+                drop = drop + a[:, e].abs().amax(1)[:, None] * b[:, e].abs().amax(1) * s
+        bound = (128 + 2 * kb + 16) * 2.0 ** -23 * size
+        if dtype != "f32":
+            bound = bound + 7 * 2.0 ** -13 * drop
+        half = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+        off = (y - want).abs()
+        bound = bound + half * want.abs() + 2.0 ** -24
+        assert bool((off <= bound).all()), (far, float((off / bound).max()))
+
+
 # ------------------------------------------------------------------ scores
 
 def _check_far(ops, x, t, k, what):
