@@ -49,7 +49,8 @@ class Head:
         :meth:`gradients` needs of the pass) for a map x [n, ..., c]."""
         y, mean, rstd = ops.group_norm(x, self.groups, self.gamma, self.beta,
                                        act="relu", carry=True)
-        pooled = y.flatten(1, -2).mean(1, dtype=torch.float32)
+        pooled = y.view(y.shape[0], -1, y.shape[-1]).mean(
+            1, dtype=torch.float32)
         out = torch.empty((x.shape[0], self.classes + 1), device=x.device)
         out[:, -1] = pooled[:, -1]
         pooled = pooled[:, :-1]          # rows keep their stride

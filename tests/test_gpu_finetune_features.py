@@ -78,3 +78,22 @@ def test_head_trains_like_its_64_bit_form():
             start = finetune.Head(c, classes, groups=groups).weight.double()
         moved = (q - start).detach()
         assert float((own.double() - start - moved).norm()) <= 0.2 * float(moved.norm())
+
+
+@pytest.mark.parametrize("dims", [(), (1,), (6,), (2, 3)])
+def test_head_takes_maps_of_any_dimensions(dims):
+    """[n, c] rows of features among them: the same numbers as [n, 1, .., c]."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_16742_amd import finetune
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x = torch.randn((5,) + dims + (32,), device="cuda", generator=g)
+    t = torch.arange(5, device="cuda", dtype=torch.int32)
+    whole = x.view(5, 1, -1, 32)
+    heads = [finetune.Head(32, 7, groups=4) for _ in range(2)]
+    loss = [h.step(v, t, 0.5) for h, v in zip(heads, (x, whole))]
+    assert torch.equal(*loss)
+    for name in ("gamma", "beta", "weight", "bias"):
+        assert torch.equal(getattr(heads[0], name), getattr(heads[1], name)), name
+    assert torch.equal(heads[0].answers(x).top_ids, heads[1].answers(whole).top_ids)
