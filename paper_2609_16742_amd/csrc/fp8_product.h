@@ -263,7 +263,9 @@ __global__ __launch_bounds__(MT < 4 ? 512 : 256) void product_rows(ProductArgs p
 // the next step's while this one's MFMAs run.  Chunk g of row r is kept in
 // slot g ^ (r & 7), which spreads the fragment reads over the banks.
 // What bounds it: the matrix unit where the tiles fill the card (8192 x 4096 x
-// 8192 to 16 bits in 231 us, 2.4 PFLOP/s; to fp32, by 128 x 128 tiles, in 479).
+// 8192 to 16 bits in 234 us, 2.34 PFLOP/s, up to 260 us among launches of the
+// same; to fp32, by 128 x 128 tiles, in 453; with a scale for each filter to
+// fp32 in 555, to 16 bits in 452).
 // ---------------------------------------------------------------------------
 template <int BM, int BN, int WM, int WN, int FA, int FB, bool SB1, bool WIDE>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product_tile(ProductArgs p, int mt, int nt,
@@ -711,6 +713,11 @@ static ProductPlan product_plan(const ProductArgs &a) {
         return done(s < most ? s : most);
     }
     const bool wide = a.ytype == F32;
+    // 256 x 256 tiles, one a CU, from 192 on (bf16, k = 4096: 3584 x 3584, 196
+    // tiles, 58 us, in 128 x 128 tiles 75; 4096 x 4096 66 and 81; 8192 x 4096
+    // 133 and 163; below, 2816 x 2816, 121 tiles, 54 and 43).  Near the limit
+    // and just past a whole round the others win or lose by more than the rule
+    // sees: 3328 x 3328, 169 tiles, 56 and 66; 4352 x 4096, 272, 112 and 100.
     const int64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
     if (!wide && a.b_block > 1 && big >= 192) {
         r.kind = BIG_TILE;

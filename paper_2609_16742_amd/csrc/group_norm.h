@@ -20,9 +20,9 @@
 // channels fp64.
 //
 // What bounds it: the bytes of the maps.  Maps held by a workgroup are read
-// once (norm_slab: 64 x 56 x 56 x 64 fp16 with a residual in 22.6 us, 3.4
+// once (norm_slab: 64 x 56 x 56 x 64 fp16 with a residual in 22.4 us, 3.4
 // TB/s), others twice, by 2048 workgroups each pass (gradients of 32 x 112 x 112
-// x 128 bf16 in 137 us: 48 for the sums at 4.3 TB/s, 7 for the joins, 65 for
+// x 128 bf16 in 138 us: 48 for the sums at 4.3 TB/s, 6 for the joins, 65 for
 // the rest at 4.7).
 #pragma once
 #include "ops_device.h"
@@ -764,11 +764,17 @@ static SlabPlan slab_plan(const NormArgs &a, bool backward) {
         };
         const int nt = v == full && fits(256, 4) ? 256 : fits(1024, backward ? 4 : 8) ? 1024 : 0;
         if (!nt) break;
-        // pieces of 16 bytes only where latency is all
+        // pieces of 16 bytes only where latency is all (gradients of 8 x 3136
+        // x 64 fp16 in 8 groups 18 us, as chunks 22; of 64 x 3136 x 64 43.5 us,
+        // as chunks 36)
         if (w * type_bytes(a.type) < 32 && a.c * type_bytes(a.type) >= 32 &&
             (double)a.n * a.hw * a.c * type_bytes(a.type) > (4 << 20))
             continue;
-        // wider slabs read longer pieces of a row, down to one workgroup a CU
+        // wider slabs read longer pieces of a row, down to one workgroup a CU,
+        // and up to the 128 bytes of a line (64 x 49 x 512 fp16 9.0 us, gradients
+        // 11.6; up to 64 bytes 9.6 and 16.5, to 256 10.2 and 12.7.  Where the
+        // slab then needs 1024 threads instead of 256 less is better: 64 x 196
+        // x 256 fp16 13.2 us, up to 64 bytes 9.5)
         if (p.ok && (w * type_bytes(a.type) > 128 || a.n * (k / m) < 256)) break;
         p.ok = true;
         p.v = v;

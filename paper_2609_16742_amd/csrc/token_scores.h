@@ -23,7 +23,7 @@
 // they are found in does not matter.
 //
 // What bounds it: the bytes of the logits (2048 x 131072 bf16 with 20
-// alternatives in 123 us, 4.35 TB/s), and the vector instructions beside them
+// alternatives in 122 us, 4.4 TB/s), and the vector instructions beside them
 // (about ten a value, 72 us there).  A workgroup takes a row, or, of fewer
 // than 512 long rows, a share of 4096 values or more of one (one row of 131072
 // in 15 us instead of 55); rows of up to 4096 a wave.
@@ -327,7 +327,9 @@ template <typename T, int NT> struct ScorePart {
             return n < k ? n : k;
         }
         // More values than places at or above T0 (many equal ones): the best
-        // of what is left, one by one.
+        // of what is left, one by one, the row read again for each (20
+        // alternatives of 2048 x 131072 equal bf16 logits in 2242 us, of normal
+        // ones in 129; 128 x 1000 36 and 9, one row of 131072 48 and 15).
         uint64_t last = ~0ull;
         for (int r = 0; r < k; r++) {
             uint64_t b = 0;
@@ -509,6 +511,12 @@ __global__ __launch_bounds__(256) void token_scores_join(ScoreArgs a, ScorePlan 
     }
 }
 
+// Threads of a row, by its length: many rows fill the card with a wave each
+// (16384 x 4000 bf16 without alternatives 36 us, 256 threads a row 57; 4096 x
+// 2000 10 and 13), few rows wait for the longest chain (64 x 16000 7.5 us, a
+// wave a row 15.5, 512 threads 8.3).  The rule does not look at the rows: 64 x
+// 4000 takes 7.0 us by a wave, 5.1 by 256 threads, 8192 x 8000 45 by 256, 35 by
+// a wave, 4096 x 20000 48 by 512, 41 by 256.
 static int score_threads(const ScoreArgs &a) {
     return a.vocab <= 4096 ? 64 : a.vocab <= 16384 ? 256 : 512;
 }
@@ -548,7 +556,7 @@ hipError_t launch_scores(const ScoreArgs &a, hipStream_t st) {
 // Gradient of the scores:
 //   dx_i = p_i (g_lse - g_lp - g_H (log p_i + H)) + [i = target] g_lp
 // one read and one write of the row; dx may be x.  Bound by the bytes: 4096 x
-// 32001 fp16 in 102 us, 5.1 TB/s.
+// 32001 fp16 in 103 us, 5.1 TB/s.
 //
 // exp(x - lse) is off by what lse was rounded by, 2^-17 up to |lse| = 256 (a
 // row of fp32's lowest value has lse = max for every length).  Past it one
