@@ -669,7 +669,7 @@ ctc_status ctc_fp8_quantize(ctc_dtype dtype, int64_t rows, int64_t cols,
  * [out][in] (b_block 128); the gradient of its input the output gradients and
  * the filters' transpose; the gradient of the filters both transposes
  * (blocks of 1, k the rows of the batch).  k = 0 gives act(bias).
- * m, k <= 2^30, n < 2^23 - 1, m * (n + 4) < 2^33 - 256. */
+ * m, k <= 2^30, n < 2^23 - 1, m * (n + 4) < 2^33 - 1024. */
 ctc_status ctc_fp8_matmul(ctc_dtype atype, ctc_dtype btype, ctc_dtype ytype,
                           int64_t m, int64_t n, int64_t k, const void *a,
                           int64_t lda, const float *a_scales, int64_t ld_as,

@@ -148,3 +148,23 @@ def test_group_norm_takes_many_images():
         for f, base in ((ctc.ctc_group_norm_forward, NORM),
                         (ctc.ctc_group_norm_backward, NORM_BACK)):
             _call(f, base, UNSUPPORTED, n=n, c=c, groups=4)
+
+
+def test_the_limits_that_the_header_names():
+    """Sizes at the limit are taken, one more is refused."""
+    mm = ctc.ctc_fp8_matmul_workspace_bytes
+    sc = ctc.ctc_token_scores_workspace_bytes
+    for f, at, past in [
+            (mm, (F16, 2 ** 21, 4091, 128, 128), (F16, 2 ** 21, 4092, 128, 128)),
+            (mm, (F16, 1, 2 ** 23 - 2, 128, 128), (F16, 1, 2 ** 23 - 1, 128, 128)),
+            (mm, (F16, 2 ** 30, 1, 128, 128), (F16, 2 ** 30 + 1, 1, 128, 128)),
+            (sc, (2 ** 22 - 1, 4096, 0), (2 ** 22, 4096, 0)),
+            (sc, (1, 2 ** 30, 1), (1, 2 ** 30 + 1, 1))]:
+        f(*at)
+        with pytest.raises(ctc.CtcError) as e:
+            f(*past)
+        assert e.value.status == UNSUPPORTED, past
+    base = dict(QUANT, rows=16 * (2 ** 22 - 1), cols=128, ldx=128, ldq=128, lds=2 ** 30)
+    # (2^22 rows / 16 by 2: past it; one row less gets to the NULL matrix)
+    _call(ctc.ctc_fp8_quantize, base, UNSUPPORTED)
+    _call(ctc.ctc_fp8_quantize, base, ARG, rows=16 * (2 ** 22 - 1) - 1, q=None)
