@@ -732,6 +732,158 @@ ctc_status ctc_token_scores_backward(ctc_dtype dtype, int64_t rows,
 ctc_status ctc_token_scores_workspace_bytes(int64_t rows, int32_t vocab,
                                             int32_t top_k, size_t *bytes);
 
+/* ---- operators of a head over a map's pixels ---------------------------- */
+
+/* Attention over the pixels of a feature map (or any tokens), what its queries
+ * and keys go through before it, and the clipping of a training step's
+ * gradients.  Rules as above: fp32 sums, caller-owned workspaces, a size of 0
+ * is a valid call. */
+
+/* Tensor [batch][tokens][heads][head size]: address and the strides of the
+ * first three in elements; a head's values are contiguous.  (The stride of a
+ * dimension of size 1 is not read.)  Outputs' elements must not overlap. */
+typedef struct {
+    void *data;
+    int64_t strides[3];
+} ctc_heads;
+
+typedef struct {
+    int32_t dtype;               /* CTC_F16 or CTC_BF16 */
+    int32_t batch, queries, keys;
+    int32_t q_heads, k_heads;    /* q_heads / k_heads query heads share each */
+    int32_t head;                /* head size: a multiple of 8, 8 .. 128 */
+    int32_t causal;
+    float scale;                 /* > 0 */
+    const int32_t *q_lengths;    /* device, [batch] or NULL (all of them) */
+    const int32_t *k_lengths;
+} ctc_attention;
+
+/* Attention: with s_ij = scale q_i k_j over the keys j that query i sees,
+ *   lse_i = log sum_j exp(s_ij),  o_i = sum_j exp(s_ij - lse_i) v_j.
+ * Sequence n has q_lengths[n] queries and k_lengths[n] keys (clamped to 0 ..
+ * queries, 0 .. keys); what stands behind them is not read.  With causal, query
+ * i sees keys j <= i + k_lengths[n] - q_lengths[n].  A query that sees nothing,
+ * or behind the last, has o = 0 and lse = -infinity.  Query head h reads key
+ * head h / (q_heads / k_heads).
+ *   q, o  [batch][queries][q_heads][head], k, v [batch][keys][k_heads][head]
+ *         in dtype: 16-byte aligned, strides multiples of 8
+ *   lse   [batch][q_heads][queries] fp32
+ * Probabilities are rounded to dtype for their product with v; a NaN or an
+ * infinity in a key or a value that a query does not see does not reach it if
+ * it stands behind the sequence's length.
+ * The same inputs give the same bits every time.  64 token strides and the
+ * strides of the query heads that share a key head: below 2^29 elements;
+ * queries * (q_heads / k_heads), keys <= 2^30; workgroups (128 rows each, or
+ * 64 pairs of a batch entry and key head) below 2^23. */
+ctc_status ctc_attention_forward(const ctc_attention *a, const ctc_heads *q,
+                                 const ctc_heads *k, const ctc_heads *v,
+                                 const ctc_heads *o, float *lse,
+                                 void *workspace, size_t ws_bytes,
+                                 void *stream);
+
+/* Its gradients, given o's (dout, laid out like o) and what the forward pass
+ * wrote.  Probabilities are computed again from lse.  With p_ij = exp(s_ij -
+ * lse_i) and ds_ij = p_ij (dout_i v_j - dout_i o_i),
+ *   dv_j = sum_i p_ij dout_i,  dk_j = scale sum_i ds_ij q_i,
+ *   dq_i = scale sum_j ds_ij k_j
+ * (p and ds rounded to dtype, in fp16 with an exponent that fits the sequence's
+ * dout and v; sums over the query heads that share a key head).  Gradients of
+ * what takes no part are zeros.  The same inputs give the same bits every
+ * time. */
+ctc_status ctc_attention_backward(const ctc_attention *a,
+                                  const ctc_heads *dout, const ctc_heads *q,
+                                  const ctc_heads *k, const ctc_heads *v,
+                                  const ctc_heads *o, const float *lse,
+                                  const ctc_heads *dq, const ctc_heads *dk,
+                                  const ctc_heads *dv, void *workspace,
+                                  size_t ws_bytes, void *stream);
+
+/* Workspace of the two (backward: 0 or 1).  Host, synchronous. */
+ctc_status ctc_attention_workspace_bytes(const ctc_attention *a,
+                                         int32_t backward, size_t *bytes);
+
+typedef struct {
+    int32_t dtype;               /* of q, k and their gradients */
+    int32_t ytype;               /* of the results: dtype, or, with CTC_F32,
+                                    any */
+    int32_t batch, tokens, q_heads, k_heads;     /* k_heads 0: queries alone */
+    int32_t head;                /* head size: even, up to 512 */
+    int32_t norm;                /* 0: rotation (and weights) alone */
+    float eps;
+    const float *q_weight, *k_weight;    /* device, [head] or NULL (1) */
+    int32_t interleaved;         /* pairs (2 p, 2 p + 1), else halves */
+    int32_t axes;                /* position axes, 0 (no rotation) .. 4 */
+    int32_t pairs[4];            /* pairs that each turns, in order */
+    int32_t per_image;           /* positions: 0 the same for all, 1 its own */
+    const int32_t *positions;    /* device, [batch or 1][tokens][axes] */
+    const float *frequencies;    /* device, [sum of pairs], radians a step */
+} ctc_head_rotary;
+
+/* The RMS norm of each head of q and k and the rotation of its pairs:
+ *   z = x / sqrt(mean(x^2) + eps) * weight,
+ *   (y_a, y_b) = (z_a cos - z_b sin, z_a sin + z_b cos)
+ * with the angle position * frequency of the pair, on the axis it belongs to
+ * (rows and columns of a map; frames).  Of R = sum of pairs, pair p is (p, p +
+ * R), or (2 p, 2 p + 1) if interleaved; values behind 2 R are not turned.  An
+ * angle is good to 2^-21 whatever the position.
+ *   q, k, yq, yk  [batch][tokens][heads][head]; yq may be q, yk may be k (in
+ *                 place, with the same strides)
+ * Heads of more than 128 values need R and head / 2 - R to be multiples of 2,
+ * more than 256 multiples of 4.  batch * tokens < 2^40. */
+ctc_status ctc_head_norm_rotary_forward(const ctc_head_rotary *h,
+                                        const ctc_heads *q, const ctc_heads *k,
+                                        const ctc_heads *yq,
+                                        const ctc_heads *yk, void *stream);
+
+/* Its gradients, with dz the results' gradients turned back and xhat = x /
+ * sqrt(mean(x^2) + eps):
+ *   dweight = sum dz xhat,
+ *   dx = (dz weight - xhat mean(dz weight xhat)) / sqrt(mean(x^2) + eps)
+ *   dyq, dyk  in ytype; dq, dk in dtype, may be dyq, dyk or q, k (in place,
+ *             with the same type and strides)
+ *   dq_weight, dk_weight  [head] fp32, each may be NULL
+ * The same inputs give the same bits every time. */
+ctc_status ctc_head_norm_rotary_backward(const ctc_head_rotary *h,
+                                         const ctc_heads *dyq,
+                                         const ctc_heads *dyk,
+                                         const ctc_heads *q,
+                                         const ctc_heads *k,
+                                         const ctc_heads *dq,
+                                         const ctc_heads *dk, float *dq_weight,
+                                         float *dk_weight, void *workspace,
+                                         size_t ws_bytes, void *stream);
+
+/* Workspace of the backward pass.  Host, synchronous. */
+ctc_status ctc_head_norm_rotary_workspace_bytes(const ctc_head_rotary *h,
+                                                size_t *bytes);
+
+/* A gradient of `size` contiguous values and where it goes. */
+typedef struct {
+    const void *x;
+    void *y;                     /* may be x (in place) */
+    int64_t size;
+    int32_t dtype;               /* CTC_F32, CTC_F16 or CTC_BF16, of both */
+    int32_t pad;
+} ctc_gradient;
+
+/* norm = sqrt(sum of all values' squares), y = x min(1, max_norm / norm).
+ * Sums are fp64, so no fp32 value is too large to be squared; a norm that is
+ * infinite or NaN leaves the values as they are (y = x).  `grads` (host) is
+ * read before the call returns.  Outputs must not overlap each other, nor
+ * another tensor's x.
+ *   max_norm  >= 0 (infinity: y = x)
+ *   norm      device, fp32, or NULL
+ * The same inputs give the same bits every time.  n <= 2^20, at most 2^45
+ * values in a tensor. */
+ctc_status ctc_clip_gradients(int32_t n, const ctc_gradient *grads,
+                              float max_norm, float *norm, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Workspace of ctc_clip_gradients.  Host, synchronous. */
+ctc_status ctc_clip_gradients_workspace_bytes(int32_t n,
+                                              const ctc_gradient *grads,
+                                              size_t *bytes);
+
 void ctc_net_destroy(ctc_net *net);
 const char *ctc_last_error(void);   /* message of this thread's last error */
 int32_t ctc_abi_version(void);

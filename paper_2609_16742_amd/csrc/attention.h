@@ -1,0 +1,898 @@
+// Attention of queries over keys and its backward pass (part of ops.hip).
+//
+//   s_ij = scale q_i k_j,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j
+//
+// over the keys j that query i sees: those before the sequence's length and,
+// with `causal`, j <= i + keys - queries.  The G = hq / hkv query heads that
+// share a key head are rows of one matrix: row r = t G + g is query t of head
+// g, so one query of many heads fills a tile, and the gradients of shared keys
+// are sums over rows.
+#pragma once
+#include "ops_device.h"
+
+namespace ctc {
+namespace ops {
+
+typedef __amdgpu_buffer_rsrc_t AttnBuf;
+typedef __attribute__((address_space(3))) void *AttnLds;
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v *AttnTr;
+
+// The 32 x 32 x 16 products.  Of an operand a lane holds 8 values of k, those
+// of 8 (lane / 32) + 0 .. 7, in row or column lane % 32; of a result column
+// lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4.  What a product leaves
+// in a lane is so what the next one takes there, with k counted as in `KEY`:
+// values 0 .. 3 and 4 .. 7 of a lane are k = 4 (lane / 32) + 0 .. 3 and + 8.
+template <typename T> struct Tile;
+template <> struct Tile<_Float16> {
+    typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 V2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f16v mul(V8 a, V8 b, f16v c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+    // p = 2^SHIFT relative to the maximum, up to 2^LIMIT: its smallest values
+    // keep their bits in fp16
+    static constexpr float SHIFT = 8.f, LIMIT = 15.f;
+};
+template <> struct Tile<__bf16> {
+    typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 V2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f16v mul(V8 a, V8 b, f16v c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    static constexpr float SHIFT = 0.f, LIMIT = 8.f;
+};
+
+// Eight fp32 values in 16 bits (to nearest), as an operand.
+template <typename T> __device__ __forceinline__ typename Tile<T>::V8 pack8(const float *v) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typename Tile<T>::V8 r;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const typename Tile<T>::V2 h =
+            __builtin_convertvector(f2{v[2 * i], v[2 * i + 1]}, typename Tile<T>::V2);
+        r[2 * i] = h[0];
+        r[2 * i + 1] = h[1];
+    }
+    return r;
+}
+
+// Tiles in LDS: rows of PITCH elements in pieces of 16 bytes, piece c of row r
+// in place c ^ swizzle(r).  Eight rows in a row have eight places for a piece
+// (operands read along rows), and each four of them four pairs of places
+// (operands read along columns, 16 columns of 4 rows at a time).
+__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+constexpr uint32_t BEYOND = 0x80000000u;        // behind every buffer: reads as zeros
+__device__ __forceinline__ AttnBuf attn_buffer(const void *p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, 0x7fffffff, 0x00020000);
+}
+
+// t = r / G for r < 2^31 (G's multiplier and shift: see attn_group).
+__device__ __forceinline__ int over_group(const AttnArgs &a, int r) {
+    return a.group == 1 ? r : (int)(__umulhi((uint32_t)r, a.gmul) >> a.gshift);
+}
+
+// Rows r of the queries (or of what is laid out like them) as one lane sees
+// them.
+struct AttnRow { int t, g; };
+__device__ __forceinline__ AttnRow attn_row(const AttnArgs &a, int r) {
+    const int t = over_group(a, r);
+    return AttnRow{t, r - t * a.group};
+}
+// What a lane asks for of a tile of ROWS rows that NW waves load.
+template <int PITCH, int ROWS, int NW> struct Loads {
+    static constexpr int CH = PITCH / 8, RPI = 64 / CH, N = ROWS / (RPI * NW);
+    static constexpr bool ODD = (NW * RPI) % 8 != 0;    // odd loads have another swizzle
+    static_assert(N * RPI * NW == ROWS, "whole loads");
+    int row;                    // of load 0
+    uint32_t piece[2];          // byte of a row
+    __device__ __forceinline__ void init(int lane, int wave, int d) {
+        row = wave * RPI + lane / CH;
+#pragma unroll
+        for (int o = 0; o < 2; o++) {
+            const int c = lane % CH ^ swizzle(row + o * NW * RPI);
+            piece[o] = c * 8 < d ? c * 16 : BEYOND;
+        }
+    }
+    __device__ __forceinline__ uint32_t at(int i) const { return piece[ODD ? i & 1 : 0]; }
+    __device__ __forceinline__ int row_of(int i) const { return row + i * (NW * RPI); }
+    static __device__ __forceinline__ char *to(char *tile, int wave, int i) {
+        return tile + (i * NW + wave) * 1024;
+    }
+    // Rows first .. first + ROWS - 1 of a matrix at `base` (rows `stride` bytes
+    // apart, those from `end` on as zeros).
+    __device__ __forceinline__ void rows(char *tile, int wave, const char *base, int64_t stride,
+                                         int first, int end) const {
+        const AttnBuf buf = attn_buffer(base + first * stride);
+        const uint32_t s = (uint32_t)stride;
+        if (first + ROWS <= end) {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (AttnLds)to(tile, wave, i), 16,
+                                                         row_of(i) * s + at(i), 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    buf, (AttnLds)to(tile, wave, i), 16,
+                    first + row_of(i) < end ? row_of(i) * s + at(i) : BEYOND, 0, 0, 0);
+        }
+    }
+    // Rows of queries (tokens st, heads sh bytes apart); zeros outside lo .. hi - 1.
+    __device__ __forceinline__ void queries(const AttnArgs &a, char *tile, int wave,
+                                            const char *base, int64_t st, int64_t sh, int first,
+                                            int lo, int hi) const {
+        if (a.group == 1 && first >= lo) {
+            rows(tile, wave, base, st, first, hi);
+            return;
+        }
+        const int t0 = over_group(a, first);
+        const AttnBuf buf = attn_buffer(base + t0 * st);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const int r = first + row_of(i);
+            const AttnRow q = attn_row(a, r);
+            const uint32_t o = (uint32_t)(q.t - t0) * (uint32_t)st + (uint32_t)q.g * (uint32_t)sh;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                buf, (AttnLds)to(tile, wave, i), 16, r >= lo && r < hi ? o + at(i) : BEYOND, 0, 0,
+                0);
+        }
+    }
+};
+
+// Operands of a tile in LDS.  `rows` is where row lane % 32, piece lane / 32
+// stands; `cols` where a lane's four values of columns begin.
+template <typename T, int PITCH> struct Operands {
+    typedef typename Tile<T>::V8 V8;
+    uint32_t rows, x, cols, y;
+    __device__ __forceinline__ void init(int lane) {
+        const int h = lane >> 5, r = lane & 31;
+        rows = r * (PITCH * 2);
+        x = (h ^ swizzle(r)) << 4;
+        const int k = 4 * h + ((lane >> 2) & 3);
+        cols = k * (PITCH * 2) + (lane & 1) * 8;
+        y = ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle(k)) << 4;
+    }
+    // rows 32 b .. of k = 16 s ..
+    __device__ __forceinline__ V8 along(const char *tile, int b, int s) const {
+        return *(const V8 *)(tile + b * 32 * PITCH * 2 + rows + (x ^ (s << 5)));
+    }
+    // columns 32 n .. of k = rows 16 b .. (counted as results are)
+    __device__ __forceinline__ V8 across(const char *tile, int b, int n) const {
+        const char *p = tile + b * 16 * PITCH * 2 + cols + (y ^ (n << 6));
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AttnTr)p);
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AttnTr)(p + 8 * PITCH * 2));
+        return __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// The same operand straight from memory: row `p` (null: zeros), k = 16 s ..
+template <typename T> __device__ __forceinline__ typename Tile<T>::V8
+row_operand(const T *p, int lane, int s, int d) {
+    typename Tile<T>::V8 v{};
+    const int e = 16 * s + 8 * (lane >> 5);
+    if (p && e < d) v = *(const typename Tile<T>::V8 *)(p + e);
+    return v;
+}
+
+__device__ __forceinline__ float other_half(float v) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+__device__ __forceinline__ f16v zeros16() {
+    f16v z;
+#pragma unroll
+    for (int i = 0; i < 16; i++) z[i] = 0.f;
+    return z;
+}
+
+// Loads of the wave have landed, and so have those of the others.
+__device__ __forceinline__ void attn_arrive() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Workgroup id as (sequence and key head, part of it).  Workgroup i runs on XCD
+// i % 8, and each XCD has an L2 of its own: where that leaves none idle, what
+// reads the same keys runs on the same XCD.
+struct AttnPlace { int b, h, part; };
+__device__ __forceinline__ AttnPlace attn_place(const AttnArgs &a, int parts) {
+    const int id = blockIdx.x, pairs = a.b * a.hkv;
+    int pair, part;
+    if (pairs % 8 == 0) {
+        pair = (id >> 3) / parts * 8 + (id & 7);
+        part = (id >> 3) % parts;
+    } else {
+        pair = id / parts;
+        part = id % parts;
+    }
+    return AttnPlace{pair / a.hkv, pair % a.hkv, part};
+}
+__device__ __forceinline__ int attn_length(const int32_t *lengths, int b, int most) {
+    if (!lengths) return most;
+    const int n = __builtin_amdgcn_readfirstlane(lengths[b]);
+    return n < 0 ? 0 : n > most ? most : n;
+}
+
+// Rows of a sequence and key head, in tiles of 32: 32 first values, 32 -delta.
+__device__ __forceinline__ int64_t attn_stats(const AttnArgs &a, int pair, int r) {
+    return ((int64_t)pair * a.row_tiles + (r >> 5)) * 64 + (r & 31);
+}
+
+// Keys and values of 64 keys at a time, in one of two stages.
+template <int PITCH, int NW> struct KeyStages {
+    static constexpr int TILE = 64 * PITCH * 2;
+    Loads<PITCH, 64, NW> ld;
+    const char *k, *v;
+    int64_t ks, vs;
+    int wave, end;
+    char *lds;
+    template <typename T>
+    __device__ __forceinline__ void init(const AttnArgs &a, const AttnPlace &at, int lane, int w,
+                                         int keys, char *to) {
+        ld.init(lane, w, a.d);
+        k = (const char *)((const T *)a.k + at.b * a.ks[0] + at.h * a.ks[2]);
+        v = (const char *)((const T *)a.v + at.b * a.vs[0] + at.h * a.vs[2]);
+        ks = a.ks[1] * 2;
+        vs = a.vs[1] * 2;
+        wave = w;
+        end = keys;
+        lds = to;
+    }
+    __device__ __forceinline__ void fetch(int key, int stage) const {
+        char *to = lds + stage * 2 * TILE;
+        ld.rows(to, wave, k, ks, key, end);
+        ld.rows(to + TILE, wave, v, vs, key, end);
+    }
+};
+// Queries and gradients of RT rows, and what attn_rows wrote of them.
+template <int PITCH, int RT> struct RowStages {
+    static constexpr int TILE = RT * PITCH * 2, STAGE = 2 * TILE + RT * 8;
+    Loads<PITCH, RT, 4> ld;
+    const char *q, *g;
+    int wave, lane, lo, hi, pair;
+    char *lds;
+    template <typename T>
+    __device__ __forceinline__ void init(const AttnArgs &a, const AttnPlace &at, int l, int w,
+                                         int from, int to_row, char *to) {
+        ld.init(l, w, a.d);
+        q = (const char *)((const T *)a.q + at.b * a.qs[0] + at.h * a.group * a.qs[2]);
+        g = (const char *)((const T *)a.dout + at.b * a.dos[0] + at.h * a.group * a.dos[2]);
+        wave = w;
+        lane = l;
+        lo = from;
+        hi = to_row;
+        pair = at.b * a.hkv + at.h;
+        lds = to;
+    }
+    __device__ __forceinline__ void fetch(const AttnArgs &a, int r, int stage) const {
+        char *to = lds + stage * STAGE;
+        ld.queries(a, to, wave, q, a.qs[1] * 2, a.qs[2] * 2, r, lo, hi);
+        ld.queries(a, to + TILE, wave, g, a.dos[1] * 2, a.dos[2] * 2, r, lo, hi);
+        if (wave < RT / 32)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                attn_buffer(a.stats + attn_stats(a, pair, r) + wave * 64),
+                (AttnLds)(to + 2 * TILE + wave * 256), 4, lane * 4, 0, 0, 0);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Forward: a workgroup takes NW tiles of 32 rows, a wave each, and goes through
+// the keys (or its range of them) 64 at a time, two stages of keys and values
+// in LDS.  A wave computes S^T = K Q^T, so a lane holds 32 scores of one row
+// and the softmax needs one exchange between two lanes; P^T then stands as the
+// operand of O^T = V^T P^T.  The sums are about a reference that is moved only
+// when a row's maximum has grown past it by LIMIT - SHIFT (in powers of two):
+// o and l are scaled anew in few steps.
+// ---------------------------------------------------------------------------
+template <typename T, int NK, int ND, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
+    typedef typename Tile<T>::V8 V8;
+    constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
+    const int lane = threadIdx.x & 63, h32 = lane >> 5;
+    const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnPlace at = attn_place(a, a.tiles * a.splits);
+    const int split = at.part % a.splits;
+    const int tile = a.causal ? a.tiles - 1 - at.part / a.splits : at.part / a.splits;
+    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
+    const int r0 = tile * (NW * 32), R = qn * a.group;
+    const int first = r0 + wave * 32, r = first + (lane & 31);
+    const AttnRow row = attn_row(a, r);
+    const bool valid = r < R;
+    // keys that the lane's row sees, the wave's first row, the workgroup's last
+    auto sees = [&](int t) {
+        if (!a.causal) return kn;
+        const int n = t + kn - qn + 1;
+        return n < 0 ? 0 : n > kn ? kn : n;
+    };
+    const int lim = valid ? sees(row.t) : 0;
+    const int least = sees(over_group(a, first));
+    const int last_row = r0 + NW * 32 <= R ? r0 + NW * 32 - 1 : R - 1;
+    const int most = r0 < R ? sees(over_group(a, last_row)) : 0;
+    const int wave_last = first + 32 <= R ? first + 31 : R - 1;
+    const int wave_most = first < R ? sees(over_group(a, wave_last)) : 0;
+    int k0 = 0, k1 = most;
+    if (a.splits > 1) {
+        k0 = split * a.per;
+        if (k1 > k0 + a.per) k1 = k0 + a.per;
+    }
+
+    V8 q[NK];
+    const T *qp = valid ? (const T *)a.q + at.b * a.qs[0] + row.t * a.qs[1] +
+                              (at.h * a.group + row.g) * a.qs[2]
+                        : nullptr;
+#pragma unroll
+    for (int s = 0; s < NK; s++) q[s] = row_operand<T>(qp, lane, s, a.d);
+    f16v acc[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++) acc[n] = zeros16();
+    float mc = -INF, l = 0.f;
+    const float c = a.scale * LOG2E;
+
+    KeyStages<PITCH, NW> in;
+    in.template init<T>(a, at, lane, wave, kn, lds);
+    Operands<T, PITCH> op;
+    op.init(lane);
+    if (k0 < k1) in.fetch(k0, 0);
+    int stage = 0;
+    for (int key = k0; key < k1; key += KT, stage ^= 1) {
+        attn_arrive();
+        if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
+        if (key >= wave_most) continue;
+        const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        f16v s[2];
+#pragma unroll
+        for (int b = 0; b < 2; b++) {
+            s[b] = zeros16();
+#pragma unroll
+            for (int i = 0; i < NK; i++) s[b] = Tile<T>::mul(op.along(kt, b, i), q[i], s[b]);
+        }
+        if (key + KT > least) {
+#pragma unroll
+            for (int b = 0; b < 2; b++)
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (key + b * 32 + 8 * (i / 4) + 4 * h32 + i % 4 >= lim) s[b][i] = -INF;
+        }
+        float m = vmax3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+        for (int i = 3; i < 15; i += 2) m = vmax3(m, s[0][i], s[0][i + 1]);
+        m = vmax3(m, s[0][15], s[1][0]);
+#pragma unroll
+        for (int i = 1; i < 15; i += 2) m = vmax3(m, s[1][i], s[1][i + 1]);
+        m = vmax(m, s[1][15]);
+        m = c * vmax(m, other_half(m));
+        if (__any(m - mc > Tile<T>::LIMIT)) {
+            if (m - mc > Tile<T>::LIMIT) {
+                const float to = m - Tile<T>::SHIFT, f = exp2_hw(mc - to);
+                mc = to;
+                l *= f;
+#pragma unroll
+                for (int n = 0; n < ND; n++) acc[n] *= f;
+            }
+        }
+        const float ref = mc == -INF ? 0.f : -mc;
+        float p[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) p[i] = exp2_hw(__builtin_fmaf(s[i / 16][i % 16], c, ref));
+#pragma unroll
+        for (int i = 0; i < 32; i++) l += p[i];
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            const V8 pb = pack8<T>(p + 8 * b);
+#pragma unroll
+            for (int n = 0; n < ND; n++) acc[n] = Tile<T>::mul(op.across(vt, b, n), pb, acc[n]);
+        }
+    }
+    l += other_half(l);
+    // (a row that sees nothing: zeros)
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float lse2 = l == 0.f ? -INF : mc + __builtin_amdgcn_logf(l);
+    if (r >= a.tq * a.group) return;
+    if (a.splits > 1) {
+        const int64_t i = (((int64_t)split * a.b + at.b) * a.hkv + at.h) * a.tq * a.group + r;
+        float *o = a.part + i * a.d;
+#pragma unroll
+        for (int n = 0; n < ND; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int e = n * 32 + j * 8 + 4 * h32;
+                if (e < a.d) {
+                    f4 v;
+#pragma unroll
+                    for (int x = 0; x < 4; x++) v[x] = acc[n][4 * j + x] * inv;
+                    __builtin_memcpy(o + e, &v, 16);
+                }
+            }
+        if (!h32) a.part_lse[i] = lse2;
+        return;
+    }
+    const int head = at.h * a.group + row.g;
+    T *o = (T *)a.o + at.b * a.os[0] + row.t * a.os[1] + head * a.os[2];
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int e = n * 32 + j * 8 + 4 * h32;
+            if (e < a.d) {
+                float v[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * inv : 0.f;
+                store<T, 4>(o + e, v);
+            }
+        }
+    if (!h32) a.lse[((int64_t)at.b * a.hq + head) * a.tq + row.t] = valid ? lse2 * LN2 : -INF;
+}
+
+// Joins the ranges of keys of a row: a wave a row.
+template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)a.b * a.hkv * a.tq * a.group;
+    const int64_t i = (int64_t)workgroup() * 4 + (threadIdx.x >> 6);
+    if (i >= rows) return;
+    const int r = (int)(i % (a.tq * a.group));
+    const int pair = (int)(i / (a.tq * a.group));
+    float m = -INF;
+    for (int s = lane; s < a.splits; s += 64) m = vmax(m, a.part_lse[s * rows + i]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) m = vmax(m, __shfl_xor(m, o));
+    const float ref = m == -INF ? 0.f : m;
+    float l = 0.f, v[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; s++) {
+        const float w = exp2_hw(a.part_lse[s * rows + i] - ref);
+        l += w;
+        const float *p = a.part + (s * rows + i) * a.d + lane;
+#pragma unroll
+        for (int e = 0; e < 2; e++)
+            if (lane + 64 * e < a.d) v[e] += w * p[64 * e];
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const AttnRow row = attn_row(a, r);
+    const int b = pair / a.hkv, head = pair % a.hkv * a.group + row.g;
+    T *o = (T *)a.o + b * a.os[0] + row.t * a.os[1] + head * a.os[2];
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+        if (lane + 64 * e < a.d) o[lane + 64 * e] = narrow<T>(v[e] * inv);
+    if (lane == 0)
+        a.lse[((int64_t)b * a.hq + head) * a.tq + row.t] =
+            l == 0.f ? -INF : (ref + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  With delta_i = do_i o_i,
+//   ds_ij = p_ij (do_i v_j - delta_i),
+//   dv_j = sum_i p_ij do_i,  dk_j = scale sum_i ds_ij q_i,
+//   dq_i = scale sum_j ds_ij k_j.
+// `attn_rows` writes what each row needs: -lse as the products' first value
+// (so p = exp2(c s), -infinity where the row is no row) and -delta.  For fp16
+// it also bounds |do| and |v|: p is scaled by the power of two 2^e with which
+// 2 |do| |v| 2^e is below 2^15, so that neither a small ds loses its bits nor
+// a large one its exponent.
+// The probabilities are computed twice, once with a lane's key fixed (dk, dv)
+// and once with its row fixed (dq): seven products instead of five, and no
+// sums between workgroups, whose order would change the result's bits.
+// ---------------------------------------------------------------------------
+template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs a) {
+    __shared__ float most[4];
+    const AttnPlace at = attn_place(a, a.q_chunks + a.v_chunks);
+    const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, pair = at.b * a.hkv + at.h;
+    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
+    const bool queries = at.part < a.q_chunks;
+    float top = 0.f;
+    if (queries) {
+        const int lo = a.causal && qn > kn ? (qn - kn) * a.group : 0, hi = kn ? qn * a.group : 0;
+        const float over = -1.f / a.scale;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int r = at.part * 64 + i * 16 + sub;
+            const bool valid = r >= lo && r < hi;
+            float dot = 0.f, size = 0.f, first = -INF;
+            if (valid) {
+                const AttnRow row = attn_row(a, r);
+                const int head = at.h * a.group + row.g;
+                if (8 * lane < a.d) {
+                    float x[8], y[8];
+                    load<T, 8>((const T *)a.dout + at.b * a.dos[0] + row.t * a.dos[1] +
+                                   head * a.dos[2] + 8 * lane, x);
+                    load<T, 8>((const T *)a.o + at.b * a.os[0] + row.t * a.os[1] +
+                                   head * a.os[2] + 8 * lane, y);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        dot += x[e] * y[e];
+                        size += x[e] * x[e];
+                    }
+                }
+                const float lse = a.lse[((int64_t)at.b * a.hq + head) * a.tq + row.t];
+                if (!(lse == -INF)) first = lse * over;
+            }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) {
+                dot += __shfl_xor(dot, o);
+                size += __shfl_xor(size, o);
+            }
+            if (lane == 0 && r < a.row_tiles * 32) {
+                float *st = a.stats + attn_stats(a, pair, r);
+                st[0] = first;
+                st[32] = first == -INF ? 0.f : -dot;
+            }
+            if (size < INF) top = vmax(top, size);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int j = (at.part - a.q_chunks) * 64 + i * 16 + sub;
+            float size = 0.f;
+            if (j < kn && 8 * lane < a.d) {
+                float x[8];
+                load<T, 8>((const T *)a.v + at.b * a.vs[0] + j * a.vs[1] + at.h * a.vs[2] +
+                               8 * lane, x);
+#pragma unroll
+                for (int e = 0; e < 8; e++) size += x[e] * x[e];
+            }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) size += __shfl_xor(size, o);
+            if (size < INF) top = vmax(top, size);
+        }
+    }
+    if (a.type != F16) return;
+    top = vmax(top, __shfl_xor(top, 16));
+    top = vmax(top, __shfl_xor(top, 32));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.bounds[(int64_t)pair * (a.q_chunks + a.v_chunks) + at.part] =
+            vmax(vmax(most[0], most[1]), vmax(most[2], most[3]));
+}
+
+// e of the sequence and key head (0 for bf16, whose exponents are fp32's).
+template <typename T> __device__ __forceinline__ float attn_exponent(const AttnArgs &a, int pair) {
+    if (sizeof(T) != 2 || a.type != F16) return 0.f;
+    const int lane = threadIdx.x & 63;
+    const float *b = a.bounds + (int64_t)pair * (a.q_chunks + a.v_chunks);
+    float q = 0.f, v = 0.f;
+    for (int i = lane; i < a.q_chunks; i += 64) q = vmax(q, b[i]);
+    for (int i = lane; i < a.v_chunks; i += 64) v = vmax(v, b[a.q_chunks + i]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        q = vmax(q, __shfl_xor(q, o));
+        v = vmax(v, __shfl_xor(v, o));
+    }
+    // log2 of 2 |do| |v|, rounded up
+    const float e = 14.f - __builtin_ceilf(1.f + 0.5f * (__builtin_amdgcn_logf(q) +
+                                                       __builtin_amdgcn_logf(v)));
+    return e > 15.f ? 15.f : e < -20.f ? -20.f : e;
+}
+
+// dk and dv: a workgroup takes 128 keys, 32 a wave, whose K and V stay in
+// registers as operands, and goes through the rows RT at a time.
+template <typename T, int NK, int ND>
+__global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_keys(AttnArgs a) {
+    typedef typename Tile<T>::V8 V8;
+    constexpr int PITCH = NK <= 4 ? 64 : 128, RT = 64, TILE = RT * PITCH * 2;
+    constexpr int STAGE = RowStages<PITCH, RT>::STAGE;
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+    const int lane = threadIdx.x & 63, h32 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnPlace at = attn_place(a, a.key_tiles);
+    const int pair = at.b * a.hkv + at.h;
+    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
+    const int key0 = at.part * 128, key = key0 + wave * 32 + (lane & 31);
+    const int lo = a.causal && qn > kn ? (qn - kn) * a.group : 0, hi = kn ? qn * a.group : 0;
+    // first row that sees the lane's key, the wave's last and the workgroup's
+    // first
+    auto seen = [&](int j) {
+        if (!a.causal) return 0;
+        const int t = j - (kn - qn);
+        return t < 0 ? 0 : t * a.group;
+    };
+    const int from = seen(key), wave_from = seen(key0 + wave * 32 + 31);
+    const int wave_first = seen(key0 + wave * 32);
+    int row = seen(key0) > lo ? seen(key0) : lo;
+    row &= ~(RT - 1);
+
+    const T *kp = key < kn ? (const T *)a.k + at.b * a.ks[0] + key * a.ks[1] + at.h * a.ks[2]
+                           : nullptr;
+    const T *vp = key < kn ? (const T *)a.v + at.b * a.vs[0] + key * a.vs[1] + at.h * a.vs[2]
+                           : nullptr;
+    V8 kf[NK], vf[NK];
+#pragma unroll
+    for (int s = 0; s < NK; s++) kf[s] = row_operand<T>(kp, lane, s, a.d);
+#pragma unroll
+    for (int s = 0; s < NK; s++) vf[s] = row_operand<T>(vp, lane, s, a.d);
+    f16v dk[ND], dv[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++) dk[n] = dv[n] = zeros16();
+    const float c = a.scale * LOG2E, e = attn_exponent<T>(a, pair);
+
+    RowStages<PITCH, RT> in;
+    in.template init<T>(a, at, lane, wave, lo, hi, lds);
+    Operands<T, PITCH> op;
+    op.init(lane);
+    if (row < hi && key0 < kn) in.fetch(a, row, 0);
+    int stage = 0;
+    for (; row < hi && key0 < kn; row += RT, stage ^= 1) {
+        attn_arrive();
+        if (row + RT < hi) in.fetch(a, row + RT, stage ^ 1);
+        const char *qt = lds + stage * STAGE, *ot = qt + TILE;
+#pragma unroll
+        for (int b = 0; b < RT / 32; b++) {
+            if (row + 32 * b + 32 <= wave_first) continue;
+            const float *st = (const float *)(ot + TILE) + b * 64 + 4 * h32;
+            f16v s, dp;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const f4 x = *(const f4 *)(st + 8 * j), y = *(const f4 *)(st + 32 + 8 * j);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    s[4 * j + i] = x[i];
+                    dp[4 * j + i] = y[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(qt, b, i), kf[i], s);
+#pragma unroll
+            for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(ot, b, i), vf[i], dp);
+            float p[16], ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) p[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            if (a.causal && row + 32 * b < wave_from) {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (row + 32 * b + 8 * (i / 4) + 4 * h32 + i % 4 < from) p[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) ds[i] = p[i] * dp[i];
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const V8 pb = pack8<T>(p + 8 * k), sb = pack8<T>(ds + 8 * k);
+#pragma unroll
+                for (int n = 0; n < ND; n++)
+                    dv[n] = Tile<T>::mul(op.across(ot, 2 * b + k, n), pb, dv[n]);
+#pragma unroll
+                for (int n = 0; n < ND; n++)
+                    dk[n] = Tile<T>::mul(op.across(qt, 2 * b + k, n), sb, dk[n]);
+            }
+        }
+    }
+    if (key >= a.tk) return;
+    const bool valid = key < kn;
+    const float back = exp2_hw(-e);
+    T *dkp = (T *)a.dk + at.b * a.dks[0] + key * a.dks[1] + at.h * a.dks[2];
+    T *dvp = (T *)a.dv + at.b * a.dvs[0] + key * a.dvs[1] + at.h * a.dvs[2];
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int i = n * 32 + j * 8 + 4 * h32;
+            if (i < a.d) {
+                float x[4], y[4];
+#pragma unroll
+                for (int z = 0; z < 4; z++) {
+                    x[z] = valid ? dk[n][4 * j + z] * (a.scale * back) : 0.f;
+                    y[z] = valid ? dv[n][4 * j + z] * back : 0.f;
+                }
+                store<T, 4>(dkp + i, x);
+                store<T, 4>(dvp + i, y);
+            }
+        }
+}
+
+// dq: like the forward pass, 32 rows a wave, the keys 64 at a time.
+template <typename T, int NK, int ND>
+__global__ __launch_bounds__(256, 2) void attend_queries(AttnArgs a) {
+    typedef typename Tile<T>::V8 V8;
+    constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
+    const int lane = threadIdx.x & 63, h32 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnPlace at = attn_place(a, a.tiles);
+    const int tile = a.causal ? a.tiles - 1 - at.part : at.part;
+    const int pair = at.b * a.hkv + at.h;
+    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
+    const int r0 = tile * 128, R = qn * a.group;
+    const int first = r0 + wave * 32, r = first + (lane & 31);
+    const AttnRow row = attn_row(a, r);
+    auto sees = [&](int t) {
+        if (!a.causal) return kn;
+        const int n = t + kn - qn + 1;
+        return n < 0 ? 0 : n > kn ? kn : n;
+    };
+    const int lim = r < R ? sees(row.t) : 0;
+    const bool valid = lim > 0;
+    const int least = sees(over_group(a, first));
+    const int last_row = r0 + 128 <= R ? r0 + 127 : R - 1;
+    const int most = r0 < R ? sees(over_group(a, last_row)) : 0;
+    const int wave_last = first + 32 <= R ? first + 31 : R - 1;
+    const int wave_most = first < R ? sees(over_group(a, wave_last)) : 0;
+
+    const int head = at.h * a.group + row.g;
+    const T *qp = valid ? (const T *)a.q + at.b * a.qs[0] + row.t * a.qs[1] + head * a.qs[2]
+                        : nullptr;
+    const T *op_ = valid ? (const T *)a.dout + at.b * a.dos[0] + row.t * a.dos[1] +
+                               head * a.dos[2]
+                         : nullptr;
+    V8 q[NK], g[NK];
+#pragma unroll
+    for (int s = 0; s < NK; s++) q[s] = row_operand<T>(qp, lane, s, a.d);
+#pragma unroll
+    for (int s = 0; s < NK; s++) g[s] = row_operand<T>(op_, lane, s, a.d);
+    f16v acc[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++) acc[n] = zeros16();
+    const float c = a.scale * LOG2E, e = attn_exponent<T>(a, pair);
+    const float *st = a.stats + attn_stats(a, pair, r < a.row_tiles * 32 ? r : 0);
+    const float first_s = valid ? st[0] : -INF, first_dp = valid ? st[32] : 0.f;
+
+    KeyStages<PITCH, 4> in;
+    in.template init<T>(a, at, lane, wave, kn, lds);
+    Operands<T, PITCH> op;
+    op.init(lane);
+    if (most) in.fetch(0, 0);
+    int stage = 0;
+    for (int key = 0; key < most; key += KT, stage ^= 1) {
+        attn_arrive();
+        if (key + KT < most) in.fetch(key + KT, stage ^ 1);
+        if (key >= wave_most) continue;
+        const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+#pragma unroll
+        for (int b = 0; b < 2; b++) {
+            f16v s, dp;
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[i] = first_s, dp[i] = first_dp;
+#pragma unroll
+            for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(kt, b, i), q[i], s);
+#pragma unroll
+            for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(vt, b, i), g[i], dp);
+            float ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) ds[i] = exp2_hw(__builtin_fmaf(s[i], c, e)) * dp[i];
+            if (key + KT > least) {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (key + b * 32 + 8 * (i / 4) + 4 * h32 + i % 4 >= lim) ds[i] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const V8 sb = pack8<T>(ds + 8 * k);
+#pragma unroll
+                for (int n = 0; n < ND; n++)
+                    acc[n] = Tile<T>::mul(op.across(kt, 2 * b + k, n), sb, acc[n]);
+            }
+        }
+    }
+    if (r >= a.tq * a.group) return;
+    const float back = a.scale * exp2_hw(-e);
+    T *o = (T *)a.dq + at.b * a.dqs[0] + row.t * a.dqs[1] + head * a.dqs[2];
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int i = n * 32 + j * 8 + 4 * h32;
+            if (i < a.d) {
+                float v[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * back : 0.f;
+                store<T, 4>(o + i, v);
+            }
+        }
+}
+
+// ------------------------------------------------------------------- host
+
+static int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Multiplier and shift of the group: r / G = (r * gmul >> 32) >> gshift for
+// r < 2^31, with gmul = ceil(2^(31 + l) / G), 2^l >= G.
+static void attn_group(AttnArgs &a) {
+    a.group = a.hq / a.hkv;
+    int l = 0;
+    while ((1 << l) < a.group) l++;
+    a.gmul = l ? (uint32_t)((((uint64_t)1 << (31 + l)) + a.group - 1) / a.group) : 0;
+    a.gshift = l ? l - 1 : 0;
+}
+// Waves of a workgroup and ranges of keys.
+struct AttnPlan { int waves, tiles, splits, per; };
+static AttnPlan attn_plan(const AttnArgs &a) {
+    AttnPlan p;
+    const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    p.waves = rows <= 32 ? 1 : 4;
+    p.tiles = (int)ceil_of(rows, p.waves * 32);
+    const int64_t steps = ceil_of(a.tk, 64), wgs = pairs * p.tiles;
+    // as many ranges as give every CU two workgroups, of four steps at least
+    int64_t s = 512 / (wgs ? wgs : 1);
+    if (s > steps / 4) s = steps / 4;
+    if (s < 1) s = 1;
+    p.per = (int)(ceil_of(steps, s) * 64);
+    p.splits = a.tk ? (int)ceil_of(a.tk, p.per) : 1;
+    return p;
+}
+size_t attention_workspace(const AttnArgs &in, bool backward) {
+    AttnArgs a = in;
+    attn_group(a);
+    const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    if (backward) {
+        const int64_t tiles = ceil_of(rows, 64) * 2, chunks = ceil_of(rows, 64) + ceil_of(a.tk, 64);
+        return (size_t)(pairs * (tiles * 64 + chunks) * 4);
+    }
+    const AttnPlan p = attn_plan(a);
+    if (p.splits == 1) return 0;
+    return (size_t)(p.splits * pairs * rows * (a.d + 1) * 4);
+}
+
+// A head's size in steps of 16 and 32 values, as the kernels are compiled.
+template <template <typename, int, int> class L, typename T>
+static hipError_t by_head(const AttnArgs &a, hipStream_t st) {
+    if (a.d <= 32) return L<T, 2, 1>::go(a, st);
+    if (a.d <= 64) return L<T, 4, 2>::go(a, st);
+    if (a.d <= 96) return L<T, 6, 3>::go(a, st);
+    return L<T, 8, 4>::go(a, st);
+}
+template <template <typename, int, int> class L>
+static hipError_t by_form(const AttnArgs &a, hipStream_t st) {
+    return a.type == F16 ? by_head<L, _Float16>(a, st) : by_head<L, __bf16>(a, st);
+}
+
+template <typename T, int NK, int ND> struct Attend {
+    static hipError_t go(const AttnArgs &a, hipStream_t st) {
+        const dim3 grid((unsigned)((int64_t)a.b * a.hkv * a.tiles * a.splits));
+        if (a.waves == 1) return start(attend<T, NK, ND, 1>, grid, 64, st, a);
+        return start(attend<T, NK, ND, 4>, grid, 256, st, a);
+    }
+};
+template <typename T, int NK, int ND> struct AttendBackward {
+    static hipError_t go(const AttnArgs &a, hipStream_t st) {
+        const int64_t pairs = (int64_t)a.b * a.hkv;
+        hipError_t e = hipSuccess;
+        if (a.key_tiles)
+            e = start(attend_keys<T, NK, ND>, dim3((unsigned)(pairs * a.key_tiles)), 256, st, a);
+        if (e == hipSuccess && a.tiles)
+            e = start(attend_queries<T, NK, ND>, dim3((unsigned)(pairs * a.tiles)), 256, st, a);
+        return e;
+    }
+};
+
+hipError_t launch_attention(const AttnArgs &in, hipStream_t st) {
+    AttnArgs a = in;
+    attn_group(a);
+    const AttnPlan p = attn_plan(a);
+    const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    a.waves = p.waves; a.tiles = p.tiles; a.splits = p.splits; a.per = p.per;
+    a.part = a.ws;
+    a.part_lse = a.ws + p.splits * pairs * rows * a.d;
+    const hipError_t e = by_form<Attend>(a, st);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const dim3 join = grid_of(ceil_of(pairs * rows, 4));
+    return a.type == F16 ? start(attend_join<_Float16>, join, 256, st, a)
+                         : start(attend_join<__bf16>, join, 256, st, a);
+}
+
+hipError_t launch_attention_backward(const AttnArgs &in, hipStream_t st) {
+    AttnArgs a = in;
+    attn_group(a);
+    const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    a.row_tiles = (int)ceil_of(rows, 64) * 2;
+    a.q_chunks = (int)ceil_of(rows, 64);
+    a.v_chunks = a.type == F16 ? (int)ceil_of(a.tk, 64) : 0;
+    a.tiles = (int)ceil_of(rows, 128);
+    a.key_tiles = (int)ceil_of(a.tk, 128);
+    a.splits = 1;
+    a.stats = a.ws;
+    a.bounds = a.ws + pairs * a.row_tiles * 64;
+    hipError_t e = hipSuccess;
+    if (a.q_chunks + a.v_chunks) {
+        const dim3 grid((unsigned)(pairs * (a.q_chunks + a.v_chunks)));
+        e = a.type == F16 ? start(attn_rows<_Float16>, grid, 256, st, a)
+                          : start(attn_rows<__bf16>, grid, 256, st, a);
+    }
+    return e == hipSuccess ? by_form<AttendBackward>(a, st) : e;
+}
+
+}  // namespace ops
+}  // namespace ctc

@@ -8,10 +8,13 @@
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
 
+#include <array>
+#include <cmath>
 #include <optional>
 #include <stdexcept>
 #include <string>
 #include <tuple>
+#include <vector>
 
 #include "../../include/ctc.h"
 
@@ -358,6 +361,291 @@ Tensor token_scores_backward(const Tensor &x, const Maybe &targets, const Tensor
     return dx;
 }
 
+// -------------------------------------------------------------- attention
+
+// A tensor [batch, tokens, heads, head] of that shape and type whose heads are
+// contiguous.
+ctc_heads heads_of(const Tensor &t, const char *name, const std::array<int64_t, 4> &shape,
+                   at::ScalarType type, const Tensor &ref) {
+    if (!t.defined() || t.scalar_type() != type || t.sizes() != at::IntArrayRef(shape) ||
+        t.device() != ref.device())
+        throw std::invalid_argument(std::string(name) + " must be a tensor of type " +
+                                    c10::toString(type) + " and shape " +
+                                    c10::str(at::IntArrayRef(shape)) + " on " +
+                                    ref.device().str());
+    if (shape[3] > 1 && t.stride(3) != 1)
+        throw std::invalid_argument(std::string("the heads of ") + name + " must be contiguous");
+    return ctc_heads{t.data_ptr(), {t.stride(0), t.stride(1), t.stride(2)}};
+}
+const int32_t *lengths_of(const Maybe &t, const char *name, int64_t b, const Tensor &ref) {
+    return (const int32_t *)like(t, name, at::kInt, std::array<int64_t, 1>{b}, ref);
+}
+bool small(int64_t v) { return v < (int64_t)1 << 31; }
+
+struct Attention {
+    ctc_attention a;
+    std::array<int64_t, 4> qs, ks;
+    ctc_heads q, k, v;
+    size_t bytes = 0;
+    Attention(const Tensor &tq, const Tensor &tk, const Tensor &tv, bool causal,
+              const Maybe &q_lengths, const Maybe &k_lengths, const std::optional<double> &scale,
+              bool backward) {
+        on_gpu(tq, "q");
+        need(tq.scalar_type() == at::kHalf || tq.scalar_type() == at::kBFloat16,
+             "q must be float16 or bfloat16");
+        need(tq.dim() == 4 && tk.dim() == 4, "q and k must be [batch, tokens, heads, head size]");
+        for (int i = 0; i < 4; i++) need(small(tq.size(i)) && small(tk.size(i)), "q or k is too large");
+        const int64_t d = tq.size(3);
+        qs = {tq.size(0), tq.size(1), tq.size(2), d};
+        ks = {qs[0], tk.size(1), tk.size(2), d};
+        q = heads_of(tq, "q", qs, tq.scalar_type(), tq);
+        k = heads_of(tk, "k", ks, tq.scalar_type(), tq);
+        v = heads_of(tv, "v", ks, tq.scalar_type(), tq);
+        need(d >= 1, "heads without values");
+        a = ctc_attention{};
+        a.dtype = code(tq);
+        a.batch = (int32_t)qs[0];
+        a.queries = (int32_t)qs[1];
+        a.keys = (int32_t)ks[1];
+        a.q_heads = (int32_t)qs[2];
+        a.k_heads = (int32_t)ks[2];
+        a.head = (int32_t)d;
+        a.causal = causal;
+        a.scale = scale ? (float)*scale : 1.f / std::sqrt((float)d);
+        a.q_lengths = lengths_of(q_lengths, "q_lengths", qs[0], tq);
+        a.k_lengths = lengths_of(k_lengths, "k_lengths", qs[0], tq);
+        done(ctc_attention_workspace_bytes(&a, backward, &bytes));
+    }
+};
+
+std::tuple<Tensor, Tensor> attention(const Tensor &q, const Tensor &k, const Tensor &v,
+                                     bool causal, const Maybe &q_lengths, const Maybe &k_lengths,
+                                     const std::optional<double> &scale, Maybe o, Maybe lse,
+                                     int64_t stream) {
+    const Attention c(q, k, v, causal, q_lengths, k_lengths, scale, false);
+    no_grad(q, k, v, o, lse);
+    c10::DeviceGuard guard(q.device());
+    const std::array<int64_t, 3> rows{c.qs[0], c.qs[2], c.qs[1]};
+    if (!o) {
+        o = empty(c.qs, q.scalar_type(), q);
+        lse = empty(rows, at::kFloat, q);
+    }
+    need(lse.has_value(), "out must hold o and lse");
+    const ctc_heads oh = heads_of(*o, "o", c.qs, q.scalar_type(), q);
+    void *lp = like(lse, "lse", at::kFloat, rows, q);
+    Tensor keep;
+    done(ctc_attention_forward(&c.a, &c.q, &c.k, &c.v, &oh, (float *)lp,
+                               scratch(c.bytes, keep, q), c.bytes, (void *)stream));
+    wrote(o);
+    wrote(lse);
+    return {*o, *lse};
+}
+
+std::tuple<Tensor, Tensor, Tensor>
+attention_backward(const Tensor &dout, const Tensor &q, const Tensor &k, const Tensor &v,
+                   const Tensor &o, const Tensor &lse, bool causal, const Maybe &q_lengths,
+                   const Maybe &k_lengths, const std::optional<double> &scale, Maybe dq, Maybe dk,
+                   Maybe dv, int64_t stream) {
+    const Attention c(q, k, v, causal, q_lengths, k_lengths, scale, true);
+    no_grad(dout, q, k, v, o, lse, dq, dk, dv);
+    c10::DeviceGuard guard(q.device());
+    const at::ScalarType type = q.scalar_type();
+    if (!dq) {
+        dq = empty(c.qs, type, q);
+        dk = empty(c.ks, type, q);
+        dv = empty(c.ks, type, q);
+    }
+    need(dk && dv, "out must hold dq, dk and dv");
+    const ctc_heads doh = heads_of(dout, "do", c.qs, type, q), oh = heads_of(o, "o", c.qs, type, q);
+    const ctc_heads dqh = heads_of(*dq, "dq", c.qs, type, q);
+    const ctc_heads dkh = heads_of(*dk, "dk", c.ks, type, q);
+    const ctc_heads dvh = heads_of(*dv, "dv", c.ks, type, q);
+    void *lp = like(lse, "lse", at::kFloat, std::array<int64_t, 3>{c.qs[0], c.qs[2], c.qs[1]}, q);
+    Tensor keep;
+    done(ctc_attention_backward(&c.a, &doh, &c.q, &c.k, &c.v, &oh, (float *)lp, &dqh, &dkh, &dvh,
+                                scratch(c.bytes, keep, q), c.bytes, (void *)stream));
+    for (const Maybe *t : {&dq, &dk, &dv}) wrote(*t);
+    return {*dq, *dk, *dv};
+}
+
+// ------------------------------------------------------------- head norms
+
+struct HeadNorm {
+    ctc_head_rotary h;
+    std::array<int64_t, 4> qs, ks;
+    ctc_heads q, k;
+    HeadNorm(const Tensor &tq, const Maybe &tk, const Maybe &qw, const Maybe &kw,
+             const Maybe &positions, const Maybe &frequencies, const std::vector<int64_t> &axes,
+             bool interleaved, bool norm, double eps, at::ScalarType out) {
+        on_gpu(tq, "q");
+        need(real_type(tq), "q must be float32, float16 or bfloat16");
+        need(out == tq.scalar_type() || (tq.scalar_type() == at::kFloat &&
+                                         (out == at::kHalf || out == at::kBFloat16)),
+             "dtype must be q's, or a narrower one for float32");
+        need(tq.dim() == 4 && (!tk || tk->dim() == 4),
+             "q and k must be [batch, tokens, heads, head size]");
+        need(axes.size() <= 4, "up to 4 position axes");
+        for (int i = 0; i < 4; i++)
+            need(small(tq.size(i)) && (!tk || small(tk->size(i))), "q or k is too large");
+        qs = {tq.size(0), tq.size(1), tq.size(2), tq.size(3)};
+        ks = {qs[0], qs[1], tk ? tk->size(2) : 0, qs[3]};
+        need(qs[3] >= 2 && qs[2] >= 1, "q without heads or values");
+        h = ctc_head_rotary{};
+        q = heads_of(tq, "q", qs, tq.scalar_type(), tq);
+        k = tk ? heads_of(*tk, "k", ks, tq.scalar_type(), tq) : ctc_heads{};
+        h.dtype = code(tq);
+        h.ytype = out == at::kFloat ? CTC_F32 : out == at::kHalf ? CTC_F16 : CTC_BF16;
+        h.batch = (int32_t)qs[0];
+        h.tokens = (int32_t)qs[1];
+        h.q_heads = (int32_t)qs[2];
+        h.k_heads = (int32_t)ks[2];
+        h.head = (int32_t)qs[3];
+        h.norm = norm;
+        h.eps = (float)eps;
+        h.interleaved = interleaved;
+        const std::array<int64_t, 1> per{qs[3]};
+        h.q_weight = (const float *)like(qw, "q_weight", at::kFloat, per, tq);
+        h.k_weight = (const float *)like(kw, "k_weight", at::kFloat, per, tq);
+        h.axes = (int32_t)axes.size();
+        int64_t turned = 0;
+        for (size_t i = 0; i < axes.size(); i++) {
+            need(axes[i] >= 0 && axes[i] <= qs[3] / 2, "bad pairs of an axis");
+            h.pairs[i] = (int32_t)axes[i];
+            turned += axes[i];
+        }
+        need(axes.empty() || (positions && frequencies), "axes need positions and frequencies");
+        if (axes.empty()) return;
+        const int64_t n = (int64_t)axes.size();
+        h.per_image = positions->dim() == 3;
+        h.positions = (const int32_t *)(
+            h.per_image ? like(positions, "positions", at::kInt,
+                               std::array<int64_t, 3>{qs[0], qs[1], n}, tq)
+                        : like(positions, "positions", at::kInt,
+                               std::array<int64_t, 2>{qs[1], n}, tq));
+        h.frequencies = (const float *)like(frequencies, "frequencies", at::kFloat,
+                                            std::array<int64_t, 1>{turned}, tq);
+    }
+};
+
+std::tuple<Tensor, Maybe> head_norm_rotary(const Tensor &q, const Maybe &k, const Maybe &qw,
+                                           const Maybe &kw, const Maybe &positions,
+                                           const Maybe &frequencies,
+                                           const std::vector<int64_t> &axes, bool interleaved,
+                                           bool norm, double eps,
+                                           const std::optional<at::ScalarType> &dtype, Maybe yq,
+                                           Maybe yk, int64_t stream) {
+    const at::ScalarType type = yq ? yq->scalar_type() : dtype ? *dtype : q.scalar_type();
+    const HeadNorm c(q, k, qw, kw, positions, frequencies, axes, interleaved, norm, eps, type);
+    no_grad(q, k, qw, kw, frequencies, yq, yk);
+    c10::DeviceGuard guard(q.device());
+    if (!yq) {
+        yq = empty(c.qs, type, q);
+        if (k) yk = empty(c.ks, type, q);
+    }
+    need(!k || yk, "out must hold both results");
+    const ctc_heads qh = heads_of(*yq, "out", c.qs, type, q);
+    const ctc_heads kh = k ? heads_of(*yk, "out", c.ks, type, q) : ctc_heads{};
+    done(ctc_head_norm_rotary_forward(&c.h, &c.q, &c.k, &qh, &kh, (void *)stream));
+    wrote(yq);
+    if (k) wrote(yk);
+    return {*yq, k ? yk : Maybe()};
+}
+
+std::tuple<Tensor, Maybe, Maybe, Maybe>
+head_norm_rotary_backward(const Tensor &dyq, const Maybe &dyk, const Tensor &q, const Maybe &k,
+                          const Maybe &qw, const Maybe &kw, const Maybe &positions,
+                          const Maybe &frequencies, const std::vector<int64_t> &axes,
+                          bool interleaved, bool norm, double eps, bool make, Maybe dq, Maybe dk,
+                          Maybe dqw, Maybe dkw, int64_t stream) {
+    need(dyq.defined(), "dq must be a tensor");
+    const at::ScalarType type = dyq.scalar_type();
+    const HeadNorm c(q, k, qw, kw, positions, frequencies, axes, interleaved, norm, eps, type);
+    no_grad(dyq, dyk, q, k, qw, kw, frequencies, dq, dk, dqw, dkw);
+    need(!k || dyk, "the gradient of the keys is needed");
+    c10::DeviceGuard guard(q.device());
+    if (make) {
+        dq = empty(c.qs, q.scalar_type(), q);
+        const Tensor both = empty({2, c.qs[3]}, at::kFloat, q);
+        dqw = both[0];
+        if (k) {
+            dk = empty(c.ks, q.scalar_type(), q);
+            dkw = both[1];
+        }
+    }
+    need(dq && (!k || dk), "out must hold the gradients of q and k");
+    const ctc_heads dyqh = heads_of(dyq, "dq", c.qs, type, q);
+    const ctc_heads dykh = k ? heads_of(*dyk, "dk", c.ks, type, q) : ctc_heads{};
+    const ctc_heads dqh = heads_of(*dq, "out", c.qs, q.scalar_type(), q);
+    const ctc_heads dkh = k ? heads_of(*dk, "out", c.ks, q.scalar_type(), q) : ctc_heads{};
+    const std::array<int64_t, 1> per{c.qs[3]};
+    void *qwp = like(dqw, "the gradient of q_weight", at::kFloat, per, q);
+    void *kwp = k ? like(dkw, "the gradient of k_weight", at::kFloat, per, q) : nullptr;
+    size_t bytes = 0;
+    Tensor keep;
+    done(ctc_head_norm_rotary_workspace_bytes(&c.h, &bytes));
+    done(ctc_head_norm_rotary_backward(&c.h, &dyqh, &dykh, &c.q, &c.k, &dqh, &dkh, (float *)qwp,
+                                       (float *)kwp, scratch(bytes, keep, q), bytes,
+                                       (void *)stream));
+    wrote(dq);
+    wrote(dqw);
+    if (k) {
+        wrote(dk);
+        wrote(dkw);
+    }
+    return {*dq, k ? dk : Maybe(), dqw, k ? dkw : Maybe()};
+}
+
+// --------------------------------------------------------------- clipping
+
+std::tuple<std::vector<Tensor>, Tensor> clip_gradients(const std::vector<Tensor> &grads,
+                                                       double max_norm,
+                                                       std::optional<std::vector<Tensor>> out,
+                                                       Maybe norm, int64_t stream) {
+    need(!grads.empty(), "no gradients");
+    const Tensor &ref = grads[0];
+    on_gpu(ref, "a gradient");
+    c10::DeviceGuard guard(ref.device());
+    need(!out || out->size() == grads.size(), "out must hold a tensor for each gradient");
+    std::vector<ctc_gradient> g(grads.size());
+    const bool make = !out;
+    if (make) {
+        out.emplace();
+        out->reserve(grads.size());
+    }
+    for (size_t i = 0; i < grads.size(); i++) {
+        const Tensor &x = grads[i];
+        need(x.defined() && real_type(x) && x.device() == ref.device(),
+             "gradients must be float32, float16 or bfloat16 tensors of one GPU");
+        need(x.is_non_overlapping_and_dense(), "gradients must be dense");
+        no_grad(x);
+        if (make) {
+            out->push_back(at::empty_like(x));
+        } else {
+            const Tensor &y = (*out)[i];
+            no_grad(y);
+            need(y.defined() && y.scalar_type() == x.scalar_type() && y.device() == x.device() &&
+                     y.sizes() == x.sizes() && (y.strides() == x.strides() ||
+                                                (y.is_contiguous() && x.is_contiguous())),
+                 "out must be like the gradients");
+        }
+        g[i] = ctc_gradient{x.data_ptr(), (*out)[i].data_ptr(), x.numel(), (int32_t)code(x), 0};
+    }
+    const bool given = norm.has_value();
+    if (!given) norm = empty({}, at::kFloat, ref);
+    need(norm->scalar_type() == at::kFloat && norm->numel() == 1 && norm->device() == ref.device(),
+         "the norm must be one float32 value");
+    size_t bytes = 0;
+    Tensor keep;
+    done(ctc_clip_gradients_workspace_bytes((int32_t)g.size(), g.data(), &bytes));
+    done(ctc_clip_gradients((int32_t)g.size(), g.data(), (float)max_norm,
+                            (float *)norm->data_ptr(), scratch(bytes, keep, ref), bytes,
+                            (void *)stream));
+    if (!make)
+        for (const Tensor &t : *out) wrote(t);
+    if (given) wrote(norm);
+    return {*out, *norm};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_binding, m) {
@@ -368,5 +656,10 @@ PYBIND11_MODULE(_binding, m) {
     m.def("fp8_matmul", &fp8_matmul);
     m.def("token_scores", &token_scores);
     m.def("token_scores_backward", &token_scores_backward);
+    m.def("attention", &attention);
+    m.def("attention_backward", &attention_backward);
+    m.def("head_norm_rotary", &head_norm_rotary);
+    m.def("head_norm_rotary_backward", &head_norm_rotary_backward);
+    m.def("clip_gradients", &clip_gradients);
     m.add_object("_cleanup", py::capsule([]() { check_status.release(); }));
 }

@@ -78,5 +78,67 @@ size_t scores_workspace(const ScoreArgs &a);
 hipError_t launch_scores(const ScoreArgs &a, hipStream_t st);
 hipError_t launch_scores_backward(const ScoreArgs &a, hipStream_t st);
 
+struct AttnArgs {
+    int type, b, tq, tk, hq, hkv, d, causal;
+    float scale;
+    const void *q, *k, *v, *dout;
+    void *o;                     // read by the backward pass
+    float *lse;                  // [b][hq][tq], as o
+    // strides in elements: sequence, token, head
+    int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];
+    const int32_t *qlen, *klen;  // [b] or null
+    void *dq, *dk, *dv;
+    float *ws;
+    // set by the launchers
+    int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks;
+    uint32_t gmul;
+    float *part, *part_lse, *stats, *bounds;
+};
+constexpr int ATTN_MAX_D = 128;
+size_t attention_workspace(const AttnArgs &a, bool backward);
+hipError_t launch_attention(const AttnArgs &a, hipStream_t st);
+hipError_t launch_attention_backward(const AttnArgs &a, hipStream_t st);
+
+struct HeadSide {                // queries or keys
+    const void *x, *dy;
+    void *y, *dx;
+    const float *weight;         // [d] or null
+    float *dweight;              // [d] or null
+    int heads;                   // 0: none
+    int64_t xs[3], ys[3], dys[3], dxs[3];        // sequence, token, head
+};
+struct HeadArgs {
+    int type, ytype;             // of x and dx, of y and dy
+    int b, t, d, norm, interleaved, n_axes, turned, per_image;
+    int axes[4];                 // pairs turned by each; their sum is `turned`
+    float eps;
+    HeadSide side[2];
+    const int32_t *positions;    // [b or 1][t][n_axes]
+    const float *frequencies;    // [turned]
+    float *ws;
+    // set by the launcher
+    int lanes, tokens;
+};
+bool head_norm_ok(const HeadArgs &a);            // its heads fit a wave
+size_t head_norm_workspace(const HeadArgs &a);   // of the backward pass
+hipError_t launch_head_norm(const HeadArgs &a, bool backward, hipStream_t st);
+
+// Tensors of one launch, in chunks: those of tensor i are first[i] ..
+// first[i + 1] - 1.
+constexpr int CLIP_TENSORS = 96;
+struct ClipTable {
+    const void *x[CLIP_TENSORS];
+    void *y[CLIP_TENSORS];
+    int64_t size[CLIP_TENSORS];
+    uint32_t first[CLIP_TENSORS + 1];
+    uint8_t type[CLIP_TENSORS];
+    int n;
+};
+int64_t clip_chunks_of(int64_t size);
+int clip_parts(const ClipTable &t);              // partial sums of a launch
+hipError_t launch_clip_squares(const ClipTable &t, double *part, hipStream_t st);
+hipError_t launch_clip_scale(const ClipTable &t, const double *part, int parts, float max_norm,
+                             float *norm, hipStream_t st);
+
 }  // namespace ops
 }  // namespace ctc

@@ -8,3 +8,6 @@
 #include "fp8_quantize.h"
 #include "fp8_product.h"
 #include "token_scores.h"
+#include "attention.h"
+#include "head_norm.h"
+#include "clip.h"

@@ -2,9 +2,12 @@
 // checks the arguments, then enqueues the kernels of ops.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <exception>
+#include <vector>
 
 #include "../../include/ctc.h"
 #include "errors.h"
@@ -104,6 +107,176 @@ ctc_status score_args(ctc_dtype dtype, int64_t rows, int32_t vocab, int64_t ld, 
     a = ScoreArgs{};
     a.type = dtype; a.rows = rows; a.ld = ld; a.vocab = vocab; a.top_k = top_k;
     return CTC_OK;
+}
+
+// -------------------------------------------------------------- attention
+
+// Strides of a tensor of heads, those of dimensions of size 1 as 0.
+void heads_strides(const ctc_heads &h, const int64_t (&size)[3], int64_t (&out)[3]) {
+    for (int i = 0; i < 3; i++) out[i] = size[i] > 1 ? h.strides[i] : 0;
+}
+// Address and strides of a tensor of heads.  Outputs must not overlap
+// themselves: each stride reaches past what smaller ones span.
+ctc_status heads_arg(const ctc_heads *h, const char *name, int64_t b, int64_t t, int64_t heads,
+                     int64_t d, bool out, const void *&data, int64_t (&strides)[3]) {
+    data = nullptr;
+    for (int64_t &v : strides) v = 0;
+    if (!(b && t && heads)) return CTC_OK;
+    if (!h || !h->data) return fail(CTC_ERR_ARG, "NULL %s", name);
+    const int64_t size[3] = {b, t, heads};
+    heads_strides(*h, size, strides);
+    for (int64_t v : strides)
+        if (v < 0 || v > (int64_t)1 << 45) return fail(CTC_ERR_ARG, "bad strides of %s", name);
+    if (out) {
+        int64_t span = d;
+        bool done[3] = {false, false, false};
+        for (int n = 0; n < 3; n++) {
+            int best = -1;
+            for (int i = 0; i < 3; i++)
+                if (!done[i] && size[i] > 1 && (best < 0 || strides[i] < strides[best])) best = i;
+            if (best < 0) break;
+            if (strides[best] < span) return fail(CTC_ERR_ARG, "elements of %s overlap", name);
+            span += (size[best] - 1) * strides[best];
+            done[best] = true;
+        }
+    }
+    data = h->data;
+    return CTC_OK;
+}
+
+ctc_status attn_args(const ctc_attention *c, AttnArgs &a) {
+    if (!c) return fail(CTC_ERR_ARG, "NULL attention");
+    if (c->dtype != CTC_F16 && c->dtype != CTC_BF16)
+        return fail(CTC_ERR_ARG, "attention takes float16 or bfloat16");
+    if (c->batch < 0 || c->queries < 0 || c->keys < 0 || c->q_heads < 1 || c->k_heads < 1)
+        return fail(CTC_ERR_ARG, "bad attention sizes");
+    if (c->q_heads % c->k_heads) return fail(CTC_ERR_ARG, "k_heads must divide q_heads");
+    if (c->head < 8 || c->head % 8 || c->head > ATTN_MAX_D)
+        return fail(CTC_ERR_ARG, "head sizes are multiples of 8 up to %d", ATTN_MAX_D);
+    if (!(c->scale > 0.f) || std::isinf(c->scale)) return fail(CTC_ERR_ARG, "scale must be > 0");
+    const double rows = (double)c->queries * (c->q_heads / c->k_heads);
+    const double pairs = (double)c->batch * c->k_heads;
+    if (rows > (1 << 30) || c->keys > (1 << 30) ||
+        !grid_ok(pairs * (rows / 64 + (double)c->keys / 64 + 2) + 512))
+        return fail(CTC_ERR_UNSUPPORTED, "attention too large");
+    a = AttnArgs{};
+    a.type = c->dtype;
+    a.b = c->batch; a.tq = c->queries; a.tk = c->keys;
+    a.hq = c->q_heads; a.hkv = c->k_heads; a.d = c->head;
+    a.causal = c->causal != 0; a.scale = c->scale;
+    a.qlen = c->q_lengths; a.klen = c->k_lengths;
+    return CTC_OK;
+}
+ctc_status attn_heads(const AttnArgs &a, const ctc_heads *h, const char *name, bool queries,
+                      bool out, const void *&data, int64_t (&strides)[3]) {
+    const int64_t t = queries ? a.tq : a.tk, heads = queries ? a.hq : a.hkv;
+    ctc_status s = heads_arg(h, name, a.b, t, heads, a.d, out, data, strides);
+    if (s != CTC_OK) return s;
+    if (!aligned(data, 16) || strides[0] % 8 || strides[1] % 8 || strides[2] % 8)
+        return fail(CTC_ERR_ARG, "%s must be 16-byte aligned, its strides multiples of 8", name);
+    // (a tile's addresses have 32 bits)
+    const double group = queries ? a.hq / a.hkv : 1;
+    if (64. * strides[1] + group * strides[2] >= (double)(1 << 29))
+        return fail(CTC_ERR_UNSUPPORTED, "strides of %s too large", name);
+    return CTC_OK;
+}
+
+// ------------------------------------------------------------ head norms
+
+ctc_status head_args(const ctc_head_rotary *c, HeadArgs &a) {
+    if (!c) return fail(CTC_ERR_ARG, "NULL head_rotary");
+    if (!real_type(c->dtype) || !real_type(c->ytype) ||
+        (c->dtype != CTC_F32 && c->ytype != c->dtype))
+        return fail(CTC_ERR_ARG, "bad dtype");
+    if (c->batch < 0 || c->tokens < 0 || c->q_heads < 1 || c->k_heads < 0)
+        return fail(CTC_ERR_ARG, "bad head_norm_rotary sizes");
+    if (c->head < 2 || c->head % 2 || c->head > 512)
+        return fail(CTC_ERR_ARG, "head sizes are even, up to 512");
+    if (!(c->eps >= 0.f) || std::isinf(c->eps)) return fail(CTC_ERR_ARG, "bad eps");
+    if (c->axes < 0 || c->axes > 4) return fail(CTC_ERR_ARG, "up to 4 position axes");
+    a = HeadArgs{};
+    for (int i = 0; i < c->axes; i++) {
+        if (c->pairs[i] < 0 || c->pairs[i] > c->head / 2)
+            return fail(CTC_ERR_ARG, "bad pairs of an axis");
+        a.axes[i] = c->pairs[i];
+        a.turned += c->pairs[i];
+    }
+    if (a.turned > c->head / 2) return fail(CTC_ERR_ARG, "more pairs than a head has");
+    a.type = c->dtype; a.ytype = c->ytype;
+    a.b = c->batch; a.t = c->tokens; a.d = c->head;
+    a.norm = c->norm != 0; a.eps = c->eps;
+    a.interleaved = c->interleaved != 0; a.n_axes = c->axes; a.per_image = c->per_image != 0;
+    a.positions = c->positions; a.frequencies = c->frequencies;
+    a.side[0].heads = c->q_heads; a.side[0].weight = c->q_weight;
+    a.side[1].heads = c->k_heads; a.side[1].weight = c->k_weight;
+    if (!head_norm_ok(a) || (double)a.b * a.t >= (double)((int64_t)1 << 40) ||
+        c->q_heads > (1 << 20) || c->k_heads > (1 << 20))
+        return fail(CTC_ERR_UNSUPPORTED, "head_norm_rotary too large");
+    return CTC_OK;
+}
+ctc_status head_positions(const HeadArgs &a) {
+    if (a.turned && a.b && a.t && (!a.positions || !a.frequencies))
+        return fail(CTC_ERR_ARG, "NULL positions or frequencies");
+    return CTC_OK;
+}
+ctc_status head_side(const HeadArgs &a, int which, const ctc_heads *h, const char *name, bool out,
+                     const void *&data, int64_t (&strides)[3]) {
+    return heads_arg(h, name, a.b, a.t, a.side[which].heads, a.d, out, data, strides);
+}
+
+// --------------------------------------------------------------- clipping
+
+ctc_status clip_args(int32_t n, const ctc_gradient *g) {
+    if (n < 0 || (n && !g)) return fail(CTC_ERR_ARG, "bad gradients");
+    if (n > (1 << 20)) return fail(CTC_ERR_UNSUPPORTED, "too many gradients");
+    double chunks = 0;
+    for (int32_t i = 0; i < n; i++) {
+        if (!real_type(g[i].dtype)) return fail(CTC_ERR_ARG, "bad dtype of gradient %d", i);
+        if (g[i].size < 0) return fail(CTC_ERR_ARG, "bad size of gradient %d", i);
+        chunks += (double)g[i].size / (1 << 14) + 1;
+        if (chunks >= 4294967295.) return fail(CTC_ERR_UNSUPPORTED, "gradients too large");
+    }
+    return CTC_OK;
+}
+// The launches' tables: f(table) for each CLIP_TENSORS tensors.
+template <typename F> ctc_status clip_tables(int32_t n, const ctc_gradient *g, F f) {
+    for (int32_t i = 0; i < n; i += CLIP_TENSORS) {
+        ClipTable t;
+        t.n = n - i < CLIP_TENSORS ? n - i : CLIP_TENSORS;
+        t.first[0] = 0;
+        for (int j = 0; j < t.n; j++) {
+            t.x[j] = g[i + j].x;
+            t.y[j] = g[i + j].y;
+            t.size[j] = g[i + j].size;
+            t.type[j] = (uint8_t)g[i + j].dtype;
+            t.first[j + 1] = t.first[j] + (uint32_t)clip_chunks_of(g[i + j].size);
+        }
+        ctc_status s = f(t);
+        if (s != CTC_OK) return s;
+    }
+    return CTC_OK;
+}
+// No output overlaps another one, or another tensor's values.
+bool clip_disjoint(int32_t n, const ctc_gradient *g) {
+    struct Span { uintptr_t from, to; int32_t i; };
+    std::vector<Span> out, in;
+    for (int32_t i = 0; i < n; i++) {
+        const size_t bytes = (size_t)g[i].size * type_bytes(g[i].dtype);
+        if (!bytes) continue;
+        out.push_back({(uintptr_t)g[i].y, (uintptr_t)g[i].y + bytes, i});
+        if (g[i].y != g[i].x) in.push_back({(uintptr_t)g[i].x, (uintptr_t)g[i].x + bytes, i});
+    }
+    auto order = [](const Span &a, const Span &b) { return a.from < b.from; };
+    std::sort(out.begin(), out.end(), order);
+    for (size_t i = 1; i < out.size(); i++)
+        if (out[i].from < out[i - 1].to) return false;
+    for (const Span &s : in) {
+        // the first output that ends behind s begins
+        auto it = std::upper_bound(out.begin(), out.end(), s.from,
+                                   [](uintptr_t v, const Span &o) { return v < o.to; });
+        if (it != out.end() && it->from < s.to) return false;
+    }
+    return true;
 }
 
 }  // namespace
@@ -270,6 +443,163 @@ ctc_status ctc_token_scores_backward(ctc_dtype dtype, int64_t rows, int32_t voca
     a.g_lse = g_lse; a.g_logprob = g_logprob; a.g_entropy = g_entropy;
     a.dx = dlogits; a.ldd = ldd;
     return done(launch_scores_backward(a, S(stream)));
+}
+
+ctc_status ctc_attention_workspace_bytes(const ctc_attention *c, int32_t backward, size_t *bytes) {
+    if (!bytes) return fail(CTC_ERR_ARG, "NULL bytes");
+    AttnArgs a;
+    ctc_status s = attn_args(c, a);
+    if (s != CTC_OK) return s;
+    *bytes = a.b && (backward || a.tq) ? attention_workspace(a, backward != 0) : 0;
+    return CTC_OK;
+}
+
+ctc_status ctc_attention_forward(const ctc_attention *c, const ctc_heads *q, const ctc_heads *k,
+                                 const ctc_heads *v, const ctc_heads *o, float *lse,
+                                 void *workspace, size_t ws_bytes, void *stream) {
+    AttnArgs a;
+    ctc_status s = attn_args(c, a);
+    if (s != CTC_OK) return s;
+    if (a.b == 0 || a.tq == 0) return CTC_OK;
+    const void *out = nullptr;
+    if ((s = attn_heads(a, q, "q", true, false, a.q, a.qs)) != CTC_OK ||
+        (s = attn_heads(a, k, "k", false, false, a.k, a.ks)) != CTC_OK ||
+        (s = attn_heads(a, v, "v", false, false, a.v, a.vs)) != CTC_OK ||
+        (s = attn_heads(a, o, "o", true, true, out, a.os)) != CTC_OK)
+        return s;
+    if (!lse) return fail(CTC_ERR_ARG, "NULL lse");
+    a.o = (void *)out; a.lse = lse; a.ws = (float *)workspace;
+    s = need_workspace(attention_workspace(a, false), workspace, ws_bytes);
+    if (s != CTC_OK) return s;
+    return done(launch_attention(a, S(stream)));
+}
+
+ctc_status ctc_attention_backward(const ctc_attention *c, const ctc_heads *dout,
+                                  const ctc_heads *q, const ctc_heads *k, const ctc_heads *v,
+                                  const ctc_heads *o, const float *lse, const ctc_heads *dq,
+                                  const ctc_heads *dk, const ctc_heads *dv, void *workspace,
+                                  size_t ws_bytes, void *stream) {
+    AttnArgs a;
+    ctc_status s = attn_args(c, a);
+    if (s != CTC_OK) return s;
+    if (a.b == 0 || (a.tq == 0 && a.tk == 0)) return CTC_OK;
+    const void *op = nullptr, *dqp = nullptr, *dkp = nullptr, *dvp = nullptr;
+    if ((s = attn_heads(a, dout, "dout", true, false, a.dout, a.dos)) != CTC_OK ||
+        (s = attn_heads(a, q, "q", true, false, a.q, a.qs)) != CTC_OK ||
+        (s = attn_heads(a, k, "k", false, false, a.k, a.ks)) != CTC_OK ||
+        (s = attn_heads(a, v, "v", false, false, a.v, a.vs)) != CTC_OK ||
+        (s = attn_heads(a, o, "o", true, false, op, a.os)) != CTC_OK ||
+        (s = attn_heads(a, dq, "dq", true, true, dqp, a.dqs)) != CTC_OK ||
+        (s = attn_heads(a, dk, "dk", false, true, dkp, a.dks)) != CTC_OK ||
+        (s = attn_heads(a, dv, "dv", false, true, dvp, a.dvs)) != CTC_OK)
+        return s;
+    if (a.tq && !lse) return fail(CTC_ERR_ARG, "NULL lse");
+    a.o = (void *)op; a.lse = (float *)lse; a.ws = (float *)workspace;
+    a.dq = (void *)dqp; a.dk = (void *)dkp; a.dv = (void *)dvp;
+    s = need_workspace(attention_workspace(a, true), workspace, ws_bytes);
+    if (s != CTC_OK) return s;
+    return done(launch_attention_backward(a, S(stream)));
+}
+
+ctc_status ctc_head_norm_rotary_workspace_bytes(const ctc_head_rotary *c, size_t *bytes) {
+    if (!bytes) return fail(CTC_ERR_ARG, "NULL bytes");
+    HeadArgs a;
+    ctc_status s = head_args(c, a);
+    if (s != CTC_OK) return s;
+    *bytes = head_norm_workspace(a);
+    return CTC_OK;
+}
+
+ctc_status ctc_head_norm_rotary_forward(const ctc_head_rotary *c, const ctc_heads *q,
+                                        const ctc_heads *k, const ctc_heads *yq,
+                                        const ctc_heads *yk, void *stream) {
+    HeadArgs a;
+    ctc_status s = head_args(c, a);
+    if (s != CTC_OK || (s = head_positions(a)) != CTC_OK) return s;
+    const ctc_heads *x[2] = {q, k}, *y[2] = {yq, yk};
+    for (int i = 0; i < 2; i++) {
+        HeadSide &h = a.side[i];
+        const void *out = nullptr;
+        if ((s = head_side(a, i, x[i], i ? "k" : "q", false, h.x, h.xs)) != CTC_OK ||
+            (s = head_side(a, i, y[i], i ? "yk" : "yq", true, out, h.ys)) != CTC_OK)
+            return s;
+        h.y = (void *)out;
+    }
+    return done(launch_head_norm(a, false, S(stream)));
+}
+
+ctc_status ctc_head_norm_rotary_backward(const ctc_head_rotary *c, const ctc_heads *dyq,
+                                         const ctc_heads *dyk, const ctc_heads *q,
+                                         const ctc_heads *k, const ctc_heads *dq,
+                                         const ctc_heads *dk, float *dq_weight, float *dk_weight,
+                                         void *workspace, size_t ws_bytes, void *stream) {
+    HeadArgs a;
+    ctc_status s = head_args(c, a);
+    if (s != CTC_OK || (s = head_positions(a)) != CTC_OK) return s;
+    const ctc_heads *x[2] = {q, k}, *dy[2] = {dyq, dyk}, *dx[2] = {dq, dk};
+    for (int i = 0; i < 2; i++) {
+        HeadSide &h = a.side[i];
+        const void *out = nullptr;
+        if ((s = head_side(a, i, x[i], i ? "k" : "q", false, h.x, h.xs)) != CTC_OK ||
+            (s = head_side(a, i, dy[i], i ? "dyk" : "dyq", false, h.dy, h.dys)) != CTC_OK ||
+            (s = head_side(a, i, dx[i], i ? "dk" : "dq", true, out, h.dxs)) != CTC_OK)
+            return s;
+        h.dx = (void *)out;
+    }
+    a.side[0].dweight = dq_weight;
+    a.side[1].dweight = a.side[1].heads ? dk_weight : nullptr;
+    a.ws = (float *)workspace;
+    s = need_workspace(head_norm_workspace(a), workspace, ws_bytes);
+    if (s != CTC_OK) return s;
+    return done(launch_head_norm(a, true, S(stream)));
+}
+
+ctc_status ctc_clip_gradients_workspace_bytes(int32_t n, const ctc_gradient *g, size_t *bytes) {
+    if (!bytes) return fail(CTC_ERR_ARG, "NULL bytes");
+    ctc_status s = clip_args(n, g);
+    if (s != CTC_OK) return s;
+    size_t parts = 0;
+    s = clip_tables(n, g, [&](const ClipTable &t) {
+        parts += clip_parts(t);
+        return CTC_OK;
+    });
+    *bytes = parts * sizeof(double);
+    return s;
+}
+
+ctc_status ctc_clip_gradients(int32_t n, const ctc_gradient *g, float max_norm, float *norm,
+                              void *workspace, size_t ws_bytes, void *stream) {
+    size_t need = 0;
+    ctc_status s = ctc_clip_gradients_workspace_bytes(n, g, &need);
+    if (s != CTC_OK) return s;
+    if (!(max_norm >= 0.f)) return fail(CTC_ERR_ARG, "max_norm must be >= 0");
+    for (int32_t i = 0; i < n; i++)
+        if (g[i].size && (!g[i].x || !g[i].y)) return fail(CTC_ERR_ARG, "NULL gradient %d", i);
+    try {
+        if (!clip_disjoint(n, g)) return fail(CTC_ERR_ARG, "outputs overlap other gradients");
+    } catch (const std::exception &e) {
+        return fail(CTC_ERR_DEVICE, "%s", e.what());
+    }
+    s = need_workspace(need, workspace, ws_bytes);
+    if (s != CTC_OK) return s;
+    double *part = (double *)workspace;
+    int parts = 0;
+    s = clip_tables(n, g, [&](const ClipTable &t) {
+        const ctc_status r = done(launch_clip_squares(t, part + parts, S(stream)));
+        parts += clip_parts(t);
+        return r;
+    });
+    if (s != CTC_OK) return s;
+    if (!n) {
+        if (!norm) return CTC_OK;
+        ClipTable t;
+        t.n = 0;
+        t.first[0] = 0;
+        return done(launch_clip_scale(t, part, 0, max_norm, norm, S(stream)));
+    }
+    return clip_tables(n, g, [&](const ClipTable &t) {
+        return done(launch_clip_scale(t, part, parts, max_norm, norm, S(stream)));
+    });
 }
 
 }  // extern "C"

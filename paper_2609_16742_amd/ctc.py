@@ -56,6 +56,11 @@ EXPORTS = ["ctc_build_filters", "ctc_build_fc", "ctc_threshold_from_samples",
            "ctc_net_role",
            "ctc_net_profile", "ctc_net_profile_read", "ctc_net_op_kernel",
            "ctc_graph_create", "ctc_graph_launch", "ctc_graph_destroy",
+           "ctc_attention_forward", "ctc_attention_backward",
+           "ctc_attention_workspace_bytes", "ctc_head_norm_rotary_forward",
+           "ctc_head_norm_rotary_backward",
+           "ctc_head_norm_rotary_workspace_bytes", "ctc_clip_gradients",
+           "ctc_clip_gradients_workspace_bytes",
            "ctc_group_norm_forward", "ctc_group_norm_backward",
            "ctc_group_norm_workspace_bytes", "ctc_fp8_quantize",
            "ctc_fp8_matmul", "ctc_fp8_matmul_workspace_bytes",
@@ -90,6 +95,37 @@ assert ctypes.sizeof(ctc_fault) == 24
 class ctc_site_info(ctypes.Structure):
     _fields_ = [("site", ctypes.c_int32), ("layer", ctypes.c_int32),
                 ("elements", ctypes.c_int64), ("bits", ctypes.c_int32),
+                ("pad", ctypes.c_int32)]
+
+
+class ctc_heads(ctypes.Structure):
+    """Tensor [batch][tokens][heads][head] (include/ctc.h)."""
+    _fields_ = [("data", ctypes.c_void_p), ("strides", ctypes.c_int64 * 3)]
+
+
+class ctc_attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in (
+        "dtype", "batch", "queries", "keys", "q_heads", "k_heads", "head",
+        "causal")] + [("scale", ctypes.c_float),
+                      ("q_lengths", ctypes.c_void_p),
+                      ("k_lengths", ctypes.c_void_p)])
+
+
+class ctc_head_rotary(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in (
+        "dtype", "ytype", "batch", "tokens", "q_heads", "k_heads", "head",
+        "norm")] + [("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                    ("k_weight", ctypes.c_void_p),
+                    ("interleaved", ctypes.c_int32),
+                    ("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4),
+                    ("per_image", ctypes.c_int32),
+                    ("positions", ctypes.c_void_p),
+                    ("frequencies", ctypes.c_void_p)])
+
+
+class ctc_gradient(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("size", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("pad", ctypes.c_int32)]
 
 
@@ -171,6 +207,23 @@ _sig("ctc_token_scores_backward", [_I32, _I64, _I32, _P, _I64] + [_P] * 7 +
      [_I64, _P])
 _sig("ctc_token_scores_workspace_bytes", [_I64, _I32, _I32,
                                           ctypes.POINTER(_SZ)])
+_HEADS = ctypes.POINTER(ctc_heads)
+_sig("ctc_attention_forward", [ctypes.POINTER(ctc_attention)] + [_HEADS] * 4 +
+     [_P, _P, _SZ, _P])
+_sig("ctc_attention_backward", [ctypes.POINTER(ctc_attention)] + [_HEADS] * 5 +
+     [_P] + [_HEADS] * 3 + [_P, _SZ, _P])
+_sig("ctc_attention_workspace_bytes", [ctypes.POINTER(ctc_attention), _I32,
+                                       ctypes.POINTER(_SZ)])
+_sig("ctc_head_norm_rotary_forward", [ctypes.POINTER(ctc_head_rotary)] +
+     [_HEADS] * 4 + [_P])
+_sig("ctc_head_norm_rotary_backward", [ctypes.POINTER(ctc_head_rotary)] +
+     [_HEADS] * 6 + [_P, _P, _P, _SZ, _P])
+_sig("ctc_head_norm_rotary_workspace_bytes", [
+    ctypes.POINTER(ctc_head_rotary), ctypes.POINTER(_SZ)])
+_sig("ctc_clip_gradients", [_I32, ctypes.POINTER(ctc_gradient), _F32, _P, _P,
+                            _SZ, _P])
+_sig("ctc_clip_gradients_workspace_bytes", [
+    _I32, ctypes.POINTER(ctc_gradient), ctypes.POINTER(_SZ)])
 _sig("ctc_net_destroy", [_P], None)
 _sig("ctc_last_error", [], ctypes.c_char_p)
 _sig("ctc_abi_version", [], _I32)
@@ -488,6 +541,48 @@ def ctc_token_scores_workspace_bytes(rows, vocab, top_k):
     b = _SZ()
     _check(_lib.ctc_token_scores_workspace_bytes(rows, vocab, top_k,
                                                  ctypes.byref(b)))
+    return b.value
+
+
+# Structures (include/ctc.h), pointers and the raw stream.
+
+def ctc_attention_forward(*args):
+    _check(_lib.ctc_attention_forward(*args))
+
+
+def ctc_attention_backward(*args):
+    _check(_lib.ctc_attention_backward(*args))
+
+
+def ctc_attention_workspace_bytes(attention, backward):
+    b = _SZ()
+    _check(_lib.ctc_attention_workspace_bytes(attention, int(backward),
+                                              ctypes.byref(b)))
+    return b.value
+
+
+def ctc_head_norm_rotary_forward(*args):
+    _check(_lib.ctc_head_norm_rotary_forward(*args))
+
+
+def ctc_head_norm_rotary_backward(*args):
+    _check(_lib.ctc_head_norm_rotary_backward(*args))
+
+
+def ctc_head_norm_rotary_workspace_bytes(rotary):
+    b = _SZ()
+    _check(_lib.ctc_head_norm_rotary_workspace_bytes(rotary, ctypes.byref(b)))
+    return b.value
+
+
+def ctc_clip_gradients(*args):
+    _check(_lib.ctc_clip_gradients(*args))
+
+
+def ctc_clip_gradients_workspace_bytes(n, gradients):
+    b = _SZ()
+    _check(_lib.ctc_clip_gradients_workspace_bytes(n, gradients,
+                                                   ctypes.byref(b)))
     return b.value
 
 

@@ -3,7 +3,10 @@
 Group norm with an activation on channels-last maps (``group_norm``), 8-bit
 matrices with a scale for each block of 128 (``fp8_quantize``) and their
 product (``fp8_matmul``), and the scores of given classes or tokens
-(``token_scores``), with the backward passes of the first and the last.
+(``token_scores``), with the backward passes of the first and the last; for a
+head over a map's pixels, attention (``attention``), the norms and rotations
+of its queries and keys (``head_norm_rotary``), both with their backward
+passes, and the clipping of all gradients by their norm (``clip_gradients``).
 Checks of arguments, outputs and workspaces (csrc/binding.cpp); the work runs
 in libctc.so's HIP kernels (include/ctc.h states what each computes).
 
@@ -156,3 +159,93 @@ def token_scores_backward(logits, targets, lse, entropy=None, g_lse=None,
         raise ValueError("lse is needed")
     return _run(_binding.token_scores_backward, logits, stream, logits,
                 targets, lse, entropy, g_lse, g_logprob, g_entropy, out)
+
+
+def attention(q, k, v, causal=False, q_lengths=None, k_lengths=None,
+              scale=None, out=None, stream=None):
+    """(o, lse) of queries ``q`` [batch, tokens, heads, head size] over keys
+    and values ``k``, ``v`` [batch, keys, key heads, head size], float16 or
+    bfloat16, head sizes multiples of 8 up to 128, strided as a projection's
+    parts are: ``o = softmax(scale q k^T) v`` (``scale``: default 1 /
+    sqrt(head size)) and the rows' log-sum-exp [batch, heads, tokens].  Each
+    key head serves heads / key heads query heads.  ``q_lengths`` and
+    ``k_lengths`` (int32 [batch]): what stands behind them takes no part.
+    With ``causal``, query i sees keys up to i + keys - queries (of the
+    sequence's own).  A query that sees nothing has o = 0, lse = -inf.
+    ``out``: an (o, lse) to write into."""
+    o, lse = out or (None, None)
+    return _run(_binding.attention, q, stream, q, k, v, causal, q_lengths,
+                k_lengths, scale, o, lse)
+
+
+def attention_backward(do, q, k, v, o, lse, causal=False, q_lengths=None,
+                       k_lengths=None, scale=None, out=None, stream=None):
+    """dq, dk, dv of :func:`attention` (same arguments, with the ``o`` and
+    ``lse`` it returned) for the gradient ``do`` of o.  Probabilities are
+    computed again.  ``out``: a (dq, dk, dv) to write into, which may be parts
+    of one projection's gradient."""
+    dq, dk, dv = out or (None, None, None)
+    return _run(_binding.attention_backward, q, stream, do, q, k, v, o, lse,
+                causal, q_lengths, k_lengths, scale, dq, dk, dv)
+
+
+def grid_positions(*sizes, device="cuda"):
+    """int32 [tokens, axes] positions of a grid's points in the order of a
+    flattened map: ``grid_positions(h, w)``, ``grid_positions(frames, h, w)``."""
+    grid = torch.meshgrid(*[torch.arange(n, dtype=torch.int32, device=device)
+                            for n in sizes], indexing="ij")
+    return torch.stack([g.flatten() for g in grid], 1).contiguous()
+
+
+def rotary_frequencies(axes, base=10000.0, device="cuda"):
+    """fp32 frequencies of ``axes`` (pairs of each): base ** (-i / pairs) for
+    pair i of each axis."""
+    return torch.cat([torch.empty(0, device=device)] + [
+        (base ** (-torch.arange(n, dtype=torch.float64, device=device) / n))
+        .float() for n in axes if n])
+
+
+def head_norm_rotary(q, k=None, q_weight=None, k_weight=None, positions=None,
+                     frequencies=None, axes=(), interleaved=False, norm=True,
+                     eps=1e-6, dtype=None, out=None, stream=None):
+    """(q', k'): the RMS norm of each head of ``q`` and ``k`` [batch, tokens,
+    heads, head size] times their weights (fp32 [head size]) and the rotation
+    of each head's pairs by their positions.  ``axes`` are the pairs turned
+    by each position axis, in order; ``positions`` int32 [tokens, axes] or
+    [batch, tokens, axes]; ``frequencies`` fp32, one a pair, in radians a step
+    (:func:`grid_positions`, :func:`rotary_frequencies`).  Pairs are (p, p +
+    all pairs) or, ``interleaved``, (2 p, 2 p + 1); values behind them are not
+    turned.  Results are in ``dtype`` (default q's; float32 narrows to 16
+    bits).  ``k`` may be None, and its result is.  ``out``: results to write
+    into; they may be q and k."""
+    yq, yk = out or (None, None)
+    return _run(_binding.head_norm_rotary, q, stream, q, k, q_weight,
+                k_weight, positions, frequencies, axes, interleaved, norm,
+                eps, dtype, yq, yk)
+
+
+def head_norm_rotary_backward(dq, dk, q, k=None, q_weight=None, k_weight=None,
+                              positions=None, frequencies=None, axes=(),
+                              interleaved=False, norm=True, eps=1e-6,
+                              out=None, stream=None):
+    """Gradients of q, k, q_weight and k_weight (fp32) of
+    :func:`head_norm_rotary` (same arguments) for the gradients ``dq`` and
+    ``dk`` of its results.  ``out``: tensors to write into (None for a
+    weight's: not wanted); those of q and k may be dq and dk."""
+    gq, gk, gqw, gkw = out or (None, None, None, None)
+    return _run(_binding.head_norm_rotary_backward, q, stream, dq, dk, q, k,
+                q_weight, k_weight, positions, frequencies, axes, interleaved,
+                norm, eps, out is None, gq, gk, gqw, gkw)
+
+
+def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
+    """(clipped, norm): the norm of all values of ``grads`` (dense tensors)
+    together and the tensors times min(1, max_norm / norm).  ``out``: tensors
+    to write into, like ``grads`` (in place: ``grads`` itself); ``norm``: one
+    fp32 value to write into.  A norm that is not finite leaves the values as
+    they are."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no gradients")
+    return _run(_binding.clip_gradients, grads[0], stream, grads, max_norm,
+                None if out is None else list(out), norm)
