@@ -13,7 +13,6 @@
 namespace ctc {
 namespace ops {
 
-typedef __amdgpu_buffer_rsrc_t AttnBuf;
 typedef __attribute__((address_space(3))) void *AttnLds;
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4v __attribute__((ext_vector_type(4)));
@@ -59,14 +58,44 @@ template <typename T> __device__ __forceinline__ typename Tile<T>::V8 pack8(cons
 }
 
 // Tiles in LDS: rows of PITCH elements in pieces of 16 bytes, piece c of row r
-// in place c ^ swizzle(r).  Eight rows in a row have eight places for a piece
-// (operands read along rows), and each four of them four pairs of places
-// (operands read along columns, 16 columns of 4 rows at a time).
-__device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// in place c ^ swizzle(r).  LDS has 64 banks, 256 bytes: sixteen rows in a row
+// have sixteen places in them for a piece (operands read along rows, 16 lanes
+// at a time), and each four of them four places of 64 bytes (operands read
+// along columns, 32 columns of 4 rows at a time).  Rows 8 apart differ in bit 1.
+template <int PITCH> __device__ __forceinline__ int swizzle(int r) {
+    return PITCH == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
+}
 
-constexpr uint32_t BEYOND = 0x80000000u;        // behind every buffer: reads as zeros
-__device__ __forceinline__ AttnBuf attn_buffer(const void *p) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, 0x7fffffff, 0x00020000);
+// Memory as a buffer of 2^31 - 1 bytes; what is asked for behind it reads as
+// zeros.
+constexpr uint32_t BEYOND = 0x80000000u;
+__device__ __forceinline__ u4 attn_buffer(const void *p) {
+    const uint64_t at = (uint64_t)p;
+    return u4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+              (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xffffu,
+              0x7fffffffu, 0x00020000u};
+}
+__device__ __forceinline__ uint32_t lds_address(const char *p) {
+    return (uint32_t)(uintptr_t)(AttnLds)p;
+}
+// 16 (or 4) bytes a lane from byte `at` of the buffer, `past` bytes further
+// (which the bounds do not see), to consecutive places in LDS.  As an
+// instruction of its own: with the builtin, the compiler has all loads to LDS
+// land before any read along columns, and an iteration's prefetch is waited
+// for within it.  Nothing but attn_arrive waits for these.  (M0, which the
+// compiler keeps nothing in, is LDS's address.)
+__device__ __forceinline__ void load_lds16(const u4 &buf, uint32_t to, uint32_t at,
+                                           uint32_t past) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(at), "s"(buf), "s"(__builtin_amdgcn_readfirstlane(past))
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds4(const u4 &buf, uint32_t to, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(at), "s"(buf)
+                 : "memory");
 }
 
 // t = r / G for r < 2^31 (G's multiplier and shift: see attn_group).
@@ -82,62 +111,79 @@ __device__ __forceinline__ AttnRow attn_row(const AttnArgs &a, int r) {
     return AttnRow{t, r - t * a.group};
 }
 // What a lane asks for of a tile of ROWS rows that NW waves load.
-template <int PITCH, int ROWS, int NW> struct Loads {
+template <int PITCH, int ROWS, int NW, bool KEEP = false> struct Loads {
     static constexpr int CH = PITCH / 8, RPI = 64 / CH, N = ROWS / (RPI * NW);
-    static constexpr bool ODD = (NW * RPI) % 8 != 0;    // odd loads have another swizzle
+    static constexpr int PER = NW * RPI < 16 ? 16 / (NW * RPI) : 1;  // swizzles of a lane's rows
     static_assert(N * RPI * NW == ROWS, "whole loads");
-    int row;                    // of load 0
-    uint32_t piece[2];          // byte of a row
-    __device__ __forceinline__ void init(int lane, int wave, int d) {
-        row = wave * RPI + lane / CH;
-#pragma unroll
-        for (int o = 0; o < 2; o++) {
-            const int c = lane % CH ^ swizzle(row + o * NW * RPI);
-            piece[o] = c * 8 < d ? c * 16 : BEYOND;
-        }
+    // The row of load 0 and the byte of its piece in load i.  Unless they are
+    // to be kept they are computed where they are used: a loop's registers are
+    // its operands'.
+    struct Lane { int row; uint32_t piece[PER]; };
+    int lane, wave, d;
+    Lane kept;
+    __device__ __forceinline__ void init(int l, int w, int head) {
+        lane = l;
+        wave = w;
+        d = head;
+        if (KEEP) kept = make(l);
     }
-    __device__ __forceinline__ uint32_t at(int i) const { return piece[ODD ? i & 1 : 0]; }
-    __device__ __forceinline__ int row_of(int i) const { return row + i * (NW * RPI); }
-    static __device__ __forceinline__ char *to(char *tile, int wave, int i) {
-        return tile + (i * NW + wave) * 1024;
+    __device__ __forceinline__ Lane place() const {
+        if (KEEP) return kept;
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return make(l);
+    }
+    __device__ __forceinline__ Lane make(int l) const {
+        Lane p;
+        p.row = wave * RPI + l / CH;
+#pragma unroll
+        for (int o = 0; o < PER; o++) {
+            const int c = l % CH ^ swizzle<PITCH>(p.row + o * NW * RPI);
+            p.piece[o] = c * 8 < d ? c * 16 : BEYOND;
+        }
+        return p;
     }
     // Rows first .. first + ROWS - 1 of a matrix at `base` (rows `stride` bytes
     // apart, those from `end` on as zeros).
-    __device__ __forceinline__ void rows(char *tile, int wave, const char *base, int64_t stride,
+    __device__ __forceinline__ void rows(uint32_t tile, const char *base, int64_t stride,
                                          int first, int end) const {
-        const AttnBuf buf = attn_buffer(base + first * stride);
+        const u4 buf = attn_buffer(base + first * stride);
         const uint32_t s = (uint32_t)stride;
+        const Lane p = place();
+        tile += wave * 1024;
         if (first + ROWS <= end) {
 #pragma unroll
             for (int i = 0; i < N; i++)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (AttnLds)to(tile, wave, i), 16,
-                                                         row_of(i) * s + at(i), 0, 0, 0);
+                load_lds16(buf, tile + i * NW * 1024, p.row * s + p.piece[i % PER],
+                           i * (NW * RPI) * s);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; i++)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    buf, (AttnLds)to(tile, wave, i), 16,
-                    first + row_of(i) < end ? row_of(i) * s + at(i) : BEYOND, 0, 0, 0);
+            for (int i = 0; i < N; i++) {
+                const int r = p.row + i * (NW * RPI);
+                load_lds16(buf, tile + i * NW * 1024,
+                           first + r < end ? r * s + p.piece[i % PER] : BEYOND, 0);
+            }
         }
     }
     // Rows of queries (tokens st, heads sh bytes apart); zeros outside lo .. hi - 1.
-    __device__ __forceinline__ void queries(const AttnArgs &a, char *tile, int wave,
-                                            const char *base, int64_t st, int64_t sh, int first,
-                                            int lo, int hi) const {
+    __device__ __forceinline__ void queries(const AttnArgs &a, uint32_t tile, const char *base,
+                                            int64_t st, int64_t sh, int first, int lo,
+                                            int hi) const {
         if (a.group == 1 && first >= lo) {
-            rows(tile, wave, base, st, first, hi);
+            rows(tile, base, st, first, hi);
             return;
         }
         const int t0 = over_group(a, first);
-        const AttnBuf buf = attn_buffer(base + t0 * st);
+        const u4 buf = attn_buffer(base + t0 * st);
+        const Lane p = place();
+        tile += wave * 1024;
 #pragma unroll
         for (int i = 0; i < N; i++) {
-            const int r = first + row_of(i);
+            const int r = first + p.row + i * (NW * RPI);
             const AttnRow q = attn_row(a, r);
             const uint32_t o = (uint32_t)(q.t - t0) * (uint32_t)st + (uint32_t)q.g * (uint32_t)sh;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                buf, (AttnLds)to(tile, wave, i), 16, r >= lo && r < hi ? o + at(i) : BEYOND, 0, 0,
-                0);
+            load_lds16(buf, tile + i * NW * 1024, r >= lo && r < hi ? o + p.piece[i % PER] : BEYOND,
+                       0);
         }
     }
 };
@@ -150,10 +196,15 @@ template <typename T, int PITCH> struct Operands {
     __device__ __forceinline__ void init(int lane) {
         const int h = lane >> 5, r = lane & 31;
         rows = r * (PITCH * 2);
-        x = (h ^ swizzle(r)) << 4;
+        x = (h ^ swizzle<PITCH>(r)) << 4;
         const int k = 4 * h + ((lane >> 2) & 3);
         cols = k * (PITCH * 2) + (lane & 1) * 8;
-        y = ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle(k)) << 4;
+        y = ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle<PITCH>(k)) << 4;
+    }
+    // Has addresses computed again where they are used: kept over a loop, they
+    // take the registers of its operands.
+    __device__ __forceinline__ void refresh() {
+        asm volatile("" : "+v"(rows), "+v"(x), "+v"(cols), "+v"(y));
     }
     // rows 32 b .. of k = 16 s ..
     __device__ __forceinline__ V8 along(const char *tile, int b, int s) const {
@@ -161,9 +212,10 @@ template <typename T, int PITCH> struct Operands {
     }
     // columns 32 n .. of k = rows 16 b .. (counted as results are)
     __device__ __forceinline__ V8 across(const char *tile, int b, int n) const {
-        const char *p = tile + b * 16 * PITCH * 2 + cols + (y ^ (n << 6));
-        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AttnTr)p);
-        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AttnTr)(p + 8 * PITCH * 2));
+        const char *p = tile + b * 16 * PITCH * 2 + cols;
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((AttnTr)(p + (y ^ (n << 6))));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (AttnTr)(p + 8 * PITCH * 2 + (y ^ 32 ^ (n << 6))));
         return __builtin_bit_cast(V8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -175,6 +227,17 @@ row_operand(const T *p, int lane, int s, int d) {
     const int e = 16 * s + 8 * (lane >> 5);
     if (p && e < d) v = *(const typename Tile<T>::V8 *)(p + e);
     return v;
+}
+
+// Has operands loaded from memory land here, not within the loop that uses
+// them, where the wait would be for its prefetch too.
+template <typename V, int N> __device__ __forceinline__ void settle(V (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        u4 t = __builtin_bit_cast(u4, v[i]);
+        asm volatile("" : "+v"(t));
+        v[i] = __builtin_bit_cast(V, t);
+    }
 }
 
 __device__ __forceinline__ float other_half(float v) {
@@ -190,6 +253,12 @@ __device__ __forceinline__ f16v zeros16() {
     return z;
 }
 
+// What the compiler is to schedule next, within its block: reads of LDS well
+// ahead of the products that take them.  (Left alone it has a read land just
+// before each product: 150 clocks for one of 32.)
+constexpr int GROUP_VALU = 0x2, GROUP_MFMA = 0x8, GROUP_READ = 0x100;
+#define ATTN_GROUP(what, n) __builtin_amdgcn_sched_group_barrier(what, n, 0)
+
 // Loads of the wave have landed, and so have those of the others.
 __device__ __forceinline__ void attn_arrive() {
     __builtin_amdgcn_sched_barrier(0);
@@ -198,12 +267,18 @@ __device__ __forceinline__ void attn_arrive() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// A value that all lanes hold, in a scalar register.
+__device__ __forceinline__ float uniform(float v) {
+    return __builtin_bit_cast(float,
+                              __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
 // Workgroup id as (sequence and key head, part of it).  Workgroup i runs on XCD
 // i % 8, and each XCD has an L2 of its own: where that leaves none idle, what
 // reads the same keys runs on the same XCD.
 struct AttnPlace { int b, h, part; };
-__device__ __forceinline__ AttnPlace attn_place(const AttnArgs &a, int parts) {
-    const int id = blockIdx.x, pairs = a.b * a.hkv;
+__device__ __forceinline__ AttnPlace attn_place(const AttnArgs &a, int parts, int id) {
+    const int pairs = a.b * a.hkv;
     int pair, part;
     if (pairs % 8 == 0) {
         pair = (id >> 3) / parts * 8 + (id & 7);
@@ -226,41 +301,39 @@ __device__ __forceinline__ int64_t attn_stats(const AttnArgs &a, int pair, int r
 }
 
 // Keys and values of 64 keys at a time, in one of two stages.
-template <int PITCH, int NW> struct KeyStages {
+template <int PITCH, int NW, bool KEEP> struct KeyStages {
     static constexpr int TILE = 64 * PITCH * 2;
-    Loads<PITCH, 64, NW> ld;
+    Loads<PITCH, 64, NW, KEEP> ld;
     const char *k, *v;
     int64_t ks, vs;
-    int wave, end;
-    char *lds;
+    int end;
+    uint32_t lds;
     template <typename T>
-    __device__ __forceinline__ void init(const AttnArgs &a, const AttnPlace &at, int lane, int w,
-                                         int keys, char *to) {
-        ld.init(lane, w, a.d);
+    __device__ __forceinline__ void init(const AttnArgs &a, const AttnPlace &at, int lane, int wave,
+                                         int keys, const char *to) {
+        ld.init(lane, wave, a.d);
         k = (const char *)((const T *)a.k + at.b * a.ks[0] + at.h * a.ks[2]);
         v = (const char *)((const T *)a.v + at.b * a.vs[0] + at.h * a.vs[2]);
         ks = a.ks[1] * 2;
         vs = a.vs[1] * 2;
-        wave = w;
         end = keys;
-        lds = to;
+        lds = lds_address(to);
     }
     __device__ __forceinline__ void fetch(int key, int stage) const {
-        char *to = lds + stage * 2 * TILE;
-        ld.rows(to, wave, k, ks, key, end);
-        ld.rows(to + TILE, wave, v, vs, key, end);
+        ld.rows(lds + stage * 2 * TILE, k, ks, key, end);
+        ld.rows(lds + stage * 2 * TILE + TILE, v, vs, key, end);
     }
 };
 // Queries and gradients of RT rows, and what attn_rows wrote of them.
-template <int PITCH, int RT> struct RowStages {
+template <int PITCH, int RT, int NW> struct RowStages {
     static constexpr int TILE = RT * PITCH * 2, STAGE = 2 * TILE + RT * 8;
-    Loads<PITCH, RT, 4> ld;
+    Loads<PITCH, RT, NW> ld;
     const char *q, *g;
     int wave, lane, lo, hi, pair;
-    char *lds;
+    uint32_t lds;
     template <typename T>
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnPlace &at, int l, int w,
-                                         int from, int to_row, char *to) {
+                                         int from, int to_row, const char *to) {
         ld.init(l, w, a.d);
         q = (const char *)((const T *)a.q + at.b * a.qs[0] + at.h * a.group * a.qs[2]);
         g = (const char *)((const T *)a.dout + at.b * a.dos[0] + at.h * a.group * a.dos[2]);
@@ -269,16 +342,15 @@ template <int PITCH, int RT> struct RowStages {
         lo = from;
         hi = to_row;
         pair = at.b * a.hkv + at.h;
-        lds = to;
+        lds = lds_address(to);
     }
     __device__ __forceinline__ void fetch(const AttnArgs &a, int r, int stage) const {
-        char *to = lds + stage * STAGE;
-        ld.queries(a, to, wave, q, a.qs[1] * 2, a.qs[2] * 2, r, lo, hi);
-        ld.queries(a, to + TILE, wave, g, a.dos[1] * 2, a.dos[2] * 2, r, lo, hi);
+        const uint32_t to = lds + stage * STAGE;
+        ld.queries(a, to, q, a.qs[1] * 2, a.qs[2] * 2, r, lo, hi);
+        ld.queries(a, to + TILE, g, a.dos[1] * 2, a.dos[2] * 2, r, lo, hi);
         if (wave < RT / 32)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                attn_buffer(a.stats + attn_stats(a, pair, r) + wave * 64),
-                (AttnLds)(to + 2 * TILE + wave * 256), 4, lane * 4, 0, 0, 0);
+            load_lds4(attn_buffer(a.stats + attn_stats(a, pair, r) + wave * 64),
+                      to + 2 * TILE + wave * 256, lane * 4);
     }
 };
 
@@ -298,7 +370,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnPlace at = attn_place(a, a.tiles * a.splits);
+    const AttnPlace at = attn_place(a, a.tiles * a.splits, blockIdx.x);
     const int split = at.part % a.splits;
     const int tile = a.causal ? a.tiles - 1 - at.part / a.splits : at.part / a.splits;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
@@ -330,13 +402,14 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
                         : nullptr;
 #pragma unroll
     for (int s = 0; s < NK; s++) q[s] = row_operand<T>(qp, lane, s, a.d);
+    settle(q);
     f16v acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; n++) acc[n] = zeros16();
     float mc = -INF, l = 0.f;
-    const float c = a.scale * LOG2E;
+    const float c = uniform(a.scale * LOG2E);
 
-    KeyStages<PITCH, NW> in;
+    KeyStages<PITCH, NW, true> in;
     in.template init<T>(a, at, lane, wave, kn, lds);
     Operands<T, PITCH> op;
     op.init(lane);
@@ -354,6 +427,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < NK; i++) s[b] = Tile<T>::mul(op.along(kt, b, i), q[i], s[b]);
         }
+        ATTN_GROUP(GROUP_READ, NK);
+#pragma unroll
+        for (int i = 0; i < NK; i++) {
+            ATTN_GROUP(GROUP_MFMA, 1);
+            ATTN_GROUP(GROUP_READ, 1);
+        }
+        ATTN_GROUP(GROUP_MFMA, NK);
         if (key + KT > least) {
 #pragma unroll
             for (int b = 0; b < 2; b++)
@@ -379,17 +459,48 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
             }
         }
         const float ref = mc == -INF ? 0.f : -mc;
+        // Half of the values' operands are read while the first half of the
+        // probabilities is taken, the rest beside the first products.
+        V8 va[2][ND], pb[2];
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int n = 0; n < ND; n++) va[b][n] = op.across(vt, b, n);
+        __builtin_amdgcn_sched_barrier(0);
         float p[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) p[i] = exp2_hw(__builtin_fmaf(s[i / 16][i % 16], c, ref));
+        for (int i = 0; i < 16; i++) p[i] = exp2_hw(__builtin_fmaf(s[0][i], c, ref));
 #pragma unroll
-        for (int i = 0; i < 32; i++) l += p[i];
+        for (int i = 0; i < 16; i++) l += p[i];
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-            const V8 pb = pack8<T>(p + 8 * b);
+        for (int b = 0; b < 2; b++) pb[b] = pack8<T>(p + 8 * b);
+        __builtin_amdgcn_sched_barrier(0);
+        V8 vc[2][ND];
 #pragma unroll
-            for (int n = 0; n < ND; n++) acc[n] = Tile<T>::mul(op.across(vt, b, n), pb, acc[n]);
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int n = 0; n < ND; n++) {
+                acc[n] = Tile<T>::mul(va[b][n], pb[b], acc[n]);
+                vc[b][n] = op.across(vt, 2 + b, n);
+            }
+#pragma unroll
+        for (int i = 16; i < 32; i++) p[i] = exp2_hw(__builtin_fmaf(s[1][i - 16], c, ref));
+#pragma unroll
+        for (int i = 16; i < 32; i++) l += p[i];
+        V8 pc[2];
+#pragma unroll
+        for (int b = 0; b < 2; b++) pc[b] = pack8<T>(p + 16 + 8 * b);
+#pragma unroll
+        for (int i = 0; i < 2 * ND; i++) {
+            ATTN_GROUP(GROUP_MFMA, 1);
+            ATTN_GROUP(GROUP_READ, 2);
+            ATTN_GROUP(GROUP_VALU, 8);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int n = 0; n < ND; n++) acc[n] = Tile<T>::mul(vc[b][n], pc[b], acc[n]);
     }
     l += other_half(l);
     // (a row that sees nothing: zeros)
@@ -481,7 +592,7 @@ template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArg
 // ---------------------------------------------------------------------------
 template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs a) {
     __shared__ float most[4];
-    const AttnPlace at = attn_place(a, a.q_chunks + a.v_chunks);
+    const AttnPlace at = attn_place(a, a.q_chunks + a.v_chunks, blockIdx.x);
     const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, pair = at.b * a.hkv + at.h;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
     const bool queries = at.part < a.q_chunks;
@@ -567,132 +678,227 @@ template <typename T> __device__ __forceinline__ float attn_exponent(const AttnA
     // log2 of 2 |do| |v|, rounded up
     const float e = 14.f - __builtin_ceilf(1.f + 0.5f * (__builtin_amdgcn_logf(q) +
                                                        __builtin_amdgcn_logf(v)));
-    return e > 15.f ? 15.f : e < -20.f ? -20.f : e;
+    return uniform(e > 15.f ? 15.f : e < -20.f ? -20.f : e);
 }
 
-// dk and dv: a workgroup takes 128 keys, 32 a wave, whose K and V stay in
-// registers as operands, and goes through the rows RT at a time.
-template <typename T, int NK, int ND>
-__global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_keys(AttnArgs a) {
-    typedef typename Tile<T>::V8 V8;
-    constexpr int PITCH = NK <= 4 ? 64 : 128, RT = 64, TILE = RT * PITCH * 2;
-    constexpr int STAGE = RowStages<PITCH, RT>::STAGE;
-    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
-    const int lane = threadIdx.x & 63, h32 = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnPlace at = attn_place(a, a.key_tiles);
-    const int pair = at.b * a.hkv + at.h;
-    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
-    const int key0 = at.part * 128, key = key0 + wave * 32 + (lane & 31);
-    const int lo = a.causal && qn > kn ? (qn - kn) * a.group : 0, hi = kn ? qn * a.group : 0;
-    // first row that sees the lane's key, the wave's last and the workgroup's
-    // first
-    auto seen = [&](int j) {
+// Where a workgroup of attend_keys stands: its keys, and the rows it goes
+// through.
+struct KeyPlace {
+    AttnPlace at;
+    int pair, split, qn, kn, key0, lo, hi, row, end, shift;
+    // first row that sees key j
+    __device__ __forceinline__ int seen(const AttnArgs &a, int j) const {
         if (!a.causal) return 0;
-        const int t = j - (kn - qn);
+        const int t = j - shift;
         return t < 0 ? 0 : t * a.group;
-    };
-    const int from = seen(key), wave_from = seen(key0 + wave * 32 + 31);
-    const int wave_first = seen(key0 + wave * 32);
-    int row = seen(key0) > lo ? seen(key0) : lo;
-    row &= ~(RT - 1);
-
-    const T *kp = key < kn ? (const T *)a.k + at.b * a.ks[0] + key * a.ks[1] + at.h * a.ks[2]
-                           : nullptr;
-    const T *vp = key < kn ? (const T *)a.v + at.b * a.vs[0] + key * a.vs[1] + at.h * a.vs[2]
-                           : nullptr;
-    V8 kf[NK], vf[NK];
-#pragma unroll
-    for (int s = 0; s < NK; s++) kf[s] = row_operand<T>(kp, lane, s, a.d);
-#pragma unroll
-    for (int s = 0; s < NK; s++) vf[s] = row_operand<T>(vp, lane, s, a.d);
-    f16v dk[ND], dv[ND];
-#pragma unroll
-    for (int n = 0; n < ND; n++) dk[n] = dv[n] = zeros16();
-    const float c = a.scale * LOG2E, e = attn_exponent<T>(a, pair);
-
-    RowStages<PITCH, RT> in;
-    in.template init<T>(a, at, lane, wave, lo, hi, lds);
-    Operands<T, PITCH> op;
-    op.init(lane);
-    if (row < hi && key0 < kn) in.fetch(a, row, 0);
-    int stage = 0;
-    for (; row < hi && key0 < kn; row += RT, stage ^= 1) {
-        attn_arrive();
-        if (row + RT < hi) in.fetch(a, row + RT, stage ^ 1);
-        const char *qt = lds + stage * STAGE, *ot = qt + TILE;
-#pragma unroll
-        for (int b = 0; b < RT / 32; b++) {
-            if (row + 32 * b + 32 <= wave_first) continue;
-            const float *st = (const float *)(ot + TILE) + b * 64 + 4 * h32;
-            f16v s, dp;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const f4 x = *(const f4 *)(st + 8 * j), y = *(const f4 *)(st + 32 + 8 * j);
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    s[4 * j + i] = x[i];
-                    dp[4 * j + i] = y[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(qt, b, i), kf[i], s);
-#pragma unroll
-            for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(ot, b, i), vf[i], dp);
-            float p[16], ds[16];
-#pragma unroll
-            for (int i = 0; i < 16; i++) p[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
-            if (a.causal && row + 32 * b < wave_from) {
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (row + 32 * b + 8 * (i / 4) + 4 * h32 + i % 4 < from) p[i] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i++) ds[i] = p[i] * dp[i];
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const V8 pb = pack8<T>(p + 8 * k), sb = pack8<T>(ds + 8 * k);
-#pragma unroll
-                for (int n = 0; n < ND; n++)
-                    dv[n] = Tile<T>::mul(op.across(ot, 2 * b + k, n), pb, dv[n]);
-#pragma unroll
-                for (int n = 0; n < ND; n++)
-                    dk[n] = Tile<T>::mul(op.across(qt, 2 * b + k, n), sb, dk[n]);
-            }
+    }
+    __device__ __forceinline__ KeyPlace(const AttnArgs &a, int rt) {
+        at = attn_place(a, a.key_tiles * a.row_splits, blockIdx.x);
+        pair = at.b * a.hkv + at.h;
+        split = at.part % a.row_splits;
+        qn = attn_length(a.qlen, at.b, a.tq);
+        kn = attn_length(a.klen, at.b, a.tk);
+        shift = kn - qn;
+        key0 = at.part / a.row_splits * 128;
+        lo = a.causal && qn > kn ? (qn - kn) * a.group : 0;
+        hi = key0 < kn ? qn * a.group : 0;
+        const int first = seen(a, key0);
+        row = (first > lo ? first : lo) & ~(rt - 1);
+        end = hi;
+        if (a.row_splits > 1 && row < hi) {
+            const int steps = (hi - row + rt - 1) / rt;
+            const int per = (steps + a.row_splits - 1) / a.row_splits;
+            row += split * per * rt;
+            if (end > row + per * rt) end = row + per * rt;
         }
     }
+};
+// Stores a wave's dk or dv, times `f` (of a range of rows: as partial sums).
+template <typename T, int ND>
+__device__ __forceinline__ void store_keys(const AttnArgs &a, const KeyPlace &p, int key, int h32,
+                                           const f16v (&acc)[ND], float f, bool values) {
     if (key >= a.tk) return;
-    const bool valid = key < kn;
-    const float back = exp2_hw(-e);
-    T *dkp = (T *)a.dk + at.b * a.dks[0] + key * a.dks[1] + at.h * a.dks[2];
-    T *dvp = (T *)a.dv + at.b * a.dvs[0] + key * a.dvs[1] + at.h * a.dvs[2];
+    const bool valid = key < p.kn;
+    if (a.row_splits > 1) {
+        const int64_t i = ((int64_t)p.split * a.b * a.hkv + p.pair) * a.tk + key;
+        float *o = a.part + (i * 2 + values) * a.d;
+#pragma unroll
+        for (int n = 0; n < ND; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int x = n * 32 + j * 8 + 4 * h32;
+                f4 u;
+#pragma unroll
+                for (int z = 0; z < 4; z++) u[z] = valid ? acc[n][4 * j + z] * f : 0.f;
+                if (x < a.d) __builtin_memcpy(o + x, &u, 16);
+            }
+        return;
+    }
+    T *o = values ? (T *)a.dv + p.at.b * a.dvs[0] + key * a.dvs[1] + p.at.h * a.dvs[2]
+                  : (T *)a.dk + p.at.b * a.dks[0] + key * a.dks[1] + p.at.h * a.dks[2];
 #pragma unroll
     for (int n = 0; n < ND; n++)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const int i = n * 32 + j * 8 + 4 * h32;
-            if (i < a.d) {
-                float x[4], y[4];
+            const int x = n * 32 + j * 8 + 4 * h32;
+            float u[4];
 #pragma unroll
-                for (int z = 0; z < 4; z++) {
-                    x[z] = valid ? dk[n][4 * j + z] * (a.scale * back) : 0.f;
-                    y[z] = valid ? dv[n][4 * j + z] * back : 0.f;
-                }
-                store<T, 4>(dkp + i, x);
-                store<T, 4>(dvp + i, y);
-            }
+            for (int z = 0; z < 4; z++) u[z] = valid ? acc[n][4 * j + z] * f : 0.f;
+            if (x < a.d) store<T, 4>(o + x, u);
         }
+}
+// Sixteen first values of a block of rows (as a result holds them).
+__device__ __forceinline__ f16v first_values(const float *st, int h32) {
+    f16v s;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const f4 x = *(const f4 *)(st + 4 * h32 + 8 * j);
+#pragma unroll
+        for (int i = 0; i < 4; i++) s[4 * j + i] = x[i];
+    }
+    return s;
+}
+
+// dk and dv: a workgroup takes 128 keys, 32 a wave, and goes through the rows
+// (or its range of them) RT at a time.  K stays in registers as operands; so
+// does V for heads up to 64; V of wider ones is read from LDS, since the sums
+// leave no more registers to two waves a SIMD.
+template <int NK> struct KeyTiles {
+    static constexpr bool WIDE = NK > 4;
+    static constexpr int PITCH = WIDE ? 128 : 64, RT = WIDE ? 32 : 64, TILE = RT * PITCH * 2;
+    static constexpr int STAGE = RowStages<PITCH, RT, 4>::STAGE;
+    static constexpr int BYTES = 2 * STAGE + (WIDE ? 128 * PITCH * 2 : 0);
+};
+template <typename T, int NK, int ND>
+__device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
+    typedef typename Tile<T>::V8 V8;
+    constexpr bool WIDE = KeyTiles<NK>::WIDE;
+    constexpr int PITCH = KeyTiles<NK>::PITCH, RT = KeyTiles<NK>::RT, TILE = KeyTiles<NK>::TILE;
+    constexpr int STAGE = KeyTiles<NK>::STAGE;
+    const int lane = threadIdx.x & 63, h32 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const KeyPlace p(a, RT);
+    const int key = p.key0 + wave * 32 + (lane & 31), from = p.seen(a, key);
+    const int wave_from = p.seen(a, p.key0 + wave * 32 + 31);
+    const int wave_first = p.seen(a, p.key0 + wave * 32);
+
+    const T *vb = (const T *)a.v + p.at.b * a.vs[0] + p.at.h * a.vs[2];
+    const T *kp = nullptr, *vp = nullptr;
+    if (key < p.kn) {
+        kp = (const T *)a.k + p.at.b * a.ks[0] + key * a.ks[1] + p.at.h * a.ks[2];
+        vp = vb + key * a.vs[1];
+    }
+    const char *vt = lds + 2 * STAGE + wave * 32 * PITCH * 2;
+    V8 kf[NK], vf[WIDE ? 1 : NK];
+#pragma unroll
+    for (int s = 0; s < NK; s++) kf[s] = row_operand<T>(kp, lane, s, a.d);
+    if constexpr (WIDE) {
+        Loads<PITCH, 128, 4> ld;
+        ld.init(lane, wave, a.d);
+        ld.rows(lds_address(lds + 2 * STAGE), (const char *)vb, a.vs[1] * 2, p.key0, p.kn);
+    } else {
+#pragma unroll
+        for (int s = 0; s < NK; s++) vf[s] = row_operand<T>(vp, lane, s, a.d);
+        settle(vf);
+    }
+    settle(kf);
+    f16v dk[ND], dv[ND];
+#pragma unroll
+    for (int n = 0; n < ND; n++) dk[n] = dv[n] = zeros16();
+    const float c = uniform(a.scale * LOG2E), e = attn_exponent<T>(a, p.pair);
+    Operands<T, PITCH> op;
+    op.init(lane);
+
+    RowStages<PITCH, RT, 4> in;
+    in.template init<T>(a, p.at, lane, wave, p.lo, p.hi, lds);
+    if (p.row < p.end) in.fetch(a, p.row, 0);
+    int stage = 0;
+    for (int row = p.row; row < p.end; row += RT, stage ^= 1) {
+        attn_arrive();
+        if (row + RT < p.end) in.fetch(a, row + RT, stage ^ 1);
+        const char *qt = lds + stage * STAGE, *ot = qt + TILE;
+        if (WIDE) op.refresh();
+#pragma unroll
+        for (int b = 0; b < RT / 32; b++) {
+            const int r = row + 32 * b;
+            if (r + 32 <= wave_first) continue;
+            f16v s = first_values((const float *)(ot + TILE) + b * 64, h32);
+#pragma unroll
+            for (int i = 0; i < NK; i++) {
+                s = Tile<T>::mul(op.along(qt, b, i), kf[i], s);
+                if (WIDE && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+            // (phases of their own: operands read ahead of them would not fit)
+            if (WIDE) __builtin_amdgcn_sched_barrier(0);
+            f16v dp = first_values((const float *)(ot + TILE) + b * 64 + 32, h32);
+#pragma unroll
+            for (int i = 0; i < NK; i++) {
+                dp = Tile<T>::mul(op.along(ot, b, i), WIDE ? op.along(vt, 0, i) : vf[WIDE ? 0 : i],
+                                  dp);
+                if (WIDE && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+            float x[16], y[16];
+#pragma unroll
+            for (int i = 0; i < 16; i++) x[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+#pragma unroll
+            for (int i = 0; i < 16; i++) y[i] = x[i] * dp[i];
+            if (r < wave_from) {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (r + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = y[i] = 0.f;
+            }
+            V8 pb[2], sb[2];
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                pb[k] = pack8<T>(x + 8 * k);
+                sb[k] = pack8<T>(y + 8 * k);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int n = 0; n < ND; n++)
+                    dv[n] = Tile<T>::mul(op.across(ot, 2 * b + k, n), pb[k], dv[n]);
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int n = 0; n < ND; n++)
+                    dk[n] = Tile<T>::mul(op.across(qt, 2 * b + k, n), sb[k], dk[n]);
+            if (WIDE) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    const float back = exp2_hw(-e);
+    store_keys<T, ND>(a, p, key, h32, dk, a.scale * back, false);
+    store_keys<T, ND>(a, p, key, h32, dv, back, true);
+}
+// Adds up the ranges' dk and dv, always in the same order: four values a lane.
+template <typename T> __global__ __launch_bounds__(256) void attend_keys_join(AttnArgs a) {
+    const int per = a.d / 2;                     // lanes of a key
+    const int64_t keys = (int64_t)a.b * a.hkv * a.tk, all = keys * per;
+    const int64_t i = (int64_t)workgroup() * 256 + threadIdx.x;
+    if (i >= all) return;
+    const int64_t key = i / per;
+    const int x = (int)(i - key * per) * 4;
+    f4 sum = (f4)(0.f);
+#pragma unroll 4
+    for (int s = 0; s < a.row_splits; s++) {
+        f4 v;
+        __builtin_memcpy(&v, a.part + ((int64_t)s * keys + key) * 2 * a.d + x, 16);
+        sum += v;
+    }
+    const int64_t pair = key / a.tk, j = key - pair * a.tk, b = pair / a.hkv, h = pair - b * a.hkv;
+    const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    if (x < a.d) store<T, 4>((T *)a.dk + b * a.dks[0] + j * a.dks[1] + h * a.dks[2] + x, v);
+    else store<T, 4>((T *)a.dv + b * a.dvs[0] + j * a.dvs[1] + h * a.dvs[2] + x - a.d, v);
 }
 
 // dq: like the forward pass, 32 rows a wave, the keys 64 at a time.
 template <typename T, int NK, int ND>
-__global__ __launch_bounds__(256, 2) void attend_queries(AttnArgs a) {
+__device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int id) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnPlace at = attn_place(a, a.tiles);
+    const AttnPlace at = attn_place(a, a.tiles, id);
     const int tile = a.causal ? a.tiles - 1 - at.part : at.part;
     const int pair = at.b * a.hkv + at.h;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
@@ -723,14 +929,16 @@ __global__ __launch_bounds__(256, 2) void attend_queries(AttnArgs a) {
     for (int s = 0; s < NK; s++) q[s] = row_operand<T>(qp, lane, s, a.d);
 #pragma unroll
     for (int s = 0; s < NK; s++) g[s] = row_operand<T>(op_, lane, s, a.d);
+    settle(q);
+    settle(g);
     f16v acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; n++) acc[n] = zeros16();
-    const float c = a.scale * LOG2E, e = attn_exponent<T>(a, pair);
+    const float c = uniform(a.scale * LOG2E), e = attn_exponent<T>(a, pair);
     const float *st = a.stats + attn_stats(a, pair, r < a.row_tiles * 32 ? r : 0);
     const float first_s = valid ? st[0] : -INF, first_dp = valid ? st[32] : 0.f;
 
-    KeyStages<PITCH, 4> in;
+    KeyStages<PITCH, 4, false> in;
     in.template init<T>(a, at, lane, wave, kn, lds);
     Operands<T, PITCH> op;
     op.init(lane);
@@ -744,6 +952,7 @@ __global__ __launch_bounds__(256, 2) void attend_queries(AttnArgs a) {
 #pragma unroll
         for (int b = 0; b < 2; b++) {
             f16v s, dp;
+            if (NK > 4) op.refresh();
 #pragma unroll
             for (int i = 0; i < 16; i++) s[i] = first_s, dp[i] = first_dp;
 #pragma unroll
@@ -784,6 +993,17 @@ __global__ __launch_bounds__(256, 2) void attend_queries(AttnArgs a) {
         }
 }
 
+// Both in one launch, so that workgroups of the second kind fill the CUs that
+// those of the first, which take longer, leave idle at their end.
+template <typename T, int NK, int ND>
+__global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
+    constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;
+    __shared__ __attribute__((aligned(16))) char lds[Q > K ? Q : K];
+    const int keys = a.b * a.hkv * a.key_tiles * a.row_splits;
+    if ((int)blockIdx.x < keys) attend_keys<T, NK, ND>(a, lds);
+    else attend_queries<T, NK, ND>(a, lds, blockIdx.x - keys);
+}
+
 // ------------------------------------------------------------------- host
 
 static int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -798,7 +1018,7 @@ static void attn_group(AttnArgs &a) {
     a.gshift = l ? l - 1 : 0;
 }
 // Waves of a workgroup and ranges of keys.
-struct AttnPlan { int waves, tiles, splits, per; };
+struct AttnPlan { int waves, tiles, splits, per, row_splits; };
 static AttnPlan attn_plan(const AttnArgs &a) {
     AttnPlan p;
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
@@ -811,17 +1031,24 @@ static AttnPlan attn_plan(const AttnArgs &a) {
     if (s < 1) s = 1;
     p.per = (int)(ceil_of(steps, s) * 64);
     p.splits = a.tk ? (int)ceil_of(a.tk, p.per) : 1;
+    // the same for the rows of the keys' gradients, of 64 at a time
+    const int64_t key_wgs = pairs * ceil_of(a.tk, 128), row_steps = ceil_of(rows, 64);
+    s = 512 / (key_wgs ? key_wgs : 1);
+    if (s > row_steps / 4) s = row_steps / 4;
+    p.row_splits = s < 1 ? 1 : (int)s;
     return p;
 }
 size_t attention_workspace(const AttnArgs &in, bool backward) {
     AttnArgs a = in;
     attn_group(a);
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    const AttnPlan p = attn_plan(a);
     if (backward) {
         const int64_t tiles = ceil_of(rows, 64) * 2, chunks = ceil_of(rows, 64) + ceil_of(a.tk, 64);
-        return (size_t)(pairs * (tiles * 64 + chunks) * 4);
+        const int64_t stats = (pairs * (tiles * 64 + chunks) + 3) / 4 * 4;
+        const int64_t sums = p.row_splits > 1 ? p.row_splits * pairs * a.tk * 2 * a.d : 0;
+        return (size_t)((stats + sums) * 4);
     }
-    const AttnPlan p = attn_plan(a);
     if (p.splits == 1) return 0;
     return (size_t)(p.splits * pairs * rows * (a.d + 1) * 4);
 }
@@ -849,11 +1076,12 @@ template <typename T, int NK, int ND> struct Attend {
 template <typename T, int NK, int ND> struct AttendBackward {
     static hipError_t go(const AttnArgs &a, hipStream_t st) {
         const int64_t pairs = (int64_t)a.b * a.hkv;
+        const int64_t wgs = pairs * ((int64_t)a.key_tiles * a.row_splits + a.tiles);
         hipError_t e = hipSuccess;
-        if (a.key_tiles)
-            e = start(attend_keys<T, NK, ND>, dim3((unsigned)(pairs * a.key_tiles)), 256, st, a);
-        if (e == hipSuccess && a.tiles)
-            e = start(attend_queries<T, NK, ND>, dim3((unsigned)(pairs * a.tiles)), 256, st, a);
+        if (wgs) e = start(attend_backward<T, NK, ND>, dim3((unsigned)wgs), 256, st, a);
+        if (e == hipSuccess && a.row_splits > 1)
+            e = start(attend_keys_join<T>, grid_of(ceil_of(pairs * a.tk * (a.d / 2), 256)), 256, st,
+                      a);
         return e;
     }
 };
@@ -883,8 +1111,10 @@ hipError_t launch_attention_backward(const AttnArgs &in, hipStream_t st) {
     a.tiles = (int)ceil_of(rows, 128);
     a.key_tiles = (int)ceil_of(a.tk, 128);
     a.splits = 1;
+    a.row_splits = attn_plan(a).row_splits;
     a.stats = a.ws;
     a.bounds = a.ws + pairs * a.row_tiles * 64;
+    a.part = a.ws + (pairs * (a.row_tiles * 64 + ceil_of(rows, 64) + ceil_of(a.tk, 64)) + 3) / 4 * 4;
     hipError_t e = hipSuccess;
     if (a.q_chunks + a.v_chunks) {
         const dim3 grid((unsigned)(pairs * (a.q_chunks + a.v_chunks)));

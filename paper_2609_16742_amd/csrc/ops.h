@@ -90,7 +90,7 @@ struct AttnArgs {
     void *dq, *dk, *dv;
     float *ws;
     // set by the launchers
-    int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks;
+    int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks, row_splits;
     uint32_t gmul;
     float *part, *part_lse, *stats, *bounds;
 };
