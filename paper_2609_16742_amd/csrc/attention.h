@@ -421,6 +421,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
         if (key >= wave_most) continue;
         const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
         f16v s[2];
+        if (NK > 4) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < 2; b++) {
             s[b] = zeros16();
@@ -434,6 +435,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
             ATTN_GROUP(GROUP_READ, 1);
         }
         ATTN_GROUP(GROUP_MFMA, NK);
+        if (NK > 4) __builtin_amdgcn_s_setprio(0);
         if (key + KT > least) {
 #pragma unroll
             for (int b = 0; b < 2; b++)
@@ -475,6 +477,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
 #pragma unroll
         for (int b = 0; b < 2; b++) pb[b] = pack8<T>(p + 8 * b);
         __builtin_amdgcn_sched_barrier(0);
+        if (NK > 4) __builtin_amdgcn_s_setprio(1);
         V8 vc[2][ND];
 #pragma unroll
         for (int b = 0; b < 2; b++)
@@ -501,6 +504,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int n = 0; n < ND; n++) acc[n] = Tile<T>::mul(vc[b][n], pc[b], acc[n]);
+        if (NK > 4) __builtin_amdgcn_s_setprio(0);
     }
     l += other_half(l);
     // (a row that sees nothing: zeros)
@@ -822,24 +826,40 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
         for (int b = 0; b < RT / 32; b++) {
             const int r = row + 32 * b;
             if (r + 32 <= wave_first) continue;
+            if (WIDE) __builtin_amdgcn_s_setprio(1);
             f16v s = first_values((const float *)(ot + TILE) + b * 64, h32);
 #pragma unroll
-            for (int i = 0; i < NK; i++) {
-                s = Tile<T>::mul(op.along(qt, b, i), kf[i], s);
-                if (WIDE && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
-            // (phases of their own: operands read ahead of them would not fit)
-            if (WIDE) __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(qt, b, i), kf[i], s);
             f16v dp = first_values((const float *)(ot + TILE) + b * 64 + 32, h32);
 #pragma unroll
-            for (int i = 0; i < NK; i++) {
+            for (int i = 0; i < NK; i++)
                 dp = Tile<T>::mul(op.along(ot, b, i), WIDE ? op.along(vt, 0, i) : vf[WIDE ? 0 : i],
                                   dp);
-                if (WIDE && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
             float x[16], y[16];
 #pragma unroll
             for (int i = 0; i < 16; i++) x[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            if (WIDE) {
+                // 8 + 3 NK reads
+                ATTN_GROUP(GROUP_READ, 4 + NK);
+#pragma unroll
+                for (int i = 0; i < NK / 2; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 1);
+                }
+#pragma unroll
+                for (int i = 0; i < NK / 2; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 2);
+                }
+#pragma unroll
+                for (int i = 0; i < NK; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 1);
+                    ATTN_GROUP(GROUP_VALU, 4);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
+            }
 #pragma unroll
             for (int i = 0; i < 16; i++) y[i] = x[i] * dp[i];
             if (r < wave_from) {
@@ -847,6 +867,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
                 for (int i = 0; i < 16; i++)
                     if (r + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = y[i] = 0.f;
             }
+            if (WIDE) __builtin_amdgcn_s_setprio(1);
             V8 pb[2], sb[2];
 #pragma unroll
             for (int k = 0; k < 2; k++) {
@@ -863,7 +884,17 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
 #pragma unroll
                 for (int n = 0; n < ND; n++)
                     dk[n] = Tile<T>::mul(op.across(qt, 2 * b + k, n), sb[k], dk[n]);
-            if (WIDE) __builtin_amdgcn_sched_barrier(0);
+            if (WIDE) {
+                ATTN_GROUP(GROUP_READ, 8);
+#pragma unroll
+                for (int i = 0; i < 4 * ND - 4; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 2);
+                }
+                ATTN_GROUP(GROUP_MFMA, 4);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
+            }
         }
     }
     const float back = exp2_hw(-e);
@@ -953,6 +984,7 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
         for (int b = 0; b < 2; b++) {
             f16v s, dp;
             if (NK > 4) op.refresh();
+            if (NK > 4) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < 16; i++) s[i] = first_s, dp[i] = first_dp;
 #pragma unroll
@@ -961,18 +993,49 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
             for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(vt, b, i), g[i], dp);
             float ds[16];
 #pragma unroll
-            for (int i = 0; i < 16; i++) ds[i] = exp2_hw(__builtin_fmaf(s[i], c, e)) * dp[i];
+            for (int i = 0; i < 16; i++) ds[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            if (NK > 4) {
+                ATTN_GROUP(GROUP_READ, 6);
+#pragma unroll
+                for (int i = 0; i < NK; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 1);
+                }
+#pragma unroll
+                for (int i = 0; i < NK; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 1);
+                    ATTN_GROUP(GROUP_VALU, 4);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++) ds[i] *= dp[i];
             if (key + KT > least) {
 #pragma unroll
                 for (int i = 0; i < 16; i++)
                     if (key + b * 32 + 8 * (i / 4) + 4 * h32 + i % 4 >= lim) ds[i] = 0.f;
             }
+            if (NK > 4) __builtin_amdgcn_s_setprio(1);
+            V8 sb[2];
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const V8 sb = pack8<T>(ds + 8 * k);
+            for (int k = 0; k < 2; k++) sb[k] = pack8<T>(ds + 8 * k);
+#pragma unroll
+            for (int k = 0; k < 2; k++)
 #pragma unroll
                 for (int n = 0; n < ND; n++)
-                    acc[n] = Tile<T>::mul(op.across(kt, 2 * b + k, n), sb, acc[n]);
+                    acc[n] = Tile<T>::mul(op.across(kt, 2 * b + k, n), sb[k], acc[n]);
+            if (NK > 4) {
+                ATTN_GROUP(GROUP_READ, 8);
+#pragma unroll
+                for (int i = 0; i < 2 * ND - 4; i++) {
+                    ATTN_GROUP(GROUP_MFMA, 1);
+                    ATTN_GROUP(GROUP_READ, 2);
+                }
+                ATTN_GROUP(GROUP_MFMA, 4);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
             }
         }
     }
