@@ -507,7 +507,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
         if (NK > 4) __builtin_amdgcn_s_setprio(0);
     }
     l += other_half(l);
-    // (a row that sees nothing: zeros)
+    // (a row that sees nothing, or is none: zeros)
+    if (!valid) l = 0.f;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float lse2 = l == 0.f ? -INF : mc + __builtin_amdgcn_logf(l);
     if (r >= a.tq * a.group) return;
@@ -522,7 +523,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
                 if (e < a.d) {
                     f4 v;
 #pragma unroll
-                    for (int x = 0; x < 4; x++) v[x] = acc[n][4 * j + x] * inv;
+                    for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * inv : 0.f;
                     __builtin_memcpy(o + e, &v, 16);
                 }
             }
@@ -543,40 +544,41 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
                 store<T, 4>(o + e, v);
             }
         }
-    if (!h32) a.lse[((int64_t)at.b * a.hq + head) * a.tq + row.t] = valid ? lse2 * LN2 : -INF;
+    if (!h32) a.lse[((int64_t)at.b * a.hq + head) * a.tq + row.t] = lse2 * LN2;
 }
 
-// Joins the ranges of keys of a row: a wave a row.
+// Joins the ranges of keys of a row: four values a lane.
 template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArgs a) {
-    const int lane = threadIdx.x & 63;
+    const int per = a.d / 4;
     const int64_t rows = (int64_t)a.b * a.hkv * a.tq * a.group;
-    const int64_t i = (int64_t)workgroup() * 4 + (threadIdx.x >> 6);
+    const int64_t n = (int64_t)workgroup() * 256 + threadIdx.x, i = n / per;
     if (i >= rows) return;
-    const int r = (int)(i % (a.tq * a.group));
-    const int pair = (int)(i / (a.tq * a.group));
+    const int x = (int)(n - i * per) * 4;
     float m = -INF;
-    for (int s = lane; s < a.splits; s += 64) m = vmax(m, a.part_lse[s * rows + i]);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) m = vmax(m, __shfl_xor(m, o));
-    const float ref = m == -INF ? 0.f : m;
-    float l = 0.f, v[2] = {0.f, 0.f};
+#pragma unroll 8
     for (int s = 0; s < a.splits; s++) {
+        const float v = a.part_lse[s * rows + i];
+        m = v > m ? v : m;
+    }
+    const float ref = m == -INF ? 0.f : m;
+    float l = 0.f;
+    f4 sum = (f4)(0.f);
+#pragma unroll 8
+    for (int s = 0; s < a.splits; s++) {
+        f4 v;
+        __builtin_memcpy(&v, a.part + (s * rows + i) * a.d + x, 16);
         const float w = exp2_hw(a.part_lse[s * rows + i] - ref);
         l += w;
-        const float *p = a.part + (s * rows + i) * a.d + lane;
-#pragma unroll
-        for (int e = 0; e < 2; e++)
-            if (lane + 64 * e < a.d) v[e] += w * p[64 * e];
+        sum += w * v;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const AttnRow row = attn_row(a, r);
-    const int b = pair / a.hkv, head = pair % a.hkv * a.group + row.g;
-    T *o = (T *)a.o + b * a.os[0] + row.t * a.os[1] + head * a.os[2];
-#pragma unroll
-    for (int e = 0; e < 2; e++)
-        if (lane + 64 * e < a.d) o[lane + 64 * e] = narrow<T>(v[e] * inv);
-    if (lane == 0)
-        a.lse[((int64_t)b * a.hq + head) * a.tq + row.t] =
+    const int64_t pair = i / (a.tq * a.group);
+    const AttnRow row = attn_row(a, (int)(i - pair * (a.tq * a.group)));
+    const int64_t b = pair / a.hkv, head = (pair - b * a.hkv) * a.group + row.g;
+    const float v[4] = {sum[0] * inv, sum[1] * inv, sum[2] * inv, sum[3] * inv};
+    store<T, 4>((T *)a.o + b * a.os[0] + row.t * a.os[1] + head * a.os[2] + x, v);
+    if (x == 0)
+        a.lse[(b * a.hq + head) * a.tq + row.t] =
             l == 0.f ? -INF : (ref + __builtin_amdgcn_logf(l)) * LN2;
 }
 
@@ -901,25 +903,42 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
     store_keys<T, ND>(a, p, key, h32, dk, a.scale * back, false);
     store_keys<T, ND>(a, p, key, h32, dv, back, true);
 }
-// Adds up the ranges' dk and dv, always in the same order: four values a lane.
-template <typename T> __global__ __launch_bounds__(256) void attend_keys_join(AttnArgs a) {
-    const int per = a.d / 2;                     // lanes of a key
-    const int64_t keys = (int64_t)a.b * a.hkv * a.tk, all = keys * per;
-    const int64_t i = (int64_t)workgroup() * 256 + threadIdx.x;
-    if (i >= all) return;
-    const int64_t key = i / per;
-    const int x = (int)(i - key * per) * 4;
+// Adds up the ranges' gradients, always in the same order: four values a lane,
+// dq's rows first, then dk and dv of each key.
+template <typename T> __global__ __launch_bounds__(256) void attend_sums(AttnArgs a) {
+    const int64_t pairs = (int64_t)a.b * a.hkv, rows = pairs * a.tq * a.group;
+    const int64_t keys = pairs * a.tk;
+    int64_t n = (int64_t)workgroup() * 256 + threadIdx.x;
+    const int64_t dq = a.q_splits > 1 ? rows * (a.d / 4) : 0;
+    const bool query = n < dq;
+    if (!query) n -= dq;
+    const int per = query ? a.d / 4 : a.d / 2, splits = query ? a.q_splits : a.row_splits;
+    const int64_t i = n / per;
+    if (!query && (a.row_splits < 2 || i >= keys)) return;
+    int x = (int)(n - i * per) * 4;
+    const float *p = (query ? a.part_q : a.part) + i * (4 * per) + x;
+    const int64_t step = (query ? rows : keys) * (4 * per);
     f4 sum = (f4)(0.f);
-#pragma unroll 4
-    for (int s = 0; s < a.row_splits; s++) {
+#pragma unroll 8
+    for (int s = 0; s < splits; s++) {
         f4 v;
-        __builtin_memcpy(&v, a.part + ((int64_t)s * keys + key) * 2 * a.d + x, 16);
+        __builtin_memcpy(&v, p + s * step, 16);
         sum += v;
     }
-    const int64_t pair = key / a.tk, j = key - pair * a.tk, b = pair / a.hkv, h = pair - b * a.hkv;
     const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    if (x < a.d) store<T, 4>((T *)a.dk + b * a.dks[0] + j * a.dks[1] + h * a.dks[2] + x, v);
-    else store<T, 4>((T *)a.dv + b * a.dvs[0] + j * a.dvs[1] + h * a.dvs[2] + x - a.d, v);
+    const int64_t of = query ? a.tq * a.group : a.tk, pair = i / of, j = i - pair * of;
+    const int64_t b = pair / a.hkv, h = pair - b * a.hkv;
+    T *o;
+    if (query) {
+        const AttnRow row = attn_row(a, (int)j);
+        o = (T *)a.dq + b * a.dqs[0] + row.t * a.dqs[1] + (h * a.group + row.g) * a.dqs[2];
+    } else if (x < a.d) {
+        o = (T *)a.dk + b * a.dks[0] + j * a.dks[1] + h * a.dks[2];
+    } else {
+        o = (T *)a.dv + b * a.dvs[0] + j * a.dvs[1] + h * a.dvs[2];
+        x -= a.d;
+    }
+    store<T, 4>(o + x, v);
 }
 
 // dq: like the forward pass, 32 rows a wave, the keys 64 at a time.
@@ -929,8 +948,9 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const AttnPlace at = attn_place(a, a.tiles, id);
-    const int tile = a.causal ? a.tiles - 1 - at.part : at.part;
+    const AttnPlace at = attn_place(a, a.tiles * a.q_splits, id);
+    const int split = at.part % a.q_splits;
+    const int tile = a.causal ? a.tiles - 1 - at.part / a.q_splits : at.part / a.q_splits;
     const int pair = at.b * a.hkv + at.h;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
     const int r0 = tile * 128, R = qn * a.group;
@@ -973,11 +993,17 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
     in.template init<T>(a, at, lane, wave, kn, lds);
     Operands<T, PITCH> op;
     op.init(lane);
-    if (most) in.fetch(0, 0);
+    int k0 = 0, k1 = most;
+    if (a.q_splits > 1) {
+        const int per = ((most + KT - 1) / KT + a.q_splits - 1) / a.q_splits * KT;
+        k0 = split * per;
+        if (k1 > k0 + per) k1 = k0 + per;
+    }
+    if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
-    for (int key = 0; key < most; key += KT, stage ^= 1) {
+    for (int key = k0; key < k1; key += KT, stage ^= 1) {
         attn_arrive();
-        if (key + KT < most) in.fetch(key + KT, stage ^ 1);
+        if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
         if (key >= wave_most) continue;
         const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
 #pragma unroll
@@ -1041,6 +1067,20 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
     }
     if (r >= a.tq * a.group) return;
     const float back = a.scale * exp2_hw(-e);
+    if (a.q_splits > 1) {
+        float *o = a.part_q + (((int64_t)split * a.b * a.hkv + pair) * a.tq * a.group + r) * a.d;
+#pragma unroll
+        for (int n = 0; n < ND; n++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int i = n * 32 + j * 8 + 4 * h32;
+                f4 v;
+#pragma unroll
+                for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * back : 0.f;
+                if (i < a.d) __builtin_memcpy(o + i, &v, 16);
+            }
+        return;
+    }
     T *o = (T *)a.dq + at.b * a.dqs[0] + row.t * a.dqs[1] + head * a.dqs[2];
 #pragma unroll
     for (int n = 0; n < ND; n++)
@@ -1080,37 +1120,49 @@ static void attn_group(AttnArgs &a) {
     a.gmul = l ? (uint32_t)((((uint64_t)1 << (31 + l)) + a.group - 1) / a.group) : 0;
     a.gshift = l ? l - 1 : 0;
 }
-// Waves of a workgroup and ranges of keys.
-struct AttnPlan { int waves, tiles, splits, per, row_splits; };
-static AttnPlan attn_plan(const AttnArgs &a) {
+// How a call is cut up.  Ranges of keys or rows, where the tiles alone would
+// leave CUs idle: as many as give two workgroups a CU, of four steps of 64 at
+// least (a range writes sums of fp32, which a second launch adds up).
+static int64_t attn_ranges(int64_t workgroups, int64_t steps) {
+    const int64_t s = workgroups ? 512 / workgroups : 1;
+    const int64_t n = s < steps / 4 ? s : steps / 4;
+    return n < 1 ? 1 : n;
+}
+// waves of a workgroup; forward: tiles of rows, ranges of keys of `per`;
+// backward: tiles of rows and keys, their ranges of keys and rows
+struct AttnPlan { int waves, tiles, splits, per, row_splits, q_splits; };
+static AttnPlan attn_plan(const AttnArgs &a, bool backward) {
     AttnPlan p;
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
-    p.waves = rows <= 32 ? 1 : 4;
+    p.waves = rows <= 32 && !backward ? 1 : 4;
     p.tiles = (int)ceil_of(rows, p.waves * 32);
-    const int64_t steps = ceil_of(a.tk, 64), wgs = pairs * p.tiles;
-    // as many ranges as give every CU two workgroups, of four steps at least
-    int64_t s = 512 / (wgs ? wgs : 1);
-    if (s > steps / 4) s = steps / 4;
-    if (s < 1) s = 1;
-    p.per = (int)(ceil_of(steps, s) * 64);
+    const int64_t steps = ceil_of(a.tk, 64), n = attn_ranges(pairs * p.tiles, steps);
+    p.per = (int)(ceil_of(steps, n) * 64);
     p.splits = a.tk ? (int)ceil_of(a.tk, p.per) : 1;
-    // the same for the rows of the keys' gradients, of 64 at a time
-    const int64_t key_wgs = pairs * ceil_of(a.tk, 128), row_steps = ceil_of(rows, 64);
-    s = 512 / (key_wgs ? key_wgs : 1);
-    if (s > row_steps / 4) s = row_steps / 4;
-    p.row_splits = s < 1 ? 1 : (int)s;
+    p.q_splits = (int)n;
+    p.row_splits = (int)attn_ranges(pairs * ceil_of(a.tk, 128), ceil_of(rows, 64));
     return p;
+}
+// Floats of the backward pass's workspace: what attn_rows writes, sums of dk
+// and dv, sums of dq.
+struct AttnSpace { int64_t stats, bounds, keys, queries; };
+static AttnSpace attn_space(const AttnArgs &a, const AttnPlan &p) {
+    const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
+    AttnSpace s;
+    s.stats = pairs * ceil_of(rows, 64) * 128;
+    s.bounds = (pairs * (ceil_of(rows, 64) + ceil_of(a.tk, 64)) + 3) / 4 * 4;
+    s.keys = p.row_splits > 1 ? p.row_splits * pairs * a.tk * 2 * a.d : 0;
+    s.queries = p.q_splits > 1 ? p.q_splits * pairs * rows * a.d : 0;
+    return s;
 }
 size_t attention_workspace(const AttnArgs &in, bool backward) {
     AttnArgs a = in;
     attn_group(a);
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
-    const AttnPlan p = attn_plan(a);
+    const AttnPlan p = attn_plan(a, backward);
     if (backward) {
-        const int64_t tiles = ceil_of(rows, 64) * 2, chunks = ceil_of(rows, 64) + ceil_of(a.tk, 64);
-        const int64_t stats = (pairs * (tiles * 64 + chunks) + 3) / 4 * 4;
-        const int64_t sums = p.row_splits > 1 ? p.row_splits * pairs * a.tk * 2 * a.d : 0;
-        return (size_t)((stats + sums) * 4);
+        const AttnSpace s = attn_space(a, p);
+        return (size_t)((s.stats + s.bounds + s.keys + s.queries) * 4);
     }
     if (p.splits == 1) return 0;
     return (size_t)(p.splits * pairs * rows * (a.d + 1) * 4);
@@ -1139,12 +1191,14 @@ template <typename T, int NK, int ND> struct Attend {
 template <typename T, int NK, int ND> struct AttendBackward {
     static hipError_t go(const AttnArgs &a, hipStream_t st) {
         const int64_t pairs = (int64_t)a.b * a.hkv;
-        const int64_t wgs = pairs * ((int64_t)a.key_tiles * a.row_splits + a.tiles);
+        const int64_t wgs =
+            pairs * ((int64_t)a.key_tiles * a.row_splits + (int64_t)a.tiles * a.q_splits);
         hipError_t e = hipSuccess;
         if (wgs) e = start(attend_backward<T, NK, ND>, dim3((unsigned)wgs), 256, st, a);
-        if (e == hipSuccess && a.row_splits > 1)
-            e = start(attend_keys_join<T>, grid_of(ceil_of(pairs * a.tk * (a.d / 2), 256)), 256, st,
-                      a);
+        const int64_t lanes = (a.q_splits > 1 ? pairs * a.tq * a.group * (a.d / 4) : 0) +
+                              (a.row_splits > 1 ? pairs * a.tk * (a.d / 2) : 0);
+        if (e == hipSuccess && lanes)
+            e = start(attend_sums<T>, grid_of(ceil_of(lanes, 256)), 256, st, a);
         return e;
     }
 };
@@ -1152,14 +1206,14 @@ template <typename T, int NK, int ND> struct AttendBackward {
 hipError_t launch_attention(const AttnArgs &in, hipStream_t st) {
     AttnArgs a = in;
     attn_group(a);
-    const AttnPlan p = attn_plan(a);
+    const AttnPlan p = attn_plan(a, false);
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
     a.waves = p.waves; a.tiles = p.tiles; a.splits = p.splits; a.per = p.per;
     a.part = a.ws;
     a.part_lse = a.ws + p.splits * pairs * rows * a.d;
     const hipError_t e = by_form<Attend>(a, st);
     if (e != hipSuccess || p.splits == 1) return e;
-    const dim3 join = grid_of(ceil_of(pairs * rows, 4));
+    const dim3 join = grid_of(ceil_of(pairs * rows * (a.d / 4), 256));
     return a.type == F16 ? start(attend_join<_Float16>, join, 256, st, a)
                          : start(attend_join<__bf16>, join, 256, st, a);
 }
@@ -1173,11 +1227,14 @@ hipError_t launch_attention_backward(const AttnArgs &in, hipStream_t st) {
     a.v_chunks = a.type == F16 ? (int)ceil_of(a.tk, 64) : 0;
     a.tiles = (int)ceil_of(rows, 128);
     a.key_tiles = (int)ceil_of(a.tk, 128);
-    a.splits = 1;
-    a.row_splits = attn_plan(a).row_splits;
+    const AttnPlan p = attn_plan(a, true);
+    const AttnSpace s = attn_space(a, p);
+    a.row_splits = p.row_splits;
+    a.q_splits = p.q_splits;
     a.stats = a.ws;
-    a.bounds = a.ws + pairs * a.row_tiles * 64;
-    a.part = a.ws + (pairs * (a.row_tiles * 64 + ceil_of(rows, 64) + ceil_of(a.tk, 64)) + 3) / 4 * 4;
+    a.bounds = a.stats + s.stats;
+    a.part = a.bounds + s.bounds;
+    a.part_q = a.part + s.keys;
     hipError_t e = hipSuccess;
     if (a.q_chunks + a.v_chunks) {
         const dim3 grid((unsigned)(pairs * (a.q_chunks + a.v_chunks)));

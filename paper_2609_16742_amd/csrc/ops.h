@@ -90,9 +90,9 @@ struct AttnArgs {
     void *dq, *dk, *dv;
     float *ws;
     // set by the launchers
-    int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks, row_splits;
+    int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks, row_splits, q_splits;
     uint32_t gmul;
-    float *part, *part_lse, *stats, *bounds;
+    float *part, *part_lse, *part_q, *stats, *bounds;
 };
 constexpr int ATTN_MAX_D = 128;
 size_t attention_workspace(const AttnArgs &a, bool backward);

@@ -197,6 +197,8 @@ def test_long_keys(ops, dtype):
     Case(dtype, 2, 1, 12544, 8, 2, 128, k_lengths=[12544, 5000]).check(ops)
     Case(dtype, 1, 2, 9001, 3, 3, 64, causal=True).check(ops)
     Case(dtype, 1, 200, 7001, 1, 1, 40).check(ops)
+    Case(dtype, 2, 150, 4000, 2, 1, 72, causal=True, q_lengths=[150, 100],
+         k_lengths=[2100, 4000]).check(ops)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
