@@ -873,8 +873,8 @@ typedef struct {
  * another tensor's x.
  *   max_norm  >= 0 (infinity: y = x)
  *   norm      device, fp32, or NULL
- * The same inputs give the same bits every time.  n <= 2^20, at most 2^45
- * values in a tensor. */
+ * The same inputs give the same bits every time.  n <= 2^20, at most 2^43
+ * values in all. */
 ctc_status ctc_clip_gradients(int32_t n, const ctc_gradient *grads,
                               float max_norm, float *norm, void *workspace,
                               size_t ws_bytes, void *stream);

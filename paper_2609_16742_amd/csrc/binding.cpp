@@ -597,20 +597,22 @@ head_norm_rotary_backward(const Tensor &dyq, const Maybe &dyk, const Tensor &q, 
 
 // --------------------------------------------------------------- clipping
 
-std::tuple<std::vector<Tensor>, Tensor> clip_gradients(const std::vector<Tensor> &grads,
-                                                       double max_norm,
-                                                       std::optional<std::vector<Tensor>> out,
-                                                       Maybe norm, int64_t stream) {
+// (the norm, and the outputs where they are made here: a list that the caller
+// holds need not become one again)
+std::tuple<Tensor, std::optional<std::vector<Tensor>>>
+clip_gradients(const std::vector<Tensor> &grads, double max_norm,
+               const std::optional<std::vector<Tensor>> &out, bool in_place, Maybe norm,
+               int64_t stream) {
     need(!grads.empty(), "no gradients");
     const Tensor &ref = grads[0];
     on_gpu(ref, "a gradient");
     c10::DeviceGuard guard(ref.device());
     need(!out || out->size() == grads.size(), "out must hold a tensor for each gradient");
     std::vector<ctc_gradient> g(grads.size());
-    const bool make = !out;
-    if (make) {
-        out.emplace();
-        out->reserve(grads.size());
+    std::optional<std::vector<Tensor>> made;
+    if (!out && !in_place) {
+        made.emplace();
+        made->reserve(grads.size());
     }
     for (size_t i = 0; i < grads.size(); i++) {
         const Tensor &x = grads[i];
@@ -618,17 +620,16 @@ std::tuple<std::vector<Tensor>, Tensor> clip_gradients(const std::vector<Tensor>
              "gradients must be float32, float16 or bfloat16 tensors of one GPU");
         need(x.is_non_overlapping_and_dense(), "gradients must be dense");
         no_grad(x);
-        if (make) {
-            out->push_back(at::empty_like(x));
-        } else {
-            const Tensor &y = (*out)[i];
+        if (made) made->push_back(at::empty_like(x));
+        const Tensor &y = made ? (*made)[i] : out ? (*out)[i] : x;
+        if (out) {
             no_grad(y);
             need(y.defined() && y.scalar_type() == x.scalar_type() && y.device() == x.device() &&
                      y.sizes() == x.sizes() && (y.strides() == x.strides() ||
                                                 (y.is_contiguous() && x.is_contiguous())),
                  "out must be like the gradients");
         }
-        g[i] = ctc_gradient{x.data_ptr(), (*out)[i].data_ptr(), x.numel(), (int32_t)code(x), 0};
+        g[i] = ctc_gradient{x.data_ptr(), y.data_ptr(), x.numel(), (int32_t)code(x), 0};
     }
     const bool given = norm.has_value();
     if (!given) norm = empty({}, at::kFloat, ref);
@@ -640,10 +641,10 @@ std::tuple<std::vector<Tensor>, Tensor> clip_gradients(const std::vector<Tensor>
     done(ctc_clip_gradients((int32_t)g.size(), g.data(), (float)max_norm,
                             (float *)norm->data_ptr(), scratch(bytes, keep, ref), bytes,
                             (void *)stream));
-    if (!make)
-        for (const Tensor &t : *out) wrote(t);
+    if (!made)
+        for (const Tensor &t : out ? *out : grads) wrote(t);
     if (given) wrote(norm);
-    return {*out, *norm};
+    return {*norm, made};
 }
 
 }  // namespace

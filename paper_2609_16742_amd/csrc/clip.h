@@ -12,18 +12,18 @@
 namespace ctc {
 namespace ops {
 
-constexpr int CLIP_CHUNK = 16384;                // elements
+constexpr int CLIP_CHUNK = 4096;                 // elements
 constexpr int CLIP_GROUPS = 1024;                // of a launch: four a CU
 
-// The tensor of chunk `c`, the last whose first chunk is not behind it.
+// The tensor of chunk `c`, the last whose first chunk is not behind it: how
+// many begin there or before, two for each lane.
+static_assert(CLIP_TENSORS <= 128, "two a lane");
 __device__ __forceinline__ int clip_find(const ClipTable &t, uint32_t c) {
-    int lo = 0, hi = t.n;
-    while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if (t.first[m] <= c) lo = m;
-        else hi = m;
-    }
-    return lo;
+    const int lane = threadIdx.x & 63;
+    const uint64_t lo = __ballot(lane < t.n && t.first[lane] <= c);
+    const uint64_t hi =
+        t.n > 64 ? __ballot(64 + lane < t.n && t.first[64 + lane] <= c) : (uint64_t)0;
+    return __builtin_amdgcn_readfirstlane(__popcll(lo) + __popcll(hi) - 1);
 }
 // f(elements of a chunk) for 16 bytes of each lane at a time.
 template <typename T, typename F>

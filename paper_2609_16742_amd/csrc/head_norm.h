@@ -143,26 +143,24 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
     const int64_t all = (int64_t)a.b * a.t;
     const HeadPairs<V, INTER> at(p, a.turned, half);
     const bool mine = p < half, turn = mine && p < a.turned;
-    float gu[2][V], gv[2][V], wu[2][V], wv[2][V];
-#pragma unroll
+    // (one side after the other: the sums of both would halve the waves)
+#pragma unroll 1
     for (int which = 0; which < 2; which++) {
+        const HeadSide &s = a.side[which];
+        if (!s.heads) continue;
+        float gu[V], gv[V], wu[V], wv[V];
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            gu[which][i] = gv[which][i] = 0.f;
-            wu[which][i] = wv[which][i] = 1.f;
+            gu[i] = gv[i] = 0.f;
+            wu[i] = wv[i] = 1.f;
         }
-        if (a.side[which].weight && mine) at.load(a.side[which].weight, wu[which], wv[which]);
-    }
-    for (int64_t token0 = (int64_t)blockIdx.x * a.tokens; token0 < all;
-         token0 += (int64_t)gridDim.x * a.tokens) {
-        const int n = all - token0 < a.tokens ? (int)(all - token0) : a.tokens;
-        __syncthreads();
-        if (a.turned) head_angles(a, token0, n, table);
-        __syncthreads();
-#pragma unroll
-        for (int which = 0; which < 2; which++) {
-            const HeadSide &s = a.side[which];
-            if (!s.heads) continue;
+        if (s.weight && mine) at.load(s.weight, wu, wv);
+        for (int64_t token0 = (int64_t)blockIdx.x * a.tokens; token0 < all;
+             token0 += (int64_t)gridDim.x * a.tokens) {
+            const int n = all - token0 < a.tokens ? (int)(all - token0) : a.tokens;
+            __syncthreads();
+            if (a.turned) head_angles(a, token0, n, table);
+            __syncthreads();
             for (int unit = sub; unit < n * s.heads; unit += 256 / L) {
                 const int k = unit / s.heads, head = unit - k * s.heads;
                 const int64_t token = token0 + k, b = token / a.t, t = token - b * a.t;
@@ -194,10 +192,10 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
                 float dot = 0.f;
 #pragma unroll
                 for (int i = 0; i < V; i++) {
-                    gu[which][i] += u[i] * xu[i];
-                    gv[which][i] += v[i] * xv[i];
-                    u[i] *= wu[which][i];
-                    v[i] *= wv[which][i];
+                    gu[i] += u[i] * xu[i];
+                    gv[i] += v[i] * xv[i];
+                    u[i] *= wu[i];
+                    v[i] *= wv[i];
                     dot += u[i] * xu[i] + v[i] * xv[i];
                 }
                 if (a.norm) {
@@ -211,14 +209,10 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
                 if (mine) at.store((T *)s.dx + b * s.dxs[0] + t * s.dxs[1] + head * s.dxs[2], u, v);
             }
         }
-    }
-    // [which][sub][d], one side at a time
-    float *sums = (float *)table;
-#pragma unroll
-    for (int which = 0; which < 2; which++) {
-        if (!a.side[which].heads || !a.side[which].dweight) continue;
+        if (!s.dweight) continue;
+        float *sums = (float *)table;            // [sub][d]
         __syncthreads();
-        if (mine) at.store(sums + sub * a.d, gu[which], gv[which]);
+        if (mine) at.store(sums + sub * a.d, gu, gv);
         __syncthreads();
         for (int e = threadIdx.x; e < a.d; e += 256) {
             float v = 0.f;
@@ -227,17 +221,30 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
         }
     }
 }
-__global__ __launch_bounds__(256) void head_norm_join(HeadArgs a, int parts) {
-    // a wave an element
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= 2 * a.d) return;
-    const int which = i / a.d, e = i % a.d;
-    float *out = a.side[which].dweight;
-    if (!out || !a.side[which].heads) return;
+// 32 elements a workgroup, 32 of the partial sums at a time.
+__global__ __launch_bounds__(1024) void head_norm_join(HeadArgs a, int parts) {
+    __shared__ double sums[32][33];
+    const int e = threadIdx.x & 31, g0 = threadIdx.x >> 5, i = blockIdx.x * 32 + e;
+    const float *p = a.ws + i;
     double v = 0;
-    for (int g = lane; g < parts; g += 64) v += a.ws[((int64_t)g * 2 + which) * a.d + e];
-    v = wave_sum(v);
-    if (lane == 0) out[e] = (float)v;
+    if (i < 2 * a.d) {
+        int g = g0;
+        for (; g + 224 < parts; g += 256) {
+            float t[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) t[k] = p[(int64_t)(g + 32 * k) * 2 * a.d];
+#pragma unroll
+            for (int k = 0; k < 8; k++) v += t[k];
+        }
+        for (; g < parts; g += 32) v += p[(int64_t)g * 2 * a.d];
+    }
+    sums[g0][e] = v;
+    __syncthreads();
+    if (g0 || i >= 2 * a.d) return;
+    for (int g = 1; g < 32; g++) v += sums[g][e];
+    const int which = i >= a.d;
+    float *out = a.side[which].dweight;
+    if (out && a.side[which].heads) out[i - which * a.d] = (float)v;
 }
 
 // ------------------------------------------------------------------- host
@@ -320,7 +327,7 @@ hipError_t launch_head_norm(const HeadArgs &in, bool backward, hipStream_t st) {
             return hipGetLastError();
         });
     if (e != hipSuccess || (!a.side[0].dweight && !a.side[1].dweight)) return e;
-    return start(head_norm_join, dim3((2 * a.d + 3) / 4), 256, st, a, parts);
+    return start(head_norm_join, dim3((2 * a.d + 31) / 32), 1024, st, a, parts);
 }
 
 }  // namespace ops

@@ -233,7 +233,7 @@ ctc_status clip_args(int32_t n, const ctc_gradient *g) {
     for (int32_t i = 0; i < n; i++) {
         if (!real_type(g[i].dtype)) return fail(CTC_ERR_ARG, "bad dtype of gradient %d", i);
         if (g[i].size < 0) return fail(CTC_ERR_ARG, "bad size of gradient %d", i);
-        chunks += (double)g[i].size / (1 << 14) + 1;
+        chunks += (double)g[i].size / (1 << 12) + 1;
         if (chunks >= 4294967295.) return fail(CTC_ERR_UNSUPPORTED, "gradients too large");
     }
     return CTC_OK;
@@ -260,6 +260,8 @@ template <typename F> ctc_status clip_tables(int32_t n, const ctc_gradient *g, F
 bool clip_disjoint(int32_t n, const ctc_gradient *g) {
     struct Span { uintptr_t from, to; int32_t i; };
     std::vector<Span> out, in;
+    out.reserve(n);
+    in.reserve(n);
     for (int32_t i = 0; i < n; i++) {
         const size_t bytes = (size_t)g[i].size * type_bytes(g[i].dtype);
         if (!bytes) continue;

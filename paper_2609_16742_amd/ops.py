@@ -244,8 +244,11 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     to write into, like ``grads`` (in place: ``grads`` itself); ``norm``: one
     fp32 value to write into.  A norm that is not finite leaves the values as
     they are."""
-    grads = list(grads)
+    if not isinstance(grads, (list, tuple)):
+        grads = list(grads)
     if not grads:
         raise ValueError("no gradients")
-    return _run(_binding.clip_gradients, grads[0], stream, grads, max_norm,
-                None if out is None else list(out), norm)
+    in_place = out is grads
+    norm, made = _run(_binding.clip_gradients, grads[0], stream, grads,
+                      max_norm, None if in_place else out, in_place, norm)
+    return (made if made is not None else out), norm
