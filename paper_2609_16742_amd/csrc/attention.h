@@ -210,6 +210,15 @@ template <typename T, int PITCH> struct Operands {
     __device__ __forceinline__ V8 along(const char *tile, int b, int s) const {
         return *(const V8 *)(tile + b * 32 * PITCH * 2 + rows + (x ^ (s << 5)));
     }
+    // rows 32 b .. of k = 16 s .. (counted as results are, lane by lane)
+    __device__ __forceinline__ V8 along_result(const char *tile, int b, int s, int h) const {
+        const char *p = tile + b * 32 * PITCH * 2 + rows + 8 * h;
+        const uint32_t f = x ^ (h << 4);         // (the piece's place without the half)
+        u2 lo, hi;
+        __builtin_memcpy(&lo, p + (f ^ (s << 5)), 8);
+        __builtin_memcpy(&hi, p + (f ^ 16 ^ (s << 5)), 8);
+        return __builtin_bit_cast(V8, u4{lo[0], lo[1], hi[0], hi[1]});
+    }
     // columns 32 n .. of k = rows 16 b .. (counted as results are)
     __device__ __forceinline__ V8 across(const char *tile, int b, int n) const {
         const char *p = tile + b * 16 * PITCH * 2 + cols;
@@ -668,14 +677,8 @@ template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs 
             vmax(vmax(most[0], most[1]), vmax(most[2], most[3]));
 }
 
-// e of the sequence and key head (0 for bf16, whose exponents are fp32's).
-template <typename T> __device__ __forceinline__ float attn_exponent(const AttnArgs &a, int pair) {
-    if (sizeof(T) != 2 || a.type != F16) return 0.f;
-    const int lane = threadIdx.x & 63;
-    const float *b = a.bounds + (int64_t)pair * (a.q_chunks + a.v_chunks);
-    float q = 0.f, v = 0.f;
-    for (int i = lane; i < a.q_chunks; i += 64) q = vmax(q, b[i]);
-    for (int i = lane; i < a.v_chunks; i += 64) v = vmax(v, b[a.q_chunks + i]);
+// e for the lanes' squared sizes of do and v.
+__device__ __forceinline__ float attn_exponent_of(float q, float v) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) {
         q = vmax(q, __shfl_xor(q, o));
@@ -685,6 +688,16 @@ template <typename T> __device__ __forceinline__ float attn_exponent(const AttnA
     const float e = 14.f - __builtin_ceilf(1.f + 0.5f * (__builtin_amdgcn_logf(q) +
                                                        __builtin_amdgcn_logf(v)));
     return uniform(e > 15.f ? 15.f : e < -20.f ? -20.f : e);
+}
+// e of the sequence and key head (0 for bf16, whose exponents are fp32's).
+template <typename T> __device__ __forceinline__ float attn_exponent(const AttnArgs &a, int pair) {
+    if (sizeof(T) != 2 || a.type != F16) return 0.f;
+    const int lane = threadIdx.x & 63;
+    const float *b = a.bounds + (int64_t)pair * (a.q_chunks + a.v_chunks);
+    float q = 0.f, v = 0.f;
+    for (int i = lane; i < a.q_chunks; i += 64) q = vmax(q, b[i]);
+    for (int i = lane; i < a.v_chunks; i += 64) v = vmax(v, b[a.q_chunks + i]);
+    return attn_exponent_of(q, v);
 }
 
 // Where a workgroup of attend_keys stands: its keys, and the rows it goes
@@ -1096,6 +1109,170 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
         }
 }
 
+// Few rows and keys, up to 64 each (a map of 7 x 7): a workgroup takes a
+// sequence's key head whole.  Four waves take 32 rows by 32 keys of p and ds
+// each, and with both in LDS as operands every product of the gradients: five
+// in all, and what attn_rows finds is found on the way, so one launch does it.
+// Its chain is one load, two exchanges of the workgroup and the stores.
+template <typename T, int NK, int ND>
+__global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(AttnArgs a) {
+    typedef typename Tile<T>::V8 V8;
+    constexpr int PITCH = NK <= 4 ? 64 : 128, TILE = 64 * PITCH * 2, PT = 64 * 64 * 2;
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE + 3 * PT + 1024];
+    char *qt = lds, *ot = lds + TILE, *kt = lds + 2 * TILE, *vt = lds + 3 * TILE;
+    char *pt = lds + 4 * TILE, *st = pt + PT, *dt = st + PT;    // p^T, ds^T, ds
+    float *first = (float *)(dt + PT), *delta = first + 64, *dsize = first + 128,
+          *vsize = first + 192;
+    const int lane = threadIdx.x & 63, h32 = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnPlace at = attn_place(a, 1, blockIdx.x);
+    const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
+    const int lo = a.causal && qn > kn ? (qn - kn) * a.group : 0, hi = kn ? qn * a.group : 0;
+    const T *kb = (const T *)a.k + at.b * a.ks[0] + at.h * a.ks[2];
+    const T *vb = (const T *)a.v + at.b * a.vs[0] + at.h * a.vs[2];
+    const T *qb = (const T *)a.q + at.b * a.qs[0] + at.h * a.group * a.qs[2];
+    const T *gb = (const T *)a.dout + at.b * a.dos[0] + at.h * a.group * a.dos[2];
+    const T *ob = (const T *)a.o + at.b * a.os[0] + at.h * a.group * a.os[2];
+    Loads<PITCH, 64, 4> ld;
+    ld.init(lane, wave, a.d);
+    ld.queries(a, lds_address(qt), (const char *)qb, a.qs[1] * 2, a.qs[2] * 2, 0, lo, hi);
+    ld.queries(a, lds_address(ot), (const char *)gb, a.dos[1] * 2, a.dos[2] * 2, 0, lo, hi);
+    ld.rows(lds_address(kt), (const char *)kb, a.ks[1] * 2, 0, kn);
+    ld.rows(lds_address(vt), (const char *)vb, a.vs[1] * 2, 0, kn);
+    {
+        // four lanes a row and a key
+        const int r = threadIdx.x >> 2, part = threadIdx.x & 3;
+        const AttnRow row = attn_row(a, r);
+        const bool valid = r >= lo && r < hi;
+        float dot = 0.f, size = 0.f, value = 0.f, lse = -INF;
+        if (valid)
+            lse = a.lse[((int64_t)at.b * a.hq + at.h * a.group + row.g) * a.tq + row.t];
+#pragma unroll
+        for (int i = 0; i < PITCH / 32; i++) {
+            const int e = (part + 4 * i) * 8;
+            if (e < a.d && valid) {
+                float x[8], y[8];
+                load<T, 8>(gb + row.t * a.dos[1] + row.g * a.dos[2] + e, x);
+                load<T, 8>(ob + row.t * a.os[1] + row.g * a.os[2] + e, y);
+#pragma unroll
+                for (int j = 0; j < 8; j++) dot += x[j] * y[j], size += x[j] * x[j];
+            }
+            if (std::is_same<T, _Float16>::value && e < a.d && r < kn) {
+                float x[8];
+                load<T, 8>(vb + r * a.vs[1] + e, x);
+#pragma unroll
+                for (int j = 0; j < 8; j++) value += x[j] * x[j];
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o *= 2) {
+            dot += __shfl_xor(dot, o);
+            size += __shfl_xor(size, o);
+            value += __shfl_xor(value, o);
+        }
+        if (part == 0) {
+            const bool in = !(lse == -INF);
+            first[r] = in ? -lse / a.scale : -INF;
+            delta[r] = in ? -dot : 0.f;
+            dsize[r] = size < INF ? size : 0.f;
+            vsize[r] = value < INF ? value : 0.f;
+        }
+    }
+    attn_arrive();
+    float e = 0.f;
+    if (std::is_same<T, _Float16>::value) e = attn_exponent_of(dsize[lane], vsize[lane]);
+    const float c = uniform(a.scale * LOG2E);
+    Operands<T, PITCH> op;
+    Operands<T, 64> pop;
+    op.init(lane);
+    pop.init(lane);
+    {
+        const int kblock = wave & 1, rblock = wave >> 1;
+        f16v s = first_values(first + 32 * rblock, h32), dp = first_values(delta + 32 * rblock, h32);
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+            s = Tile<T>::mul(op.along(qt, rblock, i), op.along(kt, kblock, i), s);
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+            dp = Tile<T>::mul(op.along(ot, rblock, i), op.along(vt, kblock, i), dp);
+        const int key = 32 * kblock + (lane & 31);
+        int from = 0;
+        if (a.causal) {
+            const int t = key - (kn - qn);
+            from = t < 0 ? 0 : t * a.group;
+        }
+        if (key >= kn) from = 64;
+        float x[16], y[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) {
+            x[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            if (32 * rblock + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = 0.f;
+            y[i] = x[i] == 0.f ? 0.f : x[i] * dp[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const V8 p = pack8<T>(x + 8 * k), d = pack8<T>(y + 8 * k);
+            const u4 pu = __builtin_bit_cast(u4, p), du = __builtin_bit_cast(u4, d);
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                // rows 32 rblock + 16 k + 8 j + 4 h32 ..
+                const int piece = 4 * rblock + 2 * k + j;
+                const int to = key * 128 + ((piece ^ swizzle<64>(key)) << 4) + 8 * h32;
+                *(u2 *)(pt + to) = u2{pu[2 * j], pu[2 * j + 1]};
+                *(u2 *)(st + to) = u2{du[2 * j], du[2 * j + 1]};
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int r = 32 * rblock + 16 * k + 8 * j + 4 * h32 + i;
+                    *(T *)(dt + r * 128 + ((key / 8 ^ swizzle<64>(r)) << 4) + key % 8 * 2) =
+                        d[4 * j + i];
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const int block = wave & 1, half = wave >> 1;
+    const float back = exp2_hw(-e);
+    const int x = 32 * block + (lane & 31);      // the lane's key, and row
+    const AttnRow row = attn_row(a, x);
+    V8 pf[4], sf[4], df[4];
+#pragma unroll
+    for (int s = 0; s < 4; s++) {
+        pf[s] = pop.along_result(pt, block, s, h32);
+        sf[s] = pop.along_result(st, block, s, h32);
+        df[s] = pop.along_result(dt, block, s, h32);
+    }
+    auto put = [&](T *o, int n, const f16v &acc, float f) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int i = n * 32 + j * 8 + 4 * h32;
+            const float v[4] = {acc[4 * j] * f, acc[4 * j + 1] * f, acc[4 * j + 2] * f,
+                                acc[4 * j + 3] * f};
+            if (i < a.d) store<T, 4>(o + i, v);
+        }
+    };
+    const bool valid = x >= lo && x < hi;
+    T *dkp = (T *)a.dk + at.b * a.dks[0] + x * a.dks[1] + at.h * a.dks[2];
+    T *dvp = (T *)a.dv + at.b * a.dvs[0] + x * a.dvs[1] + at.h * a.dvs[2];
+    T *dqp = (T *)a.dq + at.b * a.dqs[0] + row.t * a.dqs[1] +
+             (at.h * a.group + row.g) * a.dqs[2];
+#pragma unroll
+    for (int n = 0; n < ND; n++) {
+        if ((n & 1) != half) continue;
+        f16v dv = zeros16(), dk = zeros16(), dq = zeros16();
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            dv = Tile<T>::mul(op.across(ot, s, n), pf[s], dv);
+            dk = Tile<T>::mul(op.across(qt, s, n), sf[s], dk);
+            dq = Tile<T>::mul(op.across(kt, s, n), df[s], dq);
+        }
+        if (x < a.tk) {
+            put(dvp, n, dv, x < kn ? back : 0.f);
+            put(dkp, n, dk, x < kn ? a.scale * back : 0.f);
+        }
+        if (x < a.tq * a.group) put(dqp, n, valid ? dq : zeros16(), a.scale * back);
+    }
+}
+
 // Both in one launch, so that workgroups of the second kind fill the CUs that
 // those of the first, which take longer, leave idle at their end.
 template <typename T, int NK, int ND>
@@ -1119,6 +1296,10 @@ static void attn_group(AttnArgs &a) {
     while ((1 << l) < a.group) l++;
     a.gmul = l ? (uint32_t)((((uint64_t)1 << (31 + l)) + a.group - 1) / a.group) : 0;
     a.gshift = l ? l - 1 : 0;
+}
+// Gradients of which a workgroup takes a sequence's key head whole.
+static bool attn_small(const AttnArgs &a) {
+    return (int64_t)a.tq * a.group <= 64 && a.tk <= 64;
 }
 // How a call is cut up.  Ranges of keys or rows, where the tiles alone would
 // leave CUs idle: as many as give two workgroups a CU, of four steps of 64 at
@@ -1161,6 +1342,7 @@ size_t attention_workspace(const AttnArgs &in, bool backward) {
     const int64_t rows = (int64_t)a.tq * a.group, pairs = (int64_t)a.b * a.hkv;
     const AttnPlan p = attn_plan(a, backward);
     if (backward) {
+        if (attn_small(a)) return 0;
         const AttnSpace s = attn_space(a, p);
         return (size_t)((s.stats + s.bounds + s.keys + s.queries) * 4);
     }
@@ -1191,6 +1373,8 @@ template <typename T, int NK, int ND> struct Attend {
 template <typename T, int NK, int ND> struct AttendBackward {
     static hipError_t go(const AttnArgs &a, hipStream_t st) {
         const int64_t pairs = (int64_t)a.b * a.hkv;
+        if (attn_small(a))
+            return start(attend_backward_small<T, NK, ND>, dim3((unsigned)pairs), 256, st, a);
         const int64_t wgs =
             pairs * ((int64_t)a.key_tiles * a.row_splits + (int64_t)a.tiles * a.q_splits);
         hipError_t e = hipSuccess;
@@ -1236,7 +1420,7 @@ hipError_t launch_attention_backward(const AttnArgs &in, hipStream_t st) {
     a.part = a.bounds + s.bounds;
     a.part_q = a.part + s.keys;
     hipError_t e = hipSuccess;
-    if (a.q_chunks + a.v_chunks) {
+    if (!attn_small(a) && a.q_chunks + a.v_chunks) {
         const dim3 grid((unsigned)(pairs * (a.q_chunks + a.v_chunks)));
         e = a.type == F16 ? start(attn_rows<_Float16>, grid, 256, st, a)
                           : start(attn_rows<__bf16>, grid, 256, st, a);

@@ -192,6 +192,18 @@ def test_lengths(ops, causal, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [16, 64, 80, 128])
+def test_small_lengths(ops, d, causal, dtype):
+    """Sequences that one workgroup takes whole, rows of shared heads among
+    them."""
+    Case(dtype, 6, 20, 50, 6, 2, d, causal=causal, q_lengths=[20, 1, 0, 13, 20, 99],
+         k_lengths=[50, 0, 17, 1, 33, -3]).check(ops)
+    Case(dtype, 3, 64, 64, 2, 2, d, causal=causal, q_lengths=[64, 63, 33],
+         k_lengths=[64, 31, 33]).check(ops)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_long_keys(ops, dtype):
     """Few rows over many keys (ranges of keys joined), and their gradients."""
     Case(dtype, 2, 1, 12544, 8, 2, 128, k_lengths=[12544, 5000]).check(ops)
