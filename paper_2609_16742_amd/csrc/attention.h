@@ -289,7 +289,11 @@ struct AttnPlace { int b, h, part; };
 __device__ __forceinline__ AttnPlace attn_place(const AttnArgs &a, int parts, int id) {
     const int pairs = a.b * a.hkv;
     int pair, part;
-    if (pairs % 8 == 0) {
+    if (a.causal) {
+        // (longest first, of all pairs)
+        pair = id % pairs;
+        part = id / pairs;
+    } else if (pairs % 8 == 0) {
         pair = (id >> 3) / parts * 8 + (id & 7);
         part = (id >> 3) % parts;
     } else {
