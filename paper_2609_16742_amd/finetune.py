@@ -12,7 +12,13 @@ protected classifier, so :func:`ctc.ctc_verify` checks them.  The backward
 pass takes the same operators the other way: gradient of the scores, both
 8-bit products of the linear layer, gradient of the group norm.
 
+:class:`AttentionHead` lets the pixels see each other first: 8-bit projections
+of the normed map, queries and keys normed and turned by their row and column,
+attention, and the mean over the pixels of what it returns.  Its step clips
+the gradients of all parameters by their norm.
+
     python -m paper_2609_16742_amd.finetune --workload resnet18_f16_b64
+    python -m paper_2609_16742_amd.finetune --head attention
 """
 
 from __future__ import annotations
@@ -26,6 +32,13 @@ import torch
 
 from . import ctc, ops
 from .runtime import CtcNet
+
+
+def _transposed_product(d, x):
+    """d^T x in 8 bits: the gradient of a layer's filters."""
+    qd, sd = ops.fp8_quantize(d, "e5m2", transpose=True)
+    qx, sx = ops.fp8_quantize(x, transpose=True)
+    return ops.fp8_matmul(qd, sd, qx, sx, dtype=torch.float32)
 
 
 class Head:
@@ -51,39 +64,52 @@ class Head:
                                        act="relu", carry=True)
         pooled = y.view(y.shape[0], -1, y.shape[-1]).mean(
             1, dtype=torch.float32)
-        out = torch.empty((x.shape[0], self.classes + 1), device=x.device)
-        out[:, -1] = pooled[:, -1]
+        checksum = pooled[:, -1]
         pooled = pooled[:, :-1]          # rows keep their stride
+        return self._logits(pooled, checksum), (x, mean, rstd, pooled)
+
+    def _logits(self, pooled, checksum):
+        out = torch.empty((pooled.shape[0], self.classes + 1),
+                          device=pooled.device)
+        out[:, -1] = checksum
         qa, sa = ops.fp8_quantize(pooled)
         qw, sw = ops.fp8_quantize(self.weight, block_rows=128)
         ops.fp8_matmul(qa, sa, qw, sw, self.bias, out=out[:, :-1])
-        return out, (x, mean, rstd, pooled)
+        return out
+
+    def _linear_gradients(self, out, targets, pooled):
+        """(log probabilities, gradients of minus their sum with respect to
+        pooled, weight and bias)."""
+        logits = out[:, :-1]
+        s = ops.token_scores(logits, targets)
+        minus = torch.full_like(s.lse, -1.0)
+        d = ops.token_scores_backward(logits, targets, s.lse, g_logprob=minus)
+        # weight: d^T pooled; pooled: d weight
+        dw = _transposed_product(d, pooled)
+        qd, sd = ops.fp8_quantize(d, "e5m2")
+        qw, sw = ops.fp8_quantize(self.weight, block_rows=128, transpose=True)
+        dp = ops.fp8_matmul(qd, sd, qw, sw, dtype=torch.float32)
+        return s.logprob, dp, dw, d.sum(0)
 
     def gradients(self, out, targets, saved):
         """(log probabilities [n], gradients of minus their sum with respect
         to gamma, beta, weight and bias; gamma's and beta's times the
         pixels)."""
         x, mean, rstd, pooled = saved
-        logits = out[:, :-1]
-        s = ops.token_scores(logits, targets)
-        minus = torch.full_like(s.lse, -1.0)
-        d = ops.token_scores_backward(logits, targets, s.lse, g_logprob=minus)
-        # weight: d^T pooled; pooled: d weight
-        qd, sd = ops.fp8_quantize(d, "e5m2", transpose=True)
-        qp, sp = ops.fp8_quantize(pooled, transpose=True)
-        dw = ops.fp8_matmul(qd, sd, qp, sp, dtype=torch.float32)
-        qd, sd = ops.fp8_quantize(d, "e5m2")
-        qw, sw = ops.fp8_quantize(self.weight, block_rows=128, transpose=True)
-        dp = ops.fp8_matmul(qd, sd, qw, sw, dtype=torch.float32)
+        logprob, dp, dw, db = self._linear_gradients(out, targets, pooled)
         # every pixel gets dp (over the pixels: left to the caller, so that
         # 16-bit gradients do not vanish); the checksum gets none
         dy = torch.zeros_like(x)
         dy[..., :-1] = dp.view((dp.shape[0],) + (1,) * (x.dim() - 2) + (-1,))
+        dgamma, dbeta = self._norm_gradients(dy, x, mean, rstd)
+        return logprob, dgamma, dbeta, dw, db
+
+    def _norm_gradients(self, dy, x, mean, rstd):
         _, _, dgamma, dbeta = ops.group_norm_backward(
             dy, x, mean, rstd, self.groups, self.gamma, self.beta, act="relu",
             carry=True, out=(None, None, torch.empty_like(self.gamma),
                              torch.empty_like(self.beta)))
-        return s.logprob, dgamma, dbeta, dw, d.sum(0)
+        return dgamma, dbeta
 
     def step(self, x, targets, lr):
         """One step of gradient descent on the mean of -log p(target);
@@ -101,6 +127,103 @@ class Head:
         """TokenScores of the ``k`` best classes of every row."""
         return ops.token_scores(self.forward(x)[0][:, :-1], None,
                                 min(k, self.classes))
+
+
+class AttentionHead(Head):
+    """Group norm and ReLU of a map [n, h, w, channels], projections to
+    ``heads`` queries, keys and values of ``size``, attention over the pixels,
+    their mean and a linear layer."""
+
+    def __init__(self, channels, classes, groups=32, heads=8, size=64, seed=0,
+                 device="cuda"):
+        if size % 8:
+            raise ValueError("the heads' size is no multiple of 8")
+        super().__init__(channels, classes, groups, seed, device)
+        self.heads, self.size = heads, size
+        g = torch.Generator().manual_seed(seed + 1)
+        self.project = (torch.randn((3 * heads * size, channels - 1),
+                                    generator=g)
+                        / (channels - 1) ** 0.5).to(device)
+        self.q_weight = torch.ones(size, device=device)
+        self.k_weight = torch.ones(size, device=device)
+        self.weight = (torch.randn((classes, heads * size), generator=g)
+                       / (heads * size) ** 0.5).to(device)
+        # rows turn the first quarter of the values' pairs, columns the next
+        self.axes = (size // 4, size // 4)
+        self.frequencies = ops.rotary_frequencies(self.axes, 100.0, device)
+
+    def parameters(self):
+        return [self.gamma, self.beta, self.project, self.q_weight,
+                self.k_weight, self.weight, self.bias]
+
+    def _rotary(self, x):
+        return dict(q_weight=self.q_weight, k_weight=self.k_weight,
+                    positions=ops.grid_positions(*x.shape[1:3],
+                                                 device=x.device),
+                    frequencies=self.frequencies, axes=self.axes)
+
+    def forward(self, x):
+        n, c, h = x.shape[0], x.shape[-1], self.heads
+        y, mean, rstd = ops.group_norm(x, self.groups, self.gamma, self.beta,
+                                       act="relu", carry=True)
+        pixels = y.view(-1, c)[:, :-1]
+        qa, sa = ops.fp8_quantize(pixels)
+        qw, sw = ops.fp8_quantize(self.project, block_rows=128)
+        qkv = ops.fp8_matmul(qa, sa, qw, sw, dtype=torch.float16)
+        qkv = qkv.view(n, -1, 3 * h, self.size)
+        q, k = ops.head_norm_rotary(qkv[:, :, :h], qkv[:, :, h:2 * h],
+                                    **self._rotary(x))
+        o, lse = ops.attention(q, k, qkv[:, :, 2 * h:])
+        pooled = o.mean(1, dtype=torch.float32).view(n, -1)
+        checksum = y[..., -1].reshape(n, -1).mean(1, dtype=torch.float32)
+        return (self._logits(pooled, checksum),
+                (x, mean, rstd, pixels, qkv, q, k, o, lse, pooled))
+
+    def gradients(self, out, targets, saved):
+        """(log probabilities [n], gradients of minus their sum with respect
+        to :meth:`parameters`; all but the last two's times the pixels)."""
+        logprob, dp, dw, db = self._linear_gradients(out, targets, saved[-1])
+        return (logprob, *self._pixel_gradients(dp, saved), dw, db)
+
+    def _pixel_gradients(self, dp, saved):
+        """Gradients of gamma, beta, project, q_weight and k_weight, times
+        the pixels, for the gradient dp of the pooled values."""
+        x, mean, rstd, pixels, qkv, q, k, o, lse, _ = saved
+        h = self.heads
+        do = dp.view(o.shape[0], 1, h, self.size).to(o.dtype).expand(o.shape)
+        dqkv = torch.empty_like(qkv)
+        dq, dk, dv = dqkv[:, :, :h], dqkv[:, :, h:2 * h], dqkv[:, :, 2 * h:]
+        ops.attention_backward(do, q, k, qkv[:, :, 2 * h:], o, lse,
+                               out=(dq, dk, dv))
+        dqw, dkw = torch.empty_like(self.q_weight), torch.empty_like(
+            self.k_weight)
+        ops.head_norm_rotary_backward(
+            dq, dk, qkv[:, :, :h], qkv[:, :, h:2 * h],
+            out=(dq, dk, dqw, dkw), **self._rotary(x))
+        dqkv = dqkv.view(-1, 3 * h * self.size)
+        dproject = _transposed_product(dqkv, pixels)
+        qd, sd = ops.fp8_quantize(dqkv, "e5m2")
+        qw, sw = ops.fp8_quantize(self.project, block_rows=128,
+                                  transpose=True)
+        dy = torch.zeros_like(x)                 # the checksum gets none
+        ops.fp8_matmul(qd, sd, qw, sw,
+                       out=dy.view(-1, dy.shape[-1])[:, :-1])
+        dgamma, dbeta = self._norm_gradients(dy, x, mean, rstd)
+        return dgamma, dbeta, dproject, dqw, dkw
+
+    def step(self, x, targets, lr, max_norm=1.0):
+        """One step of gradient descent on the mean of -log p(target), the
+        gradient's norm at most ``max_norm``; returns that mean (a tensor;
+        nothing waits)."""
+        out, saved = self.forward(x)
+        logprob, *grads = self.gradients(out, targets, saved)
+        n, pixels = x.shape[0], x[0, ..., 0].numel()
+        for i, g in enumerate(grads):
+            g.mul_(1 / n if i >= 5 else 1 / (n * pixels))
+        ops.clip_gradients(grads, max_norm, out=grads)
+        for p, g in zip(self.parameters(), grads):
+            p.sub_(g, alpha=lr)
+        return -logprob.mean()
 
 
 def features(net, x):
@@ -126,7 +249,10 @@ def features(net, x):
     return net.tensor(at, x.shape[0])[..., :c].contiguous()
 
 
-def run(workload, classes=100, steps=200, lr=0.5, log=None):
+HEADS = {"linear": Head, "attention": AttentionHead}
+
+
+def run(workload, classes=100, steps=200, lr=0.5, log=None, head="linear"):
     """Fits a head to random classes of one batch of images; returns the loss
     before and after, how many classes are ranked first, how many rows the
     detector flags after calibration on them, and the time of a step."""
@@ -140,7 +266,7 @@ def run(workload, classes=100, steps=200, lr=0.5, log=None):
     g = torch.Generator().manual_seed(1)
     targets = torch.randint(0, classes, (w.batch,), generator=g,
                             dtype=torch.int32).cuda()
-    head = Head(f.shape[-1], classes, groups=8)
+    head = HEADS[head](f.shape[-1], classes, groups=8)
     first = float(head.step(f, targets, lr))
     torch.cuda.synchronize()
     t = time.perf_counter()
@@ -169,11 +295,13 @@ def main(argv=None):
     ap.add_argument("--classes", type=int, default=100)
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--lr", type=float, default=0.5)
+    ap.add_argument("--head", choices=sorted(HEADS), default="linear")
     a = ap.parse_args(argv)
     if not torch.cuda.is_available():
         sys.exit("training runs on the GPU")
     print(json.dumps(run(a.workload, a.classes, a.steps, a.lr,
-                         log=lambda s: print(s, flush=True))))
+                         log=lambda s: print(s, flush=True),
+                         head=a.head)))
 
 
 if __name__ == "__main__":
