@@ -768,9 +768,9 @@ typedef struct {
  *   q, o  [batch][queries][q_heads][head], k, v [batch][keys][k_heads][head]
  *         in dtype: 16-byte aligned, strides multiples of 8
  *   lse   [batch][q_heads][queries] fp32
- * Probabilities are rounded to dtype for their product with v; a NaN or an
- * infinity in a key or a value that a query does not see does not reach it if
- * it stands behind the sequence's length.
+ * Probabilities are rounded to dtype for their product with v.  A NaN or an
+ * infinity in a key or a value reaches no query that does not see it; among
+ * causal ones, an infinite value may be a NaN in the o of those that do.
  * The same inputs give the same bits every time.  64 token strides and the
  * strides of the query heads that share a key head: below 2^29 elements;
  * queries * (q_heads / k_heads), keys <= 2^30; workgroups (128 rows each, or

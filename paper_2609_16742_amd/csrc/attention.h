@@ -143,6 +143,40 @@ template <int PITCH, int ROWS, int NW, bool KEEP = false> struct Loads {
         }
         return p;
     }
+    // A causal tile that some rows see in part: a probability of zero times a
+    // NaN or an infinity would be a NaN.  `odd`: whether there is one among the
+    // pieces that the wave loaded (and that have landed); `mend` makes them
+    // zeros and keeps, for each column, the least of sign * (first + row) of
+    // such a value in `least`, if given.
+    template <typename T> __device__ __forceinline__ bool odd(const char *tile) const {
+        // (an exponent of all ones carries into the sign's place)
+        constexpr uint32_t MASK = std::is_same<T, _Float16>::value ? 0x7c007c00u : 0x7f807f80u;
+        constexpr uint32_t ADD = std::is_same<T, _Float16>::value ? 0x04000400u : 0x00800080u;
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const u4 v = *(const u4 *)(tile + (i * NW + wave) * 1024 + lane * 16);
+#pragma unroll
+            for (int j = 0; j < 4; j++) found |= (v[j] & MASK) + ADD;
+        }
+        return __any((int)(found & 0x80008000u));
+    }
+    template <typename T>
+    __device__ __forceinline__ void mend(char *tile, int *least, int sign, int first) const {
+        constexpr uint32_t ONES = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
+#pragma unroll 1
+        for (int i = 0; i < N; i++) {
+            const int row = wave * RPI + lane / CH + i * (NW * RPI);
+            const int c = (lane % CH ^ swizzle<PITCH>(row)) * 8;
+            uint16_t *v = (uint16_t *)(tile + (i * NW + wave) * 1024 + lane * 16);
+#pragma unroll 1
+            for (int j = 0; j < 8; j++)
+                if ((v[j] & ONES) == ONES) {
+                    v[j] = 0;
+                    if (least) atomicMin(least + c + j, sign * (first + row));
+                }
+        }
+    }
     // Rows first .. first + ROWS - 1 of a matrix at `base` (rows `stride` bytes
     // apart, those from `end` on as zeros).
     __device__ __forceinline__ void rows(uint32_t tile, const char *base, int64_t stride,
@@ -276,6 +310,29 @@ __device__ __forceinline__ void attn_arrive() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// LDS of what causal tiles with NaNs or infinities leave behind: for each column
+// which row had one (see Loads::mend), and for either stage the tile that did.
+struct Odd { int least[128], tile[2]; };
+__device__ __forceinline__ void odd_init(Odd &odd) {
+    for (int i = threadIdx.x; i < 130; i += blockDim.x)
+        (i < 128 ? odd.least[i] : odd.tile[i - 128]) = i < 128 ? 0x7fffffff : -1;
+    __syncthreads();
+}
+__device__ __forceinline__ void attn_landed() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Results whose column's bound is below `bound`: they saw such a value.
+template <int ND>
+__device__ __forceinline__ void odd_results(const Odd &odd, int h32, int bound, f16v (&acc)[ND]) {
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            if (odd.least[n * 32 + 8 * (i / 4) + 4 * h32 + i % 4] < bound)
+                acc[n][i] = __builtin_nanf("");
+}
+
 // A value that all lanes hold, in a scalar register.
 __device__ __forceinline__ float uniform(float v) {
     return __builtin_bit_cast(float,
@@ -377,10 +434,11 @@ template <int PITCH, int RT, int NW> struct RowStages {
 // o and l are scaled anew in few steps.
 // ---------------------------------------------------------------------------
 template <typename T, int NK, int ND, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 4 ? 4 : 2) void attend(AttnArgs a) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
+    __shared__ Odd odd;
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnPlace at = attn_place(a, a.tiles * a.splits, blockIdx.x);
@@ -398,7 +456,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
         return n < 0 ? 0 : n > kn ? kn : n;
     };
     const int lim = valid ? sees(row.t) : 0;
-    const int least = sees(over_group(a, first));
+    const int least = sees(over_group(a, first)), block_least = sees(over_group(a, r0));
     const int last_row = r0 + NW * 32 <= R ? r0 + NW * 32 - 1 : R - 1;
     const int most = r0 < R ? sees(over_group(a, last_row)) : 0;
     const int wave_last = first + 32 <= R ? first + 31 : R - 1;
@@ -426,13 +484,25 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
     in.template init<T>(a, at, lane, wave, kn, lds);
     Operands<T, PITCH> op;
     op.init(lane);
+    if (a.causal) odd_init(odd);
+    bool spoilt = false;
     if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
     for (int key = k0; key < k1; key += KT, stage ^= 1) {
+        char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        const bool look = a.causal && key + KT > block_least;
+        if (look) {
+            attn_landed();
+            if (in.ld.template odd<T>(vt)) odd.tile[stage] = key;
+        }
         attn_arrive();
         if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
+        if (look && odd.tile[stage] == key) {
+            in.ld.template mend<T>(vt, odd.least, 1, key);
+            spoilt = true;
+            __syncthreads();
+        }
         if (key >= wave_most) continue;
-        const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
         f16v s[2];
         if (NK > 4) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -519,6 +589,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attend(AttnArgs a) {
             for (int n = 0; n < ND; n++) acc[n] = Tile<T>::mul(vc[b][n], pc[b], acc[n]);
         if (NK > 4) __builtin_amdgcn_s_setprio(0);
     }
+    if (spoilt) odd_results<ND>(odd, h32, lim, acc);
     l += other_half(l);
     // (a row that sees nothing, or is none: zeros)
     if (!valid) l = 0.f;
@@ -793,7 +864,7 @@ template <int NK> struct KeyTiles {
     static constexpr int BYTES = 2 * STAGE + (WIDE ? 128 * PITCH * 2 : 0);
 };
 template <typename T, int NK, int ND>
-__device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
+__device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &odd) {
     typedef typename Tile<T>::V8 V8;
     constexpr bool WIDE = KeyTiles<NK>::WIDE;
     constexpr int PITCH = KeyTiles<NK>::PITCH, RT = KeyTiles<NK>::RT, TILE = KeyTiles<NK>::TILE;
@@ -834,12 +905,28 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
 
     RowStages<PITCH, RT, 4> in;
     in.template init<T>(a, p.at, lane, wave, p.lo, p.hi, lds);
+    // (a row with a NaN or an infinite query has it in its lse; one in its
+    // gradient, in delta, but of dv only in its own column)
+    if (a.causal) odd_init(odd);
+    bool spoilt = false;
+    const int block_from = p.seen(a, p.key0 + 127);
     if (p.row < p.end) in.fetch(a, p.row, 0);
     int stage = 0;
     for (int row = p.row; row < p.end; row += RT, stage ^= 1) {
+        char *qt = lds + stage * STAGE, *ot = qt + TILE;
+        const bool look = a.causal && row < block_from;
+        if (look) {
+            attn_landed();
+            if (in.ld.template odd<T>(qt) || in.ld.template odd<T>(ot)) odd.tile[stage] = row;
+        }
         attn_arrive();
         if (row + RT < p.end) in.fetch(a, row + RT, stage ^ 1);
-        const char *qt = lds + stage * STAGE, *ot = qt + TILE;
+        if (look && odd.tile[stage] == row) {
+            in.ld.template mend<T>(qt, nullptr, 1, 0);
+            in.ld.template mend<T>(ot, odd.least, -1, row);
+            spoilt = true;
+            __syncthreads();
+        }
         if (WIDE) op.refresh();
 #pragma unroll
         for (int b = 0; b < RT / 32; b++) {
@@ -916,6 +1003,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds) {
             }
         }
     }
+    if (spoilt) odd_results<ND>(odd, h32, 1 - from, dv);
     const float back = exp2_hw(-e);
     store_keys<T, ND>(a, p, key, h32, dk, a.scale * back, false);
     store_keys<T, ND>(a, p, key, h32, dv, back, true);
@@ -960,7 +1048,7 @@ template <typename T> __global__ __launch_bounds__(256) void attend_sums(AttnArg
 
 // dq: like the forward pass, 32 rows a wave, the keys 64 at a time.
 template <typename T, int NK, int ND>
-__device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int id) {
+__device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd &odd, int id) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
@@ -980,7 +1068,7 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
     };
     const int lim = r < R ? sees(row.t) : 0;
     const bool valid = lim > 0;
-    const int least = sees(over_group(a, first));
+    const int least = sees(over_group(a, first)), block_least = sees(over_group(a, r0));
     const int last_row = r0 + 128 <= R ? r0 + 127 : R - 1;
     const int most = r0 < R ? sees(over_group(a, last_row)) : 0;
     const int wave_last = first + 32 <= R ? first + 31 : R - 1;
@@ -1016,13 +1104,24 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, int
         k0 = split * per;
         if (k1 > k0 + per) k1 = k0 + per;
     }
+    // (a row that sees a NaN or an infinite key has it in its lse)
+    if (a.causal) odd_init(odd);
     if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
     for (int key = k0; key < k1; key += KT, stage ^= 1) {
+        char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        const bool look = a.causal && key + KT > block_least;
+        if (look) {
+            attn_landed();
+            if (in.ld.template odd<T>(kt)) odd.tile[stage] = key;
+        }
         attn_arrive();
         if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
+        if (look && odd.tile[stage] == key) {
+            in.ld.template mend<T>(kt, nullptr, 1, key);
+            __syncthreads();
+        }
         if (key >= wave_most) continue;
-        const char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
 #pragma unroll
         for (int b = 0; b < 2; b++) {
             f16v s, dp;
@@ -1123,6 +1222,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, TILE = 64 * PITCH * 2, PT = 64 * 64 * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE + 3 * PT + 1024];
+    __shared__ Odd odd;
     char *qt = lds, *ot = lds + TILE, *kt = lds + 2 * TILE, *vt = lds + 3 * TILE;
     char *pt = lds + 4 * TILE, *st = pt + PT, *dt = st + PT;    // p^T, ds^T, ds
     float *first = (float *)(dt + PT), *delta = first + 64, *dsize = first + 128,
@@ -1137,6 +1237,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     const T *qb = (const T *)a.q + at.b * a.qs[0] + at.h * a.group * a.qs[2];
     const T *gb = (const T *)a.dout + at.b * a.dos[0] + at.h * a.group * a.dos[2];
     const T *ob = (const T *)a.o + at.b * a.os[0] + at.h * a.group * a.os[2];
+    if (a.causal) odd_init(odd);
     Loads<PITCH, 64, 4> ld;
     ld.init(lane, wave, a.d);
     ld.queries(a, lds_address(qt), (const char *)qb, a.qs[1] * 2, a.qs[2] * 2, 0, lo, hi);
@@ -1182,7 +1283,13 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
             vsize[r] = value < INF ? value : 0.f;
         }
     }
+    if (a.causal) {
+        attn_landed();
+        if (ld.template odd<T>(qt) || ld.template odd<T>(ot) || ld.template odd<T>(kt))
+            odd.tile[0] = 0;
+    }
     attn_arrive();
+    const bool spoilt = a.causal && odd.tile[0] == 0;
     float e = 0.f;
     if (std::is_same<T, _Float16>::value) e = attn_exponent_of(dsize[lane], vsize[lane]);
     const float c = uniform(a.scale * LOG2E);
@@ -1233,6 +1340,12 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
             }
         }
     }
+    if (spoilt) {
+        __syncthreads();
+        ld.template mend<T>(qt, nullptr, 1, 0);
+        ld.template mend<T>(ot, odd.least, -1, 0);
+        ld.template mend<T>(kt, nullptr, 1, 0);
+    }
     __syncthreads();
     const int block = wave & 1, half = wave >> 1;
     const float back = exp2_hw(-e);
@@ -1269,6 +1382,13 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
             dk = Tile<T>::mul(op.across(qt, s, n), sf[s], dk);
             dq = Tile<T>::mul(op.across(kt, s, n), df[s], dq);
         }
+        if (spoilt) {
+            const int t = x - (kn - qn), from = t < 0 ? 0 : t * a.group;
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                if (odd.least[n * 32 + 8 * (i / 4) + 4 * h32 + i % 4] < 1 - from)
+                    dv[i] = __builtin_nanf("");
+        }
         if (x < a.tk) {
             put(dvp, n, dv, x < kn ? back : 0.f);
             put(dkp, n, dk, x < kn ? a.scale * back : 0.f);
@@ -1283,9 +1403,10 @@ template <typename T, int NK, int ND>
 __global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
     constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;
     __shared__ __attribute__((aligned(16))) char lds[Q > K ? Q : K];
+    __shared__ Odd odd;
     const int keys = a.b * a.hkv * a.key_tiles * a.row_splits;
-    if ((int)blockIdx.x < keys) attend_keys<T, NK, ND>(a, lds);
-    else attend_queries<T, NK, ND>(a, lds, blockIdx.x - keys);
+    if ((int)blockIdx.x < keys) attend_keys<T, NK, ND>(a, lds, odd);
+    else attend_queries<T, NK, ND>(a, lds, odd, blockIdx.x - keys);
 }
 
 // ------------------------------------------------------------------- host

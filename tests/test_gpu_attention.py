@@ -217,3 +217,102 @@ def test_long_keys(ops, dtype):
 def test_long_rows(ops, dtype):
     Case(dtype, 1, 3000, 40, 4, 1, 64).check(ops)
     Case(dtype, 1, 1025, 1025, 4, 2, 128, causal=True).check(ops)
+
+
+# ------------------------------------------------- NaN and infinite values
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("t,d", [(40, 64), (200, 64), (200, 128), (30, 128)])
+def test_what_stands_behind_the_lengths(ops, t, d, dtype, causal):
+    """NaN and infinities there reach nothing, forward or backward."""
+    c = Case(dtype, 3, t, t, 4, 2, d, causal=causal, q_lengths=[t, t // 2, 0],
+             k_lengths=[t - 1, 7, 5])
+    o, lse = ops.attention(c.q, c.k, c.v, **c.kw)
+    want = (o, lse) + ops.attention_backward(c.do, c.q, c.k, c.v, o, lse, **c.kw)
+    bad = {}
+    for n in ("q", "k", "v", "do"):
+        x = getattr(c, n).clone()
+        for i in range(3):
+            x[i, (c.nq if n in ("q", "do") else c.nk)[i]:] = math.nan if n != "v" else INF
+        bad[n] = x
+    o2, lse2 = ops.attention(bad["q"], bad["k"], bad["v"], **c.kw)
+    # (o behind the queries' lengths is zeros as written; the backward pass does
+    # not read it)
+    o3 = o2.clone()
+    for i in range(3):
+        o3[i, c.nq[i]:] = math.nan
+    got = (o2, lse2) + ops.attention_backward(bad["do"], bad["q"], bad["k"], bad["v"], o3, lse2,
+                                              **c.kw)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def _causal_case(ops, t, d, plant):
+    """(baseline, results with a value planted) of a causal case in bf16."""
+    c = Case("bf16", 2, t, t, 4, 2, d, causal=True)
+    x = {n: getattr(c, n).clone() for n in ("q", "k", "v", "do")}
+
+    def run():
+        o, lse = ops.attention(x["q"], x["k"], x["v"], causal=True)
+        g = ops.attention_backward(x["do"], x["q"], x["k"], x["v"], o, lse, causal=True)
+        return dict(zip(("o", "lse", "dq", "dk", "dv"), (o, lse.transpose(1, 2)) + g))
+    want = run()
+    plant(x)
+    return want, run()
+
+
+
+@pytest.mark.parametrize("value", [math.nan, INF, -INF])
+@pytest.mark.parametrize("t,d", [(50, 64), (50, 128), (64, 32), (200, 64), (200, 128), (333, 96)])
+def test_values_that_causal_queries_do_not_see(ops, t, d, value):
+    """One NaN or infinity at token j: what does not see it stays as it was,
+    bit for bit, and what does shows it."""
+    for j in (0, 1, t // 2, t - 2, t - 1):
+        before, after = slice(0, j), slice(j, t)
+        e = 5 % d
+
+        def put(n):
+            def f(x):
+                x[n][0, j, 0, e] = value
+            return f
+        # heads 0 and 1 share key head 0 of sequence 0; the rest sees nothing
+        def rest(got, want):
+            for n in got:
+                assert torch.equal(got[n][1], want[n][1]), n
+                heads = 1 if n in ("dk", "dv") else 2
+                assert torch.equal(got[n][0, :, heads:], want[n][0, :, heads:]), n
+        want, got = _causal_case(ops, t, d, put("v"))
+        rest(got, want)
+        for n in ("o", "lse", "dq", "dv"):
+            assert torch.equal(got[n][0, before], want[n][0, before]), n
+        assert torch.equal(got["lse"], want["lse"]) and torch.equal(got["dv"], want["dv"])
+        assert not bool(torch.isfinite(got["o"][0, after, :2, e]).any())
+        keep = [i for i in range(d) if i != e]
+        assert torch.equal(got["o"][0, after, :2][..., keep], want["o"][0, after, :2][..., keep])
+        assert not bool(torch.isfinite(got["dq"][0, after, :2].float()).any())
+        if math.isnan(value):
+            want, got = _causal_case(ops, t, d, put("k"))
+            rest(got, want)
+            for n in ("o", "lse", "dq"):
+                assert torch.equal(got[n][0, before], want[n][0, before]), n
+                assert bool(torch.isnan(got[n][0, after, :2]).all()), n
+            want, got = _causal_case(ops, t, d, put("q"))
+            rest(got, want)
+            others = [i for i in range(t) if i != j]
+            for n in ("o", "lse", "dq"):
+                assert torch.equal(got[n][0, others], want[n][0, others]), n
+                assert bool(torch.isnan(got[n][0, j, 0]).all()), n
+            for n in ("dk", "dv"):
+                assert torch.equal(got[n][0, j + 1:], want[n][0, j + 1:]), n
+                assert bool(torch.isnan(got[n][0, :j + 1, 0]).all()), n
+        want, got = _causal_case(ops, t, d, put("do"))
+        rest(got, want)
+        others = [i for i in range(t) if i != j]
+        assert torch.equal(got["dq"][0, others], want["dq"][0, others])
+        assert not bool(torch.isfinite(got["dq"][0, j, 0].float()).any())
+        for n in ("dk", "dv"):
+            assert torch.equal(got[n][0, j + 1:], want[n][0, j + 1:]), n
+        assert not bool(torch.isfinite(got["dk"][0, :j + 1, 0].float()).any())
+        assert not bool(torch.isfinite(got["dv"][0, :j + 1, 0, e].float()).any())
+        assert torch.equal(got["dv"][0, :j + 1, 0][..., keep], want["dv"][0, :j + 1, 0][..., keep])
