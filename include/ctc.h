@@ -771,10 +771,10 @@ typedef struct {
  * Probabilities are rounded to dtype for their product with v.  A NaN or an
  * infinity in a key or a value reaches no query that does not see it; among
  * causal ones, an infinite value may be a NaN in the o of those that do.
- * The same inputs give the same bits every time.  64 token strides and the
- * strides of the query heads that share a key head: below 2^29 elements;
- * queries * (q_heads / k_heads), keys <= 2^30; workgroups (128 rows each, or
- * 64 pairs of a batch entry and key head) below 2^23. */
+ * The same inputs give the same bits every time.  With G = q_heads / k_heads <=
+ * 65536 and R = queries * G rows: R, keys <= 2^30, batch * k_heads * (R / 64 +
+ * keys / 64 + 2) < 2^23 - 512; 64 token strides and G head strides (keys: one)
+ * together below 2^29 elements. */
 ctc_status ctc_attention_forward(const ctc_attention *a, const ctc_heads *q,
                                  const ctc_heads *k, const ctc_heads *v,
                                  const ctc_heads *o, float *lse,

@@ -156,7 +156,7 @@ ctc_status attn_args(const ctc_attention *c, AttnArgs &a) {
     if (!(c->scale > 0.f) || std::isinf(c->scale)) return fail(CTC_ERR_ARG, "scale must be > 0");
     const double rows = (double)c->queries * (c->q_heads / c->k_heads);
     const double pairs = (double)c->batch * c->k_heads;
-    if (rows > (1 << 30) || c->keys > (1 << 30) ||
+    if (rows > (1 << 30) || c->keys > (1 << 30) || c->q_heads / c->k_heads > 65536 ||
         !grid_ok(pairs * (rows / 64 + (double)c->keys / 64 + 2) + 512))
         return fail(CTC_ERR_UNSUPPORTED, "attention too large");
     a = AttnArgs{};

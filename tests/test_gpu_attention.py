@@ -7,7 +7,9 @@ error of a probability (E below).  Probabilities are rounded to the type before
 they meet v (u each), o once more.  For fp16 a probability is kept as p 2^8 of
 the row's largest or more: its subnormals cost 2^-33 of it.  The backward pass
 rounds p and ds (u each, in fp16 at least 2^-25 of 2^-e for the exponent e that
-the sequence's gradients allow), and takes delta from the rounded o.
+the sequence's gradients allow), and takes delta from the rounded o.  Below
+2^-126, the least normal number of fp32 and of bf16, probabilities and results
+may be zeros: exp(-88) and less, which scores of hundreds reach.
 """
 
 import math
@@ -19,6 +21,7 @@ pytestmark = pytest.mark.gpu
 
 DT = {"f16": torch.float16, "bf16": torch.bfloat16}
 U = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+LEAST = 2.0 ** -126
 INF = math.inf
 
 
@@ -116,10 +119,10 @@ class Case:
                 e = (mag * (d + 4) * 2.0 ** -24 + torch.where(hide, 0.0, s.abs()) * 2.0 ** -22
                      + 2.0 ** -21).amax(1, keepdim=True) + safe * 2.0 ** -22
                 e_o = 2 * e + nk * 2.0 ** -24
-                small = 2.0 ** -33 if self.dtype == "f16" else 0.0
+                small = 2.0 ** -33 if self.dtype == "f16" else LEAST
                 to = (p @ v.abs()) * (e_o + u) + u * o.abs() + small * (
                     p.amax(1, keepdim=True) * v.abs().sum(0)[None]) + (
-                        2.0 ** -25 if self.dtype == "f16" else 0.0)
+                        2.0 ** -25 if self.dtype == "f16" else LEAST)
                 out["o"][i, :nq, h], tol["o"][i, :nq, h] = o, to
                 out["lse"][i, h, :nq], tol["lse"][i, h, :nq] = lse[:, 0], \
                     (e + nk * 2.0 ** -24)[:, 0]
@@ -132,7 +135,7 @@ class Case:
                                                .norm(dim=1)).max()) for x in grp)
                     ex = min(15.0, max(-20.0, 13.0 - math.ceil(
                         1 + math.log2(max(1e-300, nd * float(nv))))))
-                floor = 2.0 ** (-25 - ex) if self.dtype == "f16" else 0.0
+                floor = 2.0 ** (-25 - ex) if self.dtype == "f16" else LEAST
                 dp, dpa = do @ v.t(), do.abs() @ v.abs().t()
                 delta = (do * o).sum(1, keepdim=True)
                 delta_off = (do.abs() * to).sum(1, keepdim=True) + (
@@ -151,7 +154,7 @@ class Case:
                 out["dq"][i, :nq, h] = self.scale * (ds @ k)
                 tol["dq"][i, :nq, h] = self.scale * ((ds_off + ds.abs() * nk * sums) @ k.abs())
         for n in ("dq", "dk", "dv"):
-            tol[n] += u * out[n].abs() + (2.0 ** -25 if self.dtype == "f16" else 0.0)
+            tol[n] += u * out[n].abs() + (2.0 ** -25 if self.dtype == "f16" else LEAST)
         return out, tol
 
     def check(self, ops, backward=True):
