@@ -3,6 +3,7 @@
 // (include/ctc.h).  Marshalling only, compiled because an operator on a
 // small batch runs for five microseconds and the same checks in Python took
 // ten.  No torch types cross the C ABI: this is its caller.
+#include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/ATen.h>
@@ -597,12 +598,33 @@ head_norm_rotary_backward(const Tensor &dyq, const Maybe &dyk, const Tensor &q, 
 
 // --------------------------------------------------------------- clipping
 
+// The tensors of a list or tuple.  (pybind11's own conversion asks each for its
+// class by name: 60 ns more of a tensor.)
+std::vector<Tensor> tensors_of(const py::object &list) {
+    const py::object held = py::reinterpret_steal<py::object>(
+        PySequence_Fast(list.ptr(), "a list or tuple of tensors is needed"));
+    if (!held) throw py::error_already_set();
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(held.ptr());
+    std::vector<Tensor> r;
+    r.reserve(n);
+    for (Py_ssize_t i = 0; i < n; i++) {
+        PyObject *o = PySequence_Fast_GET_ITEM(held.ptr(), i);
+        if ((PyObject *)Py_TYPE(o) == THPVariableClass) r.push_back(THPVariable_Unpack(o));
+        else {
+            need(THPVariable_Check(o), "a list or tuple of tensors is needed");
+            r.push_back(THPVariable_Unpack(o));
+        }
+    }
+    return r;
+}
 // (the norm, and the outputs where they are made here: a list that the caller
 // holds need not become one again)
 std::tuple<Tensor, std::optional<std::vector<Tensor>>>
-clip_gradients(const std::vector<Tensor> &grads, double max_norm,
-               const std::optional<std::vector<Tensor>> &out, bool in_place, Maybe norm,
-               int64_t stream) {
+clip_gradients(const py::object &grad_list, double max_norm, const py::object &out_list,
+               bool in_place, Maybe norm, int64_t stream) {
+    const std::vector<Tensor> grads = tensors_of(grad_list);
+    std::optional<std::vector<Tensor>> out;
+    if (!out_list.is_none()) out = tensors_of(out_list);
     need(!grads.empty(), "no gradients");
     const Tensor &ref = grads[0];
     on_gpu(ref, "a gradient");

@@ -25,21 +25,23 @@ __device__ __forceinline__ int clip_find(const ClipTable &t, uint32_t c) {
         t.n > 64 ? __ballot(64 + lane < t.n && t.first[64 + lane] <= c) : (uint64_t)0;
     return __builtin_amdgcn_readfirstlane(__popcll(lo) + __popcll(hi) - 1);
 }
-// f(elements of a chunk) for 16 bytes of each lane at a time.
+// f(elements of a chunk) for 16 bytes of each lane at a time; a whole chunk is
+// under way at once.
 template <typename T, typename F>
 __device__ __forceinline__ void clip_chunk(const T *x, int n, F f) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), U = CLIP_CHUNK / (256 * V);
     int i = threadIdx.x * V;
-    for (; i + 3 * 256 * V + V <= n; i += 4 * 256 * V) {
-        Raw<T, V> r[4];
+    if (n == CLIP_CHUNK) {
+        Raw<T, V> r[U];
 #pragma unroll
-        for (int j = 0; j < 4; j++) r[j].load(x + i + j * 256 * V);
+        for (int j = 0; j < U; j++) r[j].load(x + i + j * 256 * V);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
+        for (int j = 0; j < U; j++) {
             float v[V];
             r[j].values(v);
             f(std::integral_constant<int, V>(), i + j * 256 * V, v);
         }
+        return;
     }
     for (; i + V <= n; i += 256 * V) {
         float v[V];
@@ -47,7 +49,7 @@ __device__ __forceinline__ void clip_chunk(const T *x, int n, F f) {
         f(std::integral_constant<int, V>(), i, v);
     }
     // (the lane whose vector the end cuts)
-    for (; i < n && i < (n / V + 1) * V; i++) {
+    for (; i < n; i++) {
         float v[1] = {widen(x[i])};
         f(std::integral_constant<int, 1>(), i, v);
     }

@@ -153,7 +153,8 @@ ctc_status attn_args(const ctc_attention *c, AttnArgs &a) {
     if (c->q_heads % c->k_heads) return fail(CTC_ERR_ARG, "k_heads must divide q_heads");
     if (c->head < 8 || c->head % 8 || c->head > ATTN_MAX_D)
         return fail(CTC_ERR_ARG, "head sizes are multiples of 8 up to %d", ATTN_MAX_D);
-    if (!(c->scale > 0.f) || std::isinf(c->scale)) return fail(CTC_ERR_ARG, "scale must be > 0");
+    if (!(c->scale >= 0x1p-96f) || std::isinf(c->scale))
+        return fail(CTC_ERR_ARG, "scale must be positive, 2^-96 at least");
     const double rows = (double)c->queries * (c->q_heads / c->k_heads);
     const double pairs = (double)c->batch * c->k_heads;
     if (rows > (1 << 30) || c->keys > (1 << 30) || c->q_heads / c->k_heads > 65536 ||

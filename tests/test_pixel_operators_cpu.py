@@ -52,7 +52,7 @@ def _backward(a, do=Q, q=Q, k=K, v=K, o=Q, lse=P, dq=Q, dk=K, dv=K, ws=P,
     (ARG, dict(queries=-1)), (ARG, dict(keys=-1)), (ARG, dict(q_heads=0)),
     (ARG, dict(k_heads=0)), (ARG, dict(k_heads=3)), (ARG, dict(head=0)),
     (ARG, dict(head=60)), (ARG, dict(head=136)), (ARG, dict(scale=0.0)),
-    (ARG, dict(scale=-1.0)), (ARG, dict(scale=NAN)), (ARG, dict(scale=INF)),
+    (ARG, dict(scale=-1.0)), (ARG, dict(scale=1e-35)), (ARG, dict(scale=NAN)), (ARG, dict(scale=INF)),
     (UNSUPPORTED, dict(keys=(1 << 30) + 1)),
     (UNSUPPORTED, dict(queries=1 << 29)),
     (UNSUPPORTED, dict(q_heads=1 << 18)),
