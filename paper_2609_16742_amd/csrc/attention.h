@@ -433,8 +433,9 @@ template <int PITCH, int RT, int NW> struct RowStages {
 // when a row's maximum has grown past it by LIMIT - SHIFT (in powers of two):
 // o and l are scaled anew in few steps.
 // ---------------------------------------------------------------------------
-template <typename T, int NK, int ND, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 4 ? 4 : 2) void attend(AttnArgs a) {
+template <typename T, int NK, int ND, int NW, bool CAUSAL>
+__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 2 ? 4 : NK <= 4 && CAUSAL ? 3 : 2)
+void attend(AttnArgs a) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
@@ -443,7 +444,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 4 ? 4 : 2) void attend
     const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnPlace at = attn_place(a, a.tiles * a.splits, blockIdx.x);
     const int split = at.part % a.splits;
-    const int tile = a.causal ? a.tiles - 1 - at.part / a.splits : at.part / a.splits;
+    const int tile = CAUSAL ? a.tiles - 1 - at.part / a.splits : at.part / a.splits;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
     const int r0 = tile * (NW * 32), R = qn * a.group;
     const int first = r0 + wave * 32, r = first + (lane & 31);
@@ -451,7 +452,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 4 ? 4 : 2) void attend
     const bool valid = r < R;
     // keys that the lane's row sees, the wave's first row, the workgroup's last
     auto sees = [&](int t) {
-        if (!a.causal) return kn;
+        if (!CAUSAL) return kn;
         const int n = t + kn - qn + 1;
         return n < 0 ? 0 : n > kn ? kn : n;
     };
@@ -484,13 +485,13 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 4 ? 4 : 2) void attend
     in.template init<T>(a, at, lane, wave, kn, lds);
     Operands<T, PITCH> op;
     op.init(lane);
-    if (a.causal) odd_init(odd);
+    if (CAUSAL) odd_init(odd);
     bool spoilt = false;
     if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
     for (int key = k0; key < k1; key += KT, stage ^= 1) {
         char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
-        const bool look = a.causal && key + KT > block_least;
+        const bool look = CAUSAL && key + KT > block_least;
         if (look) {
             attn_landed();
             if (in.ld.template odd<T>(vt)) odd.tile[stage] = key;
@@ -777,12 +778,12 @@ template <typename T> __device__ __forceinline__ float attn_exponent(const AttnA
 
 // Where a workgroup of attend_keys stands: its keys, and the rows it goes
 // through.
-struct KeyPlace {
+template <bool CAUSAL> struct KeyPlace {
     AttnPlace at;
     int pair, split, qn, kn, key0, lo, hi, row, end, shift;
     // first row that sees key j
     __device__ __forceinline__ int seen(const AttnArgs &a, int j) const {
-        if (!a.causal) return 0;
+        if (!CAUSAL) return 0;
         const int t = j - shift;
         return t < 0 ? 0 : t * a.group;
     }
@@ -794,7 +795,7 @@ struct KeyPlace {
         kn = attn_length(a.klen, at.b, a.tk);
         shift = kn - qn;
         key0 = at.part / a.row_splits * 128;
-        lo = a.causal && qn > kn ? (qn - kn) * a.group : 0;
+        lo = CAUSAL && qn > kn ? (qn - kn) * a.group : 0;
         hi = key0 < kn ? qn * a.group : 0;
         const int first = seen(a, key0);
         row = (first > lo ? first : lo) & ~(rt - 1);
@@ -808,8 +809,8 @@ struct KeyPlace {
     }
 };
 // Stores a wave's dk or dv, times `f` (of a range of rows: as partial sums).
-template <typename T, int ND>
-__device__ __forceinline__ void store_keys(const AttnArgs &a, const KeyPlace &p, int key, int h32,
+template <typename T, int ND, typename Place>
+__device__ __forceinline__ void store_keys(const AttnArgs &a, const Place &p, int key, int h32,
                                            const f16v (&acc)[ND], float f, bool values) {
     if (key >= a.tk) return;
     const bool valid = key < p.kn;
@@ -863,7 +864,7 @@ template <int NK> struct KeyTiles {
     static constexpr int STAGE = RowStages<PITCH, RT, 4>::STAGE;
     static constexpr int BYTES = 2 * STAGE + (WIDE ? 128 * PITCH * 2 : 0);
 };
-template <typename T, int NK, int ND>
+template <typename T, int NK, int ND, bool CAUSAL>
 __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &odd) {
     typedef typename Tile<T>::V8 V8;
     constexpr bool WIDE = KeyTiles<NK>::WIDE;
@@ -871,7 +872,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
     constexpr int STAGE = KeyTiles<NK>::STAGE;
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const KeyPlace p(a, RT);
+    const KeyPlace<CAUSAL> p(a, RT);
     const int key = p.key0 + wave * 32 + (lane & 31), from = p.seen(a, key);
     const int wave_from = p.seen(a, p.key0 + wave * 32 + 31);
     const int wave_first = p.seen(a, p.key0 + wave * 32);
@@ -907,14 +908,14 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
     in.template init<T>(a, p.at, lane, wave, p.lo, p.hi, lds);
     // (a row with a NaN or an infinite query has it in its lse; one in its
     // gradient, in delta, but of dv only in its own column)
-    if (a.causal) odd_init(odd);
+    if (CAUSAL) odd_init(odd);
     bool spoilt = false;
     const int block_from = p.seen(a, p.key0 + 127);
     if (p.row < p.end) in.fetch(a, p.row, 0);
     int stage = 0;
     for (int row = p.row; row < p.end; row += RT, stage ^= 1) {
         char *qt = lds + stage * STAGE, *ot = qt + TILE;
-        const bool look = a.causal && row < block_from;
+        const bool look = CAUSAL && row < block_from;
         if (look) {
             attn_landed();
             if (in.ld.template odd<T>(qt) || in.ld.template odd<T>(ot)) odd.tile[stage] = row;
@@ -1047,7 +1048,7 @@ template <typename T> __global__ __launch_bounds__(256) void attend_sums(AttnArg
 }
 
 // dq: like the forward pass, 32 rows a wave, the keys 64 at a time.
-template <typename T, int NK, int ND>
+template <typename T, int NK, int ND, bool CAUSAL>
 __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd &odd, int id) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, KT = 64, TILE = KT * PITCH * 2;
@@ -1055,14 +1056,14 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnPlace at = attn_place(a, a.tiles * a.q_splits, id);
     const int split = at.part % a.q_splits;
-    const int tile = a.causal ? a.tiles - 1 - at.part / a.q_splits : at.part / a.q_splits;
+    const int tile = CAUSAL ? a.tiles - 1 - at.part / a.q_splits : at.part / a.q_splits;
     const int pair = at.b * a.hkv + at.h;
     const int qn = attn_length(a.qlen, at.b, a.tq), kn = attn_length(a.klen, at.b, a.tk);
     const int r0 = tile * 128, R = qn * a.group;
     const int first = r0 + wave * 32, r = first + (lane & 31);
     const AttnRow row = attn_row(a, r);
     auto sees = [&](int t) {
-        if (!a.causal) return kn;
+        if (!CAUSAL) return kn;
         const int n = t + kn - qn + 1;
         return n < 0 ? 0 : n > kn ? kn : n;
     };
@@ -1105,12 +1106,12 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
         if (k1 > k0 + per) k1 = k0 + per;
     }
     // (a row that sees a NaN or an infinite key has it in its lse)
-    if (a.causal) odd_init(odd);
+    if (CAUSAL) odd_init(odd);
     if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
     for (int key = k0; key < k1; key += KT, stage ^= 1) {
         char *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
-        const bool look = a.causal && key + KT > block_least;
+        const bool look = CAUSAL && key + KT > block_least;
         if (look) {
             attn_landed();
             if (in.ld.template odd<T>(kt)) odd.tile[stage] = key;
@@ -1399,14 +1400,14 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 
 // Both in one launch, so that workgroups of the second kind fill the CUs that
 // those of the first, which take longer, leave idle at their end.
-template <typename T, int NK, int ND>
+template <typename T, int NK, int ND, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
     constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;
     __shared__ __attribute__((aligned(16))) char lds[Q > K ? Q : K];
     __shared__ Odd odd;
     const int keys = a.b * a.hkv * a.key_tiles * a.row_splits;
-    if ((int)blockIdx.x < keys) attend_keys<T, NK, ND>(a, lds, odd);
-    else attend_queries<T, NK, ND>(a, lds, odd, blockIdx.x - keys);
+    if ((int)blockIdx.x < keys) attend_keys<T, NK, ND, CAUSAL>(a, lds, odd);
+    else attend_queries<T, NK, ND, CAUSAL>(a, lds, odd, blockIdx.x - keys);
 }
 
 // ------------------------------------------------------------------- host
@@ -1491,8 +1492,11 @@ static hipError_t by_form(const AttnArgs &a, hipStream_t st) {
 template <typename T, int NK, int ND> struct Attend {
     static hipError_t go(const AttnArgs &a, hipStream_t st) {
         const dim3 grid((unsigned)((int64_t)a.b * a.hkv * a.tiles * a.splits));
-        if (a.waves == 1) return start(attend<T, NK, ND, 1>, grid, 64, st, a);
-        return start(attend<T, NK, ND, 4>, grid, 256, st, a);
+        return a.causal ? go<true>(a, grid, st) : go<false>(a, grid, st);
+    }
+    template <bool C> static hipError_t go(const AttnArgs &a, dim3 grid, hipStream_t st) {
+        if (a.waves == 1) return start(attend<T, NK, ND, 1, C>, grid, 64, st, a);
+        return start(attend<T, NK, ND, 4, C>, grid, 256, st, a);
     }
 };
 template <typename T, int NK, int ND> struct AttendBackward {
@@ -1503,7 +1507,10 @@ template <typename T, int NK, int ND> struct AttendBackward {
         const int64_t wgs =
             pairs * ((int64_t)a.key_tiles * a.row_splits + (int64_t)a.tiles * a.q_splits);
         hipError_t e = hipSuccess;
-        if (wgs) e = start(attend_backward<T, NK, ND>, dim3((unsigned)wgs), 256, st, a);
+        const dim3 grid((unsigned)wgs);
+        if (wgs)
+            e = a.causal ? start(attend_backward<T, NK, ND, true>, grid, 256, st, a)
+                         : start(attend_backward<T, NK, ND, false>, grid, 256, st, a);
         const int64_t lanes = (a.q_splits > 1 ? pairs * a.tq * a.group * (a.d / 4) : 0) +
                               (a.row_splits > 1 ? pairs * a.tk * (a.d / 2) : 0);
         if (e == hipSuccess && lanes)
