@@ -2,7 +2,8 @@
 
 ``ctc`` is the ctypes binding of libctc.so (include/ctc.h); ``CtcNet`` owns
 a bound network; ``ops`` holds the operators around a protected classifier
-(group norm, 8-bit products, token scores).  Importing fails if the HIP
+(group norm, 8-bit products, token scores, attention over a map's pixels,
+head norms with rotations, clipping of gradients).  Importing fails if the HIP
 library is not built; ``ops`` is imported when it is first used, and fails
 if its binding is not.
 """

