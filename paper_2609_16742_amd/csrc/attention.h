@@ -289,6 +289,25 @@ __device__ __forceinline__ float other_half(float v) {
     return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
+// A lane's part of a result's column times f, to the row at `o`.  The two lanes
+// of a column hold alternate fours of its values: they exchange every other four,
+// so each stores eight in a row.
+template <typename T>
+__device__ __forceinline__ void store_result(T *o, const f16v &acc, float f, int n, int h32,
+                                             int d) {
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; x++) v[x] = acc[4 * j + x] * f;
+        const u4 p = __builtin_bit_cast(u4, pack8<T>(v));
+        const auto lo = __builtin_amdgcn_permlane32_swap(p[0], p[2], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(p[1], p[3], false, false);
+        const int e = n * 32 + 8 * (j + h32);
+        if (e < d) *(u4 *)(o + e) = u4{lo[0], hi[0], lo[1], hi[1]};
+    }
+}
+
 __device__ __forceinline__ f16v zeros16() {
     f16v z;
 #pragma unroll
@@ -625,16 +644,7 @@ void attend(AttnArgs a) {
     T *o = (T *)a.o + at.b * a.os[0] + row.t * a.os[1] + head * a.os[2];
 #pragma unroll
     for (int n = 0; n < ND; n++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int e = n * 32 + j * 8 + 4 * h32;
-            if (e < a.d) {
-                float v[4];
-#pragma unroll
-                for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * inv : 0.f;
-                store<T, 4>(o + e, v);
-            }
-        }
+        store_result<T>(o, valid ? acc[n] : zeros16(), inv, n, h32, a.d);
     if (!h32) a.lse[((int64_t)at.b * a.hq + head) * a.tq + row.t] = lse2 * LN2;
 }
 
@@ -841,14 +851,7 @@ __device__ __forceinline__ void store_keys(const AttnArgs &a, const Place &p, in
                   : (T *)a.dk + p.at.b * a.dks[0] + key * a.dks[1] + p.at.h * a.dks[2];
 #pragma unroll
     for (int n = 0; n < ND; n++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int x = n * 32 + j * 8 + 4 * h32;
-            float u[4];
-#pragma unroll
-            for (int z = 0; z < 4; z++) u[z] = valid ? acc[n][4 * j + z] * f : 0.f;
-            if (x < a.d) store<T, 4>(o + x, u);
-        }
+        store_result<T>(o, valid ? acc[n] : zeros16(), f, n, h32, a.d);
 }
 // Sixteen first values of a block of rows (as a result holds them).
 __device__ __forceinline__ f16v first_values(const float *st, int h32) {
@@ -1209,16 +1212,7 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
     T *o = (T *)a.dq + at.b * a.dqs[0] + row.t * a.dqs[1] + head * a.dqs[2];
 #pragma unroll
     for (int n = 0; n < ND; n++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int i = n * 32 + j * 8 + 4 * h32;
-            if (i < a.d) {
-                float v[4];
-#pragma unroll
-                for (int x = 0; x < 4; x++) v[x] = valid ? acc[n][4 * j + x] * back : 0.f;
-                store<T, 4>(o + i, v);
-            }
-        }
+        store_result<T>(o, valid ? acc[n] : zeros16(), back, n, h32, a.d);
 }
 
 // Few rows and keys, up to 64 each (a map of 7 x 7): a workgroup takes a
@@ -1369,15 +1363,6 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
         sf[s] = pop.along_result(st, block, s, h32);
         df[s] = pop.along_result(dt, block, s, h32);
     }
-    auto put = [&](T *o, int n, const f16v &acc, float f) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int i = n * 32 + j * 8 + 4 * h32;
-            const float v[4] = {acc[4 * j] * f, acc[4 * j + 1] * f, acc[4 * j + 2] * f,
-                                acc[4 * j + 3] * f};
-            if (i < a.d) store<T, 4>(o + i, v);
-        }
-    };
     const bool valid = x >= lo && x < hi;
     T *dkp = (T *)a.dk + at.b * a.dks[0] + x * a.dks[1] + at.h * a.dks[2];
     T *dvp = (T *)a.dv + at.b * a.dvs[0] + x * a.dvs[1] + at.h * a.dvs[2];
@@ -1401,10 +1386,11 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
                     dv[i] = __builtin_nanf("");
         }
         if (x < a.tk) {
-            put(dvp, n, dv, x < kn ? back : 0.f);
-            put(dkp, n, dk, x < kn ? a.scale * back : 0.f);
+            store_result<T>(dvp, x < kn ? dv : zeros16(), back, n, h32, a.d);
+            store_result<T>(dkp, x < kn ? dk : zeros16(), a.scale * back, n, h32, a.d);
         }
-        if (x < a.tq * a.group) put(dqp, n, valid ? dq : zeros16(), a.scale * back);
+        if (x < a.tq * a.group)
+            store_result<T>(dqp, valid ? dq : zeros16(), a.scale * back, n, h32, a.d);
     }
 }
 
