@@ -83,16 +83,18 @@ __device__ __forceinline__ uint32_t lds_address(const char *p) {
 // instruction of its own: with the builtin, the compiler has all loads to LDS
 // land before any read along columns, and an iteration's prefetch is waited
 // for within it.  Nothing but attn_arrive waits for these.  (M0, which the
-// compiler keeps nothing in, is LDS's address.)
+// compiler keeps nothing in, is LDS's address.  A scalar register that the
+// vector unit wrote, as readfirstlane does, may be read by a load five states
+// later: the compiler sees no load here, so the states stand in it.)
 __device__ __forceinline__ void load_lds16(const u4 &buf, uint32_t to, uint32_t at,
                                            uint32_t past) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(at), "s"(buf), "s"(__builtin_amdgcn_readfirstlane(past))
                  : "memory");
 }
 __device__ __forceinline__ void load_lds4(const u4 &buf, uint32_t to, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(at), "s"(buf)
                  : "memory");
@@ -1220,7 +1222,7 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
 // each, and with both in LDS as operands every product of the gradients: five
 // in all, and what attn_rows finds is found on the way, so one launch does it.
 // Its chain is one load, two exchanges of the workgroup and the stores.  64 maps
-// of 7 x 7, 8 heads of 64: 20 us by the general kernels, 10.8 by this.
+// of 7 x 7, 8 heads of 64: 20 us by the general kernels, 10 by this.
 template <typename T, int NK, int ND>
 __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(AttnArgs a) {
     typedef typename Tile<T>::V8 V8;
