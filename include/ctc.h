@@ -771,6 +771,8 @@ typedef struct {
  * Probabilities are rounded to dtype for their product with v.  A NaN or an
  * infinity in a key or a value reaches no query that does not see it; among
  * causal ones, an infinite value may be a NaN in the o of those that do.
+ * o may be q (the same address and strides); apart from that outputs must not
+ * overlap inputs or each other.
  * The same inputs give the same bits every time.  With G = q_heads / k_heads <=
  * 65536 and R = queries * G rows: R, keys <= 2^30, batch * k_heads * (R / 64 +
  * keys / 64 + 2) < 2^23 - 512; 64 token strides and G head strides (keys: one)
@@ -788,7 +790,9 @@ ctc_status ctc_attention_forward(const ctc_attention *a, const ctc_heads *q,
  *   dq_i = scale sum_j ds_ij k_j
  * (p and ds rounded to dtype, in fp16 with an exponent that fits the sequence's
  * dout and v; sums over the query heads that share a key head).  Gradients of
- * what takes no part are zeros.  The same inputs give the same bits every
+ * what takes no part are zeros.  dk and dv may be k or v (the same address and
+ * strides; dq then takes a launch of its own); apart from that outputs must not
+ * overlap inputs or each other.  The same inputs give the same bits every
  * time. */
 ctc_status ctc_attention_backward(const ctc_attention *a,
                                   const ctc_heads *dout, const ctc_heads *q,

@@ -1399,6 +1399,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 // Both in one launch, so that workgroups of the second kind fill the CUs that
 // those of the first, which take longer, leave idle at their end.  800 of each
 // kind on 512 places (2 x 3136, 16 heads of 128): 803 us apart, 620 together.
+// (Apart, dq first, where dk or dv is written over the keys or values: those
+// of the second kind read all of them, those of the first their own.)
 template <typename T, int NK, int ND, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
     constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;
@@ -1503,18 +1505,28 @@ template <typename T, int NK, int ND> struct AttendBackward {
         const int64_t pairs = (int64_t)a.b * a.hkv;
         if (attn_small(a))
             return start(attend_backward_small<T, NK, ND>, dim3((unsigned)pairs), 256, st, a);
-        const int64_t wgs =
-            pairs * ((int64_t)a.key_tiles * a.row_splits + (int64_t)a.tiles * a.q_splits);
+        const int64_t keys = pairs * a.key_tiles * a.row_splits;
+        const int64_t queries = pairs * a.tiles * a.q_splits;
         hipError_t e = hipSuccess;
-        const dim3 grid((unsigned)wgs);
-        if (wgs)
-            e = a.causal ? start(attend_backward<T, NK, ND, true>, grid, 256, st, a)
-                         : start(attend_backward<T, NK, ND, false>, grid, 256, st, a);
+        if (a.keys_last) {
+            AttnArgs first = a;
+            first.key_tiles = 0;
+            e = both(first, queries, st);
+            if (e == hipSuccess) e = both(a, keys, st);
+        } else {
+            e = both(a, keys + queries, st);
+        }
         const int64_t lanes = (a.q_splits > 1 ? pairs * a.tq * a.group * (a.d / 4) : 0) +
                               (a.row_splits > 1 ? pairs * a.tk * (a.d / 2) : 0);
         if (e == hipSuccess && lanes)
             e = start(attend_sums<T>, grid_of(ceil_of(lanes, 256)), 256, st, a);
         return e;
+    }
+    static hipError_t both(const AttnArgs &a, int64_t wgs, hipStream_t st) {
+        const dim3 grid((unsigned)wgs);
+        if (!wgs) return hipSuccess;
+        return a.causal ? start(attend_backward<T, NK, ND, true>, grid, 256, st, a)
+                        : start(attend_backward<T, NK, ND, false>, grid, 256, st, a);
     }
 };
 

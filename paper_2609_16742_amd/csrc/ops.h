@@ -89,6 +89,7 @@ struct AttnArgs {
     const int32_t *qlen, *klen;  // [b] or null
     void *dq, *dk, *dv;
     float *ws;
+    int keys_last;               // dk or dv is k or v: dq in a launch before
     // set by the launchers
     int group, gshift, waves, tiles, splits, per, row_tiles, key_tiles, q_chunks, v_chunks, row_splits, q_splits;
     uint32_t gmul;

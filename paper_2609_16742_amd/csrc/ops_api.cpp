@@ -7,6 +7,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <exception>
+#include <numeric>
 #include <vector>
 
 #include "../../include/ctc.h"
@@ -144,6 +145,100 @@ ctc_status heads_arg(const ctc_heads *h, const char *name, int64_t b, int64_t t,
     return CTC_OK;
 }
 
+// Elements of a tensor of heads (or, as one head, of a dense one), in bytes:
+// runs of `run` bytes at three strides.
+struct Region {
+    uintptr_t at = 0;
+    int64_t size[3] = {0, 0, 0}, stride[3] = {0, 0, 0}, run = 0;
+    bool empty() const { return !run || !size[0] || !size[1] || !size[2]; }
+    double end() const {
+        double e = (double)at + (double)run;
+        for (int i = 0; i < 3; i++) e += (double)(size[i] - 1) * (double)stride[i];
+        return e;
+    }
+    bool operator==(const Region &o) const {
+        return at == o.at && run == o.run && std::equal(size, size + 3, o.size) &&
+               std::equal(stride, stride + 3, o.stride);
+    }
+};
+Region region(const void *data, int64_t b, int64_t t, int64_t heads, const int64_t (&strides)[3],
+              int64_t d, int type) {
+    Region r;
+    const int64_t bytes = type_bytes(type), size[3] = {b, t, heads};
+    r.at = (uintptr_t)data;
+    r.run = data ? d * bytes : 0;
+    for (int i = 0; i < 3; i++) {
+        r.size[i] = size[i];
+        r.stride[i] = strides[i] * bytes;
+    }
+    return r;
+}
+Region dense(const void *data, int64_t n, int type) {
+    return region(data, 1, 1, 1, {0, 0, 0}, n, type);
+}
+// Whether a byte is of both.  Parts of one buffer may lie within each other's
+// span, so what is looked for is a run of each, at whole multiples of their
+// strides, that meet: multiples of equal strides count as one, strides are gone
+// through from the largest down, and only where what the smaller ones reach can
+// still close the gap, which for such parts leaves one or two choices each.
+struct Meeting {
+    struct Step { int64_t stride, lo, hi; };
+    Step step[6];
+    int64_t lo[7], hi[7];                        // reach of the steps from i on
+    int n = 0, left = 1 << 16;
+    void add(int64_t stride, int64_t from, int64_t to) {
+        for (int i = 0; i < n; i++)
+            if (step[i].stride == stride) {
+                step[i].lo += from;
+                step[i].hi += to;
+                return;
+            }
+        if (stride && from < to) step[n++] = Step{stride, from, to};
+    }
+    static int64_t over(int64_t a, int64_t b) { return a / b - (a % b < 0); }   // rounded down
+    // a sum of multiples of the steps from i on within from .. to
+    bool find(int i, int64_t from, int64_t to) {
+        if (to < lo[i] || from > hi[i]) return false;
+        if (i == n) return true;
+        // (choices beyond any that parts of a buffer leave: not told apart)
+        if (--left < 0) return true;
+        const Step &s = step[i];
+        int64_t a = -over(hi[i + 1] - from, s.stride), b = over(to - lo[i + 1], s.stride);
+        if (a < s.lo) a = s.lo;
+        if (b > s.hi) b = s.hi;
+        if (b - a > 8) {
+            int64_t g = 0;
+            for (int k = i; k < n; k++) g = std::gcd(g, step[k].stride);
+            if (over(to, g) * g < from) return false;
+        }
+        for (int64_t v = a; v <= b; v++)
+            if (find(i + 1, from - v * s.stride, to - v * s.stride)) return true;
+        return false;
+    }
+    bool of(const Region &a, const Region &b) {
+        for (int i = 0; i < 3; i++) {
+            add(a.stride[i], 0, a.size[i] - 1);
+            add(b.stride[i], 1 - b.size[i], 0);
+        }
+        std::sort(step, step + n, [](const Step &x, const Step &y) { return x.stride > y.stride; });
+        lo[n] = hi[n] = 0;
+        for (int i = n - 1; i >= 0; i--) {
+            lo[i] = lo[i + 1] + step[i].lo * step[i].stride;
+            hi[i] = hi[i + 1] + step[i].hi * step[i].stride;
+        }
+        const int64_t gap = (int64_t)(b.at - a.at);
+        return find(0, gap - (a.run - 1), gap + (b.run - 1));
+    }
+};
+bool meet(const Region &a, const Region &b) {
+    if (a.empty() || b.empty()) return false;
+    const double x = a.end(), y = b.end();
+    if (x <= (double)b.at || y <= (double)a.at) return false;
+    // (no memory is that long)
+    if (x >= 0x1p61 || y >= 0x1p61) return true;
+    return Meeting().of(a, b);
+}
+
 ctc_status attn_args(const ctc_attention *c, AttnArgs &a) {
     if (!c) return fail(CTC_ERR_ARG, "NULL attention");
     if (c->dtype != CTC_F16 && c->dtype != CTC_BF16)
@@ -179,6 +274,58 @@ ctc_status attn_heads(const AttnArgs &a, const ctc_heads *h, const char *name, b
     const double group = queries ? a.hq / a.hkv : 1;
     if (64. * strides[1] + group * strides[2] >= (double)(1 << 29))
         return fail(CTC_ERR_UNSUPPORTED, "strides of %s too large", name);
+    return CTC_OK;
+}
+
+struct Named {
+    const char *name;
+    Region r;
+};
+ctc_status meeting(const Named &x, const Named &y) {
+    return fail(CTC_ERR_ARG, "%s overlaps %s", x.name, y.name);
+}
+Region attn_region(const AttnArgs &a, bool queries, const void *data, const int64_t (&strides)[3]) {
+    return region(data, a.b, queries ? a.tq : a.tk, queries ? a.hq : a.hkv, strides, a.d, a.type);
+}
+Region attn_lse(const AttnArgs &a) {
+    return dense(a.lse, (int64_t)a.b * a.hq * a.tq, CTC_F32);
+}
+// o may be q: a row is read and written by one wave, or written by the launch
+// that joins ranges of keys.
+ctc_status attn_apart(const AttnArgs &a) {
+    const Named in[3] = {{"q", attn_region(a, true, a.q, a.qs)},
+                         {"k", attn_region(a, false, a.k, a.ks)},
+                         {"v", attn_region(a, false, a.v, a.vs)}};
+    const Named out[2] = {{"o", attn_region(a, true, a.o, a.os)}, {"lse", attn_lse(a)}};
+    if (meet(out[0].r, out[1].r)) return meeting(out[0], out[1]);
+    for (int i = 0; i < 2; i++)
+        for (int j = 0; j < 3; j++)
+            if (!(i == 0 && j == 0 && out[i].r == in[j].r) && meet(out[i].r, in[j].r))
+                return meeting(out[i], in[j]);
+    return CTC_OK;
+}
+// dk and dv may be k and v: a workgroup reads the keys and values of the
+// gradients that it writes and no others, so dq, which all keys go into, has to
+// be there before (`keys_last`).
+ctc_status attn_backward_apart(AttnArgs &a) {
+    const Named in[6] = {{"dout", attn_region(a, true, a.dout, a.dos)},
+                         {"q", attn_region(a, true, a.q, a.qs)},
+                         {"o", attn_region(a, true, a.o, a.os)},
+                         {"lse", attn_lse(a)},
+                         {"k", attn_region(a, false, a.k, a.ks)},
+                         {"v", attn_region(a, false, a.v, a.vs)}};
+    const Named out[3] = {{"dq", attn_region(a, true, a.dq, a.dqs)},
+                          {"dk", attn_region(a, false, a.dk, a.dks)},
+                          {"dv", attn_region(a, false, a.dv, a.dvs)}};
+    for (int i = 0; i < 3; i++) {
+        for (int j = 0; j < i; j++)
+            if (meet(out[i].r, out[j].r)) return meeting(out[i], out[j]);
+        for (int j = 0; j < 6; j++) {
+            if (!meet(out[i].r, in[j].r)) continue;
+            if (i == 0 || j < 4 || !(out[i].r == in[j].r)) return meeting(out[i], in[j]);
+            a.keys_last = 1;
+        }
+    }
     return CTC_OK;
 }
 
@@ -473,7 +620,7 @@ ctc_status ctc_attention_forward(const ctc_attention *c, const ctc_heads *q, con
     if (!lse) return fail(CTC_ERR_ARG, "NULL lse");
     a.o = (void *)out; a.lse = lse; a.ws = (float *)workspace;
     s = need_workspace(attention_workspace(a, false), workspace, ws_bytes);
-    if (s != CTC_OK) return s;
+    if (s != CTC_OK || (s = attn_apart(a)) != CTC_OK) return s;
     return done(launch_attention(a, S(stream)));
 }
 
@@ -500,7 +647,7 @@ ctc_status ctc_attention_backward(const ctc_attention *c, const ctc_heads *dout,
     a.o = (void *)op; a.lse = (float *)lse; a.ws = (float *)workspace;
     a.dq = (void *)dqp; a.dk = (void *)dkp; a.dv = (void *)dvp;
     s = need_workspace(attention_workspace(a, true), workspace, ws_bytes);
-    if (s != CTC_OK) return s;
+    if (s != CTC_OK || (s = attn_backward_apart(a)) != CTC_OK) return s;
     return done(launch_attention_backward(a, S(stream)));
 }
 

@@ -172,7 +172,8 @@ def attention(q, k, v, causal=False, q_lengths=None, k_lengths=None,
     ``k_lengths`` (int32 [batch]): what stands behind them takes no part.
     With ``causal``, query i sees keys up to i + keys - queries (of the
     sequence's own).  A query that sees nothing has o = 0, lse = -inf.
-    ``out``: an (o, lse) to write into."""
+    ``out``: an (o, lse) to write into; o may be q, but overlaps no other
+    input."""
     o, lse = out or (None, None)
     return _run(_binding.attention, q, stream, q, k, v, causal, q_lengths,
                 k_lengths, scale, o, lse)
@@ -183,7 +184,8 @@ def attention_backward(do, q, k, v, o, lse, causal=False, q_lengths=None,
     """dq, dk, dv of :func:`attention` (same arguments, with the ``o`` and
     ``lse`` it returned) for the gradient ``do`` of o.  Probabilities are
     computed again.  ``out``: a (dq, dk, dv) to write into, which may be parts
-    of one projection's gradient."""
+    of one projection's gradient; dk and dv may be k or v, but no other input
+    and not each other is overlapped."""
     dq, dk, dv = out or (None, None, None)
     return _run(_binding.attention_backward, q, stream, do, q, k, v, o, lse,
                 causal, q_lengths, k_lengths, scale, dq, dk, dv)
