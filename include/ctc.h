@@ -788,9 +788,10 @@ ctc_status ctc_attention_forward(const ctc_attention *a, const ctc_heads *q,
  * lse_i) and ds_ij = p_ij (dout_i v_j - dout_i o_i),
  *   dv_j = sum_i p_ij dout_i,  dk_j = scale sum_i ds_ij q_i,
  *   dq_i = scale sum_j ds_ij k_j
- * (p and ds rounded to dtype, in fp16 with an exponent that fits the sequence's
- * dout and v; sums over the query heads that share a key head).  Gradients of
- * what takes no part are zeros.  dk and dv may be k or v (the same address and
+ * (p and ds rounded to dtype, in fp16 as 2^15 p, and ds with an exponent that
+ * fits v and the row's dout, or for dk the largest dout of the sequence and key
+ * head; sums over the query heads that share a key head).  Gradients of what
+ * takes no part are zeros.  dk and dv may be k or v (the same address and
  * strides; dq then takes a launch of its own); apart from that outputs must not
  * overlap inputs or each other.  The same inputs give the same bits every
  * time. */

@@ -31,8 +31,8 @@ template <> struct Tile<_Float16> {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }
     // p = 2^SHIFT relative to the maximum, up to 2^LIMIT: its smallest values
-    // keep their bits in fp16
-    static constexpr float SHIFT = 8.f, LIMIT = 15.f;
+    // keep their bits in fp16.  (The backward pass's, at most 1, are 2^15 p.)
+    static constexpr float SHIFT = 8.f, LIMIT = 15.f, BACK = 15.f;
 };
 template <> struct Tile<__bf16> {
     typedef __bf16 V8 __attribute__((ext_vector_type(8)));
@@ -40,7 +40,7 @@ template <> struct Tile<__bf16> {
     static __device__ __forceinline__ f16v mul(V8 a, V8 b, f16v c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
-    static constexpr float SHIFT = 0.f, LIMIT = 8.f;
+    static constexpr float SHIFT = 0.f, LIMIT = 8.f, BACK = 0.f;
 };
 
 // Eight fp32 values in 16 bits (to nearest), as an operand.
@@ -691,10 +691,13 @@ template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArg
 //   dv_j = sum_i p_ij do_i,  dk_j = scale sum_i ds_ij q_i,
 //   dq_i = scale sum_j ds_ij k_j.
 // `attn_rows` writes what each row needs: -lse as the products' first value
-// (so p = exp2(c s), -infinity where the row is no row) and -delta.  For fp16
-// it also bounds |do| and |v|: p is scaled by the power of two 2^e with which
-// 2 |do| |v| 2^e is below 2^15, so that neither a small ds loses its bits nor
-// a large one its exponent.
+// (so p = exp2(c s), -infinity where the row is no row) and -delta.  fp16 takes
+// p for dv as 2^15 p, whatever the gradients are, and ds as 2^e ds with the
+// largest e for which 2 |do| |v| 2^e, a bound of it, is at most 2^14 (attn_rows
+// finds the sizes).  |v| is the largest of the sequence's key head, since delta
+// has a part of each.  |do| is the row's own for dq; for dk, whose sums go over
+// rows, it is the largest of those that the workgroup goes through, so a row
+// 2^24 times smaller than another in the sum for a key has few bits left there.
 // The probabilities are computed twice, once with a lane's key fixed (dk, dv)
 // and once with its row fixed (dq): seven products instead of five, and no
 // sums between workgroups, whose order would change the result's bits.
@@ -773,27 +776,32 @@ template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs 
             vmax(vmax(most[0], most[1]), vmax(most[2], most[3]));
 }
 
-// e for the lanes' squared sizes of do and v.
-__device__ __forceinline__ float attn_exponent_of(float q, float v) {
+// The largest of all lanes' values.
+__device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        q = vmax(q, __shfl_xor(q, o));
-        v = vmax(v, __shfl_xor(v, o));
-    }
+    for (int o = 32; o; o >>= 1) v = vmax(v, __shfl_xor(v, o));
+    return v;
+}
+// e for squared sizes of do and v.  (60: gradients of zeros)
+__device__ __forceinline__ float attn_exponent(float q, float v) {
     // log2 of 2 |do| |v|, rounded up
     const float e = 14.f - __builtin_ceilf(1.f + 0.5f * (__builtin_amdgcn_logf(q) +
                                                        __builtin_amdgcn_logf(v)));
-    return uniform(e > 15.f ? 15.f : e < -20.f ? -20.f : e);
+    return e > 60.f ? 60.f : e;
 }
-// e of the sequence and key head (0 for bf16, whose exponents are fp32's).
-template <typename T> __device__ __forceinline__ float attn_exponent(const AttnArgs &a, int pair) {
-    if (sizeof(T) != 2 || a.type != F16) return 0.f;
-    const int lane = threadIdx.x & 63;
+// The largest squared size of v of the sequence and key head, and of do in
+// chunks q0 .. q1 - 1 of 64 rows.
+__device__ __forceinline__ float attn_value_size(const AttnArgs &a, int pair) {
+    const float *b = a.bounds + (int64_t)pair * (a.q_chunks + a.v_chunks) + a.q_chunks;
+    float v = 0.f;
+    for (int i = threadIdx.x & 63; i < a.v_chunks; i += 64) v = vmax(v, b[i]);
+    return wave_max(v);
+}
+__device__ __forceinline__ float attn_row_size(const AttnArgs &a, int pair, int q0, int q1) {
     const float *b = a.bounds + (int64_t)pair * (a.q_chunks + a.v_chunks);
-    float q = 0.f, v = 0.f;
-    for (int i = lane; i < a.q_chunks; i += 64) q = vmax(q, b[i]);
-    for (int i = lane; i < a.v_chunks; i += 64) v = vmax(v, b[a.q_chunks + i]);
-    return attn_exponent_of(q, v);
+    float q = 0.f;
+    for (int i = q0 + (threadIdx.x & 63); i < q1; i += 64) q = vmax(q, b[i]);
+    return wave_max(q);
 }
 
 // Where a workgroup of attend_keys stands: its keys, and the rows it goes
@@ -913,7 +921,14 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
     f16v dk[ND], dv[ND];
 #pragma unroll
     for (int n = 0; n < ND; n++) dk[n] = dv[n] = zeros16();
-    const float c = uniform(a.scale * LOG2E), e = attn_exponent<T>(a, p.pair);
+    constexpr bool HALF = std::is_same<T, _Float16>::value;
+    constexpr float BACK = Tile<T>::BACK;
+    const float c = uniform(a.scale * LOG2E);
+    float e = 0.f;
+    if (HALF)
+        e = uniform(attn_exponent(attn_row_size(a, p.pair, p.row / 64, (p.end + 63) / 64),
+                                  attn_value_size(a, p.pair)));
+    const float to_ds = exp2_hw(e - BACK);       // ds = (2^BACK p) (dp - delta) times this
     Operands<T, PITCH> op;
     op.init(lane);
 
@@ -957,7 +972,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
                                   dp);
             float x[16], y[16];
 #pragma unroll
-            for (int i = 0; i < 16; i++) x[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            for (int i = 0; i < 16; i++) x[i] = exp2_hw(__builtin_fmaf(s[i], c, BACK));
             if (WIDE) {
                 // 8 + 3 NK reads
                 ATTN_GROUP(GROUP_READ, 4 + NK);
@@ -981,7 +996,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
                 __builtin_amdgcn_s_setprio(0);
             }
 #pragma unroll
-            for (int i = 0; i < 16; i++) y[i] = x[i] * dp[i];
+            for (int i = 0; i < 16; i++) y[i] = x[i] * (HALF ? dp[i] * to_ds : dp[i]);
             if (r < wave_from) {
 #pragma unroll
                 for (int i = 0; i < 16; i++)
@@ -1018,9 +1033,8 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
         }
     }
     if (spoilt) odd_results<ND>(odd, h32, 1 - from, dv);
-    const float back = exp2_hw(-e);
-    store_keys<T, ND>(a, p, key, h32, dk, a.scale * back, false);
-    store_keys<T, ND>(a, p, key, h32, dv, back, true);
+    store_keys<T, ND>(a, p, key, h32, dk, a.scale * exp2_hw(-e), false);
+    store_keys<T, ND>(a, p, key, h32, dv, exp2_hw(-BACK), true);
 }
 // Adds up the ranges' gradients, always in the same order: four values a lane,
 // dq's rows first, then dk and dv of each key.
@@ -1101,10 +1115,20 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
     for (int s = 0; s < NK; s++) g[s] = row_operand<T>(op_, lane, s, a.d);
     settle(q);
     settle(g);
+    const float c = uniform(a.scale * LOG2E);
+    float e = 0.f;
+    if (std::is_same<T, _Float16>::value) {
+        float size = 0.f;
+#pragma unroll
+        for (int s = 0; s < NK; s++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) size += (float)g[s][i] * (float)g[s][i];
+        size += other_half(size);
+        e = attn_exponent(size < INF ? size : 0.f, attn_value_size(a, pair));
+    }
     f16v acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; n++) acc[n] = zeros16();
-    const float c = uniform(a.scale * LOG2E), e = attn_exponent<T>(a, pair);
     const float *st = a.stats + attn_stats(a, pair, r < a.row_tiles * 32 ? r : 0);
     const float first_s = valid ? st[0] : -INF, first_dp = valid ? st[32] : 0.f;
 
@@ -1227,12 +1251,14 @@ template <typename T, int NK, int ND>
 __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(AttnArgs a) {
     typedef typename Tile<T>::V8 V8;
     constexpr int PITCH = NK <= 4 ? 64 : 128, TILE = 64 * PITCH * 2, PT = 64 * 64 * 2;
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE + 3 * PT + 1024];
+    constexpr bool HALF = std::is_same<T, _Float16>::value;
+    constexpr float BACK = Tile<T>::BACK;
+    __shared__ __attribute__((aligned(16))) char lds[4 * TILE + 3 * PT + 2048];
     __shared__ Odd odd;
     char *qt = lds, *ot = lds + TILE, *kt = lds + 2 * TILE, *vt = lds + 3 * TILE;
     char *pt = lds + 4 * TILE, *st = pt + PT, *dt = st + PT;    // p^T, ds^T, ds
     float *first = (float *)(dt + PT), *delta = first + 64, *dsize = first + 128,
-          *vsize = first + 192;
+          *vsize = first + 192, *to_dq = first + 256;
     const int lane = threadIdx.x & 63, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const AttnPlace at = attn_place(a, 1, blockIdx.x);
@@ -1268,7 +1294,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 #pragma unroll
                 for (int j = 0; j < 8; j++) dot += x[j] * y[j], size += x[j] * x[j];
             }
-            if (std::is_same<T, _Float16>::value && e < a.d && r < kn) {
+            if (HALF && e < a.d && r < kn) {
                 float x[8];
                 load<T, 8>(vb + r * a.vs[1] + e, x);
 #pragma unroll
@@ -1296,8 +1322,17 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     }
     attn_arrive();
     const bool spoilt = a.causal && odd.tile[0] == 0;
-    float e = 0.f;
-    if (std::is_same<T, _Float16>::value) e = attn_exponent_of(dsize[lane], vsize[lane]);
+    // exponents of the sequence's ds, and of row `lane`'s for dq (what the
+    // products take from 2^BACK p, for each wave by itself)
+    float e = 0.f, row_e = 0.f, to_dk = 1.f;
+    if (HALF) {
+        const float size = dsize[lane], value = wave_max(vsize[lane]);
+        e = uniform(attn_exponent(wave_max(size), value));
+        row_e = attn_exponent(size, value);
+        to_dk = exp2_hw(e - BACK);
+        to_dq += wave * 64;
+        to_dq[lane] = exp2_hw(row_e - BACK);
+    }
     const float c = uniform(a.scale * LOG2E);
     Operands<T, PITCH> op;
     Operands<T, 64> pop;
@@ -1320,16 +1355,20 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
             from = t < 0 ? 0 : t * a.group;
         }
         if (key >= kn) from = 64;
-        float x[16], y[16];
+        float x[16], y[16], z[16];
+        f16v rows;
+        if (HALF) rows = first_values(to_dq + 32 * rblock, h32);
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-            x[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+            x[i] = exp2_hw(__builtin_fmaf(s[i], c, BACK));
             if (32 * rblock + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = 0.f;
-            y[i] = x[i] == 0.f ? 0.f : x[i] * dp[i];
+            const float none = x[i] == 0.f ? 0.f : dp[i];
+            y[i] = x[i] * (HALF ? none * to_dk : none);
+            z[i] = HALF ? x[i] * (none * rows[i]) : y[i];
         }
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-            const V8 p = pack8<T>(x + 8 * k), d = pack8<T>(y + 8 * k);
+            const V8 p = pack8<T>(x + 8 * k), d = pack8<T>(y + 8 * k), r8 = pack8<T>(z + 8 * k);
             const u4 pu = __builtin_bit_cast(u4, p), du = __builtin_bit_cast(u4, d);
 #pragma unroll
             for (int j = 0; j < 2; j++) {
@@ -1342,7 +1381,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
                 for (int i = 0; i < 4; i++) {
                     const int r = 32 * rblock + 16 * k + 8 * j + 4 * h32 + i;
                     *(T *)(dt + r * 128 + ((key / 8 ^ swizzle<64>(r)) << 4) + key % 8 * 2) =
-                        d[4 * j + i];
+                        r8[4 * j + i];
                 }
             }
         }
@@ -1355,8 +1394,8 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     }
     __syncthreads();
     const int block = wave & 1, half = wave >> 1;
-    const float back = exp2_hw(-e);
     const int x = 32 * block + (lane & 31);      // the lane's key, and row
+    const float row_back = HALF ? exp2_hw(-__shfl(row_e, x)) : 1.f;
     const AttnRow row = attn_row(a, x);
     V8 pf[4], sf[4], df[4];
 #pragma unroll
@@ -1388,11 +1427,11 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
                     dv[i] = __builtin_nanf("");
         }
         if (x < a.tk) {
-            store_result<T>(dvp, x < kn ? dv : zeros16(), back, n, h32, a.d);
-            store_result<T>(dkp, x < kn ? dk : zeros16(), a.scale * back, n, h32, a.d);
+            store_result<T>(dvp, x < kn ? dv : zeros16(), exp2_hw(-BACK), n, h32, a.d);
+            store_result<T>(dkp, x < kn ? dk : zeros16(), a.scale * exp2_hw(-e), n, h32, a.d);
         }
         if (x < a.tq * a.group)
-            store_result<T>(dqp, valid ? dq : zeros16(), a.scale * back, n, h32, a.d);
+            store_result<T>(dqp, valid ? dq : zeros16(), a.scale * row_back, n, h32, a.d);
     }
 }
 
