@@ -770,7 +770,8 @@ typedef struct {
  *   lse   [batch][q_heads][queries] fp32
  * Probabilities are rounded to dtype for their product with v.  A NaN or an
  * infinity in a key or a value reaches no query that does not see it; among
- * causal ones, an infinite value may be a NaN in the o of those that do.
+ * causal ones, an infinite value may be a NaN in the o of those that do.  A
+ * query whose scores are all -infinity has o = 0 and lse = -infinity too.
  * o may be q (the same address and strides); apart from that outputs must not
  * overlap inputs or each other.
  * The same inputs give the same bits every time.  With G = q_heads / k_heads <=

@@ -179,6 +179,14 @@ template <int PITCH, int ROWS, int NW, bool KEEP = false> struct Loads {
                 }
         }
     }
+    // The wave's pieces of a tile, to another.
+    __device__ __forceinline__ void copy(char *to, const char *tile) const {
+#pragma unroll 1
+        for (int i = 0; i < N; i++) {
+            const int at = (i * NW + wave) * 1024 + lane * 16;
+            *(u4 *)(to + at) = *(const u4 *)(tile + at);
+        }
+    }
     // Rows first .. first + ROWS - 1 of a matrix at `base` (rows `stride` bytes
     // apart, those from `end` on as zeros).
     __device__ __forceinline__ void rows(uint32_t tile, const char *base, int64_t stride,
@@ -1142,8 +1150,13 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
         k0 = split * per;
         if (k1 > k0 + per) k1 = k0 + per;
     }
-    // (a row that sees a NaN or an infinite key has it in its lse)
+    // A causal tile with a NaN or an infinity: a row that sees a NaN has it in
+    // its lse, but an infinite key whose score is -infinity shows in nothing, so
+    // scores are taken from the tile as it is, and the product with ds from a
+    // copy with zeros.  (The copy stands in the other stage, whose tile is
+    // loaded when all are done with it.)
     if (CAUSAL) odd_init(odd);
+    bool spoilt = false;
     if (k0 < k1) in.fetch(k0, 0);
     int stage = 0;
     for (int key = k0; key < k1; key += KT, stage ^= 1) {
@@ -1154,71 +1167,84 @@ __device__ __forceinline__ void attend_queries(const AttnArgs &a, char *lds, Odd
             if (in.ld.template odd<T>(kt)) odd.tile[stage] = key;
         }
         attn_arrive();
-        if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
-        if (look && odd.tile[stage] == key) {
-            in.ld.template mend<T>(kt, nullptr, 1, key);
+        const char *kc = kt;
+        const bool apart = look && __builtin_amdgcn_readfirstlane(odd.tile[stage]) == key;
+        if (apart) {
+            char *copy = lds + (stage ^ 1) * 2 * TILE;
+            in.ld.copy(copy, kt);
+            in.ld.template mend<T>(copy, odd.least, 1, key);
+            kc = copy;
+            spoilt = true;
             __syncthreads();
+        } else if (key + KT < k1) {
+            in.fetch(key + KT, stage ^ 1);
         }
-        if (key >= wave_most) continue;
+        if (key < wave_most) {
 #pragma unroll
-        for (int b = 0; b < 2; b++) {
-            f16v s, dp;
-            if (NK > 4) op.refresh();
-            if (NK > 4) __builtin_amdgcn_s_setprio(1);
+            for (int b = 0; b < 2; b++) {
+                f16v s, dp;
+                if (NK > 4) op.refresh();
+                if (NK > 4) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 16; i++) s[i] = first_s, dp[i] = first_dp;
+                for (int i = 0; i < 16; i++) s[i] = first_s, dp[i] = first_dp;
 #pragma unroll
-            for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(kt, b, i), q[i], s);
+                for (int i = 0; i < NK; i++) s = Tile<T>::mul(op.along(kt, b, i), q[i], s);
 #pragma unroll
-            for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(vt, b, i), g[i], dp);
-            float ds[16];
+                for (int i = 0; i < NK; i++) dp = Tile<T>::mul(op.along(vt, b, i), g[i], dp);
+                float ds[16];
 #pragma unroll
-            for (int i = 0; i < 16; i++) ds[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
-            if (NK > 4) {
-                ATTN_GROUP(GROUP_READ, 6);
+                for (int i = 0; i < 16; i++) ds[i] = exp2_hw(__builtin_fmaf(s[i], c, e));
+                if (NK > 4) {
+                    ATTN_GROUP(GROUP_READ, 6);
 #pragma unroll
-                for (int i = 0; i < NK; i++) {
-                    ATTN_GROUP(GROUP_MFMA, 1);
-                    ATTN_GROUP(GROUP_READ, 1);
+                    for (int i = 0; i < NK; i++) {
+                        ATTN_GROUP(GROUP_MFMA, 1);
+                        ATTN_GROUP(GROUP_READ, 1);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NK; i++) {
+                        ATTN_GROUP(GROUP_MFMA, 1);
+                        ATTN_GROUP(GROUP_READ, 1);
+                        ATTN_GROUP(GROUP_VALU, 4);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(0);
                 }
 #pragma unroll
-                for (int i = 0; i < NK; i++) {
-                    ATTN_GROUP(GROUP_MFMA, 1);
-                    ATTN_GROUP(GROUP_READ, 1);
-                    ATTN_GROUP(GROUP_VALU, 4);
+                for (int i = 0; i < 16; i++) ds[i] *= dp[i];
+                if (key + KT > least) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++)
+                        if (key + b * 32 + 8 * (i / 4) + 4 * h32 + i % 4 >= lim) ds[i] = 0.f;
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                __builtin_amdgcn_s_setprio(0);
-            }
+                if (NK > 4) __builtin_amdgcn_s_setprio(1);
+                V8 sb[2];
 #pragma unroll
-            for (int i = 0; i < 16; i++) ds[i] *= dp[i];
-            if (key + KT > least) {
+                for (int k = 0; k < 2; k++) sb[k] = pack8<T>(ds + 8 * k);
 #pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (key + b * 32 + 8 * (i / 4) + 4 * h32 + i % 4 >= lim) ds[i] = 0.f;
-            }
-            if (NK > 4) __builtin_amdgcn_s_setprio(1);
-            V8 sb[2];
+                for (int k = 0; k < 2; k++)
 #pragma unroll
-            for (int k = 0; k < 2; k++) sb[k] = pack8<T>(ds + 8 * k);
+                    for (int n = 0; n < ND; n++)
+                        acc[n] = Tile<T>::mul(op.across(kc, 2 * b + k, n), sb[k], acc[n]);
+                if (NK > 4) {
+                    ATTN_GROUP(GROUP_READ, 8);
 #pragma unroll
-            for (int k = 0; k < 2; k++)
-#pragma unroll
-                for (int n = 0; n < ND; n++)
-                    acc[n] = Tile<T>::mul(op.across(kt, 2 * b + k, n), sb[k], acc[n]);
-            if (NK > 4) {
-                ATTN_GROUP(GROUP_READ, 8);
-#pragma unroll
-                for (int i = 0; i < 2 * ND - 4; i++) {
-                    ATTN_GROUP(GROUP_MFMA, 1);
-                    ATTN_GROUP(GROUP_READ, 2);
+                    for (int i = 0; i < 2 * ND - 4; i++) {
+                        ATTN_GROUP(GROUP_MFMA, 1);
+                        ATTN_GROUP(GROUP_READ, 2);
+                    }
+                    ATTN_GROUP(GROUP_MFMA, 4);
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(0);
                 }
-                ATTN_GROUP(GROUP_MFMA, 4);
-                __builtin_amdgcn_sched_barrier(0);
-                __builtin_amdgcn_s_setprio(0);
             }
+        }
+        if (apart) {
+            __syncthreads();
+            if (key + KT < k1) in.fetch(key + KT, stage ^ 1);
         }
     }
+    if (spoilt) odd_results<ND>(odd, h32, lim, acc);
     if (r >= a.tq * a.group) return;
     const float back = a.scale * exp2_hw(-e);
     if (a.q_splits > 1) {
@@ -1254,7 +1280,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     constexpr bool HALF = std::is_same<T, _Float16>::value;
     constexpr float BACK = Tile<T>::BACK;
     __shared__ __attribute__((aligned(16))) char lds[4 * TILE + 3 * PT + 2048];
-    __shared__ Odd odd;
+    __shared__ Odd odd, odd_keys;
     char *qt = lds, *ot = lds + TILE, *kt = lds + 2 * TILE, *vt = lds + 3 * TILE;
     char *pt = lds + 4 * TILE, *st = pt + PT, *dt = st + PT;    // p^T, ds^T, ds
     float *first = (float *)(dt + PT), *delta = first + 64, *dsize = first + 128,
@@ -1269,7 +1295,10 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
     const T *qb = (const T *)a.q + at.b * a.qs[0] + at.h * a.group * a.qs[2];
     const T *gb = (const T *)a.dout + at.b * a.dos[0] + at.h * a.group * a.dos[2];
     const T *ob = (const T *)a.o + at.b * a.os[0] + at.h * a.group * a.os[2];
-    if (a.causal) odd_init(odd);
+    if (a.causal) {
+        odd_init(odd);
+        odd_init(odd_keys);
+    }
     Loads<PITCH, 64, 4> ld;
     ld.init(lane, wave, a.d);
     ld.queries(a, lds_address(qt), (const char *)qb, a.qs[1] * 2, a.qs[2] * 2, 0, lo, hi);
@@ -1390,7 +1419,7 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
         __syncthreads();
         ld.template mend<T>(qt, nullptr, 1, 0);
         ld.template mend<T>(ot, odd.least, -1, 0);
-        ld.template mend<T>(kt, nullptr, 1, 0);
+        ld.template mend<T>(kt, odd_keys.least, 1, 0);
     }
     __syncthreads();
     const int block = wave & 1, half = wave >> 1;
@@ -1421,10 +1450,13 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
         }
         if (spoilt) {
             const int t = x - (kn - qn), from = t < 0 ? 0 : t * a.group;
+            const int lim = row.t + kn - qn + 1;
 #pragma unroll
-            for (int i = 0; i < 16; i++)
-                if (odd.least[n * 32 + 8 * (i / 4) + 4 * h32 + i % 4] < 1 - from)
-                    dv[i] = __builtin_nanf("");
+            for (int i = 0; i < 16; i++) {
+                const int e = n * 32 + 8 * (i / 4) + 4 * h32 + i % 4;
+                if (odd.least[e] < 1 - from) dv[i] = __builtin_nanf("");
+                if (odd_keys.least[e] < lim) dq[i] = __builtin_nanf("");
+            }
         }
         if (x < a.tk) {
             store_result<T>(dvp, x < kn ? dv : zeros16(), exp2_hw(-BACK), n, h32, a.d);
