@@ -1010,6 +1010,12 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, char *lds, Odd &o
                 for (int i = 0; i < 16; i++)
                     if (r + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = y[i] = 0.f;
             }
+            // (rows behind the last, zeros, times an infinite key are NaNs)
+            if (r + 32 > p.hi) {
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (r + 8 * (i / 4) + 4 * h32 + i % 4 >= p.hi) x[i] = y[i] = 0.f;
+            }
             if (WIDE) __builtin_amdgcn_s_setprio(1);
             V8 pb[2], sb[2];
 #pragma unroll
@@ -1390,7 +1396,9 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 #pragma unroll
         for (int i = 0; i < 16; i++) {
             x[i] = exp2_hw(__builtin_fmaf(s[i], c, BACK));
-            if (32 * rblock + 8 * (i / 4) + 4 * h32 + i % 4 < from) x[i] = 0.f;
+            const int at = 32 * rblock + 8 * (i / 4) + 4 * h32 + i % 4;
+            // (rows behind the last, zeros, times an infinite key are NaNs)
+            if (at < from || at >= hi) x[i] = 0.f;
             const float none = x[i] == 0.f ? 0.f : dp[i];
             y[i] = x[i] * (HALF ? none * to_dk : none);
             z[i] = HALF ? x[i] * (none * rows[i]) : y[i];

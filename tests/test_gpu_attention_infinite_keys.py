@@ -74,3 +74,29 @@ def test_infinite_key(ops, shape, sign, dtype):
             assert bool(torch.isnan(a[after, 1]).all()), n
             assert bool(torch.isfinite(a[before, 1].float()).all()) or n == "lse", n
         assert torch.equal(got["dq"][0, rows, 0][:, keep], want["dq"][0, rows, 0][:, keep])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_gradients_of_an_infinite_key(ops, shape, causal, dtype):
+    """Those of the key itself: no query has a part in it, nor has a row of a
+    tile behind the last query."""
+    tq, tk, d = shape
+    e, j = 5, tk - tq + 3
+    c = Case(dtype, 2, tq, tk, 4, 2, d, causal=causal, q_lengths=[tq, tq - 2],
+             k_lengths=[tk, tk - 2])
+    q, k = c.q.clone(), c.k.clone()
+    q[..., :2, e] = 1
+
+    def run(value):
+        k[:, j, 0, e] = value
+        o, lse = ops.attention(q, k, c.v, **c.kw)
+        return (o, lse) + ops.attention_backward(c.do, q, k, c.v, o, lse, **c.kw)
+    want = run({"f16": -60000.0, "bf16": -1e30}[dtype])
+    got = run(-INF)
+    for i in (0, 1, 3, 4):
+        assert torch.equal(got[i], want[i]), i
+    assert not got[3][:, j, 0].any() and not got[4][:, j, 0].any()
+    keep = [i for i in range(d) if i != e]
+    assert torch.equal(got[2][..., keep], want[2][..., keep])
