@@ -82,23 +82,27 @@ __device__ __forceinline__ uint32_t lds_address(const char *p) {
 // (which the bounds do not see), to consecutive places in LDS.  As an
 // instruction of its own: with the builtin, the compiler has all loads to LDS
 // land before any read along columns, and an iteration's prefetch is waited
-// for within it.  Nothing but attn_arrive waits for these.  (M0, which the
-// compiler keeps nothing in, is LDS's address.  A scalar register that the
-// vector unit wrote, as readfirstlane does, may be read by a load five states
-// later: the compiler sees no load here, so the states stand in it.)
+// for within it.  Nothing but attn_arrive waits for these.  (M0 is LDS's
+// address.  The compiler is told that it is lost, and warns that it is one that
+// it may use itself: it would write it anew for that.  A scalar register that
+// the vector unit wrote, as readfirstlane does, may be read by a load five
+// states later: the compiler sees no load here, so the states stand in it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds16(const u4 &buf, uint32_t to, uint32_t at,
                                            uint32_t past) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(at), "s"(buf), "s"(__builtin_amdgcn_readfirstlane(past))
-                 : "memory");
+                 : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds4(const u4 &buf, uint32_t to, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(to)),
                  "v"(at), "s"(buf)
-                 : "memory");
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // t = r / G for r < 2^31 (G's multiplier and shift: see attn_group).
 __device__ __forceinline__ int over_group(const AttnArgs &a, int r) {
