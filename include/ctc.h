@@ -833,7 +833,8 @@ typedef struct {
  * R), or (2 p, 2 p + 1) if interleaved; values behind 2 R are not turned.  An
  * angle is good to 2^-21 whatever the position.
  *   q, k, yq, yk  [batch][tokens][heads][head]; yq may be q, yk may be k (in
- *                 place, with the same strides)
+ *                 place, with the same type and strides); apart from that
+ *                 results must not overlap inputs or each other
  * Heads of more than 128 values need R and head / 2 - R to be multiples of 2,
  * more than 256 multiples of 4.  batch * tokens < 2^40. */
 ctc_status ctc_head_norm_rotary_forward(const ctc_head_rotary *h,
@@ -846,7 +847,8 @@ ctc_status ctc_head_norm_rotary_forward(const ctc_head_rotary *h,
  *   dweight = sum dz xhat,
  *   dx = (dz weight - xhat mean(dz weight xhat)) / sqrt(mean(x^2) + eps)
  *   dyq, dyk  in ytype; dq, dk in dtype, may be dyq, dyk or q, k (in place,
- *             with the same type and strides)
+ *             with the same type and strides); apart from that results must
+ *             not overlap inputs or each other
  *   dq_weight, dk_weight  [head] fp32, each may be NULL
  * The same inputs give the same bits every time. */
 ctc_status ctc_head_norm_rotary_backward(const ctc_head_rotary *h,

@@ -278,7 +278,7 @@ ctc_status attn_heads(const AttnArgs &a, const ctc_heads *h, const char *name, b
 }
 
 struct Named {
-    const char *name;
+    const char *name = "";
     Region r;
 };
 ctc_status meeting(const Named &x, const Named &y) {
@@ -370,6 +370,37 @@ ctc_status head_positions(const HeadArgs &a) {
 ctc_status head_side(const HeadArgs &a, int which, const ctc_heads *h, const char *name, bool out,
                      const void *&data, int64_t (&strides)[3]) {
     return heads_arg(h, name, a.b, a.t, a.side[which].heads, a.d, out, data, strides);
+}
+
+Region head_region(const HeadArgs &a, int which, const void *data, const int64_t (&strides)[3],
+                   int type) {
+    return region(data, a.b, a.t, a.side[which].heads, strides, a.d, type);
+}
+// A lane group reads a head before it writes it, so results may stand in the
+// place of the head's own values; those of other heads are read at any time.
+ctc_status head_apart(const HeadArgs &a, bool backward) {
+    Named in[6], out[4];
+    for (int i = 0; i < 2; i++) {
+        const HeadSide &s = a.side[i];
+        in[i] = {i ? "k" : "q", head_region(a, i, s.x, s.xs, a.type)};
+        in[2 + i] = {i ? "k_weight" : "q_weight", dense(s.heads ? s.weight : nullptr, a.d, F32)};
+        if (backward) {
+            in[4 + i] = {i ? "dyk" : "dyq", head_region(a, i, s.dy, s.dys, a.ytype)};
+            out[i] = {i ? "dk" : "dq", head_region(a, i, s.dx, s.dxs, a.type)};
+            out[2 + i] = {i ? "dk_weight" : "dq_weight", dense(s.dweight, a.d, F32)};
+        } else {
+            out[i] = {i ? "yk" : "yq", head_region(a, i, s.y, s.ys, a.ytype)};
+        }
+    }
+    for (int i = 0; i < (backward ? 4 : 2); i++) {
+        for (int j = 0; j < i; j++)
+            if (meet(out[i].r, out[j].r)) return meeting(out[i], out[j]);
+        for (int j = 0; j < (backward ? 6 : 4); j++)
+            if (meet(out[i].r, in[j].r) &&
+                !(i < 2 && (j == i || j == 4 + i) && out[i].r == in[j].r))
+                return meeting(out[i], in[j]);
+    }
+    return CTC_OK;
 }
 
 // --------------------------------------------------------------- clipping
@@ -675,6 +706,7 @@ ctc_status ctc_head_norm_rotary_forward(const ctc_head_rotary *c, const ctc_head
             return s;
         h.y = (void *)out;
     }
+    if ((s = head_apart(a, false)) != CTC_OK) return s;
     return done(launch_head_norm(a, false, S(stream)));
 }
 
@@ -700,7 +732,7 @@ ctc_status ctc_head_norm_rotary_backward(const ctc_head_rotary *c, const ctc_hea
     a.side[1].dweight = a.side[1].heads ? dk_weight : nullptr;
     a.ws = (float *)workspace;
     s = need_workspace(head_norm_workspace(a), workspace, ws_bytes);
-    if (s != CTC_OK) return s;
+    if (s != CTC_OK || (s = head_apart(a, true)) != CTC_OK) return s;
     return done(launch_head_norm(a, true, S(stream)));
 }
 

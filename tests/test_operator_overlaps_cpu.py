@@ -1,7 +1,7 @@
-"""Outputs of attention that lie over inputs or over each other: refused by the
-C entry points before anything is enqueued, so no GPU is needed.  What is
-accepted reaches the launch, which a machine without a GPU reports as an error
-of the device."""
+"""Outputs of attention and head norms that lie over inputs or over each other:
+refused by the C entry points before anything is enqueued, so no GPU is needed.
+What is accepted reaches the launch, which a machine without a GPU reports as an
+error of the device."""
 
 import ctypes
 import itertools
@@ -148,3 +148,55 @@ def test_against_all_elements():
         assert got == want, (b, t, h, ks, os, shift)
         seen[want] += 1
     assert min(seen.values()) > 300
+
+
+def rotary(dtype=ctc.CTC_F16, ytype=ctc.CTC_F16, b=2, t=49, hq=4, hk=4, d=64):
+    return ctc.ctc_head_rotary(dtype, ytype, b, t, hq, hk, d, 1, 1e-6, A + 8 * FAR,
+                               A + 8 * FAR + 4096, 0, 0, (ctypes.c_int32 * 4)(), 0, None, None)
+
+
+def norm_forward(h, q, k, yq, yk):
+    ctc.ctc_head_norm_rotary_forward(h, q, k, yq, yk, None)
+
+
+def norm_backward(h, dyq, dyk, q, k, dq, dk, dqw=A + 9 * FAR, dkw=A + 9 * FAR + 256):
+    ctc.ctc_head_norm_rotary_backward(h, dyq, dyk, q, k, dq, dk, dqw, dkw, A + 10 * FAR,
+                                      1 << 29, None)
+
+
+def test_head_norms():
+    h = rotary()
+    q, k, x, y, u, v = (plain(i, t=49) for i in range(6))
+    assert not refused(norm_forward, h, q, k, x, y)
+    assert not refused(norm_forward, h, q, k, q, k)
+    assert not refused(norm_forward, h, q, q, x, y)
+    for bad in ((k, y), (x, q), (k, q), (x, x), (plain(0, t=49, shift=128), y), (q, q),
+                (x, heads(A + 8 * FAR - 128, 49 * 256, 256, 64))):
+        assert refused(norm_forward, h, q, k, *bad)
+    assert refused(norm_forward, h, q, q, q, y)             # the other reads it
+    # in place, but of another type
+    narrow = rotary(ctc.CTC_F32, ctc.CTC_F16)
+    assert refused(norm_forward, narrow, q, k, q, y)
+    assert not refused(norm_forward, narrow, q, k, x, y)
+    assert not refused(norm_backward, h, x, y, q, k, u, v)
+    for fine in ((x, y), (q, k), (x, k), (q, y)):
+        assert not refused(norm_backward, h, x, y, q, k, *fine)
+    for bad in ((y, v), (k, v), (u, x), (u, q), (u, u), (plain(2, t=49, shift=64), v)):
+        assert refused(norm_backward, h, x, y, q, k, *bad)
+    assert refused(norm_backward, narrow, x, y, q, k, x, v)
+    for bad in (dict(dqw=A + 9 * FAR + 128), dict(dkw=A + 4 * FAR + 64), dict(dqw=A + 2 * FAR),
+                dict(dqw=A + 8 * FAR), dict(dkw=A)):
+        assert refused(lambda: norm_backward(h, x, y, q, k, u, v, **bad)), bad
+    # queries and keys of one projection, their gradients over each other's
+    # buffer in place, one without keys
+    t, row = 49, 64 * 12
+    part = [heads(A + 2 * i * 256, t * row, row, 64) for i in range(2)]
+    grad = [heads(A + FAR + 2 * i * 256, t * row, row, 64) for i in range(2)]
+    assert not refused(norm_forward, h, *part, *part)
+    assert not refused(norm_forward, h, *part, *grad)
+    assert not refused(norm_backward, h, *grad, *part, *grad)
+    assert refused(norm_backward, h, *grad, *part, grad[1], grad[0])
+    alone = rotary(hk=0)
+    none = heads(0, 0, 0, 0)
+    assert not refused(norm_forward, alone, q, none, q, none)
+    assert not refused(norm_backward, alone, x, none, q, none, x, none, A + 9 * FAR, None)
