@@ -875,8 +875,9 @@ typedef struct {
 } ctc_gradient;
 
 /* norm = sqrt(sum of all values' squares), y = x min(1, max_norm / norm).
- * Sums are fp64, so no fp32 value is too large to be squared; a norm that is
- * infinite or NaN leaves the values as they are (y = x).  `grads` (host) is
+ * Sums and the factor are fp64, so no fp32 value is too large to be squared or
+ * to be clipped (a norm past fp32's largest is written as infinity); values that
+ * are infinite or NaN leave all as they are (y = x).  `grads` (host) is
  * read before the call returns.  Outputs must not overlap each other, nor
  * another tensor's x.
  *   max_norm  >= 0 (infinity: y = x)
@@ -887,7 +888,12 @@ ctc_status ctc_clip_gradients(int32_t n, const ctc_gradient *grads,
                               float max_norm, float *norm, void *workspace,
                               size_t ws_bytes, void *stream);
 
-/* Workspace of ctc_clip_gradients.  Host, synchronous. */
+/* The same for a max_norm of more digits than fp32 has. */
+ctc_status ctc_clip_gradients_to(int32_t n, const ctc_gradient *grads,
+                                 double max_norm, float *norm, void *workspace,
+                                 size_t ws_bytes, void *stream);
+
+/* Workspace of the two.  Host, synchronous. */
 ctc_status ctc_clip_gradients_workspace_bytes(int32_t n,
                                               const ctc_gradient *grads,
                                               size_t *bytes);

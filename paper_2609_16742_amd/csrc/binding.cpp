@@ -662,9 +662,8 @@ clip_gradients(const py::object &grad_list, double max_norm, const py::object &o
     size_t bytes = 0;
     Tensor keep;
     done(ctc_clip_gradients_workspace_bytes((int32_t)g.size(), g.data(), &bytes));
-    done(ctc_clip_gradients((int32_t)g.size(), g.data(), (float)max_norm,
-                            (float *)norm->data_ptr(), scratch(bytes, keep, ref), bytes,
-                            (void *)stream));
+    done(ctc_clip_gradients_to((int32_t)g.size(), g.data(), max_norm, (float *)norm->data_ptr(),
+                               scratch(bytes, keep, ref), bytes, (void *)stream));
     if (!made)
         for (const Tensor *t : given_out ? out : grads) wrote(*t);
     if (given) wrote(norm);

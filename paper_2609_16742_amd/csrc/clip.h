@@ -86,15 +86,17 @@ __global__ __launch_bounds__(256) void clip_squares(ClipTable t, double *part) {
 }
 
 __global__ __launch_bounds__(256) void clip_scale(ClipTable t, const double *part, int parts,
-                                                  float max_norm, float *norm) {
+                                                  double max_norm, float *norm) {
     __shared__ double lds[4];
     double sum = 0;
     for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
     sum = __builtin_sqrt(clip_join(sum, lds));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)sum;
     // (a norm that is no number leaves everything as it is)
-    const bool over = sum > (double)max_norm && sum < __builtin_inf();
-    const float f = over ? (float)((double)max_norm / sum) : 1.f;
+    const bool over = sum > max_norm && sum < __builtin_inf();
+    // (in fp64: in fp32 the factor would cost a rounding of its own, and all its
+    // bits below 2^-126, which norms past 2^126 max_norm reach)
+    const double f = over ? max_norm / sum : 1.0;
     for (uint32_t c = blockIdx.x; c < t.first[t.n]; c += gridDim.x) {
         const int i = clip_find(t, c);
         if (!over && t.y[i] == t.x[i]) continue;
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(256) void clip_scale(ClipTable t, const double *par
                 constexpr int V = decltype(w)::value;
                 float o[V];
 #pragma unroll
-                for (int k = 0; k < V; k++) o[k] = v[k] * f;
+                for (int k = 0; k < V; k++) o[k] = (float)((double)v[k] * f);
                 store<T, V>(y + e, o);
             });
         };
@@ -127,7 +129,7 @@ int64_t clip_chunks_of(int64_t size) { return (size + CLIP_CHUNK - 1) / CLIP_CHU
 hipError_t launch_clip_squares(const ClipTable &t, double *part, hipStream_t st) {
     return clip_parts(t) ? start(clip_squares, dim3(clip_parts(t)), 256, st, t, part) : hipSuccess;
 }
-hipError_t launch_clip_scale(const ClipTable &t, const double *part, int parts, float max_norm,
+hipError_t launch_clip_scale(const ClipTable &t, const double *part, int parts, double max_norm,
                              float *norm, hipStream_t st) {
     const int groups = clip_parts(t);
     return start(clip_scale, dim3(groups ? groups : 1), 256, st, t, part, parts, max_norm, norm);

@@ -138,7 +138,7 @@ struct ClipTable {
 int64_t clip_chunks_of(int64_t size);
 int clip_parts(const ClipTable &t);              // partial sums of a launch
 hipError_t launch_clip_squares(const ClipTable &t, double *part, hipStream_t st);
-hipError_t launch_clip_scale(const ClipTable &t, const double *part, int parts, float max_norm,
+hipError_t launch_clip_scale(const ClipTable &t, const double *part, int parts, double max_norm,
                              float *norm, hipStream_t st);
 
 }  // namespace ops

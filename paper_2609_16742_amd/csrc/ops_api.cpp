@@ -751,10 +751,15 @@ ctc_status ctc_clip_gradients_workspace_bytes(int32_t n, const ctc_gradient *g, 
 
 ctc_status ctc_clip_gradients(int32_t n, const ctc_gradient *g, float max_norm, float *norm,
                               void *workspace, size_t ws_bytes, void *stream) {
+    return ctc_clip_gradients_to(n, g, max_norm, norm, workspace, ws_bytes, stream);
+}
+
+ctc_status ctc_clip_gradients_to(int32_t n, const ctc_gradient *g, double max_norm, float *norm,
+                                 void *workspace, size_t ws_bytes, void *stream) {
     size_t need = 0;
     ctc_status s = ctc_clip_gradients_workspace_bytes(n, g, &need);
     if (s != CTC_OK) return s;
-    if (!(max_norm >= 0.f)) return fail(CTC_ERR_ARG, "max_norm must be >= 0");
+    if (!(max_norm >= 0)) return fail(CTC_ERR_ARG, "max_norm must be >= 0");
     for (int32_t i = 0; i < n; i++)
         if (g[i].size && (!g[i].x || !g[i].y)) return fail(CTC_ERR_ARG, "NULL gradient %d", i);
     try {

@@ -60,7 +60,7 @@ EXPORTS = ["ctc_build_filters", "ctc_build_fc", "ctc_threshold_from_samples",
            "ctc_attention_workspace_bytes", "ctc_head_norm_rotary_forward",
            "ctc_head_norm_rotary_backward",
            "ctc_head_norm_rotary_workspace_bytes", "ctc_clip_gradients",
-           "ctc_clip_gradients_workspace_bytes",
+           "ctc_clip_gradients_to", "ctc_clip_gradients_workspace_bytes",
            "ctc_group_norm_forward", "ctc_group_norm_backward",
            "ctc_group_norm_workspace_bytes", "ctc_fp8_quantize",
            "ctc_fp8_matmul", "ctc_fp8_matmul_workspace_bytes",
@@ -222,6 +222,8 @@ _sig("ctc_head_norm_rotary_workspace_bytes", [
     ctypes.POINTER(ctc_head_rotary), ctypes.POINTER(_SZ)])
 _sig("ctc_clip_gradients", [_I32, ctypes.POINTER(ctc_gradient), _F32, _P, _P,
                             _SZ, _P])
+_sig("ctc_clip_gradients_to", [_I32, ctypes.POINTER(ctc_gradient), _F64, _P,
+                               _P, _SZ, _P])
 _sig("ctc_clip_gradients_workspace_bytes", [
     _I32, ctypes.POINTER(ctc_gradient), ctypes.POINTER(_SZ)])
 _sig("ctc_net_destroy", [_P], None)
@@ -577,6 +579,10 @@ def ctc_head_norm_rotary_workspace_bytes(rotary):
 
 def ctc_clip_gradients(*args):
     _check(_lib.ctc_clip_gradients(*args))
+
+
+def ctc_clip_gradients_to(*args):
+    _check(_lib.ctc_clip_gradients_to(*args))
 
 
 def ctc_clip_gradients_workspace_bytes(n, gradients):

@@ -245,8 +245,8 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     """(clipped, norm): the norm of all values of ``grads`` (dense tensors)
     together and the tensors times min(1, max_norm / norm).  ``out``: tensors
     to write into, like ``grads`` (in place: ``grads`` itself); ``norm``: one
-    fp32 value to write into.  A norm that is not finite leaves the values as
-    they are."""
+    fp32 value to write into (infinite past fp32's largest).  A value that is
+    not finite leaves all as they are."""
     if not isinstance(grads, (list, tuple)):
         grads = list(grads)
     if not grads:
