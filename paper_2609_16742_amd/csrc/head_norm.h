@@ -83,6 +83,36 @@ __device__ __forceinline__ float head_sum(float v, int L) {
     return v;
 }
 
+// 1 / sqrt(mean x^2 + eps) of a head.  Where the mean is infinite or has lost
+// bits in fp32 (values past 2^59 or so, or far below 1 with an eps as small), the
+// values are multiplied by a power of two `t` first, and the result is 1 / t of
+// theirs: their product is the normed value all the same.  `scaled` if a head of
+// the wave is: elsewhere t is 1 and costs nothing.
+struct HeadRoot {
+    float r, t = 1.f;
+    bool scaled;
+    template <int V>
+    __device__ __forceinline__ HeadRoot(float (&u)[V], float (&v)[V], int L, int d, float eps) {
+        const float m = mean(u, v, L, d) + eps;
+        r = 1.f / sqrtf(m);
+        scaled = __any(!(m < INF && m > 0x1p-100f));
+        if (!scaled) return;
+        if (!(m < INF)) t = 0x1p-80f;
+        else if (!(m > 0x1p-100f)) t = 0x1p110f;
+#pragma unroll
+        for (int i = 0; i < V; i++) u[i] *= t, v[i] *= t;
+        r = 1.f / sqrtf(mean(u, v, L, d) + eps * t * t);
+    }
+    template <int V>
+    static __device__ __forceinline__ float mean(const float (&u)[V], const float (&v)[V], int L,
+                                                 int d) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; i++) sum += u[i] * u[i] + v[i] * v[i];
+        return head_sum(sum, L) / d;
+    }
+};
+
 template <typename T, typename U, int V, bool INTER>
 __global__ __launch_bounds__(256) void head_norm_forward(HeadArgs a) {
     extern __shared__ float2 table[];            // [tokens][half]: cosine, sine
@@ -110,12 +140,9 @@ __global__ __launch_bounds__(256) void head_norm_forward(HeadArgs a) {
             if (mine)
                 at.load((const T *)s.x + b * s.xs[0] + t * s.xs[1] + head * s.xs[2], u, v);
             if (a.norm) {
-                float sum = 0.f;
+                const HeadRoot root(u, v, L, a.d, a.eps);
 #pragma unroll
-                for (int i = 0; i < V; i++) sum += u[i] * u[i] + v[i] * v[i];
-                const float r = 1.f / sqrtf(head_sum(sum, L) / a.d + a.eps);
-#pragma unroll
-                for (int i = 0; i < V; i++) u[i] *= r, v[i] *= r;
+                for (int i = 0; i < V; i++) u[i] *= root.r, v[i] *= root.r;
             }
 #pragma unroll
             for (int i = 0; i < V; i++) u[i] *= wu[i], v[i] *= wv[i];
@@ -181,12 +208,13 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
                         u[i] = x;
                     }
                 }
-                float r = 1.f;
+                float r = 1.f, lift = 1.f;
+                bool scaled = false;
                 if (a.norm) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int i = 0; i < V; i++) sum += xu[i] * xu[i] + xv[i] * xv[i];
-                    r = 1.f / sqrtf(head_sum(sum, L) / a.d + a.eps);
+                    const HeadRoot root(xu, xv, L, a.d, a.eps);
+                    r = root.r;
+                    lift = root.t;
+                    scaled = root.scaled;
 #pragma unroll
                     for (int i = 0; i < V; i++) xu[i] *= r, xv[i] *= r;
                 }
@@ -205,6 +233,10 @@ __global__ __launch_bounds__(256) void head_norm_backward(HeadArgs a) {
                     for (int i = 0; i < V; i++) {
                         u[i] = r * (u[i] - xu[i] * dot);
                         v[i] = r * (v[i] - xv[i] * dot);
+                    }
+                    if (scaled) {
+#pragma unroll
+                        for (int i = 0; i < V; i++) u[i] *= lift, v[i] *= lift;
                     }
                 }
                 if (mine) at.store((T *)s.dx + b * s.dxs[0] + t * s.dxs[1] + head * s.dxs[2], u, v);
