@@ -753,7 +753,7 @@ typedef struct {
     int32_t q_heads, k_heads;    /* q_heads / k_heads query heads share each */
     int32_t head;                /* head size: a multiple of 8, 8 .. 128 */
     int32_t causal;
-    float scale;                 /* 2^-96 at least */
+    float scale;                 /* 2^-96 .. 2^126 */
     const int32_t *q_lengths;    /* device, [batch] or NULL (all of them) */
     const int32_t *k_lengths;
 } ctc_attention;

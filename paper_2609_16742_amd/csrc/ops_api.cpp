@@ -248,8 +248,9 @@ ctc_status attn_args(const ctc_attention *c, AttnArgs &a) {
     if (c->q_heads % c->k_heads) return fail(CTC_ERR_ARG, "k_heads must divide q_heads");
     if (c->head < 8 || c->head % 8 || c->head > ATTN_MAX_D)
         return fail(CTC_ERR_ARG, "head sizes are multiples of 8 up to %d", ATTN_MAX_D);
-    if (!(c->scale >= 0x1p-96f) || std::isinf(c->scale))
-        return fail(CTC_ERR_ARG, "scale must be positive, 2^-96 at least");
+    // (the kernels divide by it, and multiply it by log2 e)
+    if (!(c->scale >= 0x1p-96f && c->scale <= 0x1p126f))
+        return fail(CTC_ERR_ARG, "scale must be 2^-96 .. 2^126");
     const double rows = (double)c->queries * (c->q_heads / c->k_heads);
     const double pairs = (double)c->batch * c->k_heads;
     if (rows > (1 << 30) || c->keys > (1 << 30) || c->q_heads / c->k_heads > 65536 ||
