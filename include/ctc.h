@@ -878,8 +878,8 @@ typedef struct {
  * Sums and the factor are fp64, so no fp32 value is too large to be squared or
  * to be clipped (a norm past fp32's largest is written as infinity); values that
  * are infinite or NaN leave all as they are (y = x).  `grads` (host) is
- * read before the call returns.  Outputs must not overlap each other, nor
- * another tensor's x.
+ * read before the call returns.  Outputs, the norm among them, must not overlap
+ * each other, nor another tensor's x.
  *   max_norm  >= 0 (infinity: y = x)
  *   norm      device, fp32, or NULL
  * The same inputs give the same bits every time.  n <= 2^20, at most 2^43

@@ -436,12 +436,14 @@ template <typename F> ctc_status clip_tables(int32_t n, const ctc_gradient *g, F
     }
     return CTC_OK;
 }
-// No output overlaps another one, or another tensor's values.
-bool clip_disjoint(int32_t n, const ctc_gradient *g) {
+// No output (the norm among them) overlaps another one, or another tensor's
+// values.
+bool clip_disjoint(int32_t n, const ctc_gradient *g, const float *norm) {
     struct Span { uintptr_t from, to; int32_t i; };
     std::vector<Span> out, in;
-    out.reserve(n);
+    out.reserve(n + 1);
     in.reserve(n);
+    if (norm) out.push_back({(uintptr_t)norm, (uintptr_t)(norm + 1), -1});
     for (int32_t i = 0; i < n; i++) {
         const size_t bytes = (size_t)g[i].size * type_bytes(g[i].dtype);
         if (!bytes) continue;
@@ -764,7 +766,7 @@ ctc_status ctc_clip_gradients_to(int32_t n, const ctc_gradient *g, double max_no
     for (int32_t i = 0; i < n; i++)
         if (g[i].size && (!g[i].x || !g[i].y)) return fail(CTC_ERR_ARG, "NULL gradient %d", i);
     try {
-        if (!clip_disjoint(n, g)) return fail(CTC_ERR_ARG, "outputs overlap other gradients");
+        if (!clip_disjoint(n, g, norm)) return fail(CTC_ERR_ARG, "outputs overlap other gradients");
     } catch (const std::exception &e) {
         return fail(CTC_ERR_DEVICE, "%s", e.what());
     }

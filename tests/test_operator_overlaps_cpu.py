@@ -30,7 +30,7 @@ def status(f, *args):
 
 def refused(f, *args):
     s, text = status(f, *args)
-    return s == ARG and "overlaps" in text
+    return s == ARG and "overlap" in text
 
 
 @pytest.fixture(autouse=True)
@@ -200,3 +200,19 @@ def test_head_norms():
     none = heads(0, 0, 0, 0)
     assert not refused(norm_forward, alone, q, none, q, none)
     assert not refused(norm_backward, alone, x, none, q, none, x, none, A + 9 * FAR, None)
+
+
+def test_clipping_norm():
+    """The norm over a gradient or over what one becomes."""
+    def call(norm, *g):
+        grads = (ctc.ctc_gradient * len(g))(*[ctc.ctc_gradient(*v, 0) for v in g])
+        ctc.ctc_clip_gradients(len(g), grads, 1.0, norm, A + 10 * FAR, 1 << 29, None)
+    x, y = A, A + FAR
+    for g in (((x, y, 100, ctc.CTC_F32),), ((x, x, 100, ctc.CTC_F32),),
+              ((x, x, 200, ctc.CTC_F16), (y, y, 200, ctc.CTC_BF16))):
+        for at in (x, x + 396, x + 399, x - 3):
+            assert refused(call, at, *g)
+        for at in (x - 4, x + 400, y + 400, A + 2 * FAR, None):
+            assert not refused(call, at, *g)
+    for at in (y, y + 396):
+        assert refused(call, at, (x, y, 100, ctc.CTC_F32))
