@@ -831,7 +831,9 @@ typedef struct {
  * with the angle position * frequency of the pair, on the axis it belongs to
  * (rows and columns of a map; frames).  Of R = sum of pairs, pair p is (p, p +
  * R), or (2 p, 2 p + 1) if interleaved; values behind 2 R are not turned.  An
- * angle is good to 2^-21 whatever the position.
+ * angle is good to 2^-21 where position * frequency is below 2^29, and to 2^-50
+ * of that product beyond.  Values of any size are normed (their squares need not
+ * fit fp32).
  *   q, k, yq, yk  [batch][tokens][heads][head]; yq may be q, yk may be k (in
  *                 place, with the same type and strides); apart from that
  *                 results must not overlap inputs or each other

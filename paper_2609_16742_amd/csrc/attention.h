@@ -713,8 +713,8 @@ template <typename T> __global__ __launch_bounds__(256) void attend_join(AttnArg
 // The probabilities are computed twice, once with a lane's key fixed (dk, dv)
 // and once with its row fixed (dq): seven products instead of five, and no
 // sums between workgroups, whose order would change the result's bits.
-// What bounds it: the matrix unit, 0.96 PFLOP/s of those seven (2 x 3136, 16 heads
-// of 128: 590 us).
+// What bounds it: the matrix unit, 0.93 to 0.97 PFLOP/s of those seven (2 x 3136,
+// 16 heads of 128: 580 to 605 us).
 // ---------------------------------------------------------------------------
 template <typename T> __global__ __launch_bounds__(256) void attn_rows(AttnArgs a) {
     __shared__ float most[4];
@@ -1481,9 +1481,10 @@ __global__ __launch_bounds__(256, NK <= 4 ? 2 : 1) void attend_backward_small(At
 
 // Both in one launch, so that workgroups of the second kind fill the CUs that
 // those of the first, which take longer, leave idle at their end.  800 of each
-// kind on 512 places (2 x 3136, 16 heads of 128): 803 us apart, 620 together.
-// (Apart, dq first, where dk or dv is written over the keys or values: those
-// of the second kind read all of them, those of the first their own.)
+// kind on 512 places (2 x 3136, 16 heads of 128): 400 and 270 us apart, 590 to 620
+// together.  (Apart, dq first, where dk or dv is written over the keys or
+// values: those of the second kind read all of them, those of the first their
+// own.)
 template <typename T, int NK, int ND, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void attend_backward(AttnArgs a) {
     constexpr int Q = 256 * (NK <= 4 ? 64 : 128) * 2, K = KeyTiles<NK>::BYTES;
