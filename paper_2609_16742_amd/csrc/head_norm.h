@@ -88,7 +88,7 @@ __device__ __forceinline__ float head_sum(float v, int L) {
 // bits in fp32 (values past 2^59 or so, or far below 1 with an eps as small), the
 // values are multiplied by a power of two `t` first, and the result is 1 / t of
 // theirs: their product is the normed value all the same.  `scaled` if a head of
-// the wave is: elsewhere t is 1 and costs nothing.
+// the wave is; elsewhere one comparison is all that this costs.
 struct HeadRoot {
     float r, t = 1.f;
     bool scaled;

@@ -66,3 +66,75 @@ def test_refusals(ops):
         with pytest.raises(ctc.CtcError):
             ops.attention(q, k, v, out=out)
     assert not x.any()
+
+
+@pytest.mark.parametrize("t", [60, 500])
+def test_over_inputs_in_a_graph(ops, t):
+    """Captured with the copy that restores the keys, replayed with eager work
+    between, on a stream of its own."""
+    c = Case("f16", 2, t, t, 4, 2, 64, causal=True)
+    o, lse = ops.attention(c.q, c.k, c.v, **c.kw)
+    want = ops.attention_backward(c.do, c.q, c.k, c.v, o, lse, **c.kw)
+    k, v, dq = c.k.clone(), c.v.clone(), torch.empty_like(c.q)
+
+    def once():
+        k.copy_(c.k)
+        v.copy_(c.v)
+        ops.attention_backward(c.do, c.q, k, v, o, lse, out=(dq, k, v), **c.kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        once()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once()
+    for _ in range(4):
+        for x in (dq, k, v):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((dq, k, v), want):
+            assert torch.equal(a, b)
+        ops.attention_backward(c.do, c.q, c.k, c.v, o, lse, **c.kw)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_broadcast_inputs(ops, dtype):
+    """One query for all sequences, keys and values of one sequence for all, a
+    value for all tokens: strides of zero, whose span is a part's."""
+    c = Case(dtype, 3, 5, 300, 4, 2, 64)
+    q, k = c.q[:1].expand(c.q.shape), c.k[:1].expand(c.k.shape)
+    v = c.v[:, :1].expand(c.v.shape)
+    for a in ((q, c.k, c.v), (c.q, k, c.v), (c.q, k, v), (q, k, v)):
+        plain = [x.contiguous() for x in a]
+        o, lse = ops.attention(*a)
+        want = ops.attention(*plain)
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        for x, y in zip(ops.attention_backward(c.do, *a, o, lse),
+                        ops.attention_backward(c.do, *plain, o, lse)):
+            assert torch.equal(x, y)
+
+
+def test_two_streams_at_once(ops):
+    """Calls that need workspaces, under way together."""
+    cases = [Case("f16", 1, 200, 7000, 2, 1, 64, seed=3 + i) for i in range(2)]
+    want = []
+    for c in cases:
+        o, lse = ops.attention(c.q, c.k, c.v)
+        want.append((o, lse) + ops.attention_backward(c.do, c.q, c.k, c.v, o, lse))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[] for _ in cases]
+    for _ in range(10):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                o, lse = ops.attention(c.q, c.k, c.v)
+                got[i].append((o, lse) + ops.attention_backward(c.do, c.q, c.k, c.v, o, lse))
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        for g in got[i]:
+            for a, b in zip(g, w):
+                assert torch.equal(a, b)
